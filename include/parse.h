@@ -458,6 +458,122 @@ int parse_lowrank_prefill_multi(const parse_layer *layers, const parse_patterns 
                                 const int32_t *pattern_id, int32_t P, void *const *Y, void *workspace,
                                 size_t workspace_bytes, parse_stream stream);
 
+/* ---- paged key-value cache ------------------------------------------------------------------------------------------
+ * Between the q/k/v projections of a decoder block and its o projection stand the cache of keys and values and the
+ * attention that reads it.  The cache is cut into pages of `page` tokens; a page id stands for that page of every layer,
+ * of K and of V.  Both are stored in blocks of 16 tokens whose 16-byte (fp32: 32-byte) pieces are what a lane feeds to the
+ * matrix instructions, so that kernels read them, into registers or LDS, without a transpose:
+ *     K element (layer, page id, kv head, token w, i):
+ *         ((((layer*n_pages + id)*n_kv + head)*(page/16) + w/16)*(d/8) + i/8)*128 + (w%16)*8 + i%8
+ *     V element:
+ *         ((((layer*n_pages + id)*n_kv + head)*(page/8) + w/8)*d + i)*8 + w%8
+ * Everything that changes from step to step lives in device memory and is changed by enqueued calls only, so that a
+ * whole step can be recorded into a HIP graph:
+ *     table      [n_seqs][max_pages], the page of tokens [c*page, (c+1)*page) of a sequence or -1 (given up, not yet given)
+ *     len        [n_seqs], tokens that a sequence holds
+ *     refs       [n_pages], table entries that hold the page; a page never stands in two columns of the table
+ *     free_bits  [(n_pages+31)/32] words, bit p%32 of word p/32 set iff refs[p] == 0 (bits past n_pages are 0)
+ * parse_kv_append and the attention calls use K, V, table and len alone: refs and free_bits may be NULL there.
+ * Table entries outside [0, n_pages) and sequence numbers outside [0, n_seqs) are skipped wherever they are read. */
+typedef struct {
+  int32_t n_layers;
+  int32_t n_pages;
+  int32_t page;      /* tokens per page: 16, 32, 64, 128 or 256 */
+  int32_t n_kv;      /* heads of K and V, 1..1024 */
+  int32_t d;         /* columns of a head: a multiple of 32 up to 256 */
+  int32_t dtype;     /* parse_dtype of K, V and of the rows that go in and come out */
+  int32_t n_seqs;    /* rows of the table, at most 4096 */
+  int32_t max_pages; /* columns of the table; max_pages*page <= 2^25 */
+  void *K;
+  void *V;
+  int32_t *table;
+  int32_t *len;
+  int32_t *refs;
+  uint32_t *free_bits;
+} parse_kv;
+
+/* An empty cache: table -1, len 0, refs 0, every page free.  K and V are not touched. */
+int parse_kv_clear(const parse_kv *kv, parse_stream stream);
+
+/* Forks sequences: row dst[i] of the table and its length become row src[i]'s, for all i at once (every source is read
+ * before anything is written, so that rows may be permuted); what the rows dst[i] held is given up.  No page is copied: the
+ * pages have one more user each.
+ *   src, dst  device int32 [n], 1 <= n <= 1024; a destination stands at most once.  A pair with a number outside the table
+ *             is skipped. */
+int parse_kv_fork(const parse_kv *kv, const int32_t *src, const int32_t *dst, int32_t n, parse_stream stream);
+
+/* Room for n_new[s] more tokens of every sequence s: len[s] += n_new[s]; the pages it takes are the free ones of the
+ * lowest ids, and a page that is begun and has other users is replaced by a copy of its own (K and V of all layers).
+ * The sequences are served in the order of their numbers, each as if the calls were made one after another (of
+ * several users of a begun page the last one keeps it).  A sequence that would outgrow max_pages, or asks for no token, is
+ * left as it is; from the first one that the free pages do not suffice for on, all are.
+ *   n_new      device int32 [n_seqs] (negative: 0)
+ *   served     device int32 [n_seqs] or NULL: 1 where the sequence has its new tokens, else 0
+ *   workspace  device, >= parse_kv_workspace_bytes(kv) */
+size_t parse_kv_workspace_bytes(const parse_kv *kv);
+int parse_kv_reserve(const parse_kv *kv, const int32_t *n_new, int32_t *served, void *workspace, size_t workspace_bytes,
+                     parse_stream stream);
+
+/* Gives up pages: len[s] becomes min(len[s], max(keep[s], 0)) (keep NULL: lengths stay) and the pages past it are given
+ * up; with window > 0 also those that no later token sees, which are the pages whose tokens are all at or past
+ * `sinks` and all before len[s] - window + 1.  A page without users is free. */
+int parse_kv_trim(const parse_kv *kv, const int32_t *keep, int32_t window, int32_t sinks, parse_stream stream);
+
+/* Moves the pages in use to the ids 0 .. n_live-1: the k-th of the pages at or past n_live that are in use goes to the k-th
+ * free id below it (K and V of all layers), table, refs and free_bits follow.  What stands in pages at or past n_live is
+ * left there.
+ *   n_live     device int32 [1] or NULL: pages in use
+ *   workspace  device, >= parse_kv_workspace_bytes(kv) */
+int parse_kv_compact(const parse_kv *kv, int32_t *n_live, void *workspace, size_t workspace_bytes, parse_stream stream);
+
+/* The rows of new tokens on their way from the projections to the attention: k and v into their pages, q and k rotated
+ * by their positions on the way.  The tokens of prompt p are the LAST ones of its sequence: rows [tok_offsets[p],
+ * tok_offsets[p+1]) stand at positions len - n_p .. len - 1 (parse_kv_reserve has counted them).  A token whose page is
+ * missing or that has no position is not stored.
+ *   layer        0 <= layer < n_layers
+ *   k, v         device [rows][n_kv][d], rows k_stride / v_stride elements apart (so that they may be slices of one
+ *                fused projection), strides and pointers on 16 bytes
+ *   tok_offsets  device int32 [P+1], or NULL: one row per prompt (rows == P)
+ *   seqs         device int32 [P], the table's row of each prompt, or NULL: p
+ *   rope         device float [n_pos][d], row = position: d/2 cosines, d/2 sines;
+ *                (x_i, x_{i+d/2}) -> (x_i c_i - x_{i+d/2} s_i, x_{i+d/2} c_i + x_i s_i) in 32 bits, rounded once; a
+ *                position past the table's end takes its last row.  NULL: nothing is rotated (q is only copied)
+ *   q, q_out     device [rows][n_q][d] with row strides, or both NULL.  q_out may be q.  A row without a sequence is rotated as
+ *                position 0 */
+int parse_kv_append(const parse_kv *kv, int32_t layer, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                    const void *q, int64_t q_stride, void *q_out, int64_t q_out_stride, int32_t n_q, int32_t rows,
+                    const int32_t *tok_offsets, const int32_t *seqs, int32_t P, const float *rope, int32_t n_pos,
+                    parse_stream stream);
+
+/* ---- attention over the paged cache ----------------------------------------------------------------------------------
+ * For a row at position i and query head h, over the positions j whose page is there and that i sees,
+ *     j <= i  and  (window == 0  or  j > i - window  or  j < sinks):
+ *     o = sum_j softmax_j(scale * q . k_j) v_j,     lse = ln sum_j exp(scale * q . k_j)
+ * with k and v of head h / (n_q / n_kv) (shared heads; n_q % n_kv == 0).  What stands in positions that a row does not see has
+ * no influence on it, whatever it holds (also infinities and NaN).  A row that sees nothing gives o = 0 and lse = -inf.
+ * Sums and the softmax's statistics are held in 32 bits; bf16: the weights are rounded to bf16 for the second product.
+ *   q, out        device [rows][n_q][d], rows q_stride / out_stride elements apart, 16-byte aligned; out is not q
+ *   lse           device float [rows][n_q] or NULL
+ *   window >= 0 (0: none), sinks >= 0 (read only with a window)
+ *   workspace     device, at least what the query says; contents irrelevant before, undefined after */
+
+/* One new token per sequence (its last: i = len - 1), over caches of any lengths; the caches' tokens are dealt out evenly
+ * over the card and the parts of a cache joined.
+ *   rows = number of sequences, 1..4096; seqs device int32 [rows], the table's row of each, or NULL: the row itself */
+size_t parse_attend_decode_workspace_bytes(const parse_kv *kv, int32_t n_q, int32_t rows);
+int parse_attend_decode(const parse_kv *kv, int32_t layer, const void *q, int64_t q_stride, int32_t n_q, int32_t rows,
+                        const int32_t *seqs, float scale, int32_t window, int32_t sinks, void *out, int64_t out_stride,
+                        float *lse, void *workspace, size_t workspace_bytes, parse_stream stream);
+
+/* The new tokens of a batch of prompts, which are the last ones of their sequences as in parse_kv_append (a first prompt, a
+ * later turn, a piece of a long prompt), appended before.
+ *   tok_offsets, seqs, P  as for parse_kv_append, P in 1..4096 */
+size_t parse_attend_prefill_workspace_bytes(const parse_kv *kv, int32_t n_q, int32_t rows, int32_t P);
+int parse_attend_prefill(const parse_kv *kv, int32_t layer, const void *q, int64_t q_stride, int32_t n_q, int32_t rows,
+                         const int32_t *tok_offsets, const int32_t *seqs, int32_t P, float scale, int32_t window,
+                         int32_t sinks, void *out, int64_t out_stride, float *lse, void *workspace, size_t workspace_bytes,
+                         parse_stream stream);
+
 /* ---- achievable-peak probes (measurement only) ---------------------------------------------------------------
  * Kernels with nothing but the resource a roofline prices: the caller times them with HIP events on its stream and
  * reports the rates beside the nominal peaks (MI355X: 2.5 PFLOP/s dense bf16, 8 TB/s HBM).  They only enqueue.

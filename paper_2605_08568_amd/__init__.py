@@ -13,4 +13,6 @@ from .binding import (  # noqa: F401
     lowrank_prefill_planned, lowrank_prefill_planned_workspace_bytes,
     probe_mfma_bf16, probe_read, probe_copy,
     decode_plan, lowrank_decode_planned, lowrank_decode_planned_workspace_bytes,
+    KV, kv_append, kv_clear, kv_compact, kv_fork, kv_reserve, kv_trim, kv_workspace,
+    attend_decode, attend_decode_workspace, attend_prefill, attend_prefill_workspace,
 )

@@ -38,6 +38,12 @@ class _Patterns(C.Structure):
                 ("schedule", C.c_int32)]
 
 
+class _KV(C.Structure):
+    _fields_ = [("n_layers", C.c_int32), ("n_pages", C.c_int32), ("page", C.c_int32), ("n_kv", C.c_int32), ("d", C.c_int32),
+                ("dtype", C.c_int32), ("n_seqs", C.c_int32), ("max_pages", C.c_int32), ("K", C.c_void_p), ("V", C.c_void_p),
+                ("table", C.c_void_p), ("len", C.c_void_p), ("refs", C.c_void_p), ("free_bits", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -132,6 +138,19 @@ def lib():
     L.parse_lowrank_decode_static_capacity.restype = sz; L.parse_lowrank_decode_static_capacity.argtypes = []
     L.parse_lowrank_decode_static.restype = C.c_int
     L.parse_lowrank_decode_static.argtypes = [C.POINTER(_Layer), C.POINTER(_Patterns), vp, i32, vp, vp, vp]
+    i64, kvp = C.c_int64, C.POINTER(_KV)
+    L.parse_kv_workspace_bytes.restype = sz; L.parse_kv_workspace_bytes.argtypes = [kvp]
+    L.parse_attend_decode_workspace_bytes.restype = sz; L.parse_attend_decode_workspace_bytes.argtypes = [kvp, i32, i32]
+    L.parse_attend_prefill_workspace_bytes.restype = sz; L.parse_attend_prefill_workspace_bytes.argtypes = [kvp, i32, i32, i32]
+    for name, args in [("clear", [vp]), ("fork", [vp, vp, i32, vp]), ("reserve", [vp, vp, vp, sz, vp]), ("trim", [vp, i32, i32, vp]),
+                       ("compact", [vp, vp, sz, vp]),
+                       ("append", [i32, vp, i64, vp, i64, vp, i64, vp, i64, i32, i32, vp, vp, i32, vp, i32, vp])]:
+        f = getattr(L, "parse_kv_" + name)
+        f.restype = C.c_int; f.argtypes = [kvp, *args]
+    L.parse_attend_decode.restype = C.c_int
+    L.parse_attend_decode.argtypes = [kvp, i32, vp, i64, i32, i32, vp, f32, i32, i32, vp, i64, vp, vp, sz, vp]
+    L.parse_attend_prefill.restype = C.c_int
+    L.parse_attend_prefill.argtypes = [kvp, i32, vp, i64, i32, i32, vp, vp, i32, f32, i32, i32, vp, i64, vp, vp, sz, vp]
     _lib = L
     return L
 
@@ -626,3 +645,181 @@ def router_grad(layer: Layer, Ut_rankmajor, X, tok_offsets, Y_hat, Y_dense, emb,
                                     temperature, eps, loss, grad, workspace, workspace.numel(), _stream()),
                                     "parse_router_grad")
     return loss, grad
+
+
+# ---- paged key-value cache and the attention over it ---------------------------------------------------------------
+class KV:
+    """parse_kv: the paged cache of one model.  K [n_layers][n_pages][n_kv][page/16][d/8][16][8] and
+    V [n_layers][n_pages][n_kv][page/8][d][8] (bfloat16 or float32), table int32 [n_seqs][max_pages], len int32 [n_seqs];
+    refs int32 [n_pages] and free_bits int32 [(n_pages+31)/32] for the calls that give and take pages."""
+
+    def __init__(self, K, V, table, length, refs=None, free_bits=None):
+        if K.dim() != 7 or V.dim() != 6 or K.shape[5:] != (16, 8) or V.shape[5] != 8:
+            raise ValueError(f"K [layers][pages][heads][page/16][d/8][16][8] and V [layers][pages][heads][page/8][d][8] are wanted: {tuple(K.shape)}, {tuple(V.shape)}")
+        self.n_layers, self.n_pages, self.n_kv = K.shape[:3]
+        self.page, self.d = K.shape[3] * 16, K.shape[4] * 8
+        if tuple(V.shape) != (self.n_layers, self.n_pages, self.n_kv, self.page // 8, self.d, 8):
+            raise ValueError(f"V's shape {tuple(V.shape)} does not go with K's {tuple(K.shape)}")
+        self.n_seqs, self.max_pages = table.shape
+        self.dtype = _dtype_code(K)
+        if V.dtype != K.dtype:
+            raise TypeError("K and V of one dtype are wanted")
+        for name, t, n in (("table", table, None), ("len", length, self.n_seqs), ("refs", refs, self.n_pages),
+                           ("free_bits", free_bits, (self.n_pages + 31) // 32)):
+            if t is None and name in ("refs", "free_bits"):
+                continue
+            if t.dtype != torch.int32 or (n is not None and t.numel() != n):
+                raise ValueError(f"{name}: int32{'' if n is None else f' of {n} elements'} is wanted")
+        for name, t in (("K", K), ("V", V), ("table", table), ("len", length), ("refs", refs), ("free_bits", free_bits)):
+            if t is not None and not t.is_contiguous():
+                raise ValueError(f"{name} has to be contiguous")
+        self.K, self.V, self.table, self.len, self.refs, self.free_bits = K, V, table, length, refs, free_bits
+
+    @classmethod
+    def empty(cls, n_layers, n_pages, page, n_kv, d, n_seqs, max_pages, dtype=torch.bfloat16, device="cuda"):
+        """A new cache without tokens; K and V are left as they come."""
+        def i32(*shape):
+            return torch.empty(shape, dtype=torch.int32, device=device)
+        kv = cls(torch.empty((n_layers, n_pages, n_kv, page // 16, d // 8, 16, 8), dtype=dtype, device=device),
+                 torch.empty((n_layers, n_pages, n_kv, page // 8, d, 8), dtype=dtype, device=device),
+                 i32(n_seqs, max_pages), i32(n_seqs), i32(n_pages), i32((n_pages + 31) // 32))
+        kv_clear(kv)
+        return kv
+
+    def c(self) -> _KV:
+        return _KV(self.n_layers, self.n_pages, self.page, self.n_kv, self.d, self.dtype, self.n_seqs, self.max_pages, _ptr(self.K),
+                   _ptr(self.V), _ptr(self.table), _ptr(self.len), _ptr(self.refs), _ptr(self.free_bits))
+
+
+def _rows_of(t, kv, heads, what):
+    """Row stride of [rows][heads][d] rows, whose heads stand side by side."""
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != kv.d or _dtype_code(t) != kv.dtype:
+        raise ValueError(f"{what}: [rows][{heads}][{kv.d}] of the cache's dtype is wanted, got {tuple(t.shape)} {t.dtype}")
+    if t.shape[0] and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != kv.d)):
+        raise ValueError(f"{what}: a row's heads have to stand side by side, strides are {t.stride()}")
+    return t.stride(0) if t.shape[0] > 1 else max(heads * kv.d, t.stride(0))
+
+
+def _ints(t, n, what):
+    if t is not None and (t.dtype != torch.int32 or t.numel() != n or not t.is_contiguous()):
+        raise ValueError(f"{what}: contiguous int32 of {n} elements is wanted")
+    return t
+
+
+def kv_workspace(kv: KV):
+    """Workspace of kv_reserve and kv_compact."""
+    return torch.empty(max(int(lib().parse_kv_workspace_bytes(C.byref(kv.c()))), 256), dtype=torch.uint8, device=kv.K.device)
+
+
+def kv_clear(kv: KV):
+    """parse_kv_clear."""
+    _check(_calls.parse_kv_clear(kv, _stream()), "parse_kv_clear")
+
+
+def kv_fork(kv: KV, src, dst):
+    """parse_kv_fork: rows dst of the table become rows src, all at once."""
+    n = src.numel()
+    _check(_calls.parse_kv_fork(kv, _ints(src, n, "src"), _ints(dst, n, "dst"), n, _stream()), "parse_kv_fork")
+
+
+def kv_reserve(kv: KV, n_new, served=None, workspace=None):
+    """parse_kv_reserve: room for n_new[s] more tokens of every sequence -> served [n_seqs]."""
+    if served is None:
+        served = torch.empty(kv.n_seqs, dtype=torch.int32, device=kv.K.device)
+    if workspace is None:
+        workspace = kv_workspace(kv)
+    _check(_calls.parse_kv_reserve(kv, _ints(n_new, kv.n_seqs, "n_new"), _ints(served, kv.n_seqs, "served"), workspace, workspace.numel(),
+                                   _stream()), "parse_kv_reserve")
+    return served
+
+
+def kv_trim(kv: KV, keep=None, window: int = 0, sinks: int = 0):
+    """parse_kv_trim: shortens sequences to keep[s] tokens and gives up what no later token sees."""
+    _check(_calls.parse_kv_trim(kv, _ints(keep, kv.n_seqs, "keep"), window, sinks, _stream()), "parse_kv_trim")
+
+
+def kv_compact(kv: KV, n_live=None, workspace=None):
+    """parse_kv_compact: pages in use move to the ids below their number -> n_live [1]."""
+    if n_live is None:
+        n_live = torch.empty(1, dtype=torch.int32, device=kv.K.device)
+    if workspace is None:
+        workspace = kv_workspace(kv)
+    _check(_calls.parse_kv_compact(kv, _ints(n_live, 1, "n_live"), workspace, workspace.numel(), _stream()), "parse_kv_compact")
+    return n_live
+
+
+def kv_append(kv: KV, layer: int, k, v, tok_offsets=None, seqs=None, q=None, q_out=None, rope=None):
+    """parse_kv_append: k, v [rows][n_kv][d] into the pages of the sequences' last tokens; q [rows][n_q][d] and k rotated
+    by position where rope [n_pos][d] is given.  Returns q_out (None without q)."""
+    rows = k.shape[0]
+    P = rows if tok_offsets is None else tok_offsets.numel() - 1
+    if v.shape[0] != rows:
+        raise ValueError("k and v of one number of rows are wanted")
+    n_q, q_stride, out_stride = 0, 0, 0
+    if q is not None:
+        n_q = q.shape[1]
+        if q_out is None:
+            q_out = torch.empty((rows, n_q, kv.d), dtype=q.dtype, device=q.device)
+        if q.shape[0] != rows or q_out.shape[0] != rows:
+            raise ValueError("q, q_out and k of one number of rows are wanted")
+        q_stride, out_stride = _rows_of(q, kv, n_q, "q"), _rows_of(q_out, kv, n_q, "q_out")
+    n_pos = 0
+    if rope is not None:
+        n_pos = rope.shape[0]
+        if rope.dtype != torch.float32 or rope.shape != (n_pos, kv.d) or not rope.is_contiguous():
+            raise ValueError(f"rope: contiguous float32 [positions][{kv.d}] is wanted")
+    _check(_calls.parse_kv_append(kv, layer, k, _rows_of(k, kv, kv.n_kv, "k"), v, _rows_of(v, kv, kv.n_kv, "v"), q, q_stride, q_out, out_stride,
+                                  n_q, rows, _ints(tok_offsets, P + 1, "tok_offsets"), _ints(seqs, P, "seqs"), P, rope, n_pos, _stream()),
+           "parse_kv_append")
+    return q_out
+
+
+def _attend_out(kv, q, out, lse, with_lse):
+    rows, n_q = q.shape[0], q.shape[1]
+    if out is None:
+        out = torch.empty((rows, n_q, kv.d), dtype=q.dtype, device=q.device)
+    if out.shape[0] != rows:
+        raise ValueError("out has as many rows as q")
+    if lse is None and with_lse:
+        lse = torch.empty((rows, n_q), dtype=torch.float32, device=q.device)
+    if lse is not None and (lse.dtype != torch.float32 or lse.numel() != rows * n_q or not lse.is_contiguous()):
+        raise ValueError(f"lse: contiguous float32 [{rows}][{n_q}] is wanted")
+    return rows, n_q, out, lse
+
+
+def attend_decode_workspace(kv: KV, n_q: int, rows: int):
+    need = int(lib().parse_attend_decode_workspace_bytes(C.byref(kv.c()), n_q, rows))
+    return torch.empty(max(need, 256), dtype=torch.uint8, device=kv.K.device)
+
+
+def attend_decode(kv: KV, layer: int, q, seqs=None, scale=None, window: int = 0, sinks: int = 0, out=None, lse=None, with_lse=False,
+                  workspace=None):
+    """parse_attend_decode: q [rows][n_q][d], the last token of each sequence -> out [rows][n_q][d] (with_lse: and lse
+    [rows][n_q]).  scale: d ** -0.5 where it is not given."""
+    rows, n_q, out, lse = _attend_out(kv, q, out, lse, with_lse)
+    if workspace is None:
+        workspace = attend_decode_workspace(kv, n_q, rows)
+    _check(_calls.parse_attend_decode(kv, layer, q, _rows_of(q, kv, n_q, "q"), n_q, rows, _ints(seqs, rows, "seqs"),
+                                      kv.d ** -0.5 if scale is None else scale, window, sinks, out, _rows_of(out, kv, n_q, "out"), lse,
+                                      workspace, workspace.numel(), _stream()), "parse_attend_decode")
+    return (out, lse) if with_lse else out
+
+
+def attend_prefill_workspace(kv: KV, n_q: int, rows: int, P: int):
+    need = int(lib().parse_attend_prefill_workspace_bytes(C.byref(kv.c()), n_q, rows, P))
+    return torch.empty(max(need, 256), dtype=torch.uint8, device=kv.K.device)
+
+
+def attend_prefill(kv: KV, layer: int, q, tok_offsets=None, seqs=None, scale=None, window: int = 0, sinks: int = 0, out=None, lse=None,
+                   with_lse=False, workspace=None):
+    """parse_attend_prefill: q [rows][n_q][d], the last tokens of each prompt's sequence -> out (with_lse: and lse), as
+    attend_decode."""
+    rows, n_q, out, lse = _attend_out(kv, q, out, lse, with_lse)
+    P = rows if tok_offsets is None else tok_offsets.numel() - 1
+    if workspace is None:
+        workspace = attend_prefill_workspace(kv, n_q, rows, P)
+    _check(_calls.parse_attend_prefill(kv, layer, q, _rows_of(q, kv, n_q, "q"), n_q, rows, _ints(tok_offsets, P + 1, "tok_offsets"),
+                                       _ints(seqs, P, "seqs"), P, kv.d ** -0.5 if scale is None else scale, window, sinks, out,
+                                       _rows_of(out, kv, n_q, "out"), lse, workspace, workspace.numel(), _stream()),
+           "parse_attend_prefill")
+    return (out, lse) if with_lse else out

@@ -1,0 +1,202 @@
+// What the kernels of the paged cache and of the attention over it share: reading the table, which positions a row sees, the
+// operands of the matrix instructions in bf16 and fp32, ragged batches.
+#pragma once
+#include "common.hpp"
+#include "prefill_common.hpp"
+
+namespace parse {
+
+constexpr int KV_MAXSEQ = 4096;              // sequences of a table, prompts or sequences of a call
+constexpr int KV_MAXTOKENS = 1 << 25;        // tokens that a table's row can name: counts of tiles over 4096 rows stay in 31 bits
+
+constexpr int KV_MAXROWS = 1 << 24;          // rows times the heads that share a kv head: their tiles stay countable also where offsets go back and forth
+
+int check_kv(const parse_kv *kv, bool counts);
+
+// a row's sequence: the table's row and its length; nothing where the number is out of range
+struct KvSeq {
+  int row, len;
+};
+__device__ __forceinline__ KvSeq kv_seq(const parse_kv &kv, const int32_t *__restrict__ seqs, int p) {
+  const int s = seqs ? seqs[p] : p;
+  if (s < 0 || s >= kv.n_seqs) return KvSeq{0, 0};
+  return KvSeq{s, min(max(kv.len[s], 0), kv.max_pages * kv.page)};
+}
+
+// rows of a prompt, clamped to the batch
+struct KvRows {
+  int first, n;
+};
+__device__ __forceinline__ KvRows kv_rows(const int32_t *__restrict__ tok_offsets, int p, int rows) {
+  if (!tok_offsets) return KvRows{p, p < rows ? 1 : 0};
+  const int a = min(max(tok_offsets[p], 0), rows), b = min(max(tok_offsets[p + 1], 0), rows);
+  return KvRows{a, max(b - a, 0)};
+}
+
+// Whether a row sees position j: j <= i and j >= lo or j < sinks, with lo the first position of its window.  Without branches: one
+// select per score.
+__device__ __forceinline__ int kv_window_begin(int i, int window) { return window > 0 ? max(i - window + 1, 0) : 0; }
+__device__ __forceinline__ bool kv_sees(int i, int lo, int sinks, int j) { return (j <= i) & ((j >= lo) | (j < sinks)); }
+
+// The positions that rows at [i0, i1] see, in tiles of `tile` tokens: the tiles of the sinks, then those from the first
+// row's window (all, without one) to i1.  Tile number t of them begins at token at(t) * tile.
+struct KvSpan {
+  int sink_tiles, skip, count;
+  __device__ __forceinline__ int at(int t) const { return t < sink_tiles ? t : t + skip; }
+};
+__device__ __forceinline__ KvSpan kv_span(int i0, int i1, int window, int sinks, int tile) {
+  KvSpan s{0, 0, 0};
+  if (i1 < 0) return s;
+  const int lo = kv_window_begin(i0, window);
+  const int from = lo / tile, to = i1 / tile + 1;
+  s.sink_tiles = (int)min(((int64_t)sinks + tile - 1) / tile, (int64_t)from);
+  s.skip = from - s.sink_tiles;
+  s.count = s.sink_tiles + to - from;
+  return s;
+}
+// pre[p] = sum of count(0) .. count(p - 1) for p = 0 .. P, by a whole workgroup; `wave_sums`: one int per wavefront, LDS
+template <int THREADS, class F>
+__device__ __forceinline__ void kv_prefix(int P, int *pre, int *wave_sums, F count) {
+  const int per = (P + THREADS - 1) / THREADS, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int mine = 0;
+  for (int i = 0; i < per; ++i) {
+    const int p = tid * per + i;
+    if (p < P) { const int c = count(p); pre[p] = mine; mine += c; }
+  }
+  int inc = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int v = __shfl_up(inc, o, 64);
+    if (lane >= o) inc += v;
+  }
+  if (lane == 63) wave_sums[wave] = inc;
+  __syncthreads();
+  int base = inc - mine;
+  for (int w = 0; w < wave; ++w) base += wave_sums[w];
+  for (int i = 0; i < per; ++i) {
+    const int p = tid * per + i;
+    if (p < P) pre[p] += base;
+  }
+  if (tid == THREADS - 1) pre[P] = base + mine;
+  __syncthreads();
+}
+// largest p in [0, P) with pre[p] <= v: the element that v belongs to (v < pre[P]; empty ones are passed over)
+__device__ __forceinline__ int kv_find(const int *pre, int P, int v) {
+  int lo = 0, hi = P - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (pre[mid] <= v) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+
+// Eight consecutive values of a lane's operand row (columns of K, tokens of V).  bf16: one operand of a 16x16x32 or 32x32x16
+// instruction; fp32: eight steps of 16x16x4 or 32x32x2, step e with every lane's value e.  Lane layouts are the same: operand
+// row lane % M, the eight reduction indices 8 * (lane / M) + e.
+template <class T> struct Op;
+template <> struct Op<uint16_t> {
+  typedef u32x4 frag;
+  static __device__ __forceinline__ frag zero() { return u32x4{0, 0, 0, 0}; }
+  static __device__ __forceinline__ frag load(const uint16_t *p) { return *reinterpret_cast<const u32x4 *>(p); }
+  static __device__ __forceinline__ f32x4 mma16(frag a, frag b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ f32x16 mma32(frag a, frag b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
+  }
+  // weights in [0, 2^8]: rounded to bf16, 2^-8 relative at most, independent from token to token
+  static __device__ __forceinline__ frag pack(const float *p) {
+    return u32x4{cvt_pk_bf16(p[0], p[1]), cvt_pk_bf16(p[2], p[3]), cvt_pk_bf16(p[4], p[5]), cvt_pk_bf16(p[6], p[7])};
+  }
+  // values whose bit of `keep` is clear become 0
+  static __device__ __forceinline__ frag only(frag a, uint32_t keep) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) a[w] &= (keep >> (2 * w) & 1 ? 0xffffu : 0u) | (keep >> (2 * w + 1) & 1 ? 0xffff0000u : 0u);
+    return a;
+  }
+  // infinities and NaN become 0; true if there was one
+  static __device__ __forceinline__ bool finite_only(frag &a) {
+    uint32_t bad = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const uint32_t m = ((a[w] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((a[w] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+      a[w] &= ~m;
+      bad |= m;
+    }
+    return bad != 0;
+  }
+  static __device__ __forceinline__ float value(uint16_t b) { return bf16_to_f32(b); }
+  static __device__ __forceinline__ bool finite(uint16_t b) { return (b & 0x7f80u) != 0x7f80u; }
+  static __device__ __forceinline__ void store4(uint16_t *p, float a, float b, float c, float d) {
+    *reinterpret_cast<u32x2 *>(p) = u32x2{cvt_pk_bf16(a, b), cvt_pk_bf16(c, d)};
+  }
+};
+struct f32x8_2 {
+  f32x4 lo, hi;
+};
+template <> struct Op<float> {
+  typedef f32x8_2 frag;
+  static __device__ __forceinline__ frag zero() { return frag{f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}}; }
+  static __device__ __forceinline__ frag load(const float *p) {
+    return frag{*reinterpret_cast<const f32x4 *>(p), *reinterpret_cast<const f32x4 *>(p + 4)};
+  }
+  static __device__ __forceinline__ f32x4 mma16(frag a, frag b, f32x4 c) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.lo[e], b.lo[e], c, 0, 0, 0);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.hi[e], b.hi[e], c, 0, 0, 0);
+    return c;
+  }
+  static __device__ __forceinline__ f32x16 mma32(frag a, frag b, f32x16 c) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.lo[e], b.lo[e], c, 0, 0, 0);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.hi[e], b.hi[e], c, 0, 0, 0);
+    return c;
+  }
+  static __device__ __forceinline__ frag pack(const float *p) { return frag{f32x4{p[0], p[1], p[2], p[3]}, f32x4{p[4], p[5], p[6], p[7]}}; }
+  static __device__ __forceinline__ frag only(frag a, uint32_t keep) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      a.lo[e] = keep >> e & 1 ? a.lo[e] : 0.f;
+      a.hi[e] = keep >> (e + 4) & 1 ? a.hi[e] : 0.f;
+    }
+    return a;
+  }
+  static __device__ __forceinline__ bool finite_only(frag &a) {
+    bool bad = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (!finite(a.lo[e])) { a.lo[e] = 0.f; bad = true; }
+      if (!finite(a.hi[e])) { a.hi[e] = 0.f; bad = true; }
+    }
+    return bad;
+  }
+  static __device__ __forceinline__ float value(float v) { return v; }
+  static __device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u; }
+  static __device__ __forceinline__ void store4(float *p, float a, float b, float c, float d) { *reinterpret_cast<f32x4 *>(p) = f32x4{a, b, c, d}; }
+};
+
+// max / sum with the lane 16 or 32 further on (and back): one lane swap instead of a trip through LDS
+template <int N> __device__ __forceinline__ u32x2 lane_swap(float v) {
+  const uint32_t u = __float_as_uint(v);
+  if constexpr (N == 16) return __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  else return __builtin_amdgcn_permlane32_swap(u, u, false, false);
+}
+template <int N> __device__ __forceinline__ float lane_max(float v) {
+  const u32x2 s = lane_swap<N>(v);
+  return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+}
+template <int N> __device__ __forceinline__ float lane_sum(float v) {
+  const u32x2 s = lane_swap<N>(v);
+  return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+
+// The running maximum of a softmax may lag behind by this much, in powers of two: weights stay below 2^8, and the sums are
+// multiplied over only where a maximum grows by more (the first tile of a row, then hardly ever).
+constexpr float AT_LAG = 8.f;
+// 2^x of the vector unit: one rounding; below 2^-126 it is 0
+__device__ __forceinline__ float at_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float finite_or_0(float m) { return m == -INFINITY ? 0.f : m; }
+
+}  // namespace parse

@@ -2,7 +2,7 @@
 // A step of a short prompt is eight launches of 2 us, and ctypes took as long as they do: 2-3 us to convert sixteen arguments, 1-2 us for
 // every parse_layer / parse_patterns built field by field.  Here an argument is converted by its C type:
 //   pointer          None or an object with data_ptr() (a tensor); an integer only for the two handles, the cache's and (last) the stream's
-//   parse_layer *, parse_patterns *    an object with the structure's fields as attributes; in the calls of several layers (SEVERAL) a sequence
+//   parse_layer *, parse_patterns *, parse_kv *    an object with the structure's fields as attributes; in the calls of several layers (SEVERAL) a sequence
 //                    of up to four of them
 //   void *const *    a sequence of up to four tensors
 //   int32_t, size_t  an integer (the low bits, as ctypes does);  float  a number
@@ -19,7 +19,8 @@
 namespace {
 
 PyObject *s_data_ptr, *s_n, *s_m, *s_R, *s_G, *s_dtype, *s_layout, *s_Vt, *s_Ut, *s_Vt_S, *s_Ut_S, *s_subsets, *s_subset_stride, *s_n_patterns, *s_k,
-    *s_Vt_shared, *s_Ut_shared, *s_n_shared, *s_schedule;
+    *s_Vt_shared, *s_Ut_shared, *s_n_shared, *s_schedule, *s_n_layers, *s_n_pages, *s_page, *s_n_kv, *s_d, *s_n_seqs, *s_max_pages, *s_K, *s_V, *s_table,
+    *s_len, *s_refs, *s_free_bits;
 
 bool to_int(PyObject *o, int64_t *v) {
   if (PyLong_Check(o)) {
@@ -89,6 +90,12 @@ bool to_struct(PyObject *o, parse_patterns *p) {
          pointer_field(o, s_Vt_shared, &p->Vt_shared) && pointer_field(o, s_Ut_shared, &p->Ut_shared) && int_field(o, s_n_shared, &p->n_shared) &&
          int_field(o, s_schedule, &p->schedule);
 }
+bool to_struct(PyObject *o, parse_kv *c) {
+  return int_field(o, s_n_layers, &c->n_layers) && int_field(o, s_n_pages, &c->n_pages) && int_field(o, s_page, &c->page) && int_field(o, s_n_kv, &c->n_kv) &&
+         int_field(o, s_d, &c->d) && int_field(o, s_dtype, &c->dtype) && int_field(o, s_n_seqs, &c->n_seqs) && int_field(o, s_max_pages, &c->max_pages) &&
+         pointer_field(o, s_K, &c->K, to_tensor) && pointer_field(o, s_V, &c->V, to_tensor) && pointer_field(o, s_table, &c->table, to_tensor) &&
+         pointer_field(o, s_len, &c->len, to_tensor) && pointer_field(o, s_refs, &c->refs) && pointer_field(o, s_free_bits, &c->free_bits);
+}
 bool to_struct(PyObject *o, void **p) { return to_tensor(o, p); }
 
 constexpr Py_ssize_t kMost = 4;              // layers of a call
@@ -130,6 +137,7 @@ struct Many {
 };
 template <bool SEVERAL> struct Arg<const parse_layer *, SEVERAL> : std::conditional_t<SEVERAL, Many<parse_layer>, One<parse_layer>> {};
 template <bool SEVERAL> struct Arg<const parse_patterns *, SEVERAL> : std::conditional_t<SEVERAL, Many<parse_patterns>, One<parse_patterns>> {};
+template <bool SEVERAL> struct Arg<const parse_kv *, SEVERAL> : One<parse_kv> {};
 template <> struct Arg<void *const *, true> : Many<void *> {};
 template <class T, bool SEVERAL>
 struct Arg<T *, SEVERAL> {
@@ -183,6 +191,8 @@ PyMethodDef methods[] = {
     CALL(parse_bucket_patterns), CALL(parse_bucket_and_plan), CALL(parse_prefill_plan), CALL(parse_pack_patterns), CALL(parse_pack_new_entries),
     CALL(parse_pack_ranks), CALL(parse_lowrank_forward), CALL(parse_lowrank_prefill_planned), CALL_SEVERAL(parse_lowrank_prefill_multi),
     CALL_SEVERAL(parse_lowrank_decode_planned), CALL_SEVERAL(parse_lowrank_decode_multi), CALL(parse_router_grad),
+    CALL(parse_kv_clear), CALL(parse_kv_fork), CALL(parse_kv_reserve), CALL(parse_kv_trim), CALL(parse_kv_compact), CALL(parse_kv_append),
+    CALL(parse_attend_decode), CALL(parse_attend_prefill),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
@@ -193,7 +203,9 @@ PyMODINIT_FUNC PyInit__calls(void) {
   const struct { PyObject **to; const char *name; } names[] = {
       {&s_data_ptr, "data_ptr"}, {&s_n, "n"}, {&s_m, "m"}, {&s_R, "R"}, {&s_G, "G"}, {&s_dtype, "dtype"}, {&s_layout, "layout"}, {&s_Vt, "Vt"}, {&s_Ut, "Ut"},
       {&s_Vt_S, "Vt_S"}, {&s_Ut_S, "Ut_S"}, {&s_subsets, "subsets"}, {&s_subset_stride, "subset_stride"}, {&s_n_patterns, "n_patterns"}, {&s_k, "k"},
-      {&s_Vt_shared, "Vt_shared"}, {&s_Ut_shared, "Ut_shared"}, {&s_n_shared, "n_shared"}, {&s_schedule, "schedule"}};
+      {&s_Vt_shared, "Vt_shared"}, {&s_Ut_shared, "Ut_shared"}, {&s_n_shared, "n_shared"}, {&s_schedule, "schedule"},
+      {&s_n_layers, "n_layers"}, {&s_n_pages, "n_pages"}, {&s_page, "page"}, {&s_n_kv, "n_kv"}, {&s_d, "d"}, {&s_n_seqs, "n_seqs"}, {&s_max_pages, "max_pages"},
+      {&s_K, "K"}, {&s_V, "V"}, {&s_table, "table"}, {&s_len, "len"}, {&s_refs, "refs"}, {&s_free_bits, "free_bits"}};
   for (const auto &n : names)
     if (!(*n.to = PyUnicode_InternFromString(n.name))) return nullptr;
   return PyModule_Create(&module);

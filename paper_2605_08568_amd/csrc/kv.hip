@@ -1,0 +1,510 @@
+// The paged key-value cache: its bookkeeping (clear, fork, reserve, trim, compact), the copies of pages, and the rows' way in.
+#include <algorithm>
+
+#include "attend.hpp"
+
+namespace parse {
+
+constexpr int KV_THREADS = 256, KV_ONE = 1024;       // of a workgroup among others, of one alone
+constexpr int KV_MAXFORK = 1024, KV_FORK_COLUMNS = 8;
+
+int check_kv(const parse_kv *kv, bool counts) {
+  if (!kv || !kv->K || !kv->V || !kv->table || !kv->len) return PARSE_EINVAL;
+  if (kv->dtype != PARSE_F32 && kv->dtype != PARSE_BF16) return PARSE_EINVAL;
+  if (kv->n_layers <= 0 || kv->n_pages <= 0 || kv->n_kv <= 0 || kv->n_seqs <= 0 || kv->max_pages <= 0) return PARSE_EINVAL;
+  if (counts && (!kv->refs || !kv->free_bits)) return PARSE_EINVAL;
+  if (kv->page != 16 && kv->page != 32 && kv->page != 64 && kv->page != 128 && kv->page != 256) return PARSE_ESHAPE;
+  if (kv->d < 32 || kv->d > 256 || kv->d % 32 != 0 || kv->n_kv > 1024 || kv->n_seqs > KV_MAXSEQ) return PARSE_ESHAPE;
+  if ((int64_t)kv->max_pages * kv->page > KV_MAXTOKENS) return PARSE_ESHAPE;
+  if (!aligned16(kv->K) || !aligned16(kv->V) || !aligned16(kv->table) || !aligned16(kv->len) || !aligned16(kv->refs) || !aligned16(kv->free_bits))
+    return PARSE_EALIGN;
+  return PARSE_OK;
+}
+
+// One user more or less.  The thread that takes the last user away (gives the first one) turns the page's bit.
+__device__ __forceinline__ void page_take(const parse_kv &kv, int id) {
+  if (atomicAdd(&kv.refs[id], 1) == 0) atomicAnd(&kv.free_bits[id >> 5], ~(1u << (id & 31)));
+}
+__device__ __forceinline__ void page_give(const parse_kv &kv, int id) {
+  if (atomicSub(&kv.refs[id], 1) == 1) atomicOr(&kv.free_bits[id >> 5], 1u << (id & 31));
+}
+__device__ __forceinline__ bool page_ok(const parse_kv &kv, int id) { return id >= 0 && id < kv.n_pages; }
+
+__device__ __forceinline__ uint32_t page_bits(const parse_kv &kv, int w) { return kv.n_pages - w * 32 >= 32 ? 0xffffffffu : (1u << (kv.n_pages - w * 32)) - 1u; }
+__device__ __forceinline__ uint32_t free_word(const parse_kv &kv, int w) { return kv.free_bits[w] & page_bits(kv, w); }
+
+__global__ __launch_bounds__(KV_THREADS) void kv_clear(parse_kv kv) {
+  const int64_t first = (int64_t)blockIdx.x * KV_THREADS + threadIdx.x, step = (int64_t)gridDim.x * KV_THREADS;
+  for (int64_t e = first; e < (int64_t)kv.n_seqs * kv.max_pages; e += step) kv.table[e] = -1;
+  for (int64_t e = first; e < kv.n_seqs; e += step) kv.len[e] = 0;
+  for (int64_t e = first; e < kv.n_pages; e += step) kv.refs[e] = 0;
+  for (int64_t e = first; e < (kv.n_pages + 31) / 32; e += step) kv.free_bits[e] = page_bits(kv, (int)e);
+}
+
+// Workgroup = eight columns of the table: all sources into LDS, then the destinations.  A page stands in one column only, so
+// that no other workgroup counts its users; users come before users go, so that no page is free in between.
+__global__ __launch_bounds__(KV_THREADS) void kv_fork(parse_kv kv, const int32_t *__restrict__ src, const int32_t *__restrict__ dst, int n) {
+  extern __shared__ int moved[];                                   // [n][columns], then [n] lengths
+  const int c0 = blockIdx.x * KV_FORK_COLUMNS, cols = min(KV_FORK_COLUMNS, kv.max_pages - c0);
+  auto pair = [&](int i, int &s, int &d) {
+    s = src[i]; d = dst[i];
+    return s >= 0 && s < kv.n_seqs && d >= 0 && d < kv.n_seqs;
+  };
+  int s, d;
+  for (int e = threadIdx.x; e < n * KV_FORK_COLUMNS; e += KV_THREADS) {
+    const int i = e / KV_FORK_COLUMNS, c = e % KV_FORK_COLUMNS;
+    if (c >= cols || !pair(i, s, d)) continue;
+    const int id = kv.table[(int64_t)s * kv.max_pages + c0 + c];
+    moved[e] = id;
+    if (s != d && page_ok(kv, id)) page_take(kv, id);
+    if (c == 0 && blockIdx.x == 0) moved[n * KV_FORK_COLUMNS + i] = kv.len[s];
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < n * KV_FORK_COLUMNS; e += KV_THREADS) {
+    const int i = e / KV_FORK_COLUMNS, c = e % KV_FORK_COLUMNS;
+    if (c >= cols || !pair(i, s, d)) continue;
+    if (s == d) continue;
+    int32_t *to = kv.table + (int64_t)d * kv.max_pages + c0 + c;
+    const int old = *to;
+    *to = moved[e];
+    if (page_ok(kv, old)) page_give(kv, old);
+    if (c == 0 && blockIdx.x == 0) kv.len[d] = moved[n * KV_FORK_COLUMNS + i];
+  }
+}
+
+// Workgroup = one sequence.
+__global__ __launch_bounds__(KV_THREADS) void kv_trim(parse_kv kv, const int32_t *__restrict__ keep, int window, int sinks) {
+  const int s = blockIdx.x, held = kv.len[s], most = kv.max_pages * kv.page;
+  const int len = min(min(max(held, 0), most), keep ? max(keep[s], 0) : most);
+  __syncthreads();                                                 // everybody has read the length
+  int32_t *row = kv.table + (int64_t)s * kv.max_pages;
+  for (int c = threadIdx.x; c < kv.max_pages; c += KV_THREADS) {
+    const int id = row[c], a = c * kv.page, b = a + kv.page;
+    if (id == -1) continue;
+    if (a >= len || (window > 0 && a >= sinks && b <= len - window + 1)) {
+      row[c] = -1;
+      if (page_ok(kv, id)) page_give(kv, id);
+    }
+  }
+  if (threadIdx.x == 0 && len != held) kv.len[s] = len;
+}
+
+// ---- workspace of reserve and compact: number of copies, then the copies {from, to}, then a list of page ids
+struct KvWork {
+  int32_t *count;
+  int2 *copies;                                                    // [n_pages] at most
+  int32_t *ids;                                                    // [n_pages]
+};
+static size_t kv_work_bytes(const parse_kv *kv) { return 16 + round_up((size_t)kv->n_pages * 8, 16) + round_up((size_t)kv->n_pages * 4, 16); }
+static KvWork kv_work(const parse_kv *kv, void *ws) {
+  char *p = (char *)ws;
+  return KvWork{(int32_t *)p, (int2 *)(p + 16), (int32_t *)(p + 16 + round_up((size_t)kv->n_pages * 8, 16))};
+}
+
+// exclusive sum over the threads of a workgroup alone; `sums`: one int per wavefront, LDS.  Returns this thread's, and the total.
+__device__ __forceinline__ int sum_before(int mine, int *sums, int &total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int inc = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int v = __shfl_up(inc, o, 64);
+    if (lane >= o) inc += v;
+  }
+  __syncthreads();
+  if (lane == 63) sums[wave] = inc;
+  __syncthreads();
+  int base = 0, all = 0;
+  for (int w = 0; w < KV_ONE / 64; ++w) {
+    if (w < wave) base += sums[w];
+    all += sums[w];
+  }
+  total = all;
+  return base + inc - mine;
+}
+
+// One workgroup.  A thread has `per` consecutive sequences, then `words` consecutive words of the free pages.
+__global__ __launch_bounds__(KV_ONE) void kv_reserve(parse_kv kv, const int32_t *__restrict__ n_new, int32_t *__restrict__ served, KvWork ws) {
+  __shared__ int begun[KV_MAXSEQ], last[KV_MAXSEQ], sums[KV_ONE / 64];
+  const int tid = threadIdx.x, per = (kv.n_seqs + KV_ONE - 1) / KV_ONE, page = kv.page, most = kv.max_pages * page;
+  constexpr int PER = KV_MAXSEQ / KV_ONE;
+  int len[PER], more[PER], need[PER], mine = 0, total;
+  // begun[s]: the page that the next token of s goes to, if it has other users
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int s = tid * per + i;
+    len[i] = more[i] = need[i] = 0;
+    if (i >= per || s >= kv.n_seqs) continue;
+    len[i] = min(max(kv.len[s], 0), most);
+    more[i] = max(n_new[s], 0);
+    if (more[i] > most - len[i]) more[i] = 0;
+    begun[s] = -1;
+    if (more[i] > 0) {
+      need[i] = (len[i] + more[i] + page - 1) / page - (len[i] + page - 1) / page;
+      if (len[i] % page != 0) {
+        const int id = kv.table[(int64_t)s * kv.max_pages + len[i] / page];
+        if (!page_ok(kv, id)) begun[s] = -2;                       // no page where one should be: a new one, nothing to copy
+        else if (kv.refs[id] > 1) begun[s] = id;
+      }
+    }
+  }
+  __syncthreads();
+  bool copy[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int s = tid * per + i;
+    copy[i] = false;
+    if (i >= per || s >= kv.n_seqs) continue;
+    const int id = begun[s];
+    if (id >= 0) {                                                 // the users before it have taken their copies
+      int before = 0;
+      for (int e = 0; e < s; ++e) before += begun[e] == id ? 1 : 0;
+      copy[i] = kv.refs[id] - before > 1;
+    }
+    need[i] += copy[i] || id == -2 ? 1 : 0;
+    mine += need[i];
+  }
+  int at = sum_before(mine, sums, total);
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int s = tid * per + i;
+    if (i >= per || s >= kv.n_seqs) continue;
+    at += need[i];
+    last[s] = at;                                                  // pages that the sequences up to s take
+  }
+  __syncthreads();                                                 // users are counted no more: they may change
+  // the free pages in ascending order
+  const int n_words = (kv.n_pages + 31) / 32, words = (n_words + KV_ONE - 1) / KV_ONE;
+  int found = 0, free_pages;
+  for (int w = tid * words; w < min((tid + 1) * words, n_words); ++w) found += __popc(free_word(kv, w));
+  int rank = sum_before(found, sums, free_pages);
+  // what is taken: the needs of the sequences before the first one that does not fit
+  int taken;
+  {
+    int lo = 0, hi = kv.n_seqs;                                    // first s with last[s] > free_pages
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (last[mid] > free_pages) hi = mid; else lo = mid + 1;
+    }
+    taken = lo > 0 ? last[lo - 1] : 0;
+  }
+  for (int w = tid * words; w < min((tid + 1) * words, n_words) && rank < taken; ++w) {
+    const uint32_t bits = free_word(kv, w);
+    uint32_t left = bits;
+    while (left && rank < taken) {
+      const int b = __builtin_ctz(left), id = w * 32 + b;
+      left &= left - 1;
+      ws.ids[rank++] = id;
+      kv.refs[id] = 1;
+    }
+    if (left != bits) kv.free_bits[w] = left;
+  }
+  __syncthreads();
+  int copies = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) copies += copy[i] && last[tid * per + i] <= free_pages ? 1 : 0;
+  int n_copies, slot = sum_before(copies, sums, n_copies);
+  if (tid == 0) *ws.count = n_copies;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int s = tid * per + i;
+    if (i >= per || s >= kv.n_seqs) continue;
+    const bool ok = more[i] > 0 && last[s] <= free_pages;
+    if (served) served[s] = ok ? 1 : 0;
+    if (!ok) continue;
+    kv.len[s] = len[i] + more[i];
+    if (copy[i]) {
+      ws.copies[slot++] = int2{begun[s], ws.ids[last[s] - need[i]]};
+      atomicSub(&kv.refs[begun[s]], 1);                            // one user is left at least
+    }
+    begun[s] = copy[i] || begun[s] == -2 ? len[i] / page : (len[i] + page - 1) / page;   // from now on: column of its first new page
+  }
+  __syncthreads();
+  for (int r = tid; r < taken; r += KV_ONE) {
+    int lo = 0, hi = kv.n_seqs - 1;                                // first s with last[s] > r
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (last[mid] > r) hi = mid; else lo = mid + 1;
+    }
+    const int column = begun[lo] + r - (lo > 0 ? last[lo - 1] : 0);
+    kv.table[(int64_t)lo * kv.max_pages + column] = ws.ids[r];
+  }
+}
+
+// One workgroup: which pages in use move where.
+__global__ __launch_bounds__(KV_ONE) void kv_compact(parse_kv kv, int32_t *__restrict__ n_live, KvWork ws) {
+  __shared__ int sums[KV_ONE / 64];
+  const int tid = threadIdx.x, n_words = (kv.n_pages + 31) / 32, words = (n_words + KV_ONE - 1) / KV_ONE;
+  const int w0 = tid * words, w1 = min((tid + 1) * words, n_words);
+  auto used_word = [&](int w) { return ~kv.free_bits[w] & page_bits(kv, w); };
+  auto below = [&](int w, int n) { return n >= (w + 1) * 32 ? 0xffffffffu : n <= w * 32 ? 0u : (1u << (n - w * 32)) - 1u; };   // bits of the ids under n
+  int used = 0, live;
+  for (int w = w0; w < w1; ++w) used += __popc(used_word(w));
+  sum_before(used, sums, live);
+  int holes = 0, movers = 0, n_holes, n_movers;
+  for (int w = w0; w < w1; ++w) {
+    const uint32_t under = below(w, live);
+    holes += __popc(free_word(kv, w) & under);
+    movers += __popc(used_word(w) & ~under);
+  }
+  int hole = sum_before(holes, sums, n_holes), mover = sum_before(movers, sums, n_movers);
+  for (int w = w0; w < w1; ++w)
+    for (uint32_t f = free_word(kv, w) & below(w, live); f; f &= f - 1) ws.copies[hole++].y = w * 32 + __builtin_ctz(f);
+  __syncthreads();
+  for (int w = w0; w < w1; ++w) {
+    for (uint32_t f = used_word(w) & ~below(w, live); f; f &= f - 1) {
+      const int from = w * 32 + __builtin_ctz(f), to = ws.copies[mover].y;
+      ws.copies[mover++].x = from;
+      ws.ids[from] = to;
+      kv.refs[to] = kv.refs[from];
+      kv.refs[from] = 0;
+    }
+  }
+  for (int w = w0; w < w1; ++w) kv.free_bits[w] = page_bits(kv, w) & ~below(w, live);
+  if (tid == 0) {
+    *ws.count = n_movers;
+    ws.count[1] = live;
+    if (n_live) *n_live = live;
+  }
+}
+
+// Copies pages of all layers, K and V, in pieces of 16 KiB; after a compaction the table's entries follow.
+template <bool REMAP>
+__global__ __launch_bounds__(KV_THREADS) void kv_copy(parse_kv kv, KvWork ws, int64_t page_bytes) {
+  const int n = *ws.count;
+  constexpr int PIECE = KV_THREADS * 64;
+  const int pieces = (int)((page_bytes + PIECE - 1) / PIECE);
+  const int64_t total = (int64_t)n * kv.n_layers * 2 * pieces;
+  for (int64_t t = blockIdx.x; t < total; t += gridDim.x) {
+    const int piece = (int)(t % pieces);
+    const int64_t side = t / pieces;
+    const int of_v = (int)(side & 1), layer = (int)((side >> 1) % kv.n_layers);
+    const int2 c = ws.copies[(side >> 1) / kv.n_layers];
+    char *base = (char *)(of_v ? kv.V : kv.K) + (int64_t)layer * kv.n_pages * page_bytes;
+    const char *from = base + c.x * page_bytes;
+    char *to = base + c.y * page_bytes;
+    u32x4 v[4];
+    const int64_t at = (int64_t)piece * PIECE + threadIdx.x * 16;
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (at + u * KV_THREADS * 16 < page_bytes) v[u] = *reinterpret_cast<const u32x4 *>(from + at + u * KV_THREADS * 16);
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (at + u * KV_THREADS * 16 < page_bytes) *reinterpret_cast<u32x4 *>(to + at + u * KV_THREADS * 16) = v[u];
+  }
+  if (REMAP) {
+    const int live = ws.count[1];
+    const int64_t entries = (int64_t)kv.n_seqs * kv.max_pages;
+    for (int64_t e = (int64_t)blockIdx.x * KV_THREADS + threadIdx.x; e < entries; e += (int64_t)gridDim.x * KV_THREADS) {
+      const int id = kv.table[e];
+      if (id >= live && id < kv.n_pages) kv.table[e] = ws.ids[id];
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------
+struct KaArgs {
+  parse_kv kv;
+  void *K, *V;                                       // of the layer
+  const void *k, *v, *q;
+  void *q_out;
+  int64_t k_stride, v_stride, q_stride, q_out_stride;
+  const int32_t *tok_offsets, *seqs;
+  const float *rope;
+  int n_q, rows, P, n_pos;
+};
+
+// eight values as floats, and back with one rounding
+__device__ __forceinline__ void load8(const uint16_t *p, float *f) {
+  const u32x4 v = *reinterpret_cast<const u32x4 *>(p);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) { f[2 * w] = __uint_as_float(v[w] << 16); f[2 * w + 1] = __uint_as_float(v[w] & 0xffff0000u); }
+}
+__device__ __forceinline__ void load8(const float *p, float *f) {
+  const f32x4 a = *reinterpret_cast<const f32x4 *>(p), b = *reinterpret_cast<const f32x4 *>(p + 4);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) { f[e] = a[e]; f[4 + e] = b[e]; }
+}
+__device__ __forceinline__ void store8(uint16_t *p, const float *f) { *reinterpret_cast<u32x4 *>(p) = Op<uint16_t>::pack(f); }
+__device__ __forceinline__ void store8(float *p, const float *f) {
+  *reinterpret_cast<f32x4 *>(p) = f32x4{f[0], f[1], f[2], f[3]};
+  *reinterpret_cast<f32x4 *>(p + 4) = f32x4{f[4], f[5], f[6], f[7]};
+}
+
+// Workgroup (x, y) = one block of sixteen positions of a prompt, every gridDim.y-th 256 pieces of its work.  A piece of K or
+// q is 8 columns and their 8 partners of one token; of V 8 columns of 8 tokens, transposed in registers.
+template <class T>
+__global__ __launch_bounds__(KV_THREADS) void kv_append(KaArgs a) {
+  extern __shared__ int smem[];
+  int *wave_sums = smem, *pre = smem + KV_THREADS / 64;
+  const int D = a.kv.d, half = D / 2, pairs = D / 16;               // pairs of pieces in a row
+  // blocks of a prompt: of its positions, and of its rows where they have no place in the cache
+  auto place = [&](int p, KvRows &r, KvSeq &s) {
+    r = kv_rows(a.tok_offsets, p, a.rows);
+    s = kv_seq(a.kv, a.seqs, p);
+    return s.len - r.n;
+  };
+  kv_prefix<KV_THREADS>(a.P, pre, wave_sums, [&](int p) {
+    KvRows r; KvSeq s;
+    const int base = place(p, r, s);
+    return r.n == 0 ? 0 : ((base + r.n + 15) >> 4) - (base >> 4);
+  });
+  for (int item = blockIdx.x; item < pre[a.P]; item += gridDim.x) {
+    const int p = kv_find(pre, a.P, item);
+    KvRows pr; KvSeq sq;
+    const int base = place(p, pr, sq);
+    const int block = (base >> 4) + item - pre[p];                 // tokens 16 block + 0..15 of the sequence
+    const int c = block >> (27 - __builtin_clz(a.kv.page));        // 16 block / page
+    int id = block >= 0 && c < a.kv.max_pages ? a.kv.table[(int64_t)sq.row * a.kv.max_pages + c] : -1;
+    if (!page_ok(a.kv, id)) id = -1;
+    // where the block stands for head 0; heads are page * D apart
+    const int64_t spot = (int64_t)max(id, 0) * a.kv.n_kv * a.kv.page * D + (int64_t)((block * 16) & (a.kv.page - 1)) * D;
+    const int n_k = id < 0 ? 0 : a.kv.n_kv * pairs * 16, n_v = id < 0 ? 0 : a.kv.n_kv * (D / 8) * 2, n_q = a.q ? a.n_q * pairs * 16 : 0;
+    auto rotated = [&](const T *row, int piece, int pos, float *lo, float *hi) {
+      load8(row + 8 * piece, lo);
+      load8(row + half + 8 * piece, hi);
+      if (!a.rope) return;
+      const float *t = a.rope + (int64_t)min(max(pos, 0), a.n_pos - 1) * D + 8 * piece;
+      float cs[8], sn[8];
+      load8(t, cs);
+      load8(t + half, sn);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float x = lo[e], y = hi[e];
+        lo[e] = x * cs[e] - y * sn[e];
+        hi[e] = y * cs[e] + x * sn[e];
+      }
+    };
+    for (int w = blockIdx.y * KV_THREADS + threadIdx.x; w < n_k + n_v + n_q; w += gridDim.y * KV_THREADS) {
+      float lo[8], hi[8];
+      if (w < n_k) {                                               // token fastest: 16 pieces of a column block are contiguous in the page
+        const int tok = w & 15, piece = (w >> 4) % pairs, head = (w >> 4) / pairs, row = block * 16 + tok - base;
+        if (row < 0 || row >= pr.n) continue;
+        rotated((const T *)a.k + (pr.first + row) * a.k_stride + (int64_t)head * D, piece, base + row, lo, hi);
+        T *to = (T *)a.K + spot + (int64_t)head * a.kv.page * D + piece * 128 + tok * 8;
+        store8(to, lo);
+        store8(to + half * 16, hi);
+      } else if (w < n_k + n_v) {
+        const int u = w - n_k, piece = u % (D / 8), side = u / (D / 8) & 1, head = u / (D / 8) / 2, row = block * 16 + side * 8 - base;
+        const T *from = (const T *)a.v + (int64_t)head * D + piece * 8;
+        T *to = (T *)a.V + spot + (int64_t)head * a.kv.page * D + (side * D + piece * 8) * 8;
+        if (row >= 0 && row + 8 <= pr.n) {
+          float v[8][8];
+#pragma unroll
+          for (int t = 0; t < 8; ++t) load8(from + (pr.first + row + t) * a.v_stride, v[t]);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float col[8] = {v[0][e], v[1][e], v[2][e], v[3][e], v[4][e], v[5][e], v[6][e], v[7][e]};
+            store8(to + e * 8, col);
+          }
+        } else {
+          for (int t = 0; t < 8; ++t)
+            if (row + t >= 0 && row + t < pr.n)
+              for (int e = 0; e < 8; ++e) to[e * 8 + t] = from[(pr.first + row + t) * a.v_stride + e];
+        }
+      } else {
+        const int u = w - n_k - n_v, piece = u % pairs, head = u / pairs % a.n_q, row = block * 16 + u / pairs / a.n_q - base;
+        if (row < 0 || row >= pr.n) continue;
+        rotated((const T *)a.q + (pr.first + row) * a.q_stride + (int64_t)head * D, piece, base + row, lo, hi);
+        T *to = (T *)a.q_out + (pr.first + row) * a.q_out_stride + (int64_t)head * D + 8 * piece;
+        store8(to, lo);
+        store8(to + half, hi);
+      }
+    }
+  }
+}
+
+}  // namespace parse
+
+extern "C" {
+
+using namespace parse;
+
+int parse_kv_clear(const parse_kv *kv, parse_stream stream) {
+  const int st = check_kv(kv, true);
+  if (st != PARSE_OK) return st;
+  const int64_t most = std::max((int64_t)kv->n_seqs * kv->max_pages, (int64_t)kv->n_pages);
+  kv_clear<<<dim3((uint32_t)std::min<int64_t>((most + KV_THREADS - 1) / KV_THREADS, 2048)), KV_THREADS, 0, (hipStream_t)stream>>>(*kv);
+  PARSE_LAUNCH_CHECK();
+  return PARSE_OK;
+}
+
+int parse_kv_fork(const parse_kv *kv, const int32_t *src, const int32_t *dst, int32_t n, parse_stream stream) {
+  const int st = check_kv(kv, true);
+  if (st != PARSE_OK) return st;
+  if (!src || !dst || n <= 0) return PARSE_EINVAL;
+  if (n > KV_MAXFORK) return PARSE_ESHAPE;
+  if (!aligned16(src) || !aligned16(dst)) return PARSE_EALIGN;
+  kv_fork<<<dim3((kv->max_pages + KV_FORK_COLUMNS - 1) / KV_FORK_COLUMNS), KV_THREADS, (size_t)n * (KV_FORK_COLUMNS + 1) * 4, (hipStream_t)stream>>>(*kv, src, dst, n);
+  PARSE_LAUNCH_CHECK();
+  return PARSE_OK;
+}
+
+int parse_kv_trim(const parse_kv *kv, const int32_t *keep, int32_t window, int32_t sinks, parse_stream stream) {
+  const int st = check_kv(kv, true);
+  if (st != PARSE_OK) return st;
+  if (window < 0 || sinks < 0 || (!keep && window == 0)) return PARSE_EINVAL;
+  if (!aligned16(keep)) return PARSE_EALIGN;
+  kv_trim<<<dim3(kv->n_seqs), KV_THREADS, 0, (hipStream_t)stream>>>(*kv, keep, window, sinks);
+  PARSE_LAUNCH_CHECK();
+  return PARSE_OK;
+}
+
+size_t parse_kv_workspace_bytes(const parse_kv *kv) { return check_kv(kv, false) == PARSE_OK ? kv_work_bytes(kv) : 0; }
+
+static int64_t kv_page_bytes(const parse_kv *kv) { return (int64_t)kv->n_kv * kv->page * kv->d * elem_size(kv->dtype); }
+
+int parse_kv_reserve(const parse_kv *kv, const int32_t *n_new, int32_t *served, void *workspace, size_t workspace_bytes, parse_stream stream) {
+  const int st = check_kv(kv, true);
+  if (st != PARSE_OK) return st;
+  if (!n_new) return PARSE_EINVAL;
+  if (!workspace || workspace_bytes < kv_work_bytes(kv)) return PARSE_EWORKSPACE;
+  if (!aligned16(n_new) || !aligned16(served) || !aligned16(workspace)) return PARSE_EALIGN;
+  const KvWork ws = kv_work(kv, workspace);
+  kv_reserve<<<dim3(1), KV_ONE, 0, (hipStream_t)stream>>>(*kv, n_new, served, ws);
+  PARSE_LAUNCH_CHECK();
+  kv_copy<false><<<dim3(2048), KV_THREADS, 0, (hipStream_t)stream>>>(*kv, ws, kv_page_bytes(kv));
+  PARSE_LAUNCH_CHECK();
+  return PARSE_OK;
+}
+
+int parse_kv_compact(const parse_kv *kv, int32_t *n_live, void *workspace, size_t workspace_bytes, parse_stream stream) {
+  const int st = check_kv(kv, true);
+  if (st != PARSE_OK) return st;
+  if (!workspace || workspace_bytes < kv_work_bytes(kv)) return PARSE_EWORKSPACE;
+  if (!aligned16(workspace) || (((uintptr_t)n_live) & 3u) != 0) return PARSE_EALIGN;
+  const KvWork ws = kv_work(kv, workspace);
+  kv_compact<<<dim3(1), KV_ONE, 0, (hipStream_t)stream>>>(*kv, n_live, ws);
+  PARSE_LAUNCH_CHECK();
+  kv_copy<true><<<dim3(2048), KV_THREADS, 0, (hipStream_t)stream>>>(*kv, ws, kv_page_bytes(kv));
+  PARSE_LAUNCH_CHECK();
+  return PARSE_OK;
+}
+
+int parse_kv_append(const parse_kv *kv, int32_t layer, const void *k, int64_t k_stride, const void *v, int64_t v_stride, const void *q, int64_t q_stride,
+                    void *q_out, int64_t q_out_stride, int32_t n_q, int32_t rows, const int32_t *tok_offsets, const int32_t *seqs, int32_t P,
+                    const float *rope, int32_t n_pos, parse_stream stream) {
+  const int st = check_kv(kv, false);
+  if (st != PARSE_OK) return st;
+  if (!k || !v || rows <= 0 || P <= 0 || layer < 0 || (!q != !q_out) || (q && n_q <= 0) || (rope && n_pos <= 0)) return PARSE_EINVAL;
+  if (layer >= kv->n_layers || P > KV_MAXSEQ || rows > KV_MAXROWS || (!seqs && P > kv->n_seqs) || (!tok_offsets && rows != P)) return PARSE_ESHAPE;
+  const int64_t width = (int64_t)kv->n_kv * kv->d;
+  if (k_stride < width || v_stride < width) return PARSE_ESHAPE;
+  if (q && (n_q > 65536 || q_stride < (int64_t)n_q * kv->d || q_out_stride < (int64_t)n_q * kv->d)) return PARSE_ESHAPE;
+  const int per16 = 16 / elem_size(kv->dtype);
+  if (!aligned16(k) || !aligned16(v) || !aligned16(q) || !aligned16(q_out) || !aligned16(rope) || k_stride % per16 != 0 || v_stride % per16 != 0)
+    return PARSE_EALIGN;
+  if (q && (q_stride % per16 != 0 || q_out_stride % per16 != 0)) return PARSE_EALIGN;
+  const size_t at = (size_t)layer * kv->n_pages * kv_page_bytes(kv);
+  KaArgs a{*kv, (char *)kv->K + at, (char *)kv->V + at, k, v, q, q_out, k_stride, v_stride, q_stride, q_out_stride, tok_offsets, seqs, rope, n_q, rows, P, n_pos};
+  // a prompt's first and last block may be begun only
+  const int64_t blocks = rows / 16 + 2 * (int64_t)std::min(P, rows);
+  const int64_t work = ((int64_t)kv->n_kv * 2 + (q ? n_q : 0)) * kv->d / KV_THREADS + 1;
+  const dim3 grid((uint32_t)std::min<int64_t>(blocks, 65536), (uint32_t)std::min<int64_t>(work, std::max<int64_t>(1, 4096 / blocks)));
+  const size_t lds = (KV_THREADS / 64 + P + 1) * 4;
+  if (kv->dtype == PARSE_BF16) kv_append<uint16_t><<<grid, KV_THREADS, lds, (hipStream_t)stream>>>(a);
+  else kv_append<float><<<grid, KV_THREADS, lds, (hipStream_t)stream>>>(a);
+  PARSE_LAUNCH_CHECK();
+  return PARSE_OK;
+}
+
+}  // extern "C"

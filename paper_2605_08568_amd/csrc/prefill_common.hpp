@@ -4,6 +4,9 @@
 
 namespace parse {
 
+#define PARSE_LDS_PTR(p) ((__attribute__((address_space(3))) void *)(p))
+#define PARSE_GLB_PTR(p) ((const __attribute__((address_space(1))) void *)(p))
+
 constexpr int PF_THREADS = 256;
 constexpr int PF_BK = 64;            // reduction indices per staged X tile (4 matrix instructions deep)
 constexpr int PF_XPAD = 8;           // bf16 of padding per LDS row: keeps 16-byte operand reads conflict-free

@@ -24,9 +24,6 @@
 
 namespace parse {
 
-#define PARSE_LDS_PTR(p) ((__attribute__((address_space(3))) void *)(p))
-#define PARSE_GLB_PTR(p) ((const __attribute__((address_space(1))) void *)(p))
-
 constexpr int LG_MAX_LAYERS = 4;
 
 // One product of one layer.  A launch covers up to LG_MAX_LAYERS of them (layers that share their token rows and the

@@ -1,0 +1,580 @@
+"""The paged key-value cache and the attention over it against the float64 oracle: every position that a row does not see holds
+NaN or infinities, pages stand in any order, outputs and workspaces between canaries."""
+import numpy as np
+import pytest
+import torch
+
+import synth_inputs as si
+from oracle import kv_oracle as ko
+
+pytestmark = pytest.mark.gpu
+
+pa = pytest.importorskip("paper_2605_08568_amd")
+from helpers import CANARY, check_guards, guarded_bytes, i32  # noqa: E402
+
+DEV = "cuda"
+
+
+def rounded(x, dtype):
+    """Values that the dtype has, as float64."""
+    if dtype == "fp32":
+        return x.astype(np.float32).astype(np.float64)
+    return torch.from_numpy(x.astype(np.float32)).bfloat16().double().numpy()
+
+
+def upload(x, dtype):
+    t = torch.from_numpy(np.ascontiguousarray(x, dtype=np.float32))
+    return (t.bfloat16() if dtype == "bf16" else t).to(DEV)
+
+
+class Case:
+    """A cache of one layer (behind another that holds NaN) with sequences of given lengths, pages shuffled, unseen places poisoned."""
+
+    def __init__(self, dtype, n_kv, d, page, lens, gone=None, seed=0, extra_columns=1, poison=np.nan):
+        rng = np.random.default_rng(seed)
+        self.dtype, self.n_kv, self.d, self.page, self.lens = dtype, n_kv, d, page, lens
+        counts = [-(-n // page) for n in lens]
+        total, cols = sum(counts), max(counts) + extra_columns
+        n_pages = total + 3
+        ids = rng.permutation(n_pages)[:total]
+        self.table = np.full((len(lens), cols), -1, np.int64)
+        K = np.full((n_pages, n_kv, page // 16, d // 8, 16, 8), poison)
+        V = np.full((n_pages, n_kv, page // 8, d, 8), poison)
+        self.k = [rounded(rng.standard_normal((n, n_kv, d)), dtype) for n in lens]
+        self.v = [rounded(rng.standard_normal((n, n_kv, d)), dtype) for n in lens]
+        self.there, at = [], 0
+        for s, n in enumerate(lens):
+            there = np.ones(n, bool)
+            for c in range(counts[s]):
+                if gone and gone(s, c):
+                    there[c * page:(c + 1) * page] = False
+                    continue
+                p = ids[at]; at += 1
+                self.table[s, c] = p
+                a, b = c * page, min((c + 1) * page, n)
+                full = np.full((2, page, n_kv, d), poison)
+                full[0, :b - a], full[1, :b - a] = self.k[s][a:b], self.v[s][a:b]
+                K[p], V[p] = ko.k_to_pages(full[0]), ko.v_to_pages(full[1])
+            self.there.append(there)
+        K, V = upload(K, dtype), upload(V, dtype)
+        self.kv = pa.KV(torch.stack([torch.full_like(K, torch.nan), K]), torch.stack([torch.full_like(V, torch.nan), V]),
+                        i32(self.table), i32(np.array(lens)))
+
+    def write(self, s, j, k=None, v=None):
+        """Puts single rows in place, in the cache and in the oracle's arrays."""
+        p, w = self.table[s, j // self.page], j % self.page
+        if k is not None:
+            self.k[s][j] = k
+            self.kv.K[1, p, :, w // 16, :, w % 16, :] = upload(np.broadcast_to(k, (self.n_kv, self.d)), self.dtype).view(self.n_kv, self.d // 8, 8)
+        if v is not None:
+            self.v[s][j] = v
+            self.kv.V[1, p, :, w // 8, :, w % 8] = upload(np.broadcast_to(v, (self.n_kv, self.d)), self.dtype)
+
+
+def bounds(dtype, d, n, o, lse, mag, big):
+    """What the roundings can make, element by element.  Scores: d products and sums in 32 bits, 2^-24 of |q|.|k| each, and the
+    scale's and the 2^x's rounding (2^-22 of the score, 2^-22); a weight is off by as much, the mean by twice that; n sums of weights
+    and products.  bf16 (8 significand bits): a weight and the result are rounded, 2^-8 each."""
+    w = (d + 4) * 2.0 ** -24 * big + 2.0 ** -22 * big + 2.0 ** -21 + n * 2.0 ** -24
+    tol = 2 * w[:, None] * mag + 1e-30
+    if dtype == "bf16":
+        tol = tol + 1.01 * 2.0 ** -8 * (mag + np.abs(o) + 2 * w[:, None] * mag)
+    return tol, w + 2.0 ** -22 * (1 + np.abs(lse))
+
+
+def compare(case, out, lse, want, d):
+    """want: per row (o, lse, mag, big, tokens)."""
+    out, lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    for r, (o, l, mag, big, n) in enumerate(want):
+        empty = np.isneginf(l)
+        assert np.array_equal(np.isneginf(lse[r]), empty), f"row {r}: lse"
+        tol, ltol = bounds(case.dtype, d, n, o, np.where(empty, 0, l), mag, big)
+        off = np.abs(out[r] - o) - tol
+        assert np.all(off <= 0), f"row {r}: {off.max():.3e} over the bound, at {np.unravel_index(off.argmax(), off.shape)}"
+        assert np.all(np.abs(lse[r] - l)[~empty] <= ltol[~empty]), f"row {r}: lse {np.abs(lse[r] - l).max()}"
+
+
+def guarded(rows, heads, d, like, pad=0):
+    """Output rows `pad` elements further apart than they are long."""
+    es = like.element_size()
+    buf, mid = guarded_bytes(rows * (heads * d + pad) * es)
+    t = mid[:rows * (heads * d + pad) * es].view(like.dtype).view(rows, heads * d + pad)
+    return buf, t, t[:, :heads * d].unflatten(1, (heads, d))
+
+
+def run_decode(case, n_q, window=0, sinks=0, seqs=None, scale=None, seed=1, pad=0, q=None):
+    rng = np.random.default_rng(seed)
+    rows = len(case.lens) if seqs is None else len(seqs)
+    if q is None:
+        q = rounded(2 * rng.standard_normal((rows, n_q, case.d)), case.dtype)
+    wide = torch.full((rows, n_q * case.d + pad), torch.nan, device=DEV, dtype=case.kv.K.dtype)
+    wide[:, :n_q * case.d] = upload(q, case.dtype).flatten(1)
+    qd = wide[:, :n_q * case.d].unflatten(1, (n_q, case.d))
+    buf, whole, out = guarded(rows, n_q, case.d, qd, pad)
+    lbuf, lmid = guarded_bytes(rows * n_q * 4)
+    wbuf, ws = guarded_bytes(int(pa.lib().parse_attend_decode_workspace_bytes(case.kv.c(), n_q, rows)))
+    before = whole[:, n_q * case.d:].clone()
+    lse = lmid[:rows * n_q * 4].view(torch.float32).view(rows, n_q)
+    pa.attend_decode(case.kv, 1, qd, seqs=None if seqs is None else i32(np.array(seqs)), scale=scale, window=window, sinks=sinks, out=out, lse=lse,
+                     workspace=ws)
+    for b, what in ((buf, "out"), (lbuf, "lse"), (wbuf, "workspace")):
+        check_guards(b, what)
+    assert torch.equal(whole[:, n_q * case.d:].view(torch.uint8), before.view(torch.uint8)), "stores between the rows"
+    scale = case.d ** -0.5 if scale is None else scale
+    want = []
+    for r in range(rows):
+        s = r if seqs is None else seqs[r]
+        if not 0 <= s < len(case.lens):
+            want.append((np.zeros((n_q, case.d)), np.full(n_q, -np.inf), np.zeros((n_q, case.d)), np.zeros(n_q), 1))
+            continue
+        n = case.lens[s]
+        want.append((*ko.attend_row(q[r], case.k[s], case.v[s], ko.visible(n - 1, case.there[s], window, sinks), scale), n))
+    compare(case, out, lse, want, case.d)
+    return out, lse
+
+
+def run_prefill(case, n_q, new, window=0, sinks=0, seqs=None, seed=1, pad=0, one_row=False):
+    rng = np.random.default_rng(seed)
+    rows = sum(new)
+    off = np.concatenate([[0], np.cumsum(new)])
+    q = rounded(2 * rng.standard_normal((rows, n_q, case.d)), case.dtype)
+    wide = torch.full((rows, n_q * case.d + pad), torch.nan, device=DEV, dtype=case.kv.K.dtype)
+    wide[:, :n_q * case.d] = upload(q, case.dtype).flatten(1)
+    qd = wide[:, :n_q * case.d].unflatten(1, (n_q, case.d))
+    buf, whole, out = guarded(rows, n_q, case.d, qd, pad)
+    lbuf, lmid = guarded_bytes(rows * n_q * 4)
+    wbuf, ws = guarded_bytes(int(pa.lib().parse_attend_prefill_workspace_bytes(case.kv.c(), n_q, rows, len(new))))
+    before = whole[:, n_q * case.d:].clone()
+    lse = lmid[:rows * n_q * 4].view(torch.float32).view(rows, n_q)
+    pa.attend_prefill(case.kv, 1, qd, None if one_row else i32(off), seqs=None if seqs is None else i32(np.array(seqs)), window=window, sinks=sinks,
+                      out=out, lse=lse, workspace=ws)
+    for b, what in ((buf, "out"), (lbuf, "lse"), (wbuf, "workspace")):
+        check_guards(b, what)
+    assert torch.equal(whole[:, n_q * case.d:].view(torch.uint8), before.view(torch.uint8)), "stores between the rows"
+    want = []
+    for p, n in enumerate(new):
+        s = p if seqs is None else seqs[p]
+        for t in range(n):
+            ok = 0 <= s < len(case.lens)
+            i = case.lens[s] - n + t if ok else -1
+            seen = ko.visible(i, case.there[s], window, sinks) if ok else np.zeros(1, bool)
+            k, v = (case.k[s], case.v[s]) if ok else (np.zeros((1, case.n_kv, case.d)),) * 2
+            want.append((*ko.attend_row(q[off[p] + t], k, v, seen, case.d ** -0.5), max(i + 1, 1)))
+    compare(case, out, lse, want, case.d)
+    return out, lse
+
+
+WIDTHS = [(t, d) for t in ("bf16", "fp32") for d in (32, 64, 96, 128, 160, 192, 224, 256)]
+
+
+@pytest.mark.parametrize("dtype,d", WIDTHS)
+def test_decode_widths(dtype, d):
+    run_decode(Case(dtype, 2, d, 16, [1, 16, 17, 77, 300], seed=d), 6, pad=8)
+
+
+@pytest.mark.parametrize("heads,kv", [(1, 1), (4, 4), (8, 1), (16, 1), (17, 1), (40, 2), (28, 4)])
+def test_decode_head_groups(heads, kv):
+    run_decode(Case("bf16", kv, 64, 32, [31, 32, 33, 130], seed=heads), heads)
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1, 0), (40, 0), (40, 4), (64, 21), (1000, 4), (33, 200), (1 << 31 - 1 - 1, 2 ** 31 - 1)])
+def test_decode_windows(page, window, sinks):
+    lens = [1, 5, 39, 40, 41, 127, 128, 129, 255, 500, 1025]
+    window = min(window, 2 ** 31 - 1)
+    run_decode(Case("bf16", 2, 64, page, lens, seed=page), 4, window, sinks)
+
+
+def test_decode_pages_outside_the_window_are_gone():
+    lens, page, window, sinks = [700, 90, 400], 16, 100, 5
+
+    def gone(s, c):
+        return c * page >= sinks and (c + 1) * page <= lens[s] - window
+    run_decode(Case("bf16", 2, 128, page, lens, gone, seed=3), 8, window, sinks)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_decode_rows_without_tokens(dtype):
+    """Lengths of zero, a missing page, sequences that the table does not have; every row sees nothing."""
+    run_decode(Case(dtype, 2, 64, 16, [0, 40, 0, 0, 3, 0], seed=5), 4)
+    run_decode(Case(dtype, 2, 64, 16, [40, 33], lambda s, c: s == 0, seed=6), 4)
+    run_decode(Case(dtype, 2, 64, 16, [40, 33, 20], seed=7), 4, seqs=[2, -1, 0, 3, 1, 1])
+    case = Case(dtype, 2, 64, 16, [17, 30], seed=8)
+    case.kv.len.zero_()
+    case.lens = [0, 0]
+    run_decode(case, 4)
+
+
+def test_decode_unseen_places_hold_infinities():
+    for poison in (np.inf, -np.inf):
+        run_decode(Case("bf16", 2, 64, 16, [5, 100, 250], seed=9, poison=poison), 4, 60, 3)
+        run_decode(Case("fp32", 2, 64, 64, [5, 100, 250], seed=9, poison=poison), 4, 60, 3)
+    case = Case("bf16", 2, 64, 16, [200], seed=10)
+    for j in (3, 4, 100, 139):                 # between the sinks and the window, in pages that are read
+        case.write(0, j, np.nan, np.inf)
+    run_decode(case, 4, 60, 3)
+
+
+@pytest.mark.parametrize("lens", [[20000], [5000, 1, 9000, 3], [128 * 9] * 7, [1] * 300, list(range(1, 400, 7))])
+def test_decode_splits(lens):
+    """Long caches cut over many workgroups, many short ones in one, shares that end inside a cache."""
+    run_decode(Case("bf16", 1, 32, 64, lens, seed=len(lens)), 2)
+
+
+def test_decode_large_scores_and_scale():
+    """Scores of +-300 in order and against it: the running maximum lags and grows."""
+    for order in (1, -1):
+        case = Case("fp32", 1, 32, 16, [600], seed=11)
+        direction = np.sign(np.random.default_rng(1).standard_normal(32))
+        for j in range(600):
+            case.k[0][j] = direction * (j if order == 1 else 600 - j) / 64
+        full = np.zeros((608, 1, 32)); full[:600] = case.k[0]
+        for c in range(38):
+            case.kv.K[1, case.table[0, c]] = upload(ko.k_to_pages(full[16 * c:16 * c + 16]), "fp32")
+        run_decode(case, 2, scale=1.0, q=np.stack([[direction, -direction]]))
+        run_decode(case, 2, scale=0.0)
+        run_decode(case, 2, scale=-0.3)
+
+
+def test_decode_is_the_same_every_time_and_row_by_row():
+    case = Case("bf16", 2, 128, 16, [300, 1000, 77], seed=12)
+    a, la = run_decode(case, 8)
+    b, lb = run_decode(case, 8)
+    assert torch.equal(a.view(torch.int16), b.view(torch.int16)) and torch.equal(la, lb)
+
+
+@pytest.mark.parametrize("dtype,d", WIDTHS)
+def test_prefill_widths(dtype, d):
+    run_prefill(Case(dtype, 2, d, 16, [1, 16, 17, 77], seed=d), 4, [1, 16, 5, 77], pad=8)
+
+
+@pytest.mark.parametrize("heads,kv", [(1, 1), (4, 4), (8, 1), (17, 1), (40, 2), (28, 4)])
+def test_prefill_head_groups(heads, kv):
+    run_prefill(Case("bf16", kv, 64, 32, [33, 70, 150], seed=heads), heads, [33, 1, 40])
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1, 0), (40, 4), (64, 21), (33, 200), (1000, 4), (2 ** 31 - 1, 2 ** 31 - 1)])
+def test_prefill_windows(page, window, sinks):
+    run_prefill(Case("bf16", 1, 64, page, [1, 40, 129, 300], seed=page), 2, [1, 40, 129, 70], window, sinks)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_prefill_lengths(dtype):
+    for n in (1, 15, 16, 31, 32, 33, 63, 64, 65, 127, 128, 129, 200):
+        run_prefill(Case(dtype, 1, 64, 16, [n, n + 50], seed=n), 1, [n, n])
+    run_prefill(Case(dtype, 1, 64, 16, [30, 1, 2], seed=5), 2, [1, 1, 1], one_row=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_prefill_rows_without_tokens(dtype):
+    run_prefill(Case(dtype, 2, 64, 16, [40, 33], lambda s, c: s == 0, seed=6), 4, [40, 10])
+    run_prefill(Case(dtype, 2, 64, 16, [40, 33, 20], seed=7), 4, [7, 3, 11, 0, 2], seqs=[2, -1, 0, 1, 9])
+    run_prefill(Case(dtype, 2, 64, 16, [10, 33], seed=7), 4, [25, 3])         # more rows than tokens: the first ones have no position
+    run_prefill(Case(dtype, 2, 64, 16, [100], lambda s, c: c == 2, seed=8), 2, [100])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("d", [64, 256])
+def test_prefill_infinities_and_nan_reach_only_rows_that_see_them(dtype, d):
+    """Token 70's values are infinite, 75's NaN, 90's -infinite: rows before them stay finite, rows after them follow the formula."""
+    case = Case(dtype, 1, d, 16, [128], seed=13)
+    val = case.v[0][70].copy(); val[0, 3] = np.inf; val[0, d - 1] = np.inf
+    case.write(0, 70, v=val)
+    val = case.v[0][90].copy(); val[0, 7] = -np.inf
+    case.write(0, 90, v=val)
+    val = case.v[0][75].copy(); val[0, 5] = np.nan
+    case.write(0, 75, v=val)
+    for window, sinks in ((0, 0), (20, 4)):
+        q = rounded(np.random.default_rng(2).standard_normal((128, 2, d)), dtype)
+        out = pa.attend_prefill(case.kv, 1, upload(q, dtype), i32(np.array([0, 128])), window=window, sinks=sinks).double().cpu().numpy()
+        for i in range(128):
+            o, _, mag, big = ko.attend_row(q[i], case.k[0], case.v[0], ko.visible(i, case.there[0], window, sinks), d ** -0.5)
+            assert np.array_equal(np.isnan(out[i]), np.isnan(o)), i
+            assert np.array_equal(np.isinf(out[i]), np.isinf(o)) and np.array_equal(out[i][np.isinf(o)], o[np.isinf(o)]), i
+            fine = np.isfinite(o)
+            tol, _ = bounds(dtype, d, 128, np.where(fine, o, 0), np.zeros(2), np.where(np.isfinite(mag), mag, 0), big)
+            assert np.all(np.abs(out[i][fine] - o[fine]) <= tol[fine]), i
+
+
+def test_prefill_long_and_shared():
+    """Several tiles of rows and many of tokens, heads that share, a window in the middle of it."""
+    run_prefill(Case("bf16", 2, 128, 16, [700, 333], seed=14), 8, [700, 130])
+    run_prefill(Case("bf16", 1, 128, 64, [900], seed=15), 4, [500], 256, 4)
+
+
+def test_prefill_few_rows_over_a_long_cache():
+    run_prefill(Case("bf16", 1, 64, 64, [6000, 200], seed=16), 4, [5, 3])
+    run_prefill(Case("fp32", 1, 32, 16, [3000], seed=17), 2, [9], 2500, 4)
+
+
+def test_prefill_of_single_tokens_equals_decode():
+    case = Case("bf16", 2, 64, 16, [100, 5, 333], seed=18)
+    q = upload(rounded(np.random.default_rng(3).standard_normal((3, 4, 64)), "bf16"), "bf16")
+    a = pa.attend_decode(case.kv, 1, q).float()
+    b = pa.attend_prefill(case.kv, 1, q).float()
+    assert (a - b).abs().max() <= 2.0 ** -6 * a.abs().max()
+
+
+# ---- the rows' way in -------------------------------------------------------------------------------------------------
+def rope_table(n, d):
+    angle = np.arange(n)[:, None] * 10000.0 ** (-np.arange(d // 2) / (d // 2))
+    return np.concatenate([np.cos(angle), np.sin(angle)], 1).astype(np.float32)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("d,page,rope,in_place", [(64, 16, True, False), (32, 32, True, True), (128, 64, False, False), (160, 16, True, True), (256, 256, True, False)])
+def test_append(dtype, d, page, rope, in_place):
+    rng = np.random.default_rng(d + page)
+    n_kv, n_q, lens, new, seqs = 2, 6, [40, 17, 300, 16, 9], [5, 17, 100, 0, 1], [3, 0, 2, 1, 4]
+    table = np.full((5, 300 // page + 2), -1, np.int32)
+    ids = iter(rng.permutation(60))
+    seq_len = [0] * 5
+    for p, s in enumerate(seqs):
+        seq_len[s] = lens[p]
+        for c in range(-(-lens[p] // page)):
+            table[s, c] = next(ids)
+    table[2, 250 // page] = -1                                     # a page that is not there
+    off = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    rows = int(off[-1])
+    kv = pa.KV(torch.full((2, 60, n_kv, page // 16, d // 8, 16, 8), 7.0, device=DEV, dtype=torch.bfloat16 if dtype == "bf16" else torch.float32),
+               torch.full((2, 60, n_kv, page // 8, d, 8), 7.0, device=DEV, dtype=torch.bfloat16 if dtype == "bf16" else torch.float32),
+               i32(table), i32(np.array(seq_len)))
+    x = rounded(rng.standard_normal((rows, n_q + 2 * n_kv, d)), dtype)
+    fused = upload(x, dtype)
+    table_rope = rope_table(290, d)                                # shorter than the longest sequence: the last row serves
+    q = fused[:, :n_q]
+    q_out = q if in_place else torch.empty((rows, n_q, d), dtype=fused.dtype, device=DEV)
+    pa.kv_append(kv, 1, fused[:, n_q:n_q + n_kv], fused[:, n_q + n_kv:], i32(off), i32(np.array(seqs)), q=q, q_out=q_out,
+                 rope=torch.from_numpy(table_rope).to(DEV) if rope else None)
+    pos = np.concatenate([lens[p] - n + np.arange(n) for p, n in enumerate(new)])
+    turn = table_rope[np.clip(pos, 0, 289)].astype(np.float64)
+    qk = ko.rotate(x[:, :n_q + n_kv], turn) if rope else x[:, :n_q + n_kv]
+    size = ko.rotate(np.abs(x[:, :n_q + n_kv]), np.abs(turn) * np.repeat([[1.0, -1.0]], d // 2, 1).reshape(1, -1)) if rope else np.abs(qk)
+    size = np.abs(np.concatenate([np.abs(x[:, :n_q + n_kv, :d // 2]) + np.abs(x[:, :n_q + n_kv, d // 2:])] * 2, 2)) if rope else size
+    tol = 2.0 ** -23 * size + (1.01 * 2.0 ** -8 * np.abs(qk) if dtype == "bf16" else 0)
+    assert np.all(np.abs(q_out.double().cpu().numpy() - qk[:, :n_q]) <= tol[:, :n_q])
+    if not in_place:
+        assert np.array_equal(fused.double().cpu().numpy(), x)
+    assert bool((kv.K[0] == 7).all()) and bool((kv.V[0] == 7).all()), "another layer was written"
+    K = ko.k_from_pages(kv.K[1].double().cpu().numpy())
+    V = ko.v_from_pages(kv.V[1].double().cpu().numpy())
+    touched = np.zeros((60, page), bool)
+    for p, n in enumerate(new):
+        for t in range(n):
+            j, r = lens[p] - n + t, off[p] + t
+            id_ = table[seqs[p], j // page]
+            if id_ < 0:
+                continue
+            touched[id_, j % page] = True
+            assert np.all(np.abs(K[id_, j % page] - qk[r, n_q:]) <= tol[r, n_q:]), (p, t)
+            assert np.array_equal(V[id_, j % page], x[r, n_q + n_kv:]), (p, t)
+    assert np.all(K[~touched] == 7) and np.all(V[~touched] == 7), "a place of no new token was written"
+
+
+def test_append_of_single_rows_without_offsets_or_q():
+    kv = pa.KV.empty(1, 8, 16, 3, 64, 4, 2)
+    pa.kv_reserve(kv, i32(np.array([1, 0, 17, 2])))
+    k = torch.randn((4, 3, 64), device=DEV).bfloat16(); v = torch.randn((4, 3, 64), device=DEV).bfloat16()
+    assert pa.kv_append(kv, 0, k, v) is None                       # sequence 1 is empty: its row has no position
+    table = kv.table.cpu().numpy()
+    K = ko.k_from_pages(kv.K[0].float().cpu().numpy()); V = ko.v_from_pages(kv.V[0].float().cpu().numpy())
+    for s, j in ((0, 0), (2, 16), (3, 1)):
+        assert np.array_equal(K[table[s, j // 16], j % 16], k[s].float().cpu().numpy())
+        assert np.array_equal(V[table[s, j // 16], j % 16], v[s].float().cpu().numpy())
+
+
+# ---- bookkeeping --------------------------------------------------------------------------------------------------------
+class Both:
+    """The same calls on the device and on the oracle, everything compared after each."""
+
+    def __init__(self, n_seqs, max_pages, n_pages, page, layers=2, dtype=torch.bfloat16, n_kv=2, d=32, seed=0):
+        self.kv = pa.KV.empty(layers, n_pages, page, n_kv, d, n_seqs, max_pages, dtype)
+        gen = torch.Generator(device=DEV); gen.manual_seed(seed)
+        self.kv.K.copy_(torch.randn(self.kv.K.shape, generator=gen, device=DEV)); self.kv.V.copy_(torch.randn(self.kv.V.shape, generator=gen, device=DEV))
+        self.K, self.V = self.kv.K.cpu().clone(), self.kv.V.cpu().clone()
+        self.o = ko.Pages(n_seqs, max_pages, n_pages, page)
+        self.wbuf, self.ws = guarded_bytes(int(pa.lib().parse_kv_workspace_bytes(self.kv.c())))
+        self.check()
+
+    def check(self):
+        torch.cuda.synchronize()
+        assert np.array_equal(self.kv.table.cpu().numpy(), self.o.table)
+        assert np.array_equal(self.kv.len.cpu().numpy(), self.o.len)
+        assert np.array_equal(self.kv.refs.cpu().numpy(), self.o.refs)
+        assert np.array_equal(self.kv.free_bits.cpu().numpy().view(np.uint32), self.o.free_words())
+        assert torch.equal(self.kv.K.cpu(), self.K) and torch.equal(self.kv.V.cpu(), self.V)
+        check_guards(self.wbuf, "workspace")
+
+    def copied(self, copies):
+        for a, b in copies:
+            self.K[:, b], self.V[:, b] = self.K[:, a].clone(), self.V[:, a].clone()
+
+    def reserve(self, n_new):
+        served = pa.kv_reserve(self.kv, i32(np.array(n_new)), workspace=self.ws)
+        copies, want = self.o.reserve(n_new)
+        self.copied(copies)
+        assert np.array_equal(served.cpu().numpy(), want)
+        self.check()
+        return len(copies), int(want.sum())
+
+    def fork(self, src, dst):
+        pa.kv_fork(self.kv, i32(np.array(src)), i32(np.array(dst)))
+        self.o.fork(src, dst)
+        self.check()
+
+    def trim(self, keep=None, window=0, sinks=0):
+        pa.kv_trim(self.kv, None if keep is None else i32(np.array(keep)), window, sinks)
+        self.o.trim(keep, window, sinks)
+        self.check()
+
+    def compact(self):
+        n = pa.kv_compact(self.kv, workspace=self.ws)
+        moves, live = self.o.compact()
+        self.copied(moves)
+        assert int(n.item()) == live
+        self.check()
+        return len(moves)
+
+
+def test_pages_of_forks_and_copies():
+    b = Both(8, 10, 40, 16)
+    b.reserve([20, 16, 0, 0, 0, 0, 0, 0])
+    b.fork([0, 0, 1], [2, 3, 4])
+    assert b.reserve([1, 1, 1, 1, 1, 0, 0, 0]) == (2, 5)           # three users of a begun page: two copies, the last one keeps it
+    b.fork([2, 3, 0], [0, 2, 3])                                    # a cycle
+    b.fork([0, 1], [0, 5])                                          # onto itself: nothing
+    b.trim([5, 0, 100, -3, 16, 17, 0, 0])
+    b.reserve([100, 100, 1, 0, 16, 1, 161, 160])                    # the last but one outgrows the table and takes nothing
+    b.compact()
+    b.trim(window=20, sinks=3)
+    b.reserve([3] * 8)
+    b.compact()
+    b.compact()
+
+
+def test_pages_run_out():
+    b = Both(6, 8, 5, 16)
+    assert b.reserve([16, 33, 16, 0, 1, 0]) == (0, 3)               # 1 + 3 + 1 pages; nothing is left for the fifth
+    b.trim([0, 33, 16, 0, 0, 0])
+    b.reserve([0, 0, 40, 5, 0, 1])                                  # the first does not fit: the ones behind it get nothing either
+    b.reserve([0, 15, 0, 5, 0, 1])                                  # room in a begun page needs no page
+
+
+@pytest.mark.parametrize("seed", range(6))
+def test_pages_random_histories(seed):
+    rng = np.random.default_rng(seed)
+    n_seqs = int(rng.choice([3, 30, 70])); max_pages = int(rng.choice([5, 9, 17])); n_pages = int(rng.choice([31, 64, 200]))
+    b = Both(n_seqs, max_pages, n_pages, 16, layers=1, n_kv=1, seed=seed)
+    for _ in range(25):
+        what = rng.integers(5)
+        if what <= 1:
+            b.reserve(np.where(rng.random(n_seqs) < 0.4, rng.integers(-1, 40, n_seqs), 0))
+        elif what == 2:
+            n = int(rng.integers(1, n_seqs + 1))
+            b.fork(rng.integers(0, n_seqs, n), rng.permutation(n_seqs)[:n])
+        elif what == 3:
+            b.trim(np.where(rng.random(n_seqs) < 0.3, rng.integers(0, 60, n_seqs), 1000), int(rng.choice([0, 1, 30])), int(rng.choice([0, 4, 20])))
+        else:
+            b.compact()
+
+
+def test_pages_many():
+    """More sequences than threads, more words of free pages than threads."""
+    b = Both(2500, 3, 70000, 16, layers=1, n_kv=1, d=32)
+    rng = np.random.default_rng(4)
+    b.reserve(rng.integers(0, 40, 2500))
+    b.fork(np.arange(1000), 1500 + np.arange(1000))
+    b.reserve(np.where(np.arange(2500) % 3, 1, 0))
+    b.trim(np.where(np.arange(2500) % 2, 1000, 0))
+    b.compact()
+    b.reserve(np.full(2500, 2))
+
+
+def test_fork_skips_sequences_that_are_not_there():
+    b = Both(4, 4, 20, 16)
+    b.reserve([20, 30, 0, 0])
+    pa.kv_fork(b.kv, i32(np.array([0, 9, 1, -1])), i32(np.array([2, 3, 4, 0])))
+    b.o.fork([0], [2])
+    b.check()
+
+
+def test_copies_of_wide_pages_and_fp32():
+    for dtype, n_kv, d, page in ((torch.bfloat16, 3, 160, 32), (torch.float32, 2, 32, 16), (torch.bfloat16, 1, 32, 16)):
+        b = Both(4, 4, 20, page, layers=3, dtype=dtype, n_kv=n_kv, d=d)
+        b.reserve([page + 1, 5, 0, 0])
+        b.fork([0, 1], [2, 3])
+        b.reserve([1, 1, 1, 1])
+        b.trim([0, 100, 100, 0])
+        assert b.compact() > 0
+
+
+def test_a_step_is_recorded_and_replayed():
+    """reserve, append, decode and trim as one HIP graph: every replay equals the eager step on a copy of the state."""
+    torch.manual_seed(0)
+    n_seqs, n_kv, n_q, d = 3, 2, 4, 64
+
+    def fresh():
+        kv = pa.KV.empty(1, 40, 16, n_kv, d, n_seqs, 12)
+        kv.K.zero_(); kv.V.zero_()
+        return kv
+    qkv = torch.randn((n_seqs, n_q + 2 * n_kv, d), device=DEV).bfloat16()
+    one = i32(np.ones(n_seqs))
+    rope = torch.from_numpy(rope_table(200, d)).to(DEV)
+
+    def make(kv):
+        ws, wa = pa.kv_workspace(kv), pa.attend_decode_workspace(kv, n_q, n_seqs)
+        served, q, out = torch.empty(n_seqs, dtype=torch.int32, device=DEV), torch.empty((n_seqs, n_q, d), dtype=torch.bfloat16, device=DEV), torch.empty((n_seqs, n_q, d), dtype=torch.bfloat16, device=DEV)
+
+        def step():
+            pa.kv_reserve(kv, one, served, ws)
+            pa.kv_append(kv, 0, qkv[:, n_q:n_q + n_kv], qkv[:, n_q + n_kv:], q=qkv[:, :n_q], q_out=q, rope=rope)
+            pa.attend_decode(kv, 0, q, window=30, sinks=2, out=out, workspace=wa)
+            pa.kv_trim(kv, None, 30, 2)
+        return step, out
+    a, b = fresh(), fresh()
+    step_a, out_a = make(a)
+    step_b, out_b = make(b)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step_a()                                                   # warm-up, on another stream
+    torch.cuda.current_stream().wait_stream(side)
+    step_b()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step_a()
+    for i in range(60):
+        qkv.normal_()
+        graph.replay()
+        step_b()
+        torch.cuda.synchronize()
+        assert torch.equal(out_a.view(torch.int16), out_b.view(torch.int16)), i
+        assert torch.equal(a.table, b.table) and torch.equal(a.len, b.len) and torch.equal(a.refs, b.refs) and torch.equal(a.free_bits, b.free_bits)
+    assert int(a.len[0]) == 61 and int((a.refs > 0).sum()) < 3 * 4 + 1
+
+
+def test_long_cache_past_32_bits():
+    """Elements past 2^31 in a layer, and a second layer behind it: the same tokens at low and at high page ids give the same bits."""
+    n_kv, d, page, n_pages = 16, 128, 256, 4608                    # 2.4e9 elements a layer
+    kv = pa.KV(torch.zeros((2, n_pages, n_kv, page // 16, d // 8, 16, 8), dtype=torch.bfloat16, device=DEV),
+               torch.zeros((2, n_pages, n_kv, page // 8, d, 8), dtype=torch.bfloat16, device=DEV), i32(np.array([[0, 1], [n_pages - 1, n_pages - 2]])),
+               i32(np.array([0, 0])))
+    rows = 300
+    x = torch.randn((rows, 3 * n_kv, d), device=DEV).bfloat16()
+    kv.len.fill_(rows)
+    off = i32(np.array([0, rows]))
+    outs = []
+    for s in (0, 1):
+        seqs = i32(np.array([s]))
+        pa.kv_append(kv, 1, x[:, n_kv:2 * n_kv], x[:, 2 * n_kv:], off, seqs)
+        outs.append((pa.attend_prefill(kv, 1, x[:, :n_kv], off, seqs), pa.attend_decode(kv, 1, x[-1:, :n_kv], seqs)))
+    for a, b in zip(*outs):
+        assert torch.equal(a.view(torch.int16), b.view(torch.int16)) and bool(a.float().abs().sum() > 0)
+    assert not bool(kv.K[0].any()) and int((kv.K[1].flatten(1).any(1)).sum()) == 4
+    # a copy between the ends
+    kv.refs, kv.free_bits = torch.zeros(n_pages, dtype=torch.int32, device=DEV), torch.zeros(n_pages // 32, dtype=torch.int32, device=DEV)
+    kv.table.fill_(-1); kv.table[1, 0] = n_pages - 1; kv.refs[n_pages - 1] = 1
+    kv.free_bits.fill_(-1); kv.free_bits[-1] = 2 ** 31 - 1
+    assert int(pa.kv_compact(kv)) == 1
+    assert torch.equal(kv.K[1, 0], kv.K[1, n_pages - 1]) and int(kv.table[1, 0]) == 0
