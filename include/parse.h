@@ -474,6 +474,7 @@ int parse_lowrank_prefill_multi(const parse_layer *layers, const parse_patterns 
  *     refs       [n_pages], table entries that hold the page; a page never stands in two columns of the table
  *     free_bits  [(n_pages+31)/32] words, bit p%32 of word p/32 set iff refs[p] == 0 (bits past n_pages are 0)
  * parse_kv_append and the attention calls use K, V, table and len alone: refs and free_bits may be NULL there.
+ * K and V are 16-byte aligned; arrays of int32 need their own 4 bytes only, in all calls of the paged cache.
  * Table entries outside [0, n_pages) and sequence numbers outside [0, n_seqs) are skipped wherever they are read. */
 typedef struct {
   int32_t n_layers;

@@ -11,7 +11,12 @@ constexpr int KV_MAXTOKENS = 1 << 25;        // tokens that a table's row can na
 
 constexpr int KV_MAXROWS = 1 << 24;          // rows times the heads that share a kv head: their tiles stay countable also where offsets go back and forth
 
+static inline bool aligned4(const void *p) { return (((uintptr_t)p) & 3u) == 0; }
+
+// host-side checks: counts = the call changes refs and free_bits
 int check_kv(const parse_kv *kv, bool counts);
+int check_attend(const parse_kv *kv, int layer, const void *q, int64_t q_stride, int n_q, int rows, const int32_t *tok_offsets, const int32_t *seqs, float scale,
+                 int window, int sinks, const void *out, int64_t out_stride, const float *lse);
 
 // a row's sequence: the table's row and its length; nothing where the number is out of range
 struct KvSeq {

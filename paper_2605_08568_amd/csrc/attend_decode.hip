@@ -240,15 +240,15 @@ static int ad_width(const AdArgs &a, hipStream_t s) {
   }
 }
 
-int check_attend(const parse_kv *kv, int layer, const void *q, int64_t q_stride, int n_q, int rows, float scale, int window, int sinks, const void *out,
-                 int64_t out_stride, const float *lse) {
+int check_attend(const parse_kv *kv, int layer, const void *q, int64_t q_stride, int n_q, int rows, const int32_t *tok_offsets, const int32_t *seqs, float scale,
+                 int window, int sinks, const void *out, int64_t out_stride, const float *lse) {
   const int st = check_kv(kv, false);
   if (st != PARSE_OK) return st;
   if (!q || !out || n_q <= 0 || rows <= 0 || layer < 0 || window < 0 || sinks < 0 || !(scale - scale == 0.f)) return PARSE_EINVAL;
   if (layer >= kv->n_layers || n_q % kv->n_kv != 0 || n_q > 65536 || (int64_t)rows * n_q > INT32_MAX) return PARSE_ESHAPE;
   if (q_stride < (int64_t)n_q * kv->d || out_stride < (int64_t)n_q * kv->d) return PARSE_ESHAPE;
   const int per16 = 16 / elem_size(kv->dtype);
-  if (!aligned16(q) || !aligned16(out) || (((uintptr_t)lse) & 3u) != 0 || q_stride % per16 != 0 || out_stride % per16 != 0) return PARSE_EALIGN;
+  if (!aligned16(q) || !aligned16(out) || !aligned4(lse) || !aligned4(tok_offsets) || !aligned4(seqs) || q_stride % per16 != 0 || out_stride % per16 != 0) return PARSE_EALIGN;
   return PARSE_OK;
 }
 
@@ -265,7 +265,7 @@ int parse_attend_decode(const parse_kv *kv, int32_t layer, const void *q, int64_
                         int32_t window, int32_t sinks, void *out, int64_t out_stride, float *lse, void *workspace, size_t workspace_bytes,
                         parse_stream stream) {
   using namespace parse;
-  const int st = check_attend(kv, layer, q, q_stride, n_q, rows, scale, window, sinks, out, out_stride, lse);
+  const int st = check_attend(kv, layer, q, q_stride, n_q, rows, nullptr, seqs, scale, window, sinks, out, out_stride, lse);
   if (st != PARSE_OK) return st;
   if (rows > KV_MAXSEQ || (!seqs && rows > kv->n_seqs)) return PARSE_ESHAPE;
   if (!workspace || workspace_bytes < ad_bytes(kv, n_q)) return PARSE_EWORKSPACE;

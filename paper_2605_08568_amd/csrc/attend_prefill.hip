@@ -3,9 +3,6 @@
 
 namespace parse {
 
-int check_attend(const parse_kv *kv, int layer, const void *q, int64_t q_stride, int n_q, int rows, float scale, int window, int sinks, const void *out,
-                 int64_t out_stride, const float *lse);
-
 struct ApArgs {
   parse_kv kv;
   const void *K, *V;                                 // of the layer
@@ -238,7 +235,7 @@ int parse_attend_prefill(const parse_kv *kv, int32_t layer, const void *q, int64
                          void *workspace, size_t workspace_bytes, parse_stream stream) {
   using namespace parse;
   (void)workspace; (void)workspace_bytes;
-  const int st = check_attend(kv, layer, q, q_stride, n_q, rows, scale, window, sinks, out, out_stride, lse);
+  const int st = check_attend(kv, layer, q, q_stride, n_q, rows, tok_offsets, seqs, scale, window, sinks, out, out_stride, lse);
   if (st != PARSE_OK) return st;
   if (P <= 0) return PARSE_EINVAL;
   if ((int64_t)rows * (n_q / kv->n_kv) > KV_MAXROWS || P > KV_MAXSEQ || (!seqs && P > kv->n_seqs) || (!tok_offsets && rows != P)) return PARSE_ESHAPE;

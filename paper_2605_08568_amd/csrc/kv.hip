@@ -16,7 +16,7 @@ int check_kv(const parse_kv *kv, bool counts) {
   if (kv->page != 16 && kv->page != 32 && kv->page != 64 && kv->page != 128 && kv->page != 256) return PARSE_ESHAPE;
   if (kv->d < 32 || kv->d > 256 || kv->d % 32 != 0 || kv->n_kv > 1024 || kv->n_seqs > KV_MAXSEQ) return PARSE_ESHAPE;
   if ((int64_t)kv->max_pages * kv->page > KV_MAXTOKENS) return PARSE_ESHAPE;
-  if (!aligned16(kv->K) || !aligned16(kv->V) || !aligned16(kv->table) || !aligned16(kv->len) || !aligned16(kv->refs) || !aligned16(kv->free_bits))
+  if (!aligned16(kv->K) || !aligned16(kv->V) || !aligned4(kv->table) || !aligned4(kv->len) || !aligned4(kv->refs) || !aligned4(kv->free_bits))
     return PARSE_EALIGN;
   return PARSE_OK;
 }
@@ -433,7 +433,7 @@ int parse_kv_fork(const parse_kv *kv, const int32_t *src, const int32_t *dst, in
   if (st != PARSE_OK) return st;
   if (!src || !dst || n <= 0) return PARSE_EINVAL;
   if (n > KV_MAXFORK) return PARSE_ESHAPE;
-  if (!aligned16(src) || !aligned16(dst)) return PARSE_EALIGN;
+  if (!aligned4(src) || !aligned4(dst)) return PARSE_EALIGN;
   kv_fork<<<dim3((kv->max_pages + KV_FORK_COLUMNS - 1) / KV_FORK_COLUMNS), KV_THREADS, (size_t)n * (KV_FORK_COLUMNS + 1) * 4, (hipStream_t)stream>>>(*kv, src, dst, n);
   PARSE_LAUNCH_CHECK();
   return PARSE_OK;
@@ -443,7 +443,7 @@ int parse_kv_trim(const parse_kv *kv, const int32_t *keep, int32_t window, int32
   const int st = check_kv(kv, true);
   if (st != PARSE_OK) return st;
   if (window < 0 || sinks < 0 || (!keep && window == 0)) return PARSE_EINVAL;
-  if (!aligned16(keep)) return PARSE_EALIGN;
+  if (!aligned4(keep)) return PARSE_EALIGN;
   kv_trim<<<dim3(kv->n_seqs), KV_THREADS, 0, (hipStream_t)stream>>>(*kv, keep, window, sinks);
   PARSE_LAUNCH_CHECK();
   return PARSE_OK;
@@ -458,7 +458,7 @@ int parse_kv_reserve(const parse_kv *kv, const int32_t *n_new, int32_t *served, 
   if (st != PARSE_OK) return st;
   if (!n_new) return PARSE_EINVAL;
   if (!workspace || workspace_bytes < kv_work_bytes(kv)) return PARSE_EWORKSPACE;
-  if (!aligned16(n_new) || !aligned16(served) || !aligned16(workspace)) return PARSE_EALIGN;
+  if (!aligned4(n_new) || !aligned4(served) || !aligned16(workspace)) return PARSE_EALIGN;
   const KvWork ws = kv_work(kv, workspace);
   kv_reserve<<<dim3(1), KV_ONE, 0, (hipStream_t)stream>>>(*kv, n_new, served, ws);
   PARSE_LAUNCH_CHECK();
@@ -471,7 +471,7 @@ int parse_kv_compact(const parse_kv *kv, int32_t *n_live, void *workspace, size_
   const int st = check_kv(kv, true);
   if (st != PARSE_OK) return st;
   if (!workspace || workspace_bytes < kv_work_bytes(kv)) return PARSE_EWORKSPACE;
-  if (!aligned16(workspace) || (((uintptr_t)n_live) & 3u) != 0) return PARSE_EALIGN;
+  if (!aligned16(workspace) || !aligned4(n_live)) return PARSE_EALIGN;
   const KvWork ws = kv_work(kv, workspace);
   kv_compact<<<dim3(1), KV_ONE, 0, (hipStream_t)stream>>>(*kv, n_live, ws);
   PARSE_LAUNCH_CHECK();
@@ -493,6 +493,7 @@ int parse_kv_append(const parse_kv *kv, int32_t layer, const void *k, int64_t k_
   const int per16 = 16 / elem_size(kv->dtype);
   if (!aligned16(k) || !aligned16(v) || !aligned16(q) || !aligned16(q_out) || !aligned16(rope) || k_stride % per16 != 0 || v_stride % per16 != 0)
     return PARSE_EALIGN;
+  if (!aligned4(tok_offsets) || !aligned4(seqs)) return PARSE_EALIGN;
   if (q && (q_stride % per16 != 0 || q_out_stride % per16 != 0)) return PARSE_EALIGN;
   const size_t at = (size_t)layer * kv->n_pages * kv_page_bytes(kv);
   KaArgs a{*kv, (char *)kv->K + at, (char *)kv->V + at, k, v, q, q_out, k_stride, v_stride, q_stride, q_out_stride, tok_offsets, seqs, rope, n_q, rows, P, n_pos};

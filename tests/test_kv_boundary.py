@@ -12,7 +12,7 @@ pa = pytest.importorskip("paper_2605_08568_amd")
 from paper_2605_08568_amd import binding as B  # noqa: E402
 
 FAKE = 0x1000                  # non-NULL, 16-byte aligned, never read: every check below fails first
-ODD = 0x1004
+ODD = 0x1002
 EINVAL, ESHAPE, EALIGN, EWORKSPACE = -1, -2, -3, -5
 
 
@@ -78,7 +78,7 @@ def test_bookkeeping_refuses_bad_arguments():
     for name in ("reserve", "compact"):
         need = pa.lib().parse_kv_workspace_bytes(cache())
         assert c[name](ws=None) == EWORKSPACE and c[name](wsb=need - 1) == EWORKSPACE and c[name](ws=ODD) == EALIGN
-    assert c["compact"](live=0x1002) == EALIGN
+    assert c["compact"](live=ODD) == EALIGN
     assert c["trim"](window=-1) == EINVAL and c["trim"](sinks=-1) == EINVAL and c["trim"](keep=None, window=0) == EINVAL and c["trim"](keep=ODD) == EALIGN
 
 
@@ -88,7 +88,7 @@ def test_append_refuses_bad_arguments():
         assert c(**bad) == EINVAL, bad
     for bad in (dict(layer=2), dict(P=4097), dict(seqs=None, P=4), dict(off=None), dict(ks=248), dict(vs=8), dict(qs=504), dict(qos=0), dict(rows=(1 << 24) + 1)):
         assert c(**bad) == ESHAPE, bad
-    for bad in (dict(k=ODD), dict(v=ODD), dict(q=ODD), dict(qo=ODD), dict(rope=ODD), dict(ks=260), dict(vs=260), dict(qs=516), dict(qos=516)):
+    for bad in (dict(k=ODD), dict(v=ODD), dict(q=ODD), dict(qo=ODD), dict(rope=ODD), dict(off=ODD), dict(seqs=ODD), dict(k=FAKE + 4), dict(rope=FAKE + 4), dict(ks=260), dict(vs=260), dict(qs=516), dict(qos=516)):
         assert c(**bad) == EALIGN, bad
 
 
@@ -101,7 +101,7 @@ def test_attention_refuses_bad_arguments(name):
         assert c(**{**rows, **bad}) == EINVAL, bad
     for bad in (dict(layer=2), dict(n_q=6, qs=512), dict(qs=504), dict(outs=504), dict(n_q=65540)):
         assert c(**{**rows, **bad}) == ESHAPE, bad
-    for bad in (dict(q=ODD), dict(out=ODD), dict(lse=0x1002), dict(qs=516), dict(outs=516)):
+    for bad in (dict(q=ODD), dict(out=ODD), dict(lse=ODD), dict(seqs=ODD), dict(q=FAKE + 8), dict(qs=516), dict(outs=516)):
         assert c(**{**rows, **bad}) == EALIGN, bad
     if name == "decode":
         assert c(rows=4097) == ESHAPE and c(rows=4, seqs=None) == ESHAPE
