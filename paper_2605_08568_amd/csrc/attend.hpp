@@ -18,6 +18,10 @@ int check_kv(const parse_kv *kv, bool counts);
 int check_attend(const parse_kv *kv, int layer, const void *q, int64_t q_stride, int n_q, int rows, const int32_t *tok_offsets, const int32_t *seqs, float scale,
                  int window, int sinks, const void *out, int64_t out_stride, const float *lse);
 
+// A word that every lane of the wavefront reads alike, through the scalar cache: it comes without a place in the queue of vector loads, whose
+// order the staged tiles count on.
+__device__ __forceinline__ int scalar_word(const int32_t *p) { return *(const __attribute__((address_space(4))) int32_t *)(uintptr_t)p; }
+
 // a row's sequence: the table's row and its length; nothing where the number is out of range
 struct KvSeq {
   int row, len;
@@ -95,6 +99,19 @@ __device__ __forceinline__ int kv_find(const int *pre, int P, int v) {
   return lo;
 }
 
+// The running maximum of a softmax may lag behind by this much, in powers of two: weights stay below 2^8, and the sums are
+// multiplied over only where a maximum grows by more (the first tile of a row, then hardly ever).
+constexpr float AT_LAG = 8.f;
+// Maxima are taken of the products q.k themselves; a weight is then one fused multiply-add and a 2^x.  That needs a positive scale: its
+// sign goes to q, and a scale of zero makes q zero (so that a masked score of -inf is never multiplied by 0).
+constexpr uint32_t AT_AS_IT_IS = 0, AT_TURNED = 1, AT_ZERO = 2;
+static inline void at_scale(float given, float &scale, float &lag, uint32_t &q_sign) {
+  scale = fabsf(given) * 1.4426950408889634f;
+  q_sign = scale == 0.f ? AT_ZERO : given < 0.f ? AT_TURNED : AT_AS_IT_IS;
+  if (scale == 0.f) scale = 1.f;
+  lag = fminf(AT_LAG / scale, 3e38f);
+}
+
 // Eight consecutive values of a lane's operand row (columns of K, tokens of V).  bf16: one operand of a 16x16x32 or 32x32x16
 // instruction; fp32: eight steps of 16x16x4 or 32x32x2, step e with every lane's value e.  Lane layouts are the same: operand
 // row lane % M, the eight reduction indices 8 * (lane / M) + e.
@@ -108,6 +125,12 @@ template <> struct Op<uint16_t> {
   }
   static __device__ __forceinline__ f32x16 mma32(frag a, frag b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
+  }
+  // q for a scale of either sign (AtScale): the scores' sign turned, or zeros
+  static __device__ __forceinline__ frag sign(frag a, uint32_t s) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) a[w] = s == AT_ZERO ? 0u : a[w] ^ (s == AT_TURNED ? 0x80008000u : 0u);
+    return a;
   }
   // weights in [0, 2^8]: rounded to bf16, 2^-8 relative at most, independent from token to token
   static __device__ __forceinline__ frag pack(const float *p) {
@@ -159,6 +182,12 @@ template <> struct Op<float> {
     for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.hi[e], b.hi[e], c, 0, 0, 0);
     return c;
   }
+  static __device__ __forceinline__ frag sign(frag a, uint32_t s) {
+    const float by = s == AT_TURNED ? -1.f : 1.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { a.lo[e] = s == AT_ZERO ? 0.f : a.lo[e] * by; a.hi[e] = s == AT_ZERO ? 0.f : a.hi[e] * by; }
+    return a;
+  }
   static __device__ __forceinline__ frag pack(const float *p) { return frag{f32x4{p[0], p[1], p[2], p[3]}, f32x4{p[4], p[5], p[6], p[7]}}; }
   static __device__ __forceinline__ frag only(frag a, uint32_t keep) {
 #pragma unroll
@@ -197,9 +226,6 @@ template <int N> __device__ __forceinline__ float lane_sum(float v) {
   return __uint_as_float(s[0]) + __uint_as_float(s[1]);
 }
 
-// The running maximum of a softmax may lag behind by this much, in powers of two: weights stay below 2^8, and the sums are
-// multiplied over only where a maximum grows by more (the first tile of a row, then hardly ever).
-constexpr float AT_LAG = 8.f;
 // 2^x of the vector unit: one rounding; below 2^-126 it is 0
 __device__ __forceinline__ float at_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float finite_or_0(float m) { return m == -INFINITY ? 0.f : m; }

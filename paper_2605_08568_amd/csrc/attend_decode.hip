@@ -17,7 +17,8 @@ struct AdArgs {
   const int32_t *seqs;
   int64_t q_stride, out_stride;
   int n_q, group, rows, shares, window, sinks;
-  float scale;                                       // times log2(e)
+  float scale, lag;                                  // |scale| times log2(e); AT_LAG in products of q and k
+  uint32_t q_sign;
   float *part;                                       // [kv head][group of 16 heads][share][2] of AD_HEADS * (d + 2)
 };
 
@@ -64,7 +65,7 @@ __global__ __launch_bounds__(AD_THREADS) void attend_decode(AdArgs a) {
     {
       const T *q = reinterpret_cast<const T *>(a.q) + (int64_t)b * a.q_stride + (int64_t)(kvh * a.group + hg * AD_HEADS + min(n, heads - 1)) * D;
 #pragma unroll
-      for (int k = 0; k < KB; ++k) qf[k] = Op<T>::load(q + 32 * k + 8 * quad);
+      for (int k = 0; k < KB; ++k) qf[k] = Op<T>::sign(Op<T>::load(q + 32 * k + 8 * quad), a.q_sign);
     }
     float m = -INFINITY, l = 0.f;
     f32x4 o[VB];
@@ -99,7 +100,7 @@ __global__ __launch_bounds__(AD_THREADS) void attend_decode(AdArgs a) {
       for (int k = 0; k < KB; ++k) { s0 = Op<T>::mma16(k0[k], qf[k], s0); s1 = Op<T>::mma16(k1[k], qf[k], s1); }
       float s[8];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) { s[e] = s0[e] * a.scale; s[4 + e] = s1[e] * a.scale; }
+      for (int e = 0; e < 4; ++e) { s[e] = s0[e]; s[4 + e] = s1[e]; }
       const bool whole = there[0] && there[1] && t0 + AD_STEP - 1 <= pos && (t0 >= lo || t0 + AD_STEP <= a.sinks);
       if (!whole) {                                                // what is not seen: no weight, and nothing of V to multiply it with
         uint32_t keep = 0;
@@ -116,18 +117,18 @@ __global__ __launch_bounds__(AD_THREADS) void attend_decode(AdArgs a) {
       float top = s[0];
 #pragma unroll
       for (int e = 1; e < 8; ++e) top = fmaxf(top, s[e]);
-      if (__any(top > m + AT_LAG)) {
+      if (__any(top > m + a.lag)) {
         const float grown = fmaxf(m, lane_max<32>(lane_max<16>(top)));
-        const float by = at_exp2(m - finite_or_0(grown));
+        const float by = at_exp2((m - finite_or_0(grown)) * a.scale);
         l *= by;
 #pragma unroll
         for (int v = 0; v < VB; ++v) o[v] *= by;
         m = grown;
       }
-      const float base = finite_or_0(m);
+      const float base = finite_or_0(m) * a.scale;
       float p[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) { p[e] = at_exp2(s[e] - base); l += p[e]; }
+      for (int e = 0; e < 8; ++e) { p[e] = at_exp2(fmaf(s[e], a.scale, -base)); l += p[e]; }
       const frag pf = Op<T>::pack(p);
 #pragma unroll
       for (int v = 0; v < VB; ++v) o[v] = Op<T>::mma16(vf[v], pf, o[v]);
@@ -148,7 +149,7 @@ __global__ __launch_bounds__(AD_THREADS) void attend_decode(AdArgs a) {
       for (int w = 0; w < AD_WAVES; ++w) top = fmaxf(top, red_m[w * AD_HEADS + h]);
 #pragma unroll
       for (int w = 0; w < AD_WAVES; ++w) {
-        const float by = at_exp2(red_m[w * AD_HEADS + h] - finite_or_0(top));
+        const float by = at_exp2((red_m[w * AD_HEADS + h] - finite_or_0(top)) * a.scale);
         ls += by * red_l[w * AD_HEADS + h];
         os += by * red[(w * AD_HEADS + h) * D + i];
       }
@@ -157,7 +158,7 @@ __global__ __launch_bounds__(AD_THREADS) void attend_decode(AdArgs a) {
         const float y = ls == 0.f ? 0.f : os / ls;
         if constexpr (sizeof(T) == 2) reinterpret_cast<uint16_t *>(a.out)[(int64_t)b * a.out_stride + head * D + i] = (uint16_t)cvt_pk_bf16(y, 0.f);
         else reinterpret_cast<float *>(a.out)[(int64_t)b * a.out_stride + head * D + i] = y;
-        if (a.lse && i == 0) a.lse[(int64_t)b * a.n_q + head] = (top + log2f(ls)) * 0.6931471805599453f;
+        if (a.lse && i == 0) a.lse[(int64_t)b * a.n_q + head] = (finite_or_0(top) * a.scale + log2f(ls)) * 0.6931471805599453f;
       } else {
         part[h * D + i] = os;
         if (i == 0) { part[AD_HEADS * D + h] = top; part[AD_HEADS * (D + 1) + h] = ls; }
@@ -190,7 +191,7 @@ __global__ __launch_bounds__(AD_THREADS) void attend_join(AdArgs a) {
     for (int x = x0; x <= x1; ++x) {
       const float *part = parts + ((int64_t)x * 2 + ((int64_t)x * per <= pre[b] ? 1 : 0)) * AD_HEADS * (D + 2);
       const float m = part[AD_HEADS * D + h], grown = fmaxf(top, m);
-      const float was = at_exp2(top - finite_or_0(grown)), by = at_exp2(m - finite_or_0(grown));
+      const float was = at_exp2((top - finite_or_0(grown)) * a.scale), by = at_exp2((m - finite_or_0(grown)) * a.scale);
       ls = ls * was + by * part[AD_HEADS * (D + 1) + h];
       os = os * was + by * part[h * D + i];
       top = grown;
@@ -199,7 +200,7 @@ __global__ __launch_bounds__(AD_THREADS) void attend_join(AdArgs a) {
     const float y = ls == 0.f ? 0.f : os / ls;
     if constexpr (sizeof(T) == 2) reinterpret_cast<uint16_t *>(a.out)[(int64_t)b * a.out_stride + head * D + i] = (uint16_t)cvt_pk_bf16(y, 0.f);
     else reinterpret_cast<float *>(a.out)[(int64_t)b * a.out_stride + head * D + i] = y;
-    if (a.lse && i == 0) a.lse[(int64_t)b * a.n_q + head] = (top + log2f(ls)) * 0.6931471805599453f;
+    if (a.lse && i == 0) a.lse[(int64_t)b * a.n_q + head] = (finite_or_0(top) * a.scale + log2f(ls)) * 0.6931471805599453f;
   }
 }
 
@@ -244,7 +245,7 @@ int check_attend(const parse_kv *kv, int layer, const void *q, int64_t q_stride,
                  int window, int sinks, const void *out, int64_t out_stride, const float *lse) {
   const int st = check_kv(kv, false);
   if (st != PARSE_OK) return st;
-  if (!q || !out || n_q <= 0 || rows <= 0 || layer < 0 || window < 0 || sinks < 0 || !(scale - scale == 0.f)) return PARSE_EINVAL;
+  if (!q || !out || n_q <= 0 || rows <= 0 || layer < 0 || window < 0 || sinks < 0 || !(fabsf(scale) < 1e38f)) return PARSE_EINVAL;
   if (layer >= kv->n_layers || n_q % kv->n_kv != 0 || n_q > 65536 || (int64_t)rows * n_q > INT32_MAX) return PARSE_ESHAPE;
   if (q_stride < (int64_t)n_q * kv->d || out_stride < (int64_t)n_q * kv->d) return PARSE_ESHAPE;
   const int per16 = 16 / elem_size(kv->dtype);
@@ -278,7 +279,7 @@ int parse_attend_decode(const parse_kv *kv, int32_t layer, const void *q, int64_
   a.q_stride = q_stride; a.out_stride = out_stride;
   a.n_q = n_q; a.group = n_q / kv->n_kv; a.rows = rows; a.window = window; a.sinks = sinks;
   a.shares = ad_shares(kv, n_q);
-  a.scale = scale * 1.4426950408889634f;
+  at_scale(scale, a.scale, a.lag, a.q_sign);
   a.part = (float *)workspace;
   return kv->dtype == PARSE_BF16 ? ad_width<uint16_t>(a, (hipStream_t)stream) : ad_width<float>(a, (hipStream_t)stream);
 }

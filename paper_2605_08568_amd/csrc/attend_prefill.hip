@@ -12,34 +12,67 @@ struct ApArgs {
   const int32_t *tok_offsets, *seqs;
   int64_t q_stride, out_stride;
   int n_q, group, rows, P, tiles, window, sinks;
-  float scale;                                       // times log2(e)
+  float scale, lag;                                  // |scale| times log2(e); AT_LAG in products of q and k
+  uint32_t q_sign;
 };
 
 // A workgroup has NW * 32 rows of one kv head: row r of a prompt is head r % group of token r / group, so that shared
-// heads read a tile of K and V once.  Tiles of TK tokens are staged in LDS as they stand in the pages.  Both products
-// have the cache's side as operand A and the rows as columns: a lane holds weights of one row only, the softmax needs one
-// exchange between lane halves, and what comes out of the first product is what the second takes.
-template <class T, int DT, int NW, int TK>
+// heads read a tile of K and V once.  Tiles of TK tokens are staged in LDS as they stand in the pages, ST buffers deep.  Both
+// products have the cache's side as operand A and the rows as columns: a lane holds weights of one row only, the softmax needs
+// one exchange between lane halves, and what comes out of the first product is what the second takes.
+template <class T, int DT, int NW, int TK, int ST>
 __global__ __launch_bounds__(NW * 64) void attend_prefill(ApArgs a) {
   constexpr int D = DT * 32, KB = D / 16, TB = TK / 16, TS = TK / 32, TM = NW * 32, THREADS = NW * 64;
   constexpr int BLOCK = 16 * D * (int)sizeof(T);                   // bytes of sixteen tokens of K, and of V
   constexpr int STAGE = 2 * TB * BLOCK, PIECES = STAGE / 1024, LOADS = PIECES / NW;
-  static_assert(PIECES % NW == 0, "every wavefront stages as much");
+  static_assert(PIECES % NW == 0 && ST >= 2 && ST <= 3, "every wavefront stages as much");
   typedef typename Op<T>::frag frag;
   extern __shared__ char smem[];
-  int *wave_sums = reinterpret_cast<int *>(smem + 2 * STAGE), *pre = wave_sums + NW;
+  int *wave_sums = reinterpret_cast<int *>(smem + ST * STAGE), *pre = wave_sums + NW;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, half = lane >> 5;
   const int kvh = blockIdx.x % a.kv.n_kv, item = blockIdx.x / a.kv.n_kv, group = a.group;
   kv_prefix<THREADS>(a.P, pre, wave_sums, [&](int p) { return (int)(((int64_t)kv_rows(a.tok_offsets, p, a.rows).n * group + TM - 1) / TM); });
   if (item >= pre[a.P]) return;
-  const int p = kv_find(pre, a.P, item);
+  const int p = __builtin_amdgcn_readfirstlane(kv_find(pre, a.P, item));
   const KvRows pr = kv_rows(a.tok_offsets, p, a.rows);
   const KvSeq sq = kv_seq(a.kv, a.seqs, p);
-  const int32_t *table = a.kv.table + (int64_t)sq.row * a.kv.max_pages;
-  const int r0 = (pre[p + 1] - 1 - item) * TM;                     // the rows that see most come first
-  const int r_end = pr.n * group, base = sq.len - pr.n;
+  const int seq_row = __builtin_amdgcn_readfirstlane(sq.row), len = __builtin_amdgcn_readfirstlane(sq.len), n_rows = __builtin_amdgcn_readfirstlane(pr.n),
+            row0 = __builtin_amdgcn_readfirstlane(pr.first);
+  const int32_t *table = a.kv.table + (int64_t)seq_row * a.kv.max_pages;
+  const int r0 = (__builtin_amdgcn_readfirstlane(pre[p + 1]) - 1 - item) * TM;     // the rows that see most come first
+  const int r_end = n_rows * group, base = len - n_rows;
   const int i0 = base + r0 / group, i1 = base + (min(r0 + TM, r_end) - 1) / group;
   const KvSpan span = i1 < 0 ? KvSpan{0, 0, 0} : kv_span(max(i0, 0), i1, a.window, a.sinks, TK);
+
+  // the pages of a tile's blocks of sixteen tokens, -1 for none; asked for a tile before they are used
+  const int page_bits = 31 - __builtin_clz(a.kv.page);
+  struct Ids { int id[TB]; };
+  auto ids_of = [&](int u) {
+    Ids r;
+    const int t0 = span.at(u) * TK;
+#pragma unroll
+    for (int b = 0; b < TB; ++b) r.id[b] = scalar_word(table + min((t0 + 16 * b) >> page_bits, a.kv.max_pages - 1));
+    return r;
+  };
+  const int64_t page_elems = (int64_t)a.kv.n_kv * a.kv.page * D, head0 = (int64_t)kvh * a.kv.page * D;
+  auto ok = [&](int id) { return (unsigned)id < (unsigned)a.kv.n_pages; };
+  auto stage = [&](int u, const Ids &ids, int buf) {
+    const int t0 = span.at(u) * TK;
+#pragma unroll
+    for (int q = 0; q < LOADS; ++q) {
+      const int piece = wave * LOADS + q, of_v = piece / (PIECES / 2), rest = piece % (PIECES / 2), block = rest / (BLOCK / 1024);
+      int id = ids.id[0];
+#pragma unroll
+      for (int b = 1; b < TB; ++b) id = block == b ? ids.id[b] : id;
+      id = ok(id) ? id : 0;
+      const char *src = (const char *)(of_v ? a.V : a.K) + ((int64_t)id * page_elems + head0 + (int64_t)((t0 + 16 * block) & (a.kv.page - 1)) * D) * (int64_t)sizeof(T) +
+                        (rest % (BLOCK / 1024)) * 1024;
+      __builtin_amdgcn_global_load_lds(PARSE_GLB_PTR(src + lane * 16), PARSE_LDS_PTR(smem + buf * STAGE + piece * 1024), 16, 0, 0);
+    }
+  };
+  Ids now{}, next{}, later{};                                      // of tiles u, u + 1, u + 2
+  if (span.count > 0) now = ids_of(0);
+  if (span.count > 1) next = ids_of(1);
 
   // this lane's row, and the positions of the wavefront's rows
   const int r = r0 + wave * 32 + n, token = min(r, r_end - 1) / group, head = kvh * group + (min(r, r_end - 1) - token * group);
@@ -49,42 +82,33 @@ __global__ __launch_bounds__(NW * 64) void attend_prefill(ApArgs a) {
   const bool idle = r0 + wave * 32 >= r_end;
   frag qf[KB];
   {
-    const T *q = reinterpret_cast<const T *>(a.q) + (int64_t)(pr.first + token) * a.q_stride + (int64_t)head * D + 8 * half;
+    const T *q = reinterpret_cast<const T *>(a.q) + (int64_t)(row0 + token) * a.q_stride + (int64_t)head * D + 8 * half;
 #pragma unroll
-    for (int k = 0; k < KB; ++k) qf[k] = Op<T>::load(q + 16 * k);
+    for (int k = 0; k < KB; ++k) qf[k] = Op<T>::sign(Op<T>::load(q + 16 * k), a.q_sign);
   }
+  // what a lane has asked for so far has come: from here on the loads on their way are staged tiles only
+  wait_vm<0>();
+  if (span.count > 0) stage(0, now, 0);
+  if (ST == 3 && span.count > 1) stage(1, next, 1);
   float m = -INFINITY, l = 0.f;
   f32x16 o[DT];
 #pragma unroll
   for (int d = 0; d < DT; ++d)
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
-
-  const int64_t head0 = (int64_t)kvh * a.kv.page * D, page_elems = (int64_t)a.kv.n_kv * a.kv.page * D;
-  const int page_bits = 31 - __builtin_clz(a.kv.page);
-  auto page_of = [&](int t) {                                      // of token t; -1 if there is none
-    const int c = t >> page_bits, id = c < a.kv.max_pages ? table[c] : -1;
-    return id >= 0 && id < a.kv.n_pages ? id : -1;
-  };
-  auto stage = [&](int t0, int buf) {
-#pragma unroll
-    for (int u = 0; u < LOADS; ++u) {
-      const int piece = wave * LOADS + u, of_v = piece / (PIECES / 2), rest = piece % (PIECES / 2), block = rest / (BLOCK / 1024);
-      const int id = max(page_of(t0 + 16 * block), 0);
-      const char *src = (const char *)(of_v ? a.V : a.K) +
-                        (id * page_elems + head0 + (int64_t)((t0 + 16 * block) & (a.kv.page - 1)) * D) * (int64_t)sizeof(T) + (rest % (BLOCK / 1024)) * 1024 + lane * 16;
-      __builtin_amdgcn_global_load_lds(PARSE_GLB_PTR(src), PARSE_LDS_PTR(smem + buf * STAGE + piece * 1024), 16, 0, 0);
-    }
-  };
   // the first product's operand row n of 32 tokens: token ktok, so that a lane half gets eight consecutive tokens of each sixteen
   const int ktok = 16 * (n >> 4) + 8 * ((n >> 2) & 1) + 4 * ((n >> 3) & 1) + (n & 3);
 
-  if (span.count > 0) stage(span.at(0) * TK, 0);
-  for (int u = 0; u < span.count; ++u) {
-    const int t0 = span.at(u) * TK, buf = u & 1;
-    wait_vm<0>();
-    __syncthreads();                                               // this tile has landed, the other buffer is read
-    if (u + 1 < span.count) stage(span.at(u + 1) * TK, buf ^ 1);
+  int buf = 0;
+  for (int u = 0; u < span.count; ++u, buf = buf + 1 == ST ? 0 : buf + 1) {
+    const int t0 = span.at(u) * TK;
+    if (u + 2 < span.count) later = ids_of(u + 2);
+    if (ST == 3 && u + 1 < span.count) wait_vm<LOADS>(); else wait_vm<0>();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    wg_barrier();                                                  // this tile has landed for everybody, the one before it is read by everybody
+    if (u + ST - 1 < span.count) stage(u + ST - 1, ST == 3 ? later : next, buf == 0 ? ST - 1 : buf - 1);
+    const Ids ids = now;
+    now = next; next = later;
     if (idle || t0 > wi1 || (t0 + TK <= wlo && t0 >= a.sinks)) continue;
     const T *ks = reinterpret_cast<const T *>(smem + buf * STAGE), *vs = reinterpret_cast<const T *>(smem + buf * STAGE + STAGE / 2);
     f32x16 sc[TS];
@@ -96,17 +120,10 @@ __global__ __launch_bounds__(NW * 64) void attend_prefill(ApArgs a) {
 #pragma unroll
       for (int k = 0; k < KB; ++k) sc[s] = Op<T>::mma32(Op<T>::load(kr + k * 256), qf[k], sc[s]);
     }
-    bool there = true;
     uint32_t blocks = 0;                                           // of sixteen tokens whose page is there
 #pragma unroll
-    for (int b = 0; b < TB; ++b) {
-      const bool is = page_of(t0 + 16 * b) >= 0;
-      blocks |= (is ? 1u : 0u) << b;
-      there = there && is;
-    }
-    const bool whole = there && t0 + TK - 1 <= wi0 && (t0 >= whi || t0 + TK <= a.sinks);
-#pragma unroll
-    for (int s = 0; s < TS; ++s) sc[s] *= a.scale;
+    for (int b = 0; b < TB; ++b) blocks |= (ok(ids.id[b]) ? 1u : 0u) << b;
+    const bool whole = blocks == (1u << TB) - 1u && t0 + TK - 1 <= wi0 && (t0 >= whi || t0 + TK <= a.sinks);
     if (!whole) {
 #pragma unroll
       for (int s = 0; s < TS; ++s)
@@ -121,41 +138,43 @@ __global__ __launch_bounds__(NW * 64) void attend_prefill(ApArgs a) {
     for (int s = 0; s < TS; ++s)
 #pragma unroll
       for (int x = 0; x < 16; ++x) top = fmaxf(top, sc[s][x]);
-    if (__any(top > m + AT_LAG)) {
+    if (__any(top > m + a.lag)) {
       const float grown = fmaxf(m, lane_max<32>(top));
-      const float by = at_exp2(m - finite_or_0(grown));
+      const float by = at_exp2((m - finite_or_0(grown)) * a.scale);
       l *= by;
 #pragma unroll
       for (int d = 0; d < DT; ++d) o[d] *= by;
       m = grown;
     }
-    const float low = finite_or_0(m);
+    const float low = finite_or_0(m) * a.scale;
     frag pf[TB];
 #pragma unroll
     for (int b = 0; b < TB; ++b) {
       float w[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) { w[e] = at_exp2(sc[b / 2][8 * (b % 2) + e] - low); l += w[e]; sc[b / 2][8 * (b % 2) + e] = w[e]; }
+      for (int e = 0; e < 8; ++e) { w[e] = at_exp2(fmaf(sc[b / 2][8 * (b % 2) + e], a.scale, -low)); l += w[e]; sc[b / 2][8 * (b % 2) + e] = w[e]; }
       pf[b] = Op<T>::pack(w);
+    }
+    if (whole) {
+#pragma unroll
+      for (int b = 0; b < TB; ++b) {
+        const T *vr = vs + b * 16 * D + (half * D + n) * 8;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[d] = Op<T>::mma32(Op<T>::load(vr + d * 256), pf[b], o[d]);
+      }
+      continue;
     }
     bool bad = false;
 #pragma unroll
     for (int b = 0; b < TB; ++b) {
       const T *vr = vs + b * 16 * D + (half * D + n) * 8;
-      // tokens that some row of the wavefront sees
-      uint32_t keep = 255;
-      if (!whole) {
-        keep = 0;
+      uint32_t keep = 0;                                           // tokens that some row of the wavefront sees
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int j = t0 + 16 * b + 8 * half + e;
-          keep |= (blocks >> b & 1u & (kv_sees(wi1, wlo, a.sinks, j) ? 1u : 0u)) << e;
-        }
-      }
+      for (int e = 0; e < 8; ++e) keep |= (blocks >> b & 1u & (kv_sees(wi1, wlo, a.sinks, t0 + 16 * b + 8 * half + e) ? 1u : 0u)) << e;
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
-        frag vf = Op<T>::load(vr + d * 256);
-        if (!whole) { vf = Op<T>::only(vf, keep); bad |= Op<T>::finite_only(vf); }
+        frag vf = Op<T>::only(Op<T>::load(vr + d * 256), keep);
+        bad |= Op<T>::finite_only(vf);
         o[d] = Op<T>::mma32(vf, pf[b], o[d]);
       }
     }
@@ -168,8 +187,7 @@ __global__ __launch_bounds__(NW * 64) void attend_prefill(ApArgs a) {
 #pragma unroll
         for (int c = 0; c < TB; ++c)
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (c == b && e == (j & 7)) w = sc[c / 2][8 * (c % 2) + e];
+          for (int e = 0; e < 8; ++e) w = ((c == b) & (e == (j & 7))) ? sc[c / 2][8 * (c % 2) + e] : w;
         w = __shfl(w, n + 32 * h, 64);
         if constexpr (sizeof(T) == 2) w = __uint_as_float(cvt_pk_bf16(w, 0.f) << 16);
         const bool mine = (bool)(blocks >> b & 1) & kv_sees(i, lo, a.sinks, t0 + j);
@@ -179,7 +197,8 @@ __global__ __launch_bounds__(NW * 64) void attend_prefill(ApArgs a) {
 #pragma unroll
           for (int x = 0; x < 16; ++x) {
             const T v = vr[(32 * d + 8 * (x / 4) + 4 * half + x % 4) * 8];
-            if (mine && !Op<T>::finite(v)) o[d][x] += w * Op<T>::value(v);
+            const float add = w * Op<T>::value(v);
+            o[d][x] = (mine & !Op<T>::finite(v)) ? o[d][x] + add : o[d][x];
           }
       }
     }
@@ -187,37 +206,37 @@ __global__ __launch_bounds__(NW * 64) void attend_prefill(ApArgs a) {
   if (idle || r >= r_end) return;
   l = lane_sum<32>(l);
   const float by = l == 0.f ? 0.f : 1.f / l;
-  T *out = reinterpret_cast<T *>(a.out) + (int64_t)(pr.first + token) * a.out_stride + (int64_t)head * D;
+  T *out = reinterpret_cast<T *>(a.out) + (int64_t)(row0 + token) * a.out_stride + (int64_t)head * D;
 #pragma unroll
   for (int d = 0; d < DT; ++d)
 #pragma unroll
     for (int c = 0; c < 4; ++c)
       Op<T>::store4(out + 32 * d + 8 * c + 4 * half, o[d][4 * c] * by, o[d][4 * c + 1] * by, o[d][4 * c + 2] * by, o[d][4 * c + 3] * by);
-  if (a.lse && half == 0) a.lse[(int64_t)(pr.first + token) * a.n_q + head] = (m + log2f(l)) * 0.6931471805599453f;
+  if (a.lse && half == 0) a.lse[(int64_t)(row0 + token) * a.n_q + head] = (finite_or_0(m) * a.scale + log2f(l)) * 0.6931471805599453f;
 }
 
-template <class T, int DT, int NW, int TK>
-static int ap_launch(ApArgs &a, hipStream_t s) {
+template <class T, int DT, int NW, int TK, int ST>
+static int ap_launch(const ApArgs &a, hipStream_t s) {
   // a prompt's last tile may be begun only: rows / tile + prompts in all
   const int64_t tiles = ((int64_t)a.rows * a.group) / (NW * 32) + min(a.P, a.rows);
   if (tiles * a.kv.n_kv > INT32_MAX) return PARSE_ESHAPE;
-  const size_t lds = 2 * 2 * TK * DT * 32 * sizeof(T) + (NW + a.P + 1) * 4;
-  PARSE_ALLOW_LDS((attend_prefill<T, DT, NW, TK>), 0, lds);
-  attend_prefill<T, DT, NW, TK><<<dim3((uint32_t)(tiles * a.kv.n_kv)), NW * 64, lds, s>>>(a);
+  const size_t lds = (size_t)ST * 2 * TK * DT * 32 * sizeof(T) + (NW + a.P + 1) * 4;
+  PARSE_ALLOW_LDS((attend_prefill<T, DT, NW, TK, ST>), 0, lds);
+  attend_prefill<T, DT, NW, TK, ST><<<dim3((uint32_t)(tiles * a.kv.n_kv)), NW * 64, lds, s>>>(a);
   PARSE_LAUNCH_CHECK();
   return PARSE_OK;
 }
 template <class T>
-static int ap_width(ApArgs &a, hipStream_t s) {
+static int ap_width(const ApArgs &a, hipStream_t s) {
   switch (a.kv.d / 32) {
-    case 1: return ap_launch<T, 1, 4, 32>(a, s);
-    case 2: return ap_launch<T, 2, 4, 32>(a, s);
-    case 3: return ap_launch<T, 3, 4, 32>(a, s);
-    case 4: return ap_launch<T, 4, 4, 32>(a, s);
-    case 5: return ap_launch<T, 5, 4, 32>(a, s);
-    case 6: return ap_launch<T, 6, 4, 32>(a, s);
-    case 7: return ap_launch<T, 7, 4, 32>(a, s);
-    default: return ap_launch<T, 8, 4, 32>(a, s);
+    case 1: return ap_launch<T, 1, 4, 32, 2>(a, s);
+    case 2: return ap_launch<T, 2, 4, 32, 2>(a, s);
+    case 3: return ap_launch<T, 3, 4, 32, 2>(a, s);
+    case 4: return ap_launch<T, 4, 4, 32, 2>(a, s);
+    case 5: return ap_launch<T, 5, 4, 32, 2>(a, s);
+    case 6: return ap_launch<T, 6, 4, 32, 2>(a, s);
+    case 7: return ap_launch<T, 7, 4, 32, 2>(a, s);
+    default: return ap_launch<T, 8, 4, 32, 2>(a, s);
   }
 }
 
@@ -246,7 +265,7 @@ int parse_attend_prefill(const parse_kv *kv, int32_t layer, const void *q, int64
   a.q = q; a.out = out; a.lse = lse; a.tok_offsets = tok_offsets; a.seqs = seqs;
   a.q_stride = q_stride; a.out_stride = out_stride;
   a.n_q = n_q; a.group = n_q / kv->n_kv; a.rows = rows; a.P = P; a.window = window; a.sinks = sinks;
-  a.scale = scale * 1.4426950408889634f;
+  at_scale(scale, a.scale, a.lag, a.q_sign);
   return kv->dtype == PARSE_BF16 ? ap_width<uint16_t>(a, (hipStream_t)stream) : ap_width<float>(a, (hipStream_t)stream);
 }
 
