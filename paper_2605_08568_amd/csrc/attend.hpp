@@ -112,6 +112,52 @@ static inline void at_scale(float given, float &scale, float &lag, uint32_t &q_s
   lag = fminf(AT_LAG / scale, 3e38f);
 }
 
+// Which prompt a row tile belongs to.  Prompts have ceil(rows * group / tile) tiles each, numbered through.
+struct KvItem {
+  int p, first, n, row, len, tile;             // rows, sequence, tile of the prompt; tile < 0: there is no such item
+};
+// A wavefront alone, for up to 64 prompts: a lane reads a prompt's words, all at once.
+__device__ __forceinline__ KvItem kv_item_wave(const parse_kv &kv, const int32_t *__restrict__ tok_offsets, const int32_t *__restrict__ seqs, int P, int rows, int group,
+                                               int tile, int item) {
+  const int lane = threadIdx.x & 63, p = min(lane, P - 1);
+  const KvRows r = kv_rows(tok_offsets, p, rows);
+  const KvSeq s = kv_seq(kv, seqs, p);
+  const int tiles = lane < P ? (int)(((int64_t)r.n * group + tile - 1) / tile) : 0;
+  int inc = tiles;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int v = __shfl_up(inc, o, 64);
+    if (lane >= o) inc += v;
+  }
+  const int at = __builtin_amdgcn_readfirstlane(__popcll(__ballot(inc <= item)));    // prompts whose tiles all lie before
+  KvItem f{at, 0, 0, 0, 0, -1};
+  if (at >= P) return f;
+  f.first = __builtin_amdgcn_readlane(r.first, at);
+  f.n = __builtin_amdgcn_readlane(r.n, at);
+  f.row = __builtin_amdgcn_readlane(s.row, at);
+  f.len = __builtin_amdgcn_readlane(s.len, at);
+  f.tile = item - (__builtin_amdgcn_readlane(inc, at) - __builtin_amdgcn_readlane(tiles, at));
+  return f;
+}
+// A workgroup, for any number
+template <int THREADS>
+__device__ __forceinline__ KvItem kv_item(const parse_kv &kv, const int32_t *__restrict__ tok_offsets, const int32_t *__restrict__ seqs, int P, int rows, int group,
+                                          int tile, int item, int *pre, int *wave_sums) {
+  if (P <= 64) return kv_item_wave(kv, tok_offsets, seqs, P, rows, group, tile, item);
+  kv_prefix<THREADS>(P, pre, wave_sums, [&](int p) { return (int)(((int64_t)kv_rows(tok_offsets, p, rows).n * group + tile - 1) / tile); });
+  KvItem f{0, 0, 0, 0, 0, -1};
+  if (item >= pre[P]) return f;
+  f.p = __builtin_amdgcn_readfirstlane(kv_find(pre, P, item));
+  const KvRows r = kv_rows(tok_offsets, f.p, rows);
+  const KvSeq s = kv_seq(kv, seqs, f.p);
+  f.first = __builtin_amdgcn_readfirstlane(r.first);
+  f.n = __builtin_amdgcn_readfirstlane(r.n);
+  f.row = __builtin_amdgcn_readfirstlane(s.row);
+  f.len = __builtin_amdgcn_readfirstlane(s.len);
+  f.tile = item - __builtin_amdgcn_readfirstlane(pre[f.p]);
+  return f;
+}
+
 // Eight consecutive values of a lane's operand row (columns of K, tokens of V).  bf16: one operand of a 16x16x32 or 32x32x16
 // instruction; fp32: eight steps of 16x16x4 or 32x32x2, step e with every lane's value e.  Lane layouts are the same: operand
 // row lane % M, the eight reduction indices 8 * (lane / M) + e.
@@ -142,16 +188,16 @@ template <> struct Op<uint16_t> {
     for (int w = 0; w < 4; ++w) a[w] &= (keep >> (2 * w) & 1 ? 0xffffu : 0u) | (keep >> (2 * w + 1) & 1 ? 0xffff0000u : 0u);
     return a;
   }
-  // infinities and NaN become 0; true if there was one
-  static __device__ __forceinline__ bool finite_only(frag &a) {
-    uint32_t bad = 0;
+  // infinities and NaN become the largest finite value of their sign; `most`: largest magnitude so far, in either half
+  static __device__ __forceinline__ frag finite_only(frag a, uint32_t &most) {
+    typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      const uint32_t m = ((a[w] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((a[w] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
-      a[w] &= ~m;
-      bad |= m;
+      const u16x2 size = __builtin_bit_cast(u16x2, a[w] & 0x7fff7fffu);
+      most = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(size, __builtin_bit_cast(u16x2, most)));
+      a[w] = (a[w] & 0x80008000u) | __builtin_bit_cast(uint32_t, __builtin_elementwise_min(size, u16x2{0x7f7f, 0x7f7f}));
     }
-    return bad != 0;
+    return a;
   }
   static __device__ __forceinline__ float value(uint16_t b) { return bf16_to_f32(b); }
   static __device__ __forceinline__ bool finite(uint16_t b) { return (b & 0x7f80u) != 0x7f80u; }
@@ -197,6 +243,7 @@ template <> struct Op<float> {
     }
     return a;
   }
+  // infinities and NaN become 0; true if there was one
   static __device__ __forceinline__ bool finite_only(frag &a) {
     bool bad = false;
 #pragma unroll

@@ -31,15 +31,11 @@ __global__ __launch_bounds__(NW * 64) void attend_prefill(ApArgs a) {
   int *wave_sums = reinterpret_cast<int *>(smem + ST * STAGE), *pre = wave_sums + NW;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, half = lane >> 5;
   const int kvh = blockIdx.x % a.kv.n_kv, item = blockIdx.x / a.kv.n_kv, group = a.group;
-  kv_prefix<THREADS>(a.P, pre, wave_sums, [&](int p) { return (int)(((int64_t)kv_rows(a.tok_offsets, p, a.rows).n * group + TM - 1) / TM); });
-  if (item >= pre[a.P]) return;
-  const int p = __builtin_amdgcn_readfirstlane(kv_find(pre, a.P, item));
-  const KvRows pr = kv_rows(a.tok_offsets, p, a.rows);
-  const KvSeq sq = kv_seq(a.kv, a.seqs, p);
-  const int seq_row = __builtin_amdgcn_readfirstlane(sq.row), len = __builtin_amdgcn_readfirstlane(sq.len), n_rows = __builtin_amdgcn_readfirstlane(pr.n),
-            row0 = __builtin_amdgcn_readfirstlane(pr.first);
-  const int32_t *table = a.kv.table + (int64_t)seq_row * a.kv.max_pages;
-  const int r0 = (__builtin_amdgcn_readfirstlane(pre[p + 1]) - 1 - item) * TM;     // the rows that see most come first
+  const KvItem f = kv_item<THREADS>(a.kv, a.tok_offsets, a.seqs, a.P, a.rows, group, TM, item, pre, wave_sums);
+  if (f.tile < 0) return;
+  const int n_rows = f.n, row0 = f.first, len = f.len;
+  const int32_t *table = a.kv.table + (int64_t)f.row * a.kv.max_pages;
+  const int r0 = ((int)(((int64_t)n_rows * group + TM - 1) / TM) - 1 - f.tile) * TM;     // the rows that see most come first
   const int r_end = n_rows * group, base = len - n_rows;
   const int i0 = base + r0 / group, i1 = base + (min(r0 + TM, r_end) - 1) / group;
   const KvSpan span = i1 < 0 ? KvSpan{0, 0, 0} : kv_span(max(i0, 0), i1, a.window, a.sinks, TK);
@@ -86,8 +82,8 @@ __global__ __launch_bounds__(NW * 64) void attend_prefill(ApArgs a) {
 #pragma unroll
     for (int k = 0; k < KB; ++k) qf[k] = Op<T>::sign(Op<T>::load(q + 16 * k), a.q_sign);
   }
-  // what a lane has asked for so far has come: from here on the loads on their way are staged tiles only
-  wait_vm<0>();
+  // q comes first: whoever waits for a tile has it
+  asm volatile("" ::: "memory");
   if (span.count > 0) stage(0, now, 0);
   if (ST == 3 && span.count > 1) stage(1, next, 1);
   float m = -INFINITY, l = 0.f;
@@ -215,6 +211,281 @@ __global__ __launch_bounds__(NW * 64) void attend_prefill(ApArgs a) {
   if (a.lse && half == 0) a.lse[(int64_t)(row0 + token) * a.n_q + head] = (finite_or_0(m) * a.scale + log2f(l)) * 0.6931471805599453f;
 }
 
+// The same for bf16, with the products of one tile under the softmax of the tile before it: in an iteration a wavefront has the
+// scores of tile u and the operands of K of tile u + 1 in registers, multiplies the latter between the exponentials of the former, and reads the
+// operands of K of tile u + 2 between the products with V of tile u.  K is staged two tiles ahead of V; group j of loads is K of
+// tile j and V of tile j - 2 (at the ends a tile that is there stands for the one that is not, so that all groups are alike).
+// CAREFUL: infinities and NaN of V in places that some rows of the workgroup see and others do not reach only the former (0 times infinity would
+// reach the others).  Without, something that is not finite comes out where they are met: then nothing is stored and the answer is false.
+template <int DT, int NW, int ST, bool CAREFUL>
+__device__ __forceinline__ bool ap_rows(const ApArgs &a, const KvItem &f, char *smem) {
+  typedef uint16_t T;
+  typedef Op<T> O;
+  typedef O::frag frag;
+  constexpr int D = DT * 32, KB = D / 16, TK = 32, TB = 2, TM = NW * 32, THREADS = NW * 64;
+  constexpr int BLOCK = 32 * D, TILE = TB * BLOCK, PIECES = 2 * TILE / 1024, LOADS = PIECES / NW, AHEAD = ST - 1;   // groups on their way
+  static_assert(PIECES % NW == 0, "every wavefront stages as much");
+  int *flag = reinterpret_cast<int *>(smem + 2 * ST * TILE);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, half = lane >> 5;
+  const int kvh = blockIdx.x % a.kv.n_kv, group = a.group;
+  const int n_rows = f.n, row0 = f.first, len = f.len;
+  const int32_t *table = a.kv.table + (int64_t)f.row * a.kv.max_pages;
+  const int r0 = ((int)(((int64_t)n_rows * group + TM - 1) / TM) - 1 - f.tile) * TM;     // the rows that see most come first
+  const int r_end = n_rows * group, base = len - n_rows;
+  const int i0 = base + r0 / group, i1 = base + (min(r0 + TM, r_end) - 1) / group;
+  const KvSpan span = i1 < 0 ? KvSpan{0, 0, 0} : kv_span(max(i0, 0), i1, a.window, a.sinks, TK);
+  const int count = span.count, groups = count > 0 ? count + 2 : 0;
+
+  const int page_bits = 31 - __builtin_clz(a.kv.page);
+  struct Ids { int a, b; };                                        // pages of a tile's two blocks of sixteen tokens
+  auto ids_of = [&](int u) {
+    const int t0 = span.at(min(u, count - 1)) * TK;
+    return Ids{scalar_word(table + min(t0 >> page_bits, a.kv.max_pages - 1)), scalar_word(table + min((t0 + 16) >> page_bits, a.kv.max_pages - 1))};
+  };
+  const int64_t page_elems = (int64_t)a.kv.n_kv * a.kv.page * D, head0 = (int64_t)kvh * a.kv.page * D;
+  auto ok = [&](int id) { return (unsigned)id < (unsigned)a.kv.n_pages; };
+  // pieces wave * LOADS + 0 .. LOADS - 1 of a group; its first half is K
+  auto stage = [&](int uk, const Ids k, int uv, const Ids v, int slot_k, int slot_v) {
+    const int k_a = k.a, k_b = k.b, v_a = v.a, v_b = v.b;
+    const int tk = span.at(min(uk, count - 1)) * TK, tv = span.at(max(uv, 0)) * TK;
+#pragma unroll
+    for (int q = 0; q < LOADS; ++q) {
+      const int piece = wave * LOADS + q, of_v = piece / (PIECES / 2), rest = piece % (PIECES / 2), block = rest / (BLOCK / 1024), in = rest % (BLOCK / 1024);
+      const int t = (of_v ? tv : tk) + 16 * block;
+      int id = __builtin_amdgcn_readfirstlane(of_v ? (block ? v_b : v_a) : (block ? k_b : k_a));
+      id = ok(id) ? id : 0;
+      const char *src = (const char *)(of_v ? a.V : a.K) + ((int64_t)id * page_elems + head0 + (int64_t)(t & (a.kv.page - 1)) * D) * 2 + in * 1024;
+      char *dst = smem + (of_v ? ST * TILE + slot_v * TILE : slot_k * TILE) + rest * 1024;
+      __builtin_amdgcn_global_load_lds(PARSE_GLB_PTR(src + lane * 16), PARSE_LDS_PTR(dst), 16, 0, 0);
+    }
+  };
+
+  // this lane's row, and the positions of the wavefront's rows
+  const int r = r0 + wave * 32 + n, token = min(r, r_end - 1) / group, head = kvh * group + (min(r, r_end - 1) - token * group);
+  const int i = base + token;
+  const int wi0 = base + min(r0 + wave * 32, r_end - 1) / group, wi1 = base + min(r0 + wave * 32 + 31, r_end - 1) / group;
+  const int lo = kv_window_begin(i, a.window), wlo = kv_window_begin(wi0, a.window);
+  const bool idle = r0 + wave * 32 >= r_end;
+  frag qf[KB];
+  {
+    const T *q = reinterpret_cast<const T *>(a.q) + (int64_t)(row0 + token) * a.q_stride + (int64_t)head * D + 8 * half;
+#pragma unroll
+    for (int k = 0; k < KB; ++k) qf[k] = O::sign(O::load(q + 16 * k), a.q_sign);
+  }
+  asm volatile("" ::: "memory");                                   // q comes first: whoever waits for a tile has it
+  Ids ids[ST + 3];                                                 // of tiles u .. u + ST + 2
+  if (groups) {
+#pragma unroll
+    for (int u = 0; u < ST + 3; ++u) ids[u] = ids_of(u);
+#pragma unroll
+    for (int j = 0; j < ST; ++j)
+      if (j < groups) stage(j, ids[j], j - 2, ids[j < 2 ? 0 : j - 2], j, (j + ST - 2) % ST);
+  }
+  float m = -INFINITY, l = 0.f;
+  f32x16 o[DT], sc;
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
+  const int ktok = 16 * (n >> 4) + 8 * ((n >> 2) & 1) + 4 * ((n >> 3) & 1) + (n & 3);
+  const int k_at = ((ktok >> 4) * 16 * D + (ktok & 15) * 8 + half * 128) * 2, v_at = ST * TILE + (half * D + n) * 16;
+  frag kf[KB];
+  auto read_k = [&](int slot) {
+#pragma unroll
+    for (int k = 0; k < KB; ++k) kf[k] = O::load(reinterpret_cast<const T *>(smem + slot * TILE + k_at + k * 512));
+  };
+  auto first = [&]() {                                             // scores of the tile in kf
+    f32x16 s;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+    for (int k = 0; k < KB; ++k) s = O::mma32(kf[k], qf[k], s);
+    return s;
+  };
+  auto meet = [&]() {                                              // everybody's reads of LDS are done, everybody's loads so far have landed
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    wg_barrier();
+  };
+  if (groups) {
+    wait_slices<AHEAD, LOADS>(min(ST - 1, groups - 1));            // group 0
+    wg_barrier();
+    read_k(0);
+    sc = first();
+    wait_slices<AHEAD - 1, LOADS>(min(ST - 1, groups - 1) - 1);
+    meet();
+    if (ST < groups) stage(ST, ids[ST], ST - 2, ids[ST - 2], 0, ST - 2);
+    read_k(1);
+  }
+  int slot = 0;                                                    // u % ST
+  auto begin = [&](int u) {                                        // tile u of V and u + 2 of K are there; the loads that the freed places take
+    wait_slices<AHEAD - 1, LOADS>(min(u + 1 + AHEAD, groups - 1) - (u + 2));
+    meet();
+    if (u + 2 + AHEAD < groups) stage(u + 2 + AHEAD, ids[2 + AHEAD], u + AHEAD, ids[AHEAD], (slot + 1) % ST, (slot + AHEAD) % ST);
+  };
+  auto end = [&](int u) {
+#pragma unroll
+    for (int e = 0; e < ST + 2; ++e) ids[e] = ids[e + 1];
+    ids[ST + 2] = ids_of(u + ST + 3);
+    slot = slot + 1 == ST ? 0 : slot + 1;
+  };
+  auto lag = [&]() {                                               // the running maximum, where it has to grow
+    float top = -INFINITY;
+#pragma unroll
+    for (int x = 0; x < 16; ++x) top = fmaxf(top, sc[x]);
+    if (__any(top > m + a.lag)) {
+      const float grown = fmaxf(m, lane_max<32>(top));
+      const float by = at_exp2((m - finite_or_0(grown)) * a.scale);
+      l *= by;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[d] *= by;
+      m = grown;
+    }
+  };
+  frag vf[DT * TB], pf[TB];
+  auto read_v = [&]() {
+    const T *vs = reinterpret_cast<const T *>(smem + v_at + slot * TILE);
+#pragma unroll
+    for (int b = 0; b < TB; ++b)
+#pragma unroll
+      for (int d = 0; d < DT; ++d) vf[b * DT + d] = O::load(vs + b * 16 * D + d * 256);
+  };
+  auto weigh = [&]() {
+    const float low = finite_or_0(m) * a.scale;
+    float w[16];
+#pragma unroll
+    for (int x = 0; x < 16; ++x) { w[x] = at_exp2(fmaf(sc[x], a.scale, -low)); l += w[x]; }
+    pf[0] = O::pack(w); pf[1] = O::pack(w + 8);
+  };
+  auto second = [&]() {
+#pragma unroll
+    for (int b = 0; b < TB; ++b)
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[d] = O::mma32(vf[b * DT + d], pf[b], o[d]);
+  };
+  // every row of the workgroup sees all of tile u
+  const int last = idle ? -1 : wi1;                                // the wavefront's
+  const int hi = kv_window_begin(i1, a.window), wglo = kv_window_begin(i0, a.window);
+  auto whole = [&](int u) {
+    const int t0 = span.at(u) * TK;
+    return ok(ids[0].a) && ok(ids[0].b) && t0 + TK - 1 <= i0 && (t0 >= hi || t0 + TK <= a.sinks);
+  };
+  // Tiles that some row does not see whole: what no row of the workgroup sees becomes 0 in V; infinities and NaN that some rows see and
+  // others do not (0 times infinity would reach those) become the largest finite value of their sign, and the rows that see them get them from
+  // patch().  One 16-byte piece (eight tokens of a column) a thread and step.
+  int turn = 0;
+  auto clean = [&](int u) {
+    const int t0 = span.at(u) * TK;
+    uint32_t most = 0;
+    for (int e = tid; e < TILE / 16; e += THREADS) {
+      const int side = e / D;                                      // eight tokens
+      uint32_t keep = 0;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) keep |= (ok(side < 2 ? ids[0].a : ids[0].b) & kv_sees(i1, wglo, a.sinks, t0 + 8 * side + k) ? 1u : 0u) << k;
+      T *at = reinterpret_cast<T *>(smem + ST * TILE + slot * TILE) + e * 8;
+      const frag v = O::finite_only(O::only(O::load(at), keep), most);
+      *reinterpret_cast<frag *>(at) = v;
+    }
+    const bool bad = (most & 0xffffu) >= 0x7f80u || most >= 0x7f800000u;
+    if (__any(bad) && lane == 0) flag[turn] = 1;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    wg_barrier();
+    const int f = __builtin_amdgcn_readfirstlane(flag[turn]);
+    turn ^= 1;
+    if (tid == 0) flag[turn] = 0;                                  // everybody has read it: it was the one before
+    return f != 0;
+  };
+  auto patch = [&](int u) {
+    const int t0 = span.at(u) * TK;
+#pragma unroll 1
+    for (int j = 0; j < TK; ++j) {
+      const int b = j >> 4, h = j >> 3 & 1, id = b ? ids[0].b : ids[0].a;
+      if (!ok(id)) continue;
+      uint32_t bits = 0;                                           // the weight as it was multiplied
+#pragma unroll
+      for (int x = 0; x < 16; ++x) bits = x == 8 * b + (j & 7) ? (x & 1 ? pf[x / 8][x % 8 / 2] & 0xffff0000u : pf[x / 8][x % 8 / 2] << 16) : bits;
+      const float w = __shfl(__uint_as_float(bits), n + 32 * h, 64);
+      const bool mine = kv_sees(i, lo, a.sinks, t0 + j);
+      const T *vr = reinterpret_cast<const T *>(a.V) + (int64_t)id * page_elems + head0 + (int64_t)((t0 + 16 * b) & (a.kv.page - 1)) * D + h * D * 8 + (j & 7);
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+          const T v = vr[(32 * d + 8 * (x / 4) + 4 * half + x % 4) * 8];
+          const float add = w * O::value(v);
+          o[d][x] = (mine & !O::finite(v)) ? o[d][x] + add : o[d][x];
+          if (x % 4 == 3) asm volatile("" ::: "memory");           // few of these reads at a time: the path is rare, its registers are everybody's
+        }
+    }
+  };
+  for (int u = 0; u < count; ++u) {
+    const int t0 = span.at(u) * TK;
+    const bool there_a = ok(ids[0].a), there_b = ok(ids[0].b), all = whole(u), unwritten = t0 + TK > len || !there_a || !there_b;
+    begin(u);
+    bool bad = false;
+    if (unwritten || (CAREFUL && !all)) bad = clean(u);
+    if (t0 <= last) {
+      if (!all) {
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {                             // register 8 b + e holds token 16 b + 8 half + e
+          const bool sees = (x < 8 ? there_a : there_b) & kv_sees(i, lo, a.sinks, t0 + 16 * (x / 8) + 8 * half + x % 8);
+          sc[x] = sees ? sc[x] : -INFINITY;
+        }
+      }
+      lag();
+      read_v();
+      const f32x16 sn = first();
+      weigh();
+      read_k((slot + 2) % ST);
+      second();
+      sc = sn;
+      if (bad) patch(u);
+    }
+    end(u);
+  }
+  if (!CAREFUL) {
+    float sum = l;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) sum = fmaf(o[d][x], 0.f, sum);  // NaN if one of them is not finite
+    if (__any(!(fabsf(sum) < INFINITY)) && !idle && lane == 0) flag[2] = 1;
+    __syncthreads();
+    if (__builtin_amdgcn_readfirstlane(flag[2])) return false;
+  }
+  if (r >= r_end) return true;
+  l = lane_sum<32>(l);
+  const float by = l == 0.f ? 0.f : 1.f / l;
+  T *out = reinterpret_cast<T *>(a.out) + (int64_t)(row0 + token) * a.out_stride + (int64_t)head * D;
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      O::store4(out + 32 * d + 8 * c + 4 * half, o[d][4 * c] * by, o[d][4 * c + 1] * by, o[d][4 * c + 2] * by, o[d][4 * c + 3] * by);
+  if (a.lse && half == 0) a.lse[(int64_t)(row0 + token) * a.n_q + head] = (finite_or_0(m) * a.scale + log2f(l)) * 0.6931471805599453f;
+  return true;
+}
+
+template <int DT, int NW, int ST>
+__global__ __launch_bounds__(NW * 64, DT <= 4 ? 2 : 1) void attend_prefill_bf16(ApArgs a) {
+  extern __shared__ char smem[];                                   // ST tiles of K, ST of V
+  int *flag = reinterpret_cast<int *>(smem + 2 * ST * 32 * DT * 32 * 2), *wave_sums = flag + 3, *pre = wave_sums + NW;
+  const KvItem f = kv_item<NW * 64>(a.kv, a.tok_offsets, a.seqs, a.P, a.rows, a.group, NW * 32, blockIdx.x / a.kv.n_kv, pre, wave_sums);
+  if (f.tile < 0) return;
+  if (threadIdx.x < 3) flag[threadIdx.x] = 0;                      // [2]: something is not finite
+  if (!ap_rows<DT, NW, ST, false>(a, f, smem)) ap_rows<DT, NW, ST, true>(a, f, smem);
+}
+
+template <int DT, int NW, int ST>
+static int ap_launch_bf16(const ApArgs &a, hipStream_t s) {
+  const int64_t tiles = ((int64_t)a.rows * a.group) / (NW * 32) + min(a.P, a.rows);
+  if (tiles * a.kv.n_kv > INT32_MAX) return PARSE_ESHAPE;
+  const size_t lds = (size_t)ST * 2 * 32 * DT * 32 * 2 + (3 + NW + a.P + 1) * 4;
+  PARSE_ALLOW_LDS((attend_prefill_bf16<DT, NW, ST>), 0, lds);
+  attend_prefill_bf16<DT, NW, ST><<<dim3((uint32_t)(tiles * a.kv.n_kv)), NW * 64, lds, s>>>(a);
+  PARSE_LAUNCH_CHECK();
+  return PARSE_OK;
+}
+
 template <class T, int DT, int NW, int TK, int ST>
 static int ap_launch(const ApArgs &a, hipStream_t s) {
   // a prompt's last tile may be begun only: rows / tile + prompts in all
@@ -226,17 +497,28 @@ static int ap_launch(const ApArgs &a, hipStream_t s) {
   PARSE_LAUNCH_CHECK();
   return PARSE_OK;
 }
-template <class T>
-static int ap_width(const ApArgs &a, hipStream_t s) {
+static int ap_bf16(const ApArgs &a, hipStream_t s) {
   switch (a.kv.d / 32) {
-    case 1: return ap_launch<T, 1, 4, 32, 2>(a, s);
-    case 2: return ap_launch<T, 2, 4, 32, 2>(a, s);
-    case 3: return ap_launch<T, 3, 4, 32, 2>(a, s);
-    case 4: return ap_launch<T, 4, 4, 32, 2>(a, s);
-    case 5: return ap_launch<T, 5, 4, 32, 2>(a, s);
-    case 6: return ap_launch<T, 6, 4, 32, 2>(a, s);
-    case 7: return ap_launch<T, 7, 4, 32, 2>(a, s);
-    default: return ap_launch<T, 8, 4, 32, 2>(a, s);
+    case 1: return ap_launch_bf16<1, 4, 3>(a, s);
+    case 2: return ap_launch_bf16<2, 4, 3>(a, s);
+    case 3: return ap_launch_bf16<3, 4, 3>(a, s);
+    case 4: return ap_launch_bf16<4, 4, 3>(a, s);
+    case 5: return ap_launch_bf16<5, 4, 3>(a, s);
+    case 6: return ap_launch_bf16<6, 4, 3>(a, s);
+    case 7: return ap_launch_bf16<7, 4, 3>(a, s);
+    default: return ap_launch_bf16<8, 4, 3>(a, s);
+  }
+}
+static int ap_f32(const ApArgs &a, hipStream_t s) {
+  switch (a.kv.d / 32) {
+    case 1: return ap_launch<float, 1, 4, 32, 2>(a, s);
+    case 2: return ap_launch<float, 2, 4, 32, 2>(a, s);
+    case 3: return ap_launch<float, 3, 4, 32, 2>(a, s);
+    case 4: return ap_launch<float, 4, 4, 32, 2>(a, s);
+    case 5: return ap_launch<float, 5, 4, 32, 2>(a, s);
+    case 6: return ap_launch<float, 6, 4, 32, 2>(a, s);
+    case 7: return ap_launch<float, 7, 4, 32, 2>(a, s);
+    default: return ap_launch<float, 8, 4, 32, 2>(a, s);
   }
 }
 
@@ -266,7 +548,7 @@ int parse_attend_prefill(const parse_kv *kv, int32_t layer, const void *q, int64
   a.q_stride = q_stride; a.out_stride = out_stride;
   a.n_q = n_q; a.group = n_q / kv->n_kv; a.rows = rows; a.P = P; a.window = window; a.sinks = sinks;
   at_scale(scale, a.scale, a.lag, a.q_sign);
-  return kv->dtype == PARSE_BF16 ? ap_width<uint16_t>(a, (hipStream_t)stream) : ap_width<float>(a, (hipStream_t)stream);
+  return kv->dtype == PARSE_BF16 ? ap_bf16(a, (hipStream_t)stream) : ap_f32(a, (hipStream_t)stream);
 }
 
 }  // extern "C"
