@@ -217,14 +217,17 @@ __global__ __launch_bounds__(NW * 64) void attend_prefill(ApArgs a) {
 // tile j and V of tile j - 2 (at the ends a tile that is there stands for the one that is not, so that all groups are alike).
 // CAREFUL: infinities and NaN of V in places that some rows of the workgroup see and others do not reach only the former (0 times infinity would
 // reach the others).  Without, something that is not finite comes out where they are met: then nothing is stored and the answer is false.
-template <int DT, int NW, int ST, bool CAREFUL>
+constexpr int AP_WAVES = 4, AP_ROWS = AP_WAVES * 32, AP_TILE = 32;
+constexpr int AP_STAGES = 4;                 // tiles of K, and of V, in LDS
+constexpr int ap_lds_bytes(int DT) { return 2 * AP_STAGES * AP_TILE * DT * 32 * 2; }
+
+template <int DT, bool CAREFUL>
 __device__ __forceinline__ bool ap_rows(const ApArgs &a, const KvItem &f, char *smem) {
   typedef uint16_t T;
   typedef Op<T> O;
   typedef O::frag frag;
-  constexpr int D = DT * 32, KB = D / 16, TK = 32, TB = 2, TM = NW * 32, THREADS = NW * 64;
-  constexpr int BLOCK = 32 * D, TILE = TB * BLOCK, PIECES = 2 * TILE / 1024, LOADS = PIECES / NW, AHEAD = ST - 1;   // groups on their way
-  static_assert(PIECES % NW == 0, "every wavefront stages as much");
+  constexpr int D = DT * 32, KB = D / 16, TK = AP_TILE, TB = 2, TM = AP_ROWS, THREADS = AP_WAVES * 64, ST = AP_STAGES;
+  constexpr int BLOCK = 32 * D, TILE = TB * BLOCK, LOADS = BLOCK / 1024, AHEAD = ST - 1;   // groups on their way
   int *flag = reinterpret_cast<int *>(smem + 2 * ST * TILE);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, half = lane >> 5;
   const int kvh = blockIdx.x % a.kv.n_kv, group = a.group;
@@ -237,27 +240,43 @@ __device__ __forceinline__ bool ap_rows(const ApArgs &a, const KvItem &f, char *
   const int count = span.count, groups = count > 0 ? count + 2 : 0;
 
   const int page_bits = 31 - __builtin_clz(a.kv.page);
-  struct Ids { int a, b; };                                        // pages of a tile's two blocks of sixteen tokens
-  auto ids_of = [&](int u) {
-    const int t0 = span.at(min(u, count - 1)) * TK;
-    return Ids{scalar_word(table + min(t0 >> page_bits, a.kv.max_pages - 1)), scalar_word(table + min((t0 + 16) >> page_bits, a.kv.max_pages - 1))};
-  };
   const int64_t page_elems = (int64_t)a.kv.n_kv * a.kv.page * D, head0 = (int64_t)kvh * a.kv.page * D;
   auto ok = [&](int id) { return (unsigned)id < (unsigned)a.kv.n_pages; };
-  // pieces wave * LOADS + 0 .. LOADS - 1 of a group; its first half is K
-  auto stage = [&](int uk, const Ids k, int uv, const Ids v, int slot_k, int slot_v) {
-    const int k_a = k.a, k_b = k.b, v_a = v.a, v_b = v.b;
-    const int tk = span.at(min(uk, count - 1)) * TK, tv = span.at(max(uv, 0)) * TK;
+  auto page_at = [&](int t) { return table[min(t >> page_bits, a.kv.max_pages - 1)]; };
+  // Of every group wavefront w stages one block of sixteen tokens: w / 2 says K or V, w % 2 which block.  Where the tiles stand is worked out
+  // for 64 of them at once, a lane each, and read lane by lane: scalar instructions for every tile would take as long as the products.
+  const int of_v = wave >> 1, blk = wave & 1;
+  const char *const pool = (const char *)(of_v ? a.V : a.K) + head0 * 2;
+  int next_group = 0, next_slot = of_v ? ST - 2 : 0;
+  uint32_t place_lo = 0, place_hi = 0;                             // lane j: bytes from pool to this wavefront's block of group 64 * (next_group / 64) + j
+  auto places = [&]() {
+    const int g = next_group + lane, t = span.at(of_v ? max(min(g, groups - 1) - 2, 0) : min(g, count - 1)) * TK + 16 * blk, id = page_at(t);
+    const int64_t at = (int64_t)(ok(id) ? id : 0) * (page_elems * 2) + (t & (a.kv.page - 1)) * (D * 2);
+    place_lo = (uint32_t)at;
+    place_hi = (uint32_t)(at >> 32);
+  };
+  uint32_t infos = 0;                                              // lane j: first token of tile 64 * (u / 64) + j, and
+  constexpr uint32_t THERE_A = 1, THERE_B = 2, WHOLE = 4;          // pages of its two blocks there; every row of the workgroup sees all of it
+  const int hi = kv_window_begin(i1, a.window), wglo = kv_window_begin(i0, a.window);
+  auto look = [&](int u) {
+    const int t0 = span.at(min(u + lane, count - 1)) * TK;
+    const bool there_a = ok(page_at(t0)), there_b = ok(page_at(t0 + 16));
+    const bool all = there_a & there_b & (t0 + TK - 1 <= i0) & ((t0 >= hi) | (t0 + TK <= a.sinks));
+    infos = (uint32_t)t0 | (there_a ? THERE_A : 0u) | (there_b ? THERE_B : 0u) | (all ? WHOLE : 0u);
+  };
+  auto stage = [&]() {
+    const char *src = pool + ((uint64_t)(uint32_t)__builtin_amdgcn_readlane(place_hi, next_group & 63) << 32 | (uint32_t)__builtin_amdgcn_readlane(place_lo, next_group & 63));
+    char *dst = smem + of_v * ST * TILE + blk * BLOCK + next_slot * TILE;
 #pragma unroll
-    for (int q = 0; q < LOADS; ++q) {
-      const int piece = wave * LOADS + q, of_v = piece / (PIECES / 2), rest = piece % (PIECES / 2), block = rest / (BLOCK / 1024), in = rest % (BLOCK / 1024);
-      const int t = (of_v ? tv : tk) + 16 * block;
-      int id = __builtin_amdgcn_readfirstlane(of_v ? (block ? v_b : v_a) : (block ? k_b : k_a));
-      id = ok(id) ? id : 0;
-      const char *src = (const char *)(of_v ? a.V : a.K) + ((int64_t)id * page_elems + head0 + (int64_t)(t & (a.kv.page - 1)) * D) * 2 + in * 1024;
-      char *dst = smem + (of_v ? ST * TILE + slot_v * TILE : slot_k * TILE) + rest * 1024;
-      __builtin_amdgcn_global_load_lds(PARSE_GLB_PTR(src + lane * 16), PARSE_LDS_PTR(dst), 16, 0, 0);
+    for (int q = 0; q < LOADS; q += 4) {
+      // the offset moves both sides
+      __builtin_amdgcn_global_load_lds(PARSE_GLB_PTR(src + q * 1024 + lane * 16), PARSE_LDS_PTR(dst + q * 1024), 16, 0, 0);
+      if (q + 1 < LOADS) __builtin_amdgcn_global_load_lds(PARSE_GLB_PTR(src + q * 1024 + lane * 16), PARSE_LDS_PTR(dst + q * 1024), 16, 1024, 0);
+      if (q + 2 < LOADS) __builtin_amdgcn_global_load_lds(PARSE_GLB_PTR(src + q * 1024 + lane * 16), PARSE_LDS_PTR(dst + q * 1024), 16, 2048, 0);
+      if (q + 3 < LOADS) __builtin_amdgcn_global_load_lds(PARSE_GLB_PTR(src + q * 1024 + lane * 16), PARSE_LDS_PTR(dst + q * 1024), 16, 3072, 0);
     }
+    next_slot = next_slot + 1 == ST ? 0 : next_slot + 1;
+    if ((++next_group & 63) == 0) places();
   };
 
   // this lane's row, and the positions of the wavefront's rows
@@ -273,13 +292,12 @@ __device__ __forceinline__ bool ap_rows(const ApArgs &a, const KvItem &f, char *
     for (int k = 0; k < KB; ++k) qf[k] = O::sign(O::load(q + 16 * k), a.q_sign);
   }
   asm volatile("" ::: "memory");                                   // q comes first: whoever waits for a tile has it
-  Ids ids[ST + 3];                                                 // of tiles u .. u + ST + 2
   if (groups) {
-#pragma unroll
-    for (int u = 0; u < ST + 3; ++u) ids[u] = ids_of(u);
+    places();
+    look(0);
 #pragma unroll
     for (int j = 0; j < ST; ++j)
-      if (j < groups) stage(j, ids[j], j - 2, ids[j < 2 ? 0 : j - 2], j, (j + ST - 2) % ST);
+      if (j < groups) stage();
   }
   float m = -INFINITY, l = 0.f;
   f32x16 o[DT], sc;
@@ -313,22 +331,16 @@ __device__ __forceinline__ bool ap_rows(const ApArgs &a, const KvItem &f, char *
     sc = first();
     wait_slices<AHEAD - 1, LOADS>(min(ST - 1, groups - 1) - 1);
     meet();
-    if (ST < groups) stage(ST, ids[ST], ST - 2, ids[ST - 2], 0, ST - 2);
+    if (ST < groups) stage();
     read_k(1);
   }
   int slot = 0;                                                    // u % ST
   auto begin = [&](int u) {                                        // tile u of V and u + 2 of K are there; the loads that the freed places take
-    wait_slices<AHEAD - 1, LOADS>(min(u + 1 + AHEAD, groups - 1) - (u + 2));
+    if (u + 1 + AHEAD < groups) wait_vm<(AHEAD - 1) * LOADS>(); else wait_slices<AHEAD - 1, LOADS>(groups - 1 - (u + 2));
     meet();
-    if (u + 2 + AHEAD < groups) stage(u + 2 + AHEAD, ids[2 + AHEAD], u + AHEAD, ids[AHEAD], (slot + 1) % ST, (slot + AHEAD) % ST);
+    if (next_group < groups) stage();
   };
-  auto end = [&](int u) {
-#pragma unroll
-    for (int e = 0; e < ST + 2; ++e) ids[e] = ids[e + 1];
-    ids[ST + 2] = ids_of(u + ST + 3);
-    slot = slot + 1 == ST ? 0 : slot + 1;
-  };
-  auto lag = [&]() {                                               // the running maximum, where it has to grow
+  auto lag = [&](const f32x16 &sc) {                               // the running maximum, where it has to grow
     float top = -INFINITY;
 #pragma unroll
     for (int x = 0; x < 16; ++x) top = fmaxf(top, sc[x]);
@@ -341,6 +353,7 @@ __device__ __forceinline__ bool ap_rows(const ApArgs &a, const KvItem &f, char *
       m = grown;
     }
   };
+  const int last = idle ? -1 : wi1;                                // position of the wavefront's last row
   frag vf[DT * TB], pf[TB];
   auto read_v = [&]() {
     const T *vs = reinterpret_cast<const T *>(smem + v_at + slot * TILE);
@@ -349,7 +362,7 @@ __device__ __forceinline__ bool ap_rows(const ApArgs &a, const KvItem &f, char *
 #pragma unroll
       for (int d = 0; d < DT; ++d) vf[b * DT + d] = O::load(vs + b * 16 * D + d * 256);
   };
-  auto weigh = [&]() {
+  auto weigh = [&](const f32x16 &sc) {
     const float low = finite_or_0(m) * a.scale;
     float w[16];
 #pragma unroll
@@ -362,25 +375,18 @@ __device__ __forceinline__ bool ap_rows(const ApArgs &a, const KvItem &f, char *
 #pragma unroll
       for (int d = 0; d < DT; ++d) o[d] = O::mma32(vf[b * DT + d], pf[b], o[d]);
   };
-  // every row of the workgroup sees all of tile u
-  const int last = idle ? -1 : wi1;                                // the wavefront's
-  const int hi = kv_window_begin(i1, a.window), wglo = kv_window_begin(i0, a.window);
-  auto whole = [&](int u) {
-    const int t0 = span.at(u) * TK;
-    return ok(ids[0].a) && ok(ids[0].b) && t0 + TK - 1 <= i0 && (t0 >= hi || t0 + TK <= a.sinks);
-  };
   // Tiles that some row does not see whole: what no row of the workgroup sees becomes 0 in V; infinities and NaN that some rows see and
   // others do not (0 times infinity would reach those) become the largest finite value of their sign, and the rows that see them get them from
   // patch().  One 16-byte piece (eight tokens of a column) a thread and step.
   int turn = 0;
-  auto clean = [&](int u) {
-    const int t0 = span.at(u) * TK;
+  auto clean = [&](uint32_t info) {
+    const int t0 = info & ~31u;
     uint32_t most = 0;
     for (int e = tid; e < TILE / 16; e += THREADS) {
       const int side = e / D;                                      // eight tokens
       uint32_t keep = 0;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) keep |= (ok(side < 2 ? ids[0].a : ids[0].b) & kv_sees(i1, wglo, a.sinks, t0 + 8 * side + k) ? 1u : 0u) << k;
+      for (int k = 0; k < 8; ++k) keep |= ((bool)(info & (side < 2 ? THERE_A : THERE_B)) & kv_sees(i1, wglo, a.sinks, t0 + 8 * side + k) ? 1u : 0u) << k;
       T *at = reinterpret_cast<T *>(smem + ST * TILE + slot * TILE) + e * 8;
       const frag v = O::finite_only(O::only(O::load(at), keep), most);
       *reinterpret_cast<frag *>(at) = v;
@@ -394,12 +400,13 @@ __device__ __forceinline__ bool ap_rows(const ApArgs &a, const KvItem &f, char *
     if (tid == 0) flag[turn] = 0;                                  // everybody has read it: it was the one before
     return f != 0;
   };
-  auto patch = [&](int u) {
-    const int t0 = span.at(u) * TK;
+  auto patch = [&](uint32_t info) {
+    const int t0 = info & ~31u;
 #pragma unroll 1
     for (int j = 0; j < TK; ++j) {
-      const int b = j >> 4, h = j >> 3 & 1, id = b ? ids[0].b : ids[0].a;
-      if (!ok(id)) continue;
+      const int b = j >> 4, h = j >> 3 & 1;
+      if (!(info & (b ? THERE_B : THERE_A))) continue;
+      const int id = page_at(t0 + 16 * b);
       uint32_t bits = 0;                                           // the weight as it was multiplied
 #pragma unroll
       for (int x = 0; x < 16; ++x) bits = x == 8 * b + (j & 7) ? (x & 1 ? pf[x / 8][x % 8 / 2] & 0xffff0000u : pf[x / 8][x % 8 / 2] << 16) : bits;
@@ -417,33 +424,46 @@ __device__ __forceinline__ bool ap_rows(const ApArgs &a, const KvItem &f, char *
         }
     }
   };
-  for (int u = 0; u < count; ++u) {
-    const int t0 = span.at(u) * TK;
-    const bool there_a = ok(ids[0].a), there_b = ok(ids[0].b), all = whole(u), unwritten = t0 + TK > len || !there_a || !there_b;
+  bool odd = false;                                                // something of V was not finite in a tile that was cleaned
+  auto tile = [&](int u, f32x16 &sc, f32x16 &sn) {                 // scores of tile u in sc; those of tile u + 1 come into sn
+    const uint32_t info = __builtin_amdgcn_readlane(infos, u & 63);
+    const int t0 = info & ~31u;
     begin(u);
     bool bad = false;
-    if (unwritten || (CAREFUL && !all)) bad = clean(u);
+    if (!(info & WHOLE) && (CAREFUL || t0 + TK > len || (info & (THERE_A | THERE_B)) != (THERE_A | THERE_B))) bad = clean(info);
     if (t0 <= last) {
-      if (!all) {
+      if (!(info & WHOLE)) {
+        const bool there_a = info & THERE_A, there_b = info & THERE_B;
 #pragma unroll
         for (int x = 0; x < 16; ++x) {                             // register 8 b + e holds token 16 b + 8 half + e
           const bool sees = (x < 8 ? there_a : there_b) & kv_sees(i, lo, a.sinks, t0 + 16 * (x / 8) + 8 * half + x % 8);
           sc[x] = sees ? sc[x] : -INFINITY;
         }
       }
-      lag();
+      lag(sc);
       read_v();
-      const f32x16 sn = first();
-      weigh();
+      sn = first();
+      weigh(sc);
       read_k((slot + 2) % ST);
       second();
-      sc = sn;
-      if (bad) patch(u);
+      if (CAREFUL) {
+        if (bad) patch(info);
+      } else {
+        odd |= bad;
+      }
     }
-    end(u);
+    if (((u + 1) & 63) == 0) look(u + 1);
+    slot = slot + 1 == ST ? 0 : slot + 1;
+  };
+  f32x16 sn = sc;
+  int u = 0;
+  for (; u + 1 < count; u += 2) {
+    tile(u, sc, sn);
+    tile(u + 1, sn, sc);
   }
+  if (u < count) tile(u, sc, sn);
   if (!CAREFUL) {
-    float sum = l;
+    float sum = odd ? INFINITY : l;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -465,23 +485,24 @@ __device__ __forceinline__ bool ap_rows(const ApArgs &a, const KvItem &f, char *
   return true;
 }
 
-template <int DT, int NW, int ST>
-__global__ __launch_bounds__(NW * 64, DT <= 4 ? 2 : 1) void attend_prefill_bf16(ApArgs a) {
-  extern __shared__ char smem[];                                   // ST tiles of K, ST of V
-  int *flag = reinterpret_cast<int *>(smem + 2 * ST * 32 * DT * 32 * 2), *wave_sums = flag + 3, *pre = wave_sums + NW;
-  const KvItem f = kv_item<NW * 64>(a.kv, a.tok_offsets, a.seqs, a.P, a.rows, a.group, NW * 32, blockIdx.x / a.kv.n_kv, pre, wave_sums);
+template <int DT>
+__global__ __launch_bounds__(AP_WAVES * 64, DT <= 4 ? 2 : 1) void attend_prefill_bf16(ApArgs a) {
+  extern __shared__ char smem[];                                   // AP_STAGES tiles of K, as many of V, three flags, the prompts' tiles
+  int *flag = reinterpret_cast<int *>(smem + ap_lds_bytes(DT)), *wave_sums = flag + 3, *pre = wave_sums + AP_WAVES;
+  const KvItem f = kv_item<AP_WAVES * 64>(a.kv, a.tok_offsets, a.seqs, a.P, a.rows, a.group, AP_ROWS, blockIdx.x / a.kv.n_kv, pre, wave_sums);
   if (f.tile < 0) return;
   if (threadIdx.x < 3) flag[threadIdx.x] = 0;                      // [2]: something is not finite
-  if (!ap_rows<DT, NW, ST, false>(a, f, smem)) ap_rows<DT, NW, ST, true>(a, f, smem);
+  if (!ap_rows<DT, false>(a, f, smem)) ap_rows<DT, true>(a, f, smem);
 }
 
-template <int DT, int NW, int ST>
+template <int DT>
 static int ap_launch_bf16(const ApArgs &a, hipStream_t s) {
-  const int64_t tiles = ((int64_t)a.rows * a.group) / (NW * 32) + min(a.P, a.rows);
+  // a prompt's last tile may be begun only: rows / tile + prompts in all
+  const int64_t tiles = ((int64_t)a.rows * a.group) / AP_ROWS + min(a.P, a.rows);
   if (tiles * a.kv.n_kv > INT32_MAX) return PARSE_ESHAPE;
-  const size_t lds = (size_t)ST * 2 * 32 * DT * 32 * 2 + (3 + NW + a.P + 1) * 4;
-  PARSE_ALLOW_LDS((attend_prefill_bf16<DT, NW, ST>), 0, lds);
-  attend_prefill_bf16<DT, NW, ST><<<dim3((uint32_t)(tiles * a.kv.n_kv)), NW * 64, lds, s>>>(a);
+  const size_t lds = ap_lds_bytes(DT) + (3 + AP_WAVES + (a.P > 64 ? a.P + 1 : 0)) * 4;
+  PARSE_ALLOW_LDS((attend_prefill_bf16<DT>), 0, lds);
+  attend_prefill_bf16<DT><<<dim3((uint32_t)(tiles * a.kv.n_kv)), AP_WAVES * 64, lds, s>>>(a);
   PARSE_LAUNCH_CHECK();
   return PARSE_OK;
 }
@@ -499,14 +520,14 @@ static int ap_launch(const ApArgs &a, hipStream_t s) {
 }
 static int ap_bf16(const ApArgs &a, hipStream_t s) {
   switch (a.kv.d / 32) {
-    case 1: return ap_launch_bf16<1, 4, 3>(a, s);
-    case 2: return ap_launch_bf16<2, 4, 3>(a, s);
-    case 3: return ap_launch_bf16<3, 4, 3>(a, s);
-    case 4: return ap_launch_bf16<4, 4, 3>(a, s);
-    case 5: return ap_launch_bf16<5, 4, 3>(a, s);
-    case 6: return ap_launch_bf16<6, 4, 3>(a, s);
-    case 7: return ap_launch_bf16<7, 4, 3>(a, s);
-    default: return ap_launch_bf16<8, 4, 3>(a, s);
+    case 1: return ap_launch_bf16<1>(a, s);
+    case 2: return ap_launch_bf16<2>(a, s);
+    case 3: return ap_launch_bf16<3>(a, s);
+    case 4: return ap_launch_bf16<4>(a, s);
+    case 5: return ap_launch_bf16<5>(a, s);
+    case 6: return ap_launch_bf16<6>(a, s);
+    case 7: return ap_launch_bf16<7>(a, s);
+    default: return ap_launch_bf16<8>(a, s);
   }
 }
 static int ap_f32(const ApArgs &a, hipStream_t s) {
