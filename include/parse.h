@@ -556,11 +556,15 @@ int parse_kv_append(const parse_kv *kv, int32_t layer, const void *k, int64_t k_
  *   q, out        device [rows][n_q][d], rows q_stride / out_stride elements apart, 16-byte aligned; out is not q
  *   lse           device float [rows][n_q] or NULL
  *   window >= 0 (0: none), sinks >= 0 (read only with a window)
- *   workspace     device, at least what the query says; contents irrelevant before, undefined after */
+ *   workspace     device, at least what the query says; undefined after the call */
 
 /* One new token per sequence (its last: i = len - 1), over caches of any lengths; the caches' tokens are dealt out evenly
  * over the card and the parts of a cache joined.
- *   rows = number of sequences, 1..4096; seqs device int32 [rows], the table's row of each, or NULL: the row itself */
+ *   rows = number of sequences, 1..4096; seqs device int32 [rows], the table's row of each, or NULL: the row itself
+ *   workspace  its first PARSE_ATTEND_DECODE_ZERO_BYTES are tickets with which the workgroups that share a cache find out
+ *              which of them joins its parts: ZERO before the first call, zero again after every call.  The rest may hold anything.  A workspace serves one call at
+ *              a time: calls that overlap need one each. */
+#define PARSE_ATTEND_DECODE_ZERO_BYTES 2048
 size_t parse_attend_decode_workspace_bytes(const parse_kv *kv, int32_t n_q, int32_t rows);
 int parse_attend_decode(const parse_kv *kv, int32_t layer, const void *q, int64_t q_stride, int32_t n_q, int32_t rows,
                         const int32_t *seqs, float scale, int32_t window, int32_t sinks, void *out, int64_t out_stride,

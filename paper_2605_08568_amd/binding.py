@@ -693,11 +693,12 @@ class KV:
 
 def _rows_of(t, kv, heads, what):
     """Row stride of [rows][heads][d] rows, whose heads stand side by side."""
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != kv.d or _dtype_code(t) != kv.dtype:
+    if t.dtype is not kv.K.dtype or t.dim() != 3 or t.shape[1:] != (heads, kv.d):
         raise ValueError(f"{what}: [rows][{heads}][{kv.d}] of the cache's dtype is wanted, got {tuple(t.shape)} {t.dtype}")
-    if t.shape[0] and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != kv.d)):
+    row, head, column = t.stride()
+    if column != 1 or (heads > 1 and head != kv.d):
         raise ValueError(f"{what}: a row's heads have to stand side by side, strides are {t.stride()}")
-    return t.stride(0) if t.shape[0] > 1 else max(heads * kv.d, t.stride(0))
+    return row if row >= heads * kv.d else max(row, heads * kv.d) if t.shape[0] <= 1 else row
 
 
 def _ints(t, n, what):
@@ -774,34 +775,41 @@ def kv_append(kv: KV, layer: int, k, v, tok_offsets=None, seqs=None, q=None, q_o
     return q_out
 
 
-def _attend_out(kv, q, out, lse, with_lse):
-    rows, n_q = q.shape[0], q.shape[1]
+def _attend_out(kv, q, n_q, q_stride, out, lse, with_lse):
+    """(out, its row stride, lse)"""
+    rows = q.shape[0]
     if out is None:
-        out = torch.empty((rows, n_q, kv.d), dtype=q.dtype, device=q.device)
-    if out.shape[0] != rows:
+        out, out_stride = (torch.empty_like(q) if q_stride == n_q * kv.d else q.new_empty((rows, n_q, kv.d))), n_q * kv.d
+    elif out.shape[0] != rows:
         raise ValueError("out has as many rows as q")
-    if lse is None and with_lse:
-        lse = torch.empty((rows, n_q), dtype=torch.float32, device=q.device)
-    if lse is not None and (lse.dtype != torch.float32 or lse.numel() != rows * n_q or not lse.is_contiguous()):
+    else:
+        out_stride = _rows_of(out, kv, n_q, "out")
+    if lse is None:
+        if with_lse:
+            lse = torch.empty((rows, n_q), dtype=torch.float32, device=q.device)
+    elif lse.dtype != torch.float32 or lse.numel() != rows * n_q or not lse.is_contiguous():
         raise ValueError(f"lse: contiguous float32 [{rows}][{n_q}] is wanted")
-    return rows, n_q, out, lse
+    return out, out_stride, lse
 
 
 def attend_decode_workspace(kv: KV, n_q: int, rows: int):
+    """Workspace of attend_decode, its tickets zero: made once and kept, it saves every call the clearing.  One call at a time has it."""
     need = int(lib().parse_attend_decode_workspace_bytes(C.byref(kv.c()), n_q, rows))
-    return torch.empty(max(need, 256), dtype=torch.uint8, device=kv.K.device)
+    return torch.zeros(max(need, 256), dtype=torch.uint8, device=kv.K.device)
 
 
 def attend_decode(kv: KV, layer: int, q, seqs=None, scale=None, window: int = 0, sinks: int = 0, out=None, lse=None, with_lse=False,
                   workspace=None):
     """parse_attend_decode: q [rows][n_q][d], the last token of each sequence -> out [rows][n_q][d] (with_lse: and lse
     [rows][n_q]).  scale: d ** -0.5 where it is not given."""
-    rows, n_q, out, lse = _attend_out(kv, q, out, lse, with_lse)
+    rows, n_q = q.shape[:2]
+    q_stride = _rows_of(q, kv, n_q, "q")
+    out, out_stride, lse = _attend_out(kv, q, n_q, q_stride, out, lse, with_lse)
     if workspace is None:
         workspace = attend_decode_workspace(kv, n_q, rows)
-    _check(_calls.parse_attend_decode(kv, layer, q, _rows_of(q, kv, n_q, "q"), n_q, rows, _ints(seqs, rows, "seqs"),
-                                      kv.d ** -0.5 if scale is None else scale, window, sinks, out, _rows_of(out, kv, n_q, "out"), lse,
-                                      workspace, workspace.numel(), _stream()), "parse_attend_decode")
+    _check(_calls.parse_attend_decode(kv, layer, q, q_stride, n_q, rows, seqs if seqs is None else _ints(seqs, rows, "seqs"),
+                                      kv.d ** -0.5 if scale is None else scale, window, sinks, out, out_stride, lse, workspace,
+                                      workspace.numel(), _stream()), "parse_attend_decode")
     return (out, lse) if with_lse else out
 
 
@@ -814,12 +822,13 @@ def attend_prefill(kv: KV, layer: int, q, tok_offsets=None, seqs=None, scale=Non
                    with_lse=False, workspace=None):
     """parse_attend_prefill: q [rows][n_q][d], the last tokens of each prompt's sequence -> out (with_lse: and lse), as
     attend_decode."""
-    rows, n_q, out, lse = _attend_out(kv, q, out, lse, with_lse)
+    rows, n_q = q.shape[:2]
+    q_stride = _rows_of(q, kv, n_q, "q")
+    out, out_stride, lse = _attend_out(kv, q, n_q, q_stride, out, lse, with_lse)
     P = rows if tok_offsets is None else tok_offsets.numel() - 1
     if workspace is None:
         workspace = attend_prefill_workspace(kv, n_q, rows, P)
-    _check(_calls.parse_attend_prefill(kv, layer, q, _rows_of(q, kv, n_q, "q"), n_q, rows, _ints(tok_offsets, P + 1, "tok_offsets"),
-                                       _ints(seqs, P, "seqs"), P, kv.d ** -0.5 if scale is None else scale, window, sinks, out,
-                                       _rows_of(out, kv, n_q, "out"), lse, workspace, workspace.numel(), _stream()),
-           "parse_attend_prefill")
+    _check(_calls.parse_attend_prefill(kv, layer, q, q_stride, n_q, rows, _ints(tok_offsets, P + 1, "tok_offsets"), _ints(seqs, P, "seqs"), P,
+                                       kv.d ** -0.5 if scale is None else scale, window, sinks, out, out_stride, lse, workspace,
+                                       workspace.numel(), _stream()), "parse_attend_prefill")
     return (out, lse) if with_lse else out

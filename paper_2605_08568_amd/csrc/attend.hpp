@@ -166,6 +166,7 @@ template <> struct Op<uint16_t> {
   typedef u32x4 frag;
   static __device__ __forceinline__ frag zero() { return u32x4{0, 0, 0, 0}; }
   static __device__ __forceinline__ frag load(const uint16_t *p) { return *reinterpret_cast<const u32x4 *>(p); }
+  static __device__ __forceinline__ frag load_nt(const uint16_t *p) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p)); }
   static __device__ __forceinline__ f32x4 mma16(frag a, frag b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
   }
@@ -181,6 +182,13 @@ template <> struct Op<uint16_t> {
   // weights in [0, 2^8]: rounded to bf16, 2^-8 relative at most, independent from token to token
   static __device__ __forceinline__ frag pack(const float *p) {
     return u32x4{cvt_pk_bf16(p[0], p[1]), cvt_pk_bf16(p[2], p[3]), cvt_pk_bf16(p[4], p[5]), cvt_pk_bf16(p[6], p[7])};
+  }
+  // ... and what that leaves of them, rounded again
+  static __device__ __forceinline__ frag pack_rest(const float *p, frag r) {
+    float d[8];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) { d[2 * w] = p[2 * w] - __uint_as_float(r[w] << 16); d[2 * w + 1] = p[2 * w + 1] - __uint_as_float(r[w] & 0xffff0000u); }
+    return pack(d);
   }
   // values whose bit of `keep` is clear become 0
   static __device__ __forceinline__ frag only(frag a, uint32_t keep) {
@@ -213,6 +221,9 @@ template <> struct Op<float> {
   static __device__ __forceinline__ frag zero() { return frag{f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}}; }
   static __device__ __forceinline__ frag load(const float *p) {
     return frag{*reinterpret_cast<const f32x4 *>(p), *reinterpret_cast<const f32x4 *>(p + 4)};
+  }
+  static __device__ __forceinline__ frag load_nt(const float *p) {
+    return frag{__builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(p)), __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(p + 4))};
   }
   static __device__ __forceinline__ f32x4 mma16(frag a, frag b, f32x4 c) {
 #pragma unroll

@@ -1,12 +1,17 @@
 // Attention of one new token per sequence over the paged cache (parse_attend_decode).
+#include <algorithm>
+#include <type_traits>
+
 #include "attend.hpp"
 
 namespace parse {
 
 constexpr int AD_WAVES = 4, AD_THREADS = AD_WAVES * 64;
 constexpr int AD_STEP = 32;                          // tokens of a wavefront's step
-constexpr int AD_TILE = AD_WAVES * AD_STEP;
 constexpr int AD_HEADS = 16;                         // query heads of a workgroup, the N side of the 16-wide instruction
+constexpr int AD_GROUPS = 512;                       // workgroups of a call: two for each compute unit
+constexpr size_t AD_TICKET_BYTES = PARSE_ATTEND_DECODE_ZERO_BYTES;
+static_assert(AD_GROUPS * 4 <= AD_TICKET_BYTES, "a ticket for every share of every column that has several");
 
 struct AdArgs {
   parse_kv kv;
@@ -20,11 +25,111 @@ struct AdArgs {
   float scale, lag;                                  // |scale| times log2(e); AT_LAG in products of q and k
   uint32_t q_sign;
   float *part;                                       // [kv head][group of 16 heads][share][2] of AD_HEADS * (d + 2)
+  int32_t *tickets;                                  // [kv head][group of 16 heads][share]: parts that have come of the row that begins in the share
 };
 
-// A workgroup has sixteen query heads of one kv head, and one share of all tokens that the batch sees.
-template <class T, int DT>
-__global__ __launch_bounds__(AD_THREADS) void attend_decode(AdArgs a) {
+template <class T>
+__device__ __forceinline__ void ad_store(const AdArgs &a, int row, int head, int i, int D, float top, float ls, float os) {
+  const float y = ls == 0.f ? 0.f : os / ls;
+  T *out = reinterpret_cast<T *>(a.out) + (int64_t)row * a.out_stride + (int64_t)head * D + i;
+  if constexpr (sizeof(T) == 2) *out = (uint16_t)cvt_pk_bf16(y, 0.f);
+  else *out = y;
+  if (a.lse && i == 0) a.lse[(int64_t)row * a.n_q + head] = (finite_or_0(top) * a.scale + log2f(ls)) * 0.6931471805599453f;
+}
+
+// How the batch's steps are dealt out: sequence b has the steps [before, before + its count) of `total`, a workgroup `per` of them.
+struct AdDeal {
+  int total, per;
+};
+// A wavefront alone, for up to 64 sequences: lane b has sequence b's words
+struct AdLane {
+  KvSeq seq;
+  KvSpan span;
+  int before;
+};
+__device__ __forceinline__ KvSpan ad_span(const AdArgs &a, int len) { return kv_span(len - 1, len - 1, a.window, a.sinks, AD_STEP); }
+__device__ __forceinline__ AdDeal ad_deal(const AdArgs &a, int total) {
+  const int per = (total + a.shares - 1) / a.shares;
+  return AdDeal{total, max((per + AD_WAVES - 1) / AD_WAVES, 1) * AD_WAVES};    // the wavefronts take turns
+}
+__device__ __forceinline__ AdDeal ad_lanes(const AdArgs &a, AdLane &w) {
+  const int lane = threadIdx.x & 63;
+  w.seq = kv_seq(a.kv, a.seqs, min(lane, a.rows - 1));
+  w.span = ad_span(a, w.seq.len);
+  const int mine = lane < a.rows ? w.span.count : 0;
+  int inc = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int v = __shfl_up(inc, o, 64);
+    if (lane >= o) inc += v;
+  }
+  w.before = inc - mine;
+  return ad_deal(a, __builtin_amdgcn_readlane(inc, 63));
+}
+
+template <bool SHARED>
+__device__ __forceinline__ void ad_part(float *p, float v) {
+  if (SHARED) __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  else *p = v;
+}
+// The parts of row b: shares x0 .. x0 + parts - 1, of all heads of the workgroup, added in the order of the shares (same inputs, same bits).  A wavefront
+// has a head's weights, then a thread has two columns of every so many parts.  `lds`: 2 * heads * parts floats; `per_head`: two numbers a head.
+template <class T>
+__device__ __forceinline__ void ad_join(const AdArgs &a, int b, int kvh, int hg, int heads, int x0, int parts, int before, int per, float *lds, float *per_head) {
+  const int D = a.kv.d, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const float *base = a.part + ((int64_t)kvh * gridDim.z + hg) * a.shares * 2 * AD_HEADS * (D + 2);
+  auto part_of = [&](int x) { return base + ((int64_t)(x0 + x) * 2 + ((int64_t)(x0 + x) * per <= before ? 1 : 0)) * AD_HEADS * (D + 2); };
+  auto get = [&](const float *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+  for (int h = wave; h < heads; h += AD_WAVES) {
+    float top = -INFINITY, ls = 0.f;
+    for (int x = lane; x < parts; x += 64) {
+      const float m = get(part_of(x) + AD_HEADS * D + h), l = get(part_of(x) + AD_HEADS * (D + 1) + h);
+      lds[h * parts + x] = m;
+      lds[(heads + h) * parts + x] = l;
+      top = fmaxf(top, m);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+    for (int x = lane; x < parts; x += 64) {
+      const float by = at_exp2((lds[h * parts + x] - finite_or_0(top)) * a.scale);
+      lds[h * parts + x] = by;
+      ls += by * lds[(heads + h) * parts + x];
+    }
+    ls = wave_sum(ls);
+    if (lane == 0) { per_head[h] = top; per_head[AD_HEADS + h] = ls; }
+  }
+  __syncthreads();
+  auto columns = [&](auto at_once) {                               // two a thread, so many parts on their way
+    constexpr int N = decltype(at_once)::value;
+    for (int v = tid; v < heads * D / 2; v += AD_THREADS) {
+      const int h = 2 * v / D, i = 2 * v % D;
+      float y0 = 0.f, y1 = 0.f;
+      for (int first = 0; first < parts; first += N) {
+        uint64_t two[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+          two[k] = __hip_atomic_load(reinterpret_cast<const uint64_t *>(part_of(min(first + k, parts - 1)) + h * D + i), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          const float by = lds[h * parts + min(first + k, parts - 1)];
+          const bool is = first + k < parts;
+          y0 = is ? fmaf(by, __uint_as_float((uint32_t)two[k]), y0) : y0;
+          y1 = is ? fmaf(by, __uint_as_float((uint32_t)(two[k] >> 32)), y1) : y1;
+        }
+      }
+      const int head = kvh * a.group + hg * AD_HEADS + h;
+      ad_store<T>(a, b, head, i, D, per_head[h], per_head[AD_HEADS + h], y0);
+      ad_store<T>(a, b, head, i + 1, D, per_head[h], per_head[AD_HEADS + h], y1);
+    }
+  };
+  if (parts <= 2) columns(std::integral_constant<int, 2>{});
+  else if (parts <= 16) columns(std::integral_constant<int, 8>{});
+  else columns(std::integral_constant<int, 32>{});
+}
+
+// A workgroup has sixteen query heads of one kv head, and one share of all steps that the batch sees.
+template <class T, int DT, bool NT, bool TICKETS>
+__global__ __launch_bounds__(AD_THREADS, 2) void attend_decode(AdArgs a) {
   constexpr int D = DT * 32, KB = D / 32, VB = D / 16;
   typedef typename Op<T>::frag frag;
   extern __shared__ char smem[];
@@ -34,32 +139,49 @@ __global__ __launch_bounds__(AD_THREADS) void attend_decode(AdArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 15, quad = lane >> 4;
   const int share = blockIdx.x, kvh = blockIdx.y, hg = blockIdx.z;
-  kv_prefix<AD_THREADS>(a.rows, pre, wave_sums, [&](int p) {
-    const int i = kv_seq(a.kv, a.seqs, p).len - 1;
-    return kv_span(i, i, a.window, a.sinks, AD_TILE).count;
-  });
-  const int total = pre[a.rows], per = max((total + a.shares - 1) / a.shares, 1);
-  const int64_t begin = (int64_t)share * per;
+  const bool few = a.rows <= 64;
+  AdLane w{};
+  AdDeal deal;
+  if (few) {
+    deal = ad_lanes(a, w);
+  } else {
+    kv_prefix<AD_THREADS>(a.rows, pre, wave_sums, [&](int p) { return ad_span(a, kv_seq(a.kv, a.seqs, p).len).count; });
+    deal = ad_deal(a, pre[a.rows]);
+  }
   const int heads = min(a.group - hg * AD_HEADS, AD_HEADS);
   for (int e = share; e < a.rows; e += a.shares) {                 // rows that see nothing
-    if (pre[e] != pre[e + 1]) continue;
+    const int count = few ? __builtin_amdgcn_readlane(w.span.count, e) : pre[e + 1] - pre[e];
+    if (count > 0) continue;
     for (int v = tid; v < heads * D; v += AD_THREADS) {
       const int h = kvh * a.group + hg * AD_HEADS + v / D;
       reinterpret_cast<T *>(a.out)[(int64_t)e * a.out_stride + h * D + v % D] = 0;
       if (a.lse && v % D == 0) a.lse[(int64_t)e * a.n_q + h] = -INFINITY;
     }
   }
-  if (begin >= total) return;
-  const int end = (int)min(begin + per, (int64_t)total);
-  const int64_t page_elems = (int64_t)a.kv.n_kv * a.kv.page * D;
+  const int64_t begin = (int64_t)share * deal.per;
+  if (begin >= deal.total) return;
+  const int end = (int)min(begin + deal.per, (int64_t)deal.total);
+  const int64_t page_elems = (int64_t)a.kv.n_kv * a.kv.page * D, head0 = (int64_t)kvh * a.kv.page * D;
   const int tok = 8 * (n >> 2) + (n & 3);                          // the first instruction's row n: tokens 8 quad + 0..3 of a step come back to a lane
   const int page_bits = 31 - __builtin_clz(a.kv.page);
-  int b = kv_find(pre, a.rows, (int)begin);
+  // where this lane's pieces of K and of V stand in their block of sixteen tokens, elements
+  const int k_in = quad * 128 + (tok & 15) * 8, v_in = ((quad & 1) * D + n) * 8;
+  int b = few ? 63 - __builtin_clzll(__ballot(lane < a.rows && w.before <= (int)begin && w.span.count > 0)) : kv_find(pre, a.rows, (int)begin);
   for (int at = (int)begin; at < end;) {
-    const KvSeq sq = kv_seq(a.kv, a.seqs, b);
+    KvSeq sq;
+    KvSpan span;
+    int before;
+    if (few) {
+      sq = KvSeq{__builtin_amdgcn_readlane(w.seq.row, b), __builtin_amdgcn_readlane(w.seq.len, b)};
+      span = KvSpan{__builtin_amdgcn_readlane(w.span.sink_tiles, b), __builtin_amdgcn_readlane(w.span.skip, b), __builtin_amdgcn_readlane(w.span.count, b)};
+      before = __builtin_amdgcn_readlane(w.before, b);
+    } else {
+      sq = kv_seq(a.kv, a.seqs, b);
+      span = ad_span(a, sq.len);
+      before = pre[b];
+    }
     const int pos = sq.len - 1, lo = kv_window_begin(pos, a.window);
-    const KvSpan span = kv_span(pos, pos, a.window, a.sinks, AD_TILE);
-    const int first = at - pre[b], last = min(end - pre[b], span.count);
+    const int first = at - before, last = min(end - before, span.count);
     const int32_t *table = a.kv.table + (int64_t)sq.row * a.kv.max_pages;
     frag qf[KB];
     {
@@ -71,48 +193,52 @@ __global__ __launch_bounds__(AD_THREADS) void attend_decode(AdArgs a) {
     f32x4 o[VB];
 #pragma unroll
     for (int v = 0; v < VB; ++v) o[v] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int u = first; u < last; ++u) {
-      const int t0 = span.at(u) * AD_TILE + wave * AD_STEP;
-      if (t0 > pos || (t0 + AD_STEP <= lo && t0 >= a.sinks)) continue;
-      // the pages of the step's two blocks of sixteen tokens
-      int id[2];
-      bool there[2];
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const int c = min((t0 + 16 * k) >> page_bits, a.kv.max_pages - 1);
-        id[k] = table[c];
-        there[k] = id[k] >= 0 && id[k] < a.kv.n_pages;
-        if (!there[k]) id[k] = 0;
+    // the pages of the wavefront's next 64 steps, a lane each: blocks of tokens 0..15 and 16..31, -1 for none
+    int id_a = -1, id_b = -1;
+    struct Step {
+      frag k0[KB], k1[KB], v[VB];
+      int t0;
+      bool there_a, there_b;
+    };
+    // Operands of step number j of the wavefront, straight from the pages; all of them asked for before the step ahead of it is worked on
+    auto load = [&](Step &x, int j) {
+      const int u = first + wave + j * AD_WAVES;
+      if ((j & 63) == 0) {
+        const int t = span.at(min(u + lane * AD_WAVES, span.count - 1)) * AD_STEP;
+        id_a = table[min(t >> page_bits, a.kv.max_pages - 1)];
+        id_b = table[min((t + 16) >> page_bits, a.kv.max_pages - 1)];
       }
-      const int64_t head0 = (int64_t)kvh * a.kv.page * D;
-      const int w0 = t0 & (a.kv.page - 1), w1 = (t0 + 16) & (a.kv.page - 1);
-      const T *kp = reinterpret_cast<const T *>(a.K) + (n < 8 ? (int64_t)id[0] * page_elems + (int64_t)w0 * D : (int64_t)id[1] * page_elems + (int64_t)w1 * D) + head0 +
-                    quad * 128 + (tok & 15) * 8;
-      const T *vp = reinterpret_cast<const T *>(a.V) + (quad < 2 ? (int64_t)id[0] * page_elems + (int64_t)w0 * D : (int64_t)id[1] * page_elems + (int64_t)w1 * D) + head0 +
-                    (quad & 1) * 8 * D + n * 8;
-      frag k0[KB], k1[KB], vf[VB];
+      x.t0 = span.at(u) * AD_STEP;
+      const int ida = __builtin_amdgcn_readlane(id_a, j & 63), idb = __builtin_amdgcn_readlane(id_b, j & 63);
+      x.there_a = (unsigned)ida < (unsigned)a.kv.n_pages;
+      x.there_b = (unsigned)idb < (unsigned)a.kv.n_pages;
+      const int64_t at_a = (int64_t)(x.there_a ? ida : 0) * page_elems + head0 + (int64_t)(x.t0 & (a.kv.page - 1)) * D;
+      const int64_t at_b = (int64_t)(x.there_b ? idb : 0) * page_elems + head0 + (int64_t)((x.t0 + 16) & (a.kv.page - 1)) * D;
+      const T *kp = reinterpret_cast<const T *>(a.K) + (n < 8 ? at_a : at_b) + k_in;
+      const T *vp = reinterpret_cast<const T *>(a.V) + (quad < 2 ? at_a : at_b) + v_in;
 #pragma unroll
-      for (int k = 0; k < KB; ++k) { k0[k] = Op<T>::load(kp + k * 512); k1[k] = Op<T>::load(kp + k * 512 + 32); }
+      for (int k = 0; k < KB; ++k) { x.k0[k] = NT ? Op<T>::load_nt(kp + k * 512) : Op<T>::load(kp + k * 512); x.k1[k] = NT ? Op<T>::load_nt(kp + k * 512 + 32) : Op<T>::load(kp + k * 512 + 32); }
 #pragma unroll
-      for (int v = 0; v < VB; ++v) vf[v] = Op<T>::load(vp + v * 128);
+      for (int v = 0; v < VB; ++v) x.v[v] = NT ? Op<T>::load_nt(vp + v * 128) : Op<T>::load(vp + v * 128);
+    };
+    auto work = [&](Step &x) {
       f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
 #pragma unroll
-      for (int k = 0; k < KB; ++k) { s0 = Op<T>::mma16(k0[k], qf[k], s0); s1 = Op<T>::mma16(k1[k], qf[k], s1); }
+      for (int k = 0; k < KB; ++k) { s0 = Op<T>::mma16(x.k0[k], qf[k], s0); s1 = Op<T>::mma16(x.k1[k], qf[k], s1); }
       float s[8];
 #pragma unroll
       for (int e = 0; e < 4; ++e) { s[e] = s0[e]; s[4 + e] = s1[e]; }
-      const bool whole = there[0] && there[1] && t0 + AD_STEP - 1 <= pos && (t0 >= lo || t0 + AD_STEP <= a.sinks);
+      const bool whole = x.there_a && x.there_b && x.t0 + AD_STEP - 1 <= pos && (x.t0 >= lo || x.t0 + AD_STEP <= a.sinks);
       if (!whole) {                                                // what is not seen: no weight, and nothing of V to multiply it with
         uint32_t keep = 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const int j = t0 + 8 * quad + e;
-          const bool sees = (quad < 2 ? there[0] : there[1]) & kv_sees(pos, lo, a.sinks, j);
+          const bool sees = (quad < 2 ? x.there_a : x.there_b) & kv_sees(pos, lo, a.sinks, x.t0 + 8 * quad + e);
           s[e] = sees ? s[e] : -INFINITY;
           keep |= (sees ? 1u : 0u) << e;
         }
 #pragma unroll
-        for (int v = 0; v < VB; ++v) vf[v] = Op<T>::only(vf[v], keep);
+        for (int v = 0; v < VB; ++v) x.v[v] = Op<T>::only(x.v[v], keep);
       }
       float top = s[0];
 #pragma unroll
@@ -131,7 +257,31 @@ __global__ __launch_bounds__(AD_THREADS) void attend_decode(AdArgs a) {
       for (int e = 0; e < 8; ++e) { p[e] = at_exp2(fmaf(s[e], a.scale, -base)); l += p[e]; }
       const frag pf = Op<T>::pack(p);
 #pragma unroll
-      for (int v = 0; v < VB; ++v) o[v] = Op<T>::mma16(vf[v], pf, o[v]);
+      for (int v = 0; v < VB; ++v) o[v] = Op<T>::mma16(x.v[v], pf, o[v]);
+      if constexpr (sizeof(T) == 2) {                              // what the rounding of the weights left: the pipes are idle, and the result is as exact as from fp32 weights
+        const frag rest = Op<T>::pack_rest(p, pf);
+#pragma unroll
+        for (int v = 0; v < VB; ++v) o[v] = Op<T>::mma16(x.v[v], rest, o[v]);
+      }
+    };
+    const int steps = last > first + wave ? (last - first - wave + AD_WAVES - 1) / AD_WAVES : 0;
+    Step even;
+    if constexpr (DT * sizeof(T) <= 8) {                           // two steps fit the registers
+      Step odd;
+      if (steps > 0) load(even, 0);
+      for (int j = 0; j < steps; j += 2) {
+        if (j + 1 < steps) load(odd, j + 1);
+        work(even);
+        if (j + 1 < steps) {
+          if (j + 2 < steps) load(even, j + 2);
+          work(odd);
+        }
+      }
+    } else {
+      for (int j = 0; j < steps; ++j) {
+        load(even, j);
+        work(even);
+      }
     }
     // the wavefronts' sums meet
     l = lane_sum<32>(lane_sum<16>(l));
@@ -146,98 +296,161 @@ __global__ __launch_bounds__(AD_THREADS) void attend_decode(AdArgs a) {
       const int h = v / D, i = v % D;
       float top = -INFINITY, ls = 0.f, os = 0.f;
 #pragma unroll
-      for (int w = 0; w < AD_WAVES; ++w) top = fmaxf(top, red_m[w * AD_HEADS + h]);
+      for (int x = 0; x < AD_WAVES; ++x) top = fmaxf(top, red_m[x * AD_HEADS + h]);
 #pragma unroll
-      for (int w = 0; w < AD_WAVES; ++w) {
-        const float by = at_exp2((red_m[w * AD_HEADS + h] - finite_or_0(top)) * a.scale);
-        ls += by * red_l[w * AD_HEADS + h];
-        os += by * red[(w * AD_HEADS + h) * D + i];
+      for (int x = 0; x < AD_WAVES; ++x) {
+        const float by = at_exp2((red_m[x * AD_HEADS + h] - finite_or_0(top)) * a.scale);
+        ls += by * red_l[x * AD_HEADS + h];
+        os += by * red[(x * AD_HEADS + h) * D + i];
       }
-      if (all) {
-        const int head = kvh * a.group + hg * AD_HEADS + h;
-        const float y = ls == 0.f ? 0.f : os / ls;
-        if constexpr (sizeof(T) == 2) reinterpret_cast<uint16_t *>(a.out)[(int64_t)b * a.out_stride + head * D + i] = (uint16_t)cvt_pk_bf16(y, 0.f);
-        else reinterpret_cast<float *>(a.out)[(int64_t)b * a.out_stride + head * D + i] = y;
-        if (a.lse && i == 0) a.lse[(int64_t)b * a.n_q + head] = (finite_or_0(top) * a.scale + log2f(ls)) * 0.6931471805599453f;
-      } else {
-        part[h * D + i] = os;
-        if (i == 0) { part[AD_HEADS * D + h] = top; part[AD_HEADS * (D + 1) + h] = ls; }
+      if (all) ad_store<T>(a, b, kvh * a.group + hg * AD_HEADS + h, i, D, top, ls, os);
+      else {
+        ad_part<TICKETS>(part + h * D + i, os);
+        if (i == 0) { ad_part<TICKETS>(part + AD_HEADS * D + h, top); ad_part<TICKETS>(part + AD_HEADS * (D + 1) + h, ls); }
       }
     }
-    at = pre[b] + last;
-    while (++b < a.rows && pre[b + 1] == at) {}
+    if (TICKETS && !all) {
+      // Parts and tickets are device-scope accesses, past the die's L2: every thread waits until its own stores are acknowledged, the barrier
+      // collects all of them, then thread 0 draws.  The workgroup that draws a row's last ticket joins the row; nobody waits for anybody.
+      const int x0 = before / deal.per, parts = (before + span.count - 1) / deal.per - x0 + 1;
+      int32_t *ticket = a.tickets + ((int64_t)kvh * gridDim.z + hg) * a.shares + x0;
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      if (tid == 0) {
+        const int t = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (t == parts - 1) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);    // ready for the next call
+        *wave_sums = t == parts - 1;
+      }
+      __syncthreads();
+      if (*wave_sums) ad_join<T>(a, b, kvh, hg, heads, x0, parts, before, deal.per, red, red_m);
+    }
+    at = before + last;
+    if (few) {
+      const uint64_t rest = __ballot(lane > b && lane < a.rows && w.span.count > 0);
+      b = rest ? __builtin_ctzll(rest) : a.rows;
+    } else {
+      while (++b < a.rows && pre[b + 1] == at) {}
+    }
   }
 }
 
-// the parts of the rows that more than one share had
+// The parts of a row that more than one share had; workgroup (x, head) has the row that begins in share x and goes on behind it.  The weights of all
+// parts first, then four columns a thread of every so many parts, none of which waits for another.
 template <class T>
 __global__ __launch_bounds__(AD_THREADS) void attend_join(AdArgs a) {
   extern __shared__ char smem[];
-  int *wave_sums = reinterpret_cast<int *>(smem), *pre = wave_sums + AD_WAVES;
-  const int D = a.kv.d, tid = threadIdx.x, b = blockIdx.x, kvh = blockIdx.y, hg = blockIdx.z;
-  kv_prefix<AD_THREADS>(a.rows, pre, wave_sums, [&](int p) {
-    const int i = kv_seq(a.kv, a.seqs, p).len - 1;
-    return kv_span(i, i, a.window, a.sinks, AD_TILE).count;
-  });
-  const int total = pre[a.rows], per = max((total + a.shares - 1) / a.shares, 1);
-  if (pre[b] == pre[b + 1]) return;
-  const int x0 = pre[b] / per, x1 = (pre[b + 1] - 1) / per;
-  if (x0 == x1) return;
-  const int heads = min(a.group - hg * AD_HEADS, AD_HEADS);
-  const float *parts = a.part + ((int64_t)kvh * gridDim.z + hg) * a.shares * 2 * AD_HEADS * (D + 2);
-  for (int v = tid; v < heads * D; v += AD_THREADS) {
-    const int h = v / D, i = v % D;
-    float top = -INFINITY, ls = 0.f, os = 0.f;
-    for (int x = x0; x <= x1; ++x) {
-      const float *part = parts + ((int64_t)x * 2 + ((int64_t)x * per <= pre[b] ? 1 : 0)) * AD_HEADS * (D + 2);
-      const float m = part[AD_HEADS * D + h], grown = fmaxf(top, m);
-      const float was = at_exp2((top - finite_or_0(grown)) * a.scale), by = at_exp2((m - finite_or_0(grown)) * a.scale);
-      ls = ls * was + by * part[AD_HEADS * (D + 1) + h];
-      os = os * was + by * part[h * D + i];
-      top = grown;
-    }
-    const int head = kvh * a.group + hg * AD_HEADS + h;
-    const float y = ls == 0.f ? 0.f : os / ls;
-    if constexpr (sizeof(T) == 2) reinterpret_cast<uint16_t *>(a.out)[(int64_t)b * a.out_stride + head * D + i] = (uint16_t)cvt_pk_bf16(y, 0.f);
-    else reinterpret_cast<float *>(a.out)[(int64_t)b * a.out_stride + head * D + i] = y;
-    if (a.lse && i == 0) a.lse[(int64_t)b * a.n_q + head] = (finite_or_0(top) * a.scale + log2f(ls)) * 0.6931471805599453f;
+  float *weight = reinterpret_cast<float *>(smem), *sums = weight + AD_GROUPS;       // [parts]; [part group][D] and two numbers a wavefront
+  const int D = a.kv.d, tid = threadIdx.x, x0 = blockIdx.x, head = blockIdx.y, kvh = head / a.group, hg = head % a.group / AD_HEADS, h = head % a.group % AD_HEADS;
+  const int zs = (a.group + AD_HEADS - 1) / AD_HEADS;
+  int *wave_sums = reinterpret_cast<int *>(sums + AD_THREADS * 4 + 2 * AD_WAVES), *pre = wave_sums + AD_WAVES;
+  int b, before, count;
+  AdDeal deal;
+  if (a.rows <= 64) {
+    AdLane w;
+    deal = ad_lanes(a, w);
+    const int64_t end = (int64_t)(x0 + 1) * deal.per;              // of the share
+    if (end >= deal.total) return;
+    b = 63 - __builtin_clzll(__ballot((int)(threadIdx.x & 63) < a.rows && w.before < (int)end && w.span.count > 0));
+    before = __builtin_amdgcn_readlane(w.before, b);
+    count = __builtin_amdgcn_readlane(w.span.count, b);
+  } else {
+    kv_prefix<AD_THREADS>(a.rows, pre, wave_sums, [&](int p) { return ad_span(a, kv_seq(a.kv, a.seqs, p).len).count; });
+    deal = ad_deal(a, pre[a.rows]);
+    const int64_t end = (int64_t)(x0 + 1) * deal.per;
+    if (end >= deal.total) return;
+    b = kv_find(pre, a.rows, (int)end - 1);
+    before = pre[b];
+    count = pre[b + 1] - before;
+  }
+  const int x1 = (before + count - 1) / deal.per, parts = x1 - x0 + 1;
+  if (parts == 1 || before / deal.per != x0) return;
+  const float *base = a.part + ((int64_t)kvh * zs + hg) * a.shares * 2 * AD_HEADS * (D + 2);
+  auto part_of = [&](int x) { return base + ((int64_t)(x0 + x) * 2 + ((int64_t)(x0 + x) * deal.per <= before ? 1 : 0)) * AD_HEADS * (D + 2); };
+  float top = -INFINITY;
+  for (int x = tid; x < parts; x += AD_THREADS) {
+    const float m = part_of(x)[AD_HEADS * D + h];
+    weight[x] = m;
+    top = fmaxf(top, m);
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+  float *tops = sums + AD_THREADS * 4, *totals = tops + AD_WAVES;
+  if ((tid & 63) == 0) tops[tid >> 6] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+  float ls = 0.f;
+  for (int x = tid; x < parts; x += AD_THREADS) {
+    const float by = at_exp2((weight[x] - finite_or_0(top)) * a.scale);
+    weight[x] = by;
+    ls += by * part_of(x)[AD_HEADS * (D + 1) + h];
+  }
+  ls = wave_sum(ls);
+  if ((tid & 63) == 0) totals[tid >> 6] = ls;
+  __syncthreads();
+  ls = (totals[0] + totals[1]) + (totals[2] + totals[3]);
+  const int wide = D / 4, groups = AD_THREADS / wide, g = tid / wide, i = tid % wide;
+  f32x4 os = {0.f, 0.f, 0.f, 0.f};
+  if (g < groups) {
+#pragma unroll 4
+    for (int x = g; x < parts; x += groups) os += weight[x] * *reinterpret_cast<const f32x4 *>(part_of(x) + h * D + 4 * i);
+    *reinterpret_cast<f32x4 *>(sums + (g * wide + i) * 4) = os;
+  }
+  __syncthreads();
+  for (int v = tid; v < D; v += AD_THREADS) {
+    float y = 0.f;
+    for (int k = 0; k < groups; ++k) y += sums[k * D + v];
+    ad_store<T>(a, b, head, v, D, top, ls, y);
   }
 }
 
-// shares of a kv head's tokens: about four workgroups a compute unit in all
+// shares of a kv head's tokens: one of them has no parts to join
 static int ad_shares(const parse_kv *kv, int n_q) {
   const int columns = kv->n_kv * ((n_q / kv->n_kv + AD_HEADS - 1) / AD_HEADS);
-  return columns >= 1024 ? 1 : 1024 / columns;
+  return columns >= AD_GROUPS ? 1 : AD_GROUPS / columns;
 }
 static size_t ad_bytes(const parse_kv *kv, int n_q) {
   const int columns = kv->n_kv * ((n_q / kv->n_kv + AD_HEADS - 1) / AD_HEADS);
-  return round_up((size_t)columns * ad_shares(kv, n_q) * 2 * AD_HEADS * (kv->d + 2) * 4, 256);
+  return AD_TICKET_BYTES + round_up((size_t)columns * ad_shares(kv, n_q) * 2 * AD_HEADS * (kv->d + 2) * 4, 256);
 }
 
-template <class T, int DT>
+// One launch where the workgroup that comes last has little to join (at most 256 KiB of parts); where it has more, a second launch spreads it over the heads
+static bool ad_tickets(const parse_kv *kv, int n_q) {
+  const int64_t weights = (int64_t)ad_shares(kv, n_q) * std::min(n_q / kv->n_kv, AD_HEADS);
+  return weights * kv->d <= 65536 && 2 * weights <= AD_WAVES * AD_HEADS * kv->d;    // ... in the LDS that the sums left
+}
+
+template <class T, int DT, bool NT, bool TICKETS>
 static int ad_launch(const AdArgs &a, hipStream_t s) {
-  const int zs = (a.group + AD_HEADS - 1) / AD_HEADS;
-  const size_t lds = (size_t)AD_WAVES * AD_HEADS * (DT * 32 + 2) * 4 + (AD_WAVES + a.rows + 1) * 4;
-  PARSE_ALLOW_LDS((attend_decode<T, DT>), 0, lds);
-  attend_decode<T, DT><<<dim3(a.shares, a.kv.n_kv, zs), AD_THREADS, lds, s>>>(a);
+  const int zs = (a.group + AD_HEADS - 1) / AD_HEADS, scan = a.rows > 64 ? a.rows + 1 : 0;
+  const size_t lds = (size_t)AD_WAVES * AD_HEADS * (DT * 32 + 2) * 4 + (AD_WAVES + scan) * 4;
+  PARSE_ALLOW_LDS((attend_decode<T, DT, NT, TICKETS>), 0, lds);
+  attend_decode<T, DT, NT, TICKETS><<<dim3(a.shares, a.kv.n_kv, zs), AD_THREADS, lds, s>>>(a);
   PARSE_LAUNCH_CHECK();
-  if (a.shares > 1) {
-    attend_join<T><<<dim3(a.rows, a.kv.n_kv, zs), AD_THREADS, (AD_WAVES + a.rows + 1) * 4, s>>>(a);
+  if (!TICKETS && a.shares > 1) {
+    attend_join<T><<<dim3(a.shares - 1, a.n_q), AD_THREADS, (AD_GROUPS + AD_THREADS * 4 + 3 * AD_WAVES + scan) * 4, s>>>(a);
     PARSE_LAUNCH_CHECK();
   }
   return PARSE_OK;
 }
+// A cache larger than the last-level cache is new to it in every step: loads that do not stay there (100003 tokens of 8 heads 81.5 -> 77.8 us, 192 windows 162 -> 153); a
+// smaller one may be found there again (four caches of 3000 to 4000 tokens, 16 heads of 64 columns: 18.1 us, 20.2 with such loads)
+template <class T, int DT>
+static int ad_form(const AdArgs &a, hipStream_t s) {
+  const bool nt = (size_t)a.kv.n_layers * a.kv.n_pages * a.kv.n_kv * a.kv.page * a.kv.d * sizeof(T) * 2 > ((size_t)192 << 20), tickets = ad_tickets(&a.kv, a.n_q);
+  if (nt) return tickets ? ad_launch<T, DT, true, true>(a, s) : ad_launch<T, DT, true, false>(a, s);
+  return tickets ? ad_launch<T, DT, false, true>(a, s) : ad_launch<T, DT, false, false>(a, s);
+}
 template <class T>
 static int ad_width(const AdArgs &a, hipStream_t s) {
   switch (a.kv.d / 32) {
-    case 1: return ad_launch<T, 1>(a, s);
-    case 2: return ad_launch<T, 2>(a, s);
-    case 3: return ad_launch<T, 3>(a, s);
-    case 4: return ad_launch<T, 4>(a, s);
-    case 5: return ad_launch<T, 5>(a, s);
-    case 6: return ad_launch<T, 6>(a, s);
-    case 7: return ad_launch<T, 7>(a, s);
-    default: return ad_launch<T, 8>(a, s);
+    case 1: return ad_form<T, 1>(a, s);
+    case 2: return ad_form<T, 2>(a, s);
+    case 3: return ad_form<T, 3>(a, s);
+    case 4: return ad_form<T, 4>(a, s);
+    case 5: return ad_form<T, 5>(a, s);
+    case 6: return ad_form<T, 6>(a, s);
+    case 7: return ad_form<T, 7>(a, s);
+    default: return ad_form<T, 8>(a, s);
   }
 }
 
@@ -280,7 +493,8 @@ int parse_attend_decode(const parse_kv *kv, int32_t layer, const void *q, int64_
   a.n_q = n_q; a.group = n_q / kv->n_kv; a.rows = rows; a.window = window; a.sinks = sinks;
   a.shares = ad_shares(kv, n_q);
   at_scale(scale, a.scale, a.lag, a.q_sign);
-  a.part = (float *)workspace;
+  a.tickets = (int32_t *)workspace;
+  a.part = (float *)((char *)workspace + AD_TICKET_BYTES);
   return kv->dtype == PARSE_BF16 ? ad_width<uint16_t>(a, (hipStream_t)stream) : ad_width<float>(a, (hipStream_t)stream);
 }
 

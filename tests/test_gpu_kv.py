@@ -113,12 +113,14 @@ def run_decode(case, n_q, window=0, sinks=0, seqs=None, scale=None, seed=1, pad=
     buf, whole, out = guarded(rows, n_q, case.d, qd, pad)
     lbuf, lmid = guarded_bytes(rows * n_q * 4)
     wbuf, ws = guarded_bytes(int(pa.lib().parse_attend_decode_workspace_bytes(case.kv.c(), n_q, rows)))
+    ws[:2048] = 0                                                  # the tickets; the rest holds anything
     before = whole[:, n_q * case.d:].clone()
     lse = lmid[:rows * n_q * 4].view(torch.float32).view(rows, n_q)
     pa.attend_decode(case.kv, 1, qd, seqs=None if seqs is None else i32(np.array(seqs)), scale=scale, window=window, sinks=sinks, out=out, lse=lse,
                      workspace=ws)
     for b, what in ((buf, "out"), (lbuf, "lse"), (wbuf, "workspace")):
         check_guards(b, what)
+    assert not bool(ws[:2048].any()), "tickets left"
     assert torch.equal(whole[:, n_q * case.d:].view(torch.uint8), before.view(torch.uint8)), "stores between the rows"
     scale = case.d ** -0.5 if scale is None else scale
     want = []
