@@ -702,7 +702,7 @@ def _rows_of(t, kv, heads, what):
 
 
 def _ints(t, n, what):
-    if t is not None and (t.dtype != torch.int32 or t.numel() != n or not t.is_contiguous()):
+    if t is not None and (t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous()):
         raise ValueError(f"{what}: contiguous int32 of {n} elements is wanted")
     return t
 
@@ -760,17 +760,18 @@ def kv_append(kv: KV, layer: int, k, v, tok_offsets=None, seqs=None, q=None, q_o
     if q is not None:
         n_q = q.shape[1]
         if q_out is None:
-            q_out = torch.empty((rows, n_q, kv.d), dtype=q.dtype, device=q.device)
+            q_out = q.new_empty((rows, n_q, kv.d))
         if q.shape[0] != rows or q_out.shape[0] != rows:
             raise ValueError("q, q_out and k of one number of rows are wanted")
         q_stride, out_stride = _rows_of(q, kv, n_q, "q"), _rows_of(q_out, kv, n_q, "q_out")
     n_pos = 0
     if rope is not None:
-        n_pos = rope.shape[0]
-        if rope.dtype != torch.float32 or rope.shape != (n_pos, kv.d) or not rope.is_contiguous():
+        n_pos, d = rope.shape
+        if rope.dtype is not torch.float32 or d != kv.d or not rope.is_contiguous():
             raise ValueError(f"rope: contiguous float32 [positions][{kv.d}] is wanted")
     _check(_calls.parse_kv_append(kv, layer, k, _rows_of(k, kv, kv.n_kv, "k"), v, _rows_of(v, kv, kv.n_kv, "v"), q, q_stride, q_out, out_stride,
-                                  n_q, rows, _ints(tok_offsets, P + 1, "tok_offsets"), _ints(seqs, P, "seqs"), P, rope, n_pos, _stream()),
+                                  n_q, rows, tok_offsets if tok_offsets is None else _ints(tok_offsets, P + 1, "tok_offsets"),
+                                  seqs if seqs is None else _ints(seqs, P, "seqs"), P, rope, n_pos, _stream()),
            "parse_kv_append")
     return q_out
 

@@ -63,6 +63,17 @@ __device__ __forceinline__ KvSpan kv_span(int i0, int i1, int window, int sinks,
   s.count = s.sink_tiles + to - from;
   return s;
 }
+// sum over the lanes up to this one: within rows of sixteen, then the rows' ends carried on (data moves from lane to lane in the vector unit, without LDS)
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // row_shr:1
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);  // row_shr:2
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);  // row_shr:4
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);  // row_shr:8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // row_bcast:15, into rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // row_bcast:31, into rows 2 and 3
+  return v;
+}
+
 // pre[p] = sum of count(0) .. count(p - 1) for p = 0 .. P, by a whole workgroup; `wave_sums`: one int per wavefront, LDS
 template <int THREADS, class F>
 __device__ __forceinline__ void kv_prefix(int P, int *pre, int *wave_sums, F count) {
@@ -72,12 +83,7 @@ __device__ __forceinline__ void kv_prefix(int P, int *pre, int *wave_sums, F cou
     const int p = tid * per + i;
     if (p < P) { const int c = count(p); pre[p] = mine; mine += c; }
   }
-  int inc = mine;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int v = __shfl_up(inc, o, 64);
-    if (lane >= o) inc += v;
-  }
+  const int inc = wave_scan(mine);
   if (lane == 63) wave_sums[wave] = inc;
   __syncthreads();
   int base = inc - mine;
@@ -112,49 +118,44 @@ static inline void at_scale(float given, float &scale, float &lag, uint32_t &q_s
   lag = fminf(AT_LAG / scale, 3e38f);
 }
 
-// Which prompt a row tile belongs to.  Prompts have ceil(rows * group / tile) tiles each, numbered through.
+// Which prompt an item belongs to, where prompt p has count(rows, sequence) of them, numbered through.
 struct KvItem {
-  int p, first, n, row, len, tile;             // rows, sequence, tile of the prompt; tile < 0: there is no such item
+  int first, n, row, len, item;                // rows, sequence, number of the item in its prompt; item < 0: there is no such one
 };
 // A wavefront alone, for up to 64 prompts: a lane reads a prompt's words, all at once.
-__device__ __forceinline__ KvItem kv_item_wave(const parse_kv &kv, const int32_t *__restrict__ tok_offsets, const int32_t *__restrict__ seqs, int P, int rows, int group,
-                                               int tile, int item) {
+template <class F>
+__device__ __forceinline__ KvItem kv_item_wave(const parse_kv &kv, const int32_t *__restrict__ tok_offsets, const int32_t *__restrict__ seqs, int P, int rows, int item,
+                                               F count) {
   const int lane = threadIdx.x & 63, p = min(lane, P - 1);
   const KvRows r = kv_rows(tok_offsets, p, rows);
   const KvSeq s = kv_seq(kv, seqs, p);
-  const int tiles = lane < P ? (int)(((int64_t)r.n * group + tile - 1) / tile) : 0;
-  int inc = tiles;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int v = __shfl_up(inc, o, 64);
-    if (lane >= o) inc += v;
-  }
-  const int at = __builtin_amdgcn_readfirstlane(__popcll(__ballot(inc <= item)));    // prompts whose tiles all lie before
-  KvItem f{at, 0, 0, 0, 0, -1};
+  const int mine = lane < P ? count(r, s) : 0, inc = wave_scan(mine);
+  const int at = __builtin_amdgcn_readfirstlane(__popcll(__ballot(inc <= item)));    // prompts whose items all lie before
+  KvItem f{0, 0, 0, 0, -1};
   if (at >= P) return f;
   f.first = __builtin_amdgcn_readlane(r.first, at);
   f.n = __builtin_amdgcn_readlane(r.n, at);
   f.row = __builtin_amdgcn_readlane(s.row, at);
   f.len = __builtin_amdgcn_readlane(s.len, at);
-  f.tile = item - (__builtin_amdgcn_readlane(inc, at) - __builtin_amdgcn_readlane(tiles, at));
+  f.item = item - (__builtin_amdgcn_readlane(inc, at) - __builtin_amdgcn_readlane(mine, at));
   return f;
 }
-// A workgroup, for any number
-template <int THREADS>
-__device__ __forceinline__ KvItem kv_item(const parse_kv &kv, const int32_t *__restrict__ tok_offsets, const int32_t *__restrict__ seqs, int P, int rows, int group,
-                                          int tile, int item, int *pre, int *wave_sums) {
-  if (P <= 64) return kv_item_wave(kv, tok_offsets, seqs, P, rows, group, tile, item);
-  kv_prefix<THREADS>(P, pre, wave_sums, [&](int p) { return (int)(((int64_t)kv_rows(tok_offsets, p, rows).n * group + tile - 1) / tile); });
-  KvItem f{0, 0, 0, 0, 0, -1};
+// A workgroup, for any number; `pre`, `wave_sums`: as for kv_prefix
+template <int THREADS, class F>
+__device__ __forceinline__ KvItem kv_item(const parse_kv &kv, const int32_t *__restrict__ tok_offsets, const int32_t *__restrict__ seqs, int P, int rows, int item,
+                                          int *pre, int *wave_sums, F count) {
+  if (P <= 64) return kv_item_wave(kv, tok_offsets, seqs, P, rows, item, count);
+  kv_prefix<THREADS>(P, pre, wave_sums, [&](int p) { return count(kv_rows(tok_offsets, p, rows), kv_seq(kv, seqs, p)); });
+  KvItem f{0, 0, 0, 0, -1};
   if (item >= pre[P]) return f;
-  f.p = __builtin_amdgcn_readfirstlane(kv_find(pre, P, item));
-  const KvRows r = kv_rows(tok_offsets, f.p, rows);
-  const KvSeq s = kv_seq(kv, seqs, f.p);
+  const int p = __builtin_amdgcn_readfirstlane(kv_find(pre, P, item));
+  const KvRows r = kv_rows(tok_offsets, p, rows);
+  const KvSeq s = kv_seq(kv, seqs, p);
   f.first = __builtin_amdgcn_readfirstlane(r.first);
   f.n = __builtin_amdgcn_readfirstlane(r.n);
   f.row = __builtin_amdgcn_readfirstlane(s.row);
   f.len = __builtin_amdgcn_readfirstlane(s.len);
-  f.tile = item - __builtin_amdgcn_readfirstlane(pre[f.p]);
+  f.item = item - __builtin_amdgcn_readfirstlane(pre[p]);
   return f;
 }
 

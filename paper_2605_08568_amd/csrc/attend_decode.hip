@@ -57,12 +57,7 @@ __device__ __forceinline__ AdDeal ad_lanes(const AdArgs &a, AdLane &w) {
   w.seq = kv_seq(a.kv, a.seqs, min(lane, a.rows - 1));
   w.span = ad_span(a, w.seq.len);
   const int mine = lane < a.rows ? w.span.count : 0;
-  int inc = mine;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int v = __shfl_up(inc, o, 64);
-    if (lane >= o) inc += v;
-  }
+  const int inc = wave_scan(mine);
   w.before = inc - mine;
   return ad_deal(a, __builtin_amdgcn_readlane(inc, 63));
 }

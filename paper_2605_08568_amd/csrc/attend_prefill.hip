@@ -16,6 +16,9 @@ struct ApArgs {
   uint32_t q_sign;
 };
 
+// tiles of rows of a prompt
+__device__ __forceinline__ int ap_tiles(int n, int group, int tile) { return (int)(((int64_t)n * group + tile - 1) / tile); }
+
 // A workgroup has NW * 32 rows of one kv head: row r of a prompt is head r % group of token r / group, so that shared
 // heads read a tile of K and V once.  Tiles of TK tokens are staged in LDS as they stand in the pages, ST buffers deep.  Both
 // products have the cache's side as operand A and the rows as columns: a lane holds weights of one row only, the softmax needs
@@ -31,11 +34,11 @@ __global__ __launch_bounds__(NW * 64) void attend_prefill(ApArgs a) {
   int *wave_sums = reinterpret_cast<int *>(smem + ST * STAGE), *pre = wave_sums + NW;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, half = lane >> 5;
   const int kvh = blockIdx.x % a.kv.n_kv, item = blockIdx.x / a.kv.n_kv, group = a.group;
-  const KvItem f = kv_item<THREADS>(a.kv, a.tok_offsets, a.seqs, a.P, a.rows, group, TM, item, pre, wave_sums);
-  if (f.tile < 0) return;
+  const KvItem f = kv_item<THREADS>(a.kv, a.tok_offsets, a.seqs, a.P, a.rows, item, pre, wave_sums, [&](const KvRows &r, const KvSeq &) { return ap_tiles(r.n, group, TM); });
+  if (f.item < 0) return;
   const int n_rows = f.n, row0 = f.first, len = f.len;
   const int32_t *table = a.kv.table + (int64_t)f.row * a.kv.max_pages;
-  const int r0 = ((int)(((int64_t)n_rows * group + TM - 1) / TM) - 1 - f.tile) * TM;     // the rows that see most come first
+  const int r0 = (ap_tiles(n_rows, group, TM) - 1 - f.item) * TM;     // the rows that see most come first
   const int r_end = n_rows * group, base = len - n_rows;
   const int i0 = base + r0 / group, i1 = base + (min(r0 + TM, r_end) - 1) / group;
   const KvSpan span = i1 < 0 ? KvSpan{0, 0, 0} : kv_span(max(i0, 0), i1, a.window, a.sinks, TK);
@@ -233,7 +236,7 @@ __device__ __forceinline__ bool ap_rows(const ApArgs &a, const KvItem &f, char *
   const int kvh = blockIdx.x % a.kv.n_kv, group = a.group;
   const int n_rows = f.n, row0 = f.first, len = f.len;
   const int32_t *table = a.kv.table + (int64_t)f.row * a.kv.max_pages;
-  const int r0 = ((int)(((int64_t)n_rows * group + TM - 1) / TM) - 1 - f.tile) * TM;     // the rows that see most come first
+  const int r0 = (ap_tiles(n_rows, group, TM) - 1 - f.item) * TM;     // the rows that see most come first
   const int r_end = n_rows * group, base = len - n_rows;
   const int i0 = base + r0 / group, i1 = base + (min(r0 + TM, r_end) - 1) / group;
   const KvSpan span = i1 < 0 ? KvSpan{0, 0, 0} : kv_span(max(i0, 0), i1, a.window, a.sinks, TK);
@@ -472,15 +475,21 @@ __device__ __forceinline__ bool ap_rows(const ApArgs &a, const KvItem &f, char *
     __syncthreads();
     if (__builtin_amdgcn_readfirstlane(flag[2])) return false;
   }
-  if (r >= r_end) return true;
+  if (idle) return true;
   l = lane_sum<32>(l);
   const float by = l == 0.f ? 0.f : 1.f / l;
-  T *out = reinterpret_cast<T *>(a.out) + (int64_t)(row0 + token) * a.out_stride + (int64_t)head * D;
+  // the lane halves hold columns 8 c + 0..3 and 8 c + 4..7 of a row: they swap, so that each has eight of them, of every other c
+  T *out = reinterpret_cast<T *>(a.out) + (int64_t)(row0 + token) * a.out_stride + (int64_t)head * D + 8 * half;
 #pragma unroll
   for (int d = 0; d < DT; ++d)
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
-      O::store4(out + 32 * d + 8 * c + 4 * half, o[d][4 * c] * by, o[d][4 * c + 1] * by, o[d][4 * c + 2] * by, o[d][4 * c + 3] * by);
+    for (int c = 0; c < 4; c += 2) {
+      const float *u = reinterpret_cast<const float *>(&o[d]) + 4 * c;
+      const u32x2 x = __builtin_amdgcn_permlane32_swap(cvt_pk_bf16(u[0] * by, u[1] * by), cvt_pk_bf16(u[4] * by, u[5] * by), false, false);
+      const u32x2 y = __builtin_amdgcn_permlane32_swap(cvt_pk_bf16(u[2] * by, u[3] * by), cvt_pk_bf16(u[6] * by, u[7] * by), false, false);
+      if (r < r_end) *reinterpret_cast<u32x4 *>(out + 32 * d + 8 * c) = u32x4{x[0], y[0], x[1], y[1]};
+    }
+  if (r >= r_end) return true;
   if (a.lse && half == 0) a.lse[(int64_t)(row0 + token) * a.n_q + head] = (finite_or_0(m) * a.scale + log2f(l)) * 0.6931471805599453f;
   return true;
 }
@@ -489,8 +498,9 @@ template <int DT>
 __global__ __launch_bounds__(AP_WAVES * 64, DT <= 4 ? 2 : 1) void attend_prefill_bf16(ApArgs a) {
   extern __shared__ char smem[];                                   // AP_STAGES tiles of K, as many of V, three flags, the prompts' tiles
   int *flag = reinterpret_cast<int *>(smem + ap_lds_bytes(DT)), *wave_sums = flag + 3, *pre = wave_sums + AP_WAVES;
-  const KvItem f = kv_item<AP_WAVES * 64>(a.kv, a.tok_offsets, a.seqs, a.P, a.rows, a.group, AP_ROWS, blockIdx.x / a.kv.n_kv, pre, wave_sums);
-  if (f.tile < 0) return;
+  const KvItem f = kv_item<AP_WAVES * 64>(a.kv, a.tok_offsets, a.seqs, a.P, a.rows, blockIdx.x / a.kv.n_kv, pre, wave_sums,
+                                          [&](const KvRows &r, const KvSeq &) { return ap_tiles(r.n, a.group, AP_ROWS); });
+  if (f.item < 0) return;
   if (threadIdx.x < 3) flag[threadIdx.x] = 0;                      // [2]: something is not finite
   if (!ap_rows<DT, false>(a, f, smem)) ap_rows<DT, true>(a, f, smem);
 }

@@ -104,12 +104,7 @@ static KvWork kv_work(const parse_kv *kv, void *ws) {
 // exclusive sum over the threads of a workgroup alone; `sums`: one int per wavefront, LDS.  Returns this thread's, and the total.
 __device__ __forceinline__ int sum_before(int mine, int *sums, int &total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int inc = mine;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int v = __shfl_up(inc, o, 64);
-    if (lane >= o) inc += v;
-  }
+  const int inc = wave_scan(mine);
   __syncthreads();
   if (lane == 63) sums[wave] = inc;
   __syncthreads();
@@ -330,43 +325,59 @@ __device__ __forceinline__ void store8(float *p, const float *f) {
   *reinterpret_cast<f32x4 *>(p + 4) = f32x4{f[4], f[5], f[6], f[7]};
 }
 
-// Workgroup (x, y) = one block of sixteen positions of a prompt, every gridDim.y-th 256 pieces of its work.  A piece of K or
-// q is 8 columns and their 8 partners of one token; of V 8 columns of 8 tokens, transposed in registers.
+// Two neighbouring columns of eight tokens, and the same as two pieces of V
+__device__ __forceinline__ void turn8(const uint16_t *from, int64_t stride, uint16_t *to) {
+  uint32_t x[8];
+#pragma unroll
+  for (int t = 0; t < 8; ++t) x[t] = *reinterpret_cast<const uint32_t *>(from + t * stride);
+  u32x4 lo, hi;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    lo[w] = (x[2 * w] & 0xffffu) | (x[2 * w + 1] << 16);
+    hi[w] = (x[2 * w] >> 16) | (x[2 * w + 1] & 0xffff0000u);
+  }
+  reinterpret_cast<u32x4 *>(to)[0] = lo;
+  reinterpret_cast<u32x4 *>(to)[1] = hi;
+}
+__device__ __forceinline__ void turn8(const float *from, int64_t stride, float *to) {
+  float lo[8], hi[8];
+#pragma unroll
+  for (int t = 0; t < 8; ++t) {
+    const float2 x = *reinterpret_cast<const float2 *>(from + t * stride);
+    lo[t] = x.x; hi[t] = x.y;
+  }
+  store8(to, lo);
+  store8(to + 8, hi);
+}
+
+// Workgroup (x, y) = one block of sixteen positions of a prompt, some of its heads.  A thread has one token's 8 columns and their 8 partners, whose angles it reads
+// once, head after head (of K token fastest: the pieces of a column block are contiguous in the page); of V two columns of eight tokens, transposed
+// in registers, or 8 columns of one token where not all eight are new.
 template <class T>
 __global__ __launch_bounds__(KV_THREADS) void kv_append(KaArgs a) {
   extern __shared__ int smem[];
   int *wave_sums = smem, *pre = smem + KV_THREADS / 64;
-  const int D = a.kv.d, half = D / 2, pairs = D / 16;               // pairs of pieces in a row
-  // blocks of a prompt: of its positions, and of its rows where they have no place in the cache
-  auto place = [&](int p, KvRows &r, KvSeq &s) {
-    r = kv_rows(a.tok_offsets, p, a.rows);
-    s = kv_seq(a.kv, a.seqs, p);
-    return s.len - r.n;
-  };
-  kv_prefix<KV_THREADS>(a.P, pre, wave_sums, [&](int p) {
-    KvRows r; KvSeq s;
-    const int base = place(p, r, s);
-    return r.n == 0 ? 0 : ((base + r.n + 15) >> 4) - (base >> 4);
-  });
-  for (int item = blockIdx.x; item < pre[a.P]; item += gridDim.x) {
-    const int p = kv_find(pre, a.P, item);
-    KvRows pr; KvSeq sq;
-    const int base = place(p, pr, sq);
-    const int block = (base >> 4) + item - pre[p];                 // tokens 16 block + 0..15 of the sequence
+  const int D = a.kv.d, half = D / 2, pairs = D / 16, tid = threadIdx.x;     // pairs of pieces in a row
+  for (int item = blockIdx.x;; item += gridDim.x) {
+    const KvItem f = kv_item<KV_THREADS>(a.kv, a.tok_offsets, a.seqs, a.P, a.rows, item, pre, wave_sums,
+                                         [&](const KvRows &r, const KvSeq &s) { return r.n == 0 ? 0 : ((s.len + 15) >> 4) - ((s.len - r.n) >> 4); });
+    if (f.item < 0) return;
+    const int base = f.len - f.n, block = (base >> 4) + f.item;     // positions 16 block + 0..15; before 0: rows without a place in the cache
+    const int from = max(block * 16, base), tokens = min(block * 16 + 16, f.len) - from, row0 = f.first + from - base;
     const int c = block >> (27 - __builtin_clz(a.kv.page));        // 16 block / page
-    int id = block >= 0 && c < a.kv.max_pages ? a.kv.table[(int64_t)sq.row * a.kv.max_pages + c] : -1;
-    if (!page_ok(a.kv, id)) id = -1;
+    const int id = block >= 0 && c < a.kv.max_pages ? a.kv.table[(int64_t)f.row * a.kv.max_pages + c] : -1;
+    const bool there = page_ok(a.kv, id);
     // where the block stands for head 0; heads are page * D apart
-    const int64_t spot = (int64_t)max(id, 0) * a.kv.n_kv * a.kv.page * D + (int64_t)((block * 16) & (a.kv.page - 1)) * D;
-    const int n_k = id < 0 ? 0 : a.kv.n_kv * pairs * 16, n_v = id < 0 ? 0 : a.kv.n_kv * (D / 8) * 2, n_q = a.q ? a.n_q * pairs * 16 : 0;
-    auto rotated = [&](const T *row, int piece, int pos, float *lo, float *hi) {
-      load8(row + 8 * piece, lo);
-      load8(row + half + 8 * piece, hi);
-      if (!a.rope) return;
-      const float *t = a.rope + (int64_t)min(max(pos, 0), a.n_pos - 1) * D + 8 * piece;
-      float cs[8], sn[8];
+    const int64_t spot = there ? (int64_t)id * a.kv.n_kv * a.kv.page * D + (int64_t)((block * 16) & (a.kv.page - 1)) * D : 0, step = (int64_t)a.kv.page * D;
+    const int w0 = from & 15;                                      // first token's place in the block
+    const int per = tokens * pairs, at_once = KV_THREADS / per, sub = tid / per, in = tid - sub * per;   // per <= 256
+    auto angles = [&](int tok, int piece, float *cs, float *sn) {
+      const float *t = a.rope + (int64_t)min(max(from + tok, 0), a.n_pos - 1) * D + 8 * piece;
       load8(t, cs);
       load8(t + half, sn);
+    };
+    auto turn = [&](const float *cs, const float *sn, float *lo, float *hi) {
+      if (!a.rope) return;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float x = lo[e], y = hi[e];
@@ -374,42 +385,61 @@ __global__ __launch_bounds__(KV_THREADS) void kv_append(KaArgs a) {
         hi[e] = y * cs[e] + x * sn[e];
       }
     };
-    for (int w = blockIdx.y * KV_THREADS + threadIdx.x; w < n_k + n_v + n_q; w += gridDim.y * KV_THREADS) {
-      float lo[8], hi[8];
-      if (w < n_k) {                                               // token fastest: 16 pieces of a column block are contiguous in the page
-        const int tok = w & 15, piece = (w >> 4) % pairs, head = (w >> 4) / pairs, row = block * 16 + tok - base;
-        if (row < 0 || row >= pr.n) continue;
-        rotated((const T *)a.k + (pr.first + row) * a.k_stride + (int64_t)head * D, piece, base + row, lo, hi);
-        T *to = (T *)a.K + spot + (int64_t)head * a.kv.page * D + piece * 128 + tok * 8;
-        store8(to, lo);
-        store8(to + half * 16, hi);
-      } else if (w < n_k + n_v) {
-        const int u = w - n_k, piece = u % (D / 8), side = u / (D / 8) & 1, head = u / (D / 8) / 2, row = block * 16 + side * 8 - base;
-        const T *from = (const T *)a.v + (int64_t)head * D + piece * 8;
-        T *to = (T *)a.V + spot + (int64_t)head * a.kv.page * D + (side * D + piece * 8) * 8;
-        if (row >= 0 && row + 8 <= pr.n) {
-          float v[8][8];
-#pragma unroll
-          for (int t = 0; t < 8; ++t) load8(from + (pr.first + row + t) * a.v_stride, v[t]);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float col[8] = {v[0][e], v[1][e], v[2][e], v[3][e], v[4][e], v[5][e], v[6][e], v[7][e]};
-            store8(to + e * 8, col);
-          }
-        } else {
-          for (int t = 0; t < 8; ++t)
-            if (row + t >= 0 && row + t < pr.n)
-              for (int e = 0; e < 8; ++e) to[e * 8 + t] = from[(pr.first + row + t) * a.v_stride + e];
+    // two heads of a thread on their way; where they go, a head's columns and their partners are to_gap apart
+    auto heads = [&](const T *src, T *to, int n, int64_t to_head, int to_gap, int y, const float *cs, const float *sn) {
+      const int next = gridDim.y * at_once;
+      for (int h = y * at_once + sub; h < n; h += 2 * next) {
+        float lo[2][8], hi[2][8];
+        const bool two = h + next < n;
+        load8(src + (int64_t)h * D, lo[0]);
+        load8(src + (int64_t)h * D + half, hi[0]);
+        if (two) {
+          load8(src + (int64_t)(h + next) * D, lo[1]);
+          load8(src + (int64_t)(h + next) * D + half, hi[1]);
         }
-      } else {
-        const int u = w - n_k - n_v, piece = u % pairs, head = u / pairs % a.n_q, row = block * 16 + u / pairs / a.n_q - base;
-        if (row < 0 || row >= pr.n) continue;
-        rotated((const T *)a.q + (pr.first + row) * a.q_stride + (int64_t)head * D, piece, base + row, lo, hi);
-        T *to = (T *)a.q_out + (pr.first + row) * a.q_out_stride + (int64_t)head * D + 8 * piece;
-        store8(to, lo);
-        store8(to + half, hi);
+        turn(cs, sn, lo[0], hi[0]);
+        store8(to + h * to_head, lo[0]);
+        store8(to + h * to_head + to_gap, hi[0]);
+        if (two) {
+          turn(cs, sn, lo[1], hi[1]);
+          store8(to + (h + next) * to_head, lo[1]);
+          store8(to + (h + next) * to_head + to_gap, hi[1]);
+        }
+      }
+    };
+    float cs[8], sn[8];
+    if (there && sub < at_once) {
+      const int piece = in / tokens, tok = in - piece * tokens;
+      if (a.rope) angles(tok, piece, cs, sn);
+      heads((const T *)a.k + (row0 + tok) * a.k_stride + 8 * piece, (T *)a.K + spot + piece * 128 + (w0 + tok) * 8, a.kv.n_kv, step, half * 16, blockIdx.y, cs, sn);
+    }
+    if (a.q && sub < at_once) {
+      const int tok = in / pairs, piece = in - tok * pairs;
+      if (a.rope) angles(tok, piece, cs, sn);
+      heads((const T *)a.q + (row0 + tok) * a.q_stride + 8 * piece, (T *)a.q_out + (row0 + tok) * a.q_out_stride + 8 * piece, a.n_q, D, half, gridDim.y - 1 - blockIdx.y, cs, sn);
+    }
+    if (there) {
+      const bool left = w0 == 0 && tokens >= 8, right = w0 <= 8 && w0 + tokens == 16;   // all eight of a half are new
+      const int halves = (left ? 1 : 0) + (right ? 1 : 0), loose = tokens - 8 * halves;
+      const int turns = halves * half, all = turns + loose * (D / 8);                   // work of a head
+      for (int w = blockIdx.y * KV_THREADS + tid; w < all * a.kv.n_kv; w += gridDim.y * KV_THREADS) {
+        const int h = w / all, u = w - h * all;
+        if (u < turns) {
+          const int side = halves == 2 ? (u >= half ? 1 : 0) : left ? 0 : 1, i = 2 * (u >= half ? u - half : u);
+          turn8((const T *)a.v + (row0 + side * 8 - w0) * a.v_stride + (int64_t)h * D + i, a.v_stride, (T *)a.V + spot + h * step + (side * D + i) * 8);
+        } else {
+          const int v = u - turns, t = v / (D / 8), piece = v - t * (D / 8), tok = t + (left ? 8 : 0);
+          const T *src = (const T *)a.v + (row0 + tok) * a.v_stride + (int64_t)h * D + piece * 8;
+          T *to = (T *)a.V + spot + h * step + ((w0 + tok) / 8 * D + piece * 8) * 8 + (w0 + tok) % 8;
+          T x[8];
+          *reinterpret_cast<u32x4 *>(x) = *reinterpret_cast<const u32x4 *>(src);
+          if constexpr (sizeof(T) == 4) reinterpret_cast<u32x4 *>(x)[1] = reinterpret_cast<const u32x4 *>(src)[1];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) to[e * 8] = x[e];
+        }
       }
     }
+    if (a.P > 64) __syncthreads();                                 // the prompts' sums are made anew
   }
 }
 
@@ -497,11 +527,14 @@ int parse_kv_append(const parse_kv *kv, int32_t layer, const void *k, int64_t k_
   if (q && (q_stride % per16 != 0 || q_out_stride % per16 != 0)) return PARSE_EALIGN;
   const size_t at = (size_t)layer * kv->n_pages * kv_page_bytes(kv);
   KaArgs a{*kv, (char *)kv->K + at, (char *)kv->V + at, k, v, q, q_out, k_stride, v_stride, q_stride, q_out_stride, tok_offsets, seqs, rope, n_q, rows, P, n_pos};
-  // a prompt's first and last block may be begun only
-  const int64_t blocks = rows / 16 + 2 * (int64_t)std::min(P, rows);
-  const int64_t work = ((int64_t)kv->n_kv * 2 + (q ? n_q : 0)) * kv->d / KV_THREADS + 1;
-  const dim3 grid((uint32_t)std::min<int64_t>(blocks, 65536), (uint32_t)std::min<int64_t>(work, std::max<int64_t>(1, 4096 / blocks)));
-  const size_t lds = (KV_THREADS / 64 + P + 1) * 4;
+  // a prompt's first and last block may be begun only, and every block has a row.  About 4096 workgroups, all with as many heads (of blocks with as many rows as
+  // they have on average)
+  const int64_t blocks = std::min<int64_t>(rows / 16 + 2 * (int64_t)std::min(P, rows), rows);
+  const int per = (int)std::min<int64_t>((rows + blocks - 1) / blocks, 16) * (kv->d / 16), at_once = KV_THREADS / per;
+  const int most = (int)std::max<int64_t>(1, 4096 / blocks), turns = (kv->n_kv + at_once * most - 1) / (at_once * most);
+  // ... four of a block at least where there is room: one has the heads of k, another those of q, all of them v
+  const dim3 grid((uint32_t)std::min<int64_t>(blocks, 65536), (uint32_t)std::max((kv->n_kv + at_once * turns - 1) / (at_once * turns), std::min(most, 4)));
+  const size_t lds = P > 64 ? (KV_THREADS / 64 + P + 1) * 4 : 0;
   if (kv->dtype == PARSE_BF16) kv_append<uint16_t><<<grid, KV_THREADS, lds, (hipStream_t)stream>>>(a);
   else kv_append<float><<<grid, KV_THREADS, lds, (hipStream_t)stream>>>(a);
   PARSE_LAUNCH_CHECK();
