@@ -1,4 +1,6 @@
 // Causal attention of the new tokens of a batch of prompts over the paged cache (parse_attend_prefill).
+#include <algorithm>
+
 #include "attend.hpp"
 
 namespace parse {
@@ -11,20 +13,36 @@ struct ApArgs {
   float *lse;
   const int32_t *tok_offsets, *seqs;
   int64_t q_stride, out_stride;
-  int n_q, group, rows, P, tiles, window, sinks;
+  int n_q, group, rows, P, window, sinks;
+  int splits;                                        // workgroups that share the tokens of a tile of rows
+  float *part;                                       // [tile of rows and kv head][split] of AP_ROWS * (d + 2): sums, maxima, totals
   float scale, lag;                                  // |scale| times log2(e); AT_LAG in products of q and k
   uint32_t q_sign;
 };
 
+constexpr int AP_WAVES = 4, AP_ROWS = AP_WAVES * 32, AP_TILE = 32;
+constexpr int AP_LEAST = 8;                          // tiles of tokens that a split has at least
+constexpr int AP_GROUPS = 512;                       // workgroups that fill the card, two a compute unit
+
+// The tiles of tokens [first, last) that a workgroup has of the `count` that its rows see, and how many share them
+struct ApShare {
+  int first, last, parts;
+};
+__device__ __forceinline__ ApShare ap_share(int count, int splits, int split) {
+  const int each = max((count + splits - 1) / splits, AP_LEAST), parts = max((count + each - 1) / each, 1);
+  return ApShare{min(split * each, count), min((split + 1) * each, count), parts};
+}
 // tiles of rows of a prompt
 __device__ __forceinline__ int ap_tiles(int n, int group, int tile) { return (int)(((int64_t)n * group + tile - 1) / tile); }
 
 // A workgroup has NW * 32 rows of one kv head: row r of a prompt is head r % group of token r / group, so that shared
-// heads read a tile of K and V once.  Tiles of TK tokens are staged in LDS as they stand in the pages, ST buffers deep.  Both
+// heads read a tile of K and V once.  Tiles of TK tokens are staged in LDS as they stand in the pages, one while the one before it is worked on.  Both
 // products have the cache's side as operand A and the rows as columns: a lane holds weights of one row only, the softmax needs
 // one exchange between lane halves, and what comes out of the first product is what the second takes.
-template <class T, int DT, int NW, int TK, int ST>
-__global__ __launch_bounds__(NW * 64) void attend_prefill(ApArgs a) {
+template <int DT>
+__global__ __launch_bounds__(AP_WAVES * 64) void attend_prefill_f32(ApArgs a) {
+  typedef float T;
+  constexpr int NW = AP_WAVES, TK = AP_TILE, ST = 2;
   constexpr int D = DT * 32, KB = D / 16, TB = TK / 16, TS = TK / 32, TM = NW * 32, THREADS = NW * 64;
   constexpr int BLOCK = 16 * D * (int)sizeof(T);                   // bytes of sixteen tokens of K, and of V
   constexpr int STAGE = 2 * TB * BLOCK, PIECES = STAGE / 1024, LOADS = PIECES / NW;
@@ -42,6 +60,8 @@ __global__ __launch_bounds__(NW * 64) void attend_prefill(ApArgs a) {
   const int r_end = n_rows * group, base = len - n_rows;
   const int i0 = base + r0 / group, i1 = base + (min(r0 + TM, r_end) - 1) / group;
   const KvSpan span = i1 < 0 ? KvSpan{0, 0, 0} : kv_span(max(i0, 0), i1, a.window, a.sinks, TK);
+  const ApShare share = ap_share(span.count, a.splits, blockIdx.y);
+  if ((int)blockIdx.y >= share.parts) return;
 
   // the pages of a tile's blocks of sixteen tokens, -1 for none; asked for a tile before they are used
   const int page_bits = 31 - __builtin_clz(a.kv.page);
@@ -70,8 +90,8 @@ __global__ __launch_bounds__(NW * 64) void attend_prefill(ApArgs a) {
     }
   };
   Ids now{}, next{}, later{};                                      // of tiles u, u + 1, u + 2
-  if (span.count > 0) now = ids_of(0);
-  if (span.count > 1) next = ids_of(1);
+  if (share.first < share.last) now = ids_of(share.first);
+  if (share.first + 1 < share.last) next = ids_of(share.first + 1);
 
   // this lane's row, and the positions of the wavefront's rows
   const int r = r0 + wave * 32 + n, token = min(r, r_end - 1) / group, head = kvh * group + (min(r, r_end - 1) - token * group);
@@ -87,8 +107,8 @@ __global__ __launch_bounds__(NW * 64) void attend_prefill(ApArgs a) {
   }
   // q comes first: whoever waits for a tile has it
   asm volatile("" ::: "memory");
-  if (span.count > 0) stage(0, now, 0);
-  if (ST == 3 && span.count > 1) stage(1, next, 1);
+  if (share.first < share.last) stage(share.first, now, 0);
+  if (ST == 3 && share.first + 1 < share.last) stage(share.first + 1, next, 1);
   float m = -INFINITY, l = 0.f;
   f32x16 o[DT];
 #pragma unroll
@@ -99,13 +119,13 @@ __global__ __launch_bounds__(NW * 64) void attend_prefill(ApArgs a) {
   const int ktok = 16 * (n >> 4) + 8 * ((n >> 2) & 1) + 4 * ((n >> 3) & 1) + (n & 3);
 
   int buf = 0;
-  for (int u = 0; u < span.count; ++u, buf = buf + 1 == ST ? 0 : buf + 1) {
+  for (int u = share.first; u < share.last; ++u, buf = buf + 1 == ST ? 0 : buf + 1) {
     const int t0 = span.at(u) * TK;
-    if (u + 2 < span.count) later = ids_of(u + 2);
-    if (ST == 3 && u + 1 < span.count) wait_vm<LOADS>(); else wait_vm<0>();
+    if (u + 2 < share.last) later = ids_of(u + 2);
+    if (ST == 3 && u + 1 < share.last) wait_vm<LOADS>(); else wait_vm<0>();
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     wg_barrier();                                                  // this tile has landed for everybody, the one before it is read by everybody
-    if (u + ST - 1 < span.count) stage(u + ST - 1, ST == 3 ? later : next, buf == 0 ? ST - 1 : buf - 1);
+    if (u + ST - 1 < share.last) stage(u + ST - 1, ST == 3 ? later : next, buf == 0 ? ST - 1 : buf - 1);
     const Ids ids = now;
     now = next; next = later;
     if (idle || t0 > wi1 || (t0 + TK <= wlo && t0 >= a.sinks)) continue;
@@ -204,6 +224,17 @@ __global__ __launch_bounds__(NW * 64) void attend_prefill(ApArgs a) {
   }
   if (idle || r >= r_end) return;
   l = lane_sum<32>(l);
+  const int row = wave * 32 + n;                                   // of the tile
+  if (share.parts > 1) {
+    float *part = a.part + ((int64_t)blockIdx.x * a.splits + blockIdx.y) * AP_ROWS * (D + 2);
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        *reinterpret_cast<f32x4 *>(part + row * D + 32 * d + 8 * c + 4 * half) = f32x4{o[d][4 * c], o[d][4 * c + 1], o[d][4 * c + 2], o[d][4 * c + 3]};
+    if (half == 0) { part[AP_ROWS * D + row] = m; part[AP_ROWS * (D + 1) + row] = l; }
+    return;
+  }
   const float by = l == 0.f ? 0.f : 1.f / l;
   T *out = reinterpret_cast<T *>(a.out) + (int64_t)(row0 + token) * a.out_stride + (int64_t)head * D;
 #pragma unroll
@@ -220,7 +251,6 @@ __global__ __launch_bounds__(NW * 64) void attend_prefill(ApArgs a) {
 // tile j and V of tile j - 2 (at the ends a tile that is there stands for the one that is not, so that all groups are alike).
 // CAREFUL: infinities and NaN of V in places that some rows of the workgroup see and others do not reach only the former (0 times infinity would
 // reach the others).  Without, something that is not finite comes out where they are met: then nothing is stored and the answer is false.
-constexpr int AP_WAVES = 4, AP_ROWS = AP_WAVES * 32, AP_TILE = 32;
 constexpr int AP_STAGES = 4;                 // tiles of K, and of V, in LDS
 constexpr int ap_lds_bytes(int DT) { return 2 * AP_STAGES * AP_TILE * DT * 32 * 2; }
 
@@ -240,7 +270,9 @@ __device__ __forceinline__ bool ap_rows(const ApArgs &a, const KvItem &f, char *
   const int r_end = n_rows * group, base = len - n_rows;
   const int i0 = base + r0 / group, i1 = base + (min(r0 + TM, r_end) - 1) / group;
   const KvSpan span = i1 < 0 ? KvSpan{0, 0, 0} : kv_span(max(i0, 0), i1, a.window, a.sinks, TK);
-  const int count = span.count, groups = count > 0 ? count + 2 : 0;
+  const ApShare share = ap_share(span.count, a.splits, blockIdx.y);
+  if ((int)blockIdx.y >= share.parts) return true;
+  const int count = share.last - share.first, groups = count > 0 ? count + 2 : 0;   // tiles are numbered from the share's first
 
   const int page_bits = 31 - __builtin_clz(a.kv.page);
   const int64_t page_elems = (int64_t)a.kv.n_kv * a.kv.page * D, head0 = (int64_t)kvh * a.kv.page * D;
@@ -253,7 +285,7 @@ __device__ __forceinline__ bool ap_rows(const ApArgs &a, const KvItem &f, char *
   int next_group = 0, next_slot = of_v ? ST - 2 : 0;
   uint32_t place_lo = 0, place_hi = 0;                             // lane j: bytes from pool to this wavefront's block of group 64 * (next_group / 64) + j
   auto places = [&]() {
-    const int g = next_group + lane, t = span.at(of_v ? max(min(g, groups - 1) - 2, 0) : min(g, count - 1)) * TK + 16 * blk, id = page_at(t);
+    const int g = next_group + lane, t = span.at(share.first + (of_v ? max(min(g, groups - 1) - 2, 0) : min(g, count - 1))) * TK + 16 * blk, id = page_at(t);
     const int64_t at = (int64_t)(ok(id) ? id : 0) * (page_elems * 2) + (t & (a.kv.page - 1)) * (D * 2);
     place_lo = (uint32_t)at;
     place_hi = (uint32_t)(at >> 32);
@@ -262,7 +294,7 @@ __device__ __forceinline__ bool ap_rows(const ApArgs &a, const KvItem &f, char *
   constexpr uint32_t THERE_A = 1, THERE_B = 2, WHOLE = 4;          // pages of its two blocks there; every row of the workgroup sees all of it
   const int hi = kv_window_begin(i1, a.window), wglo = kv_window_begin(i0, a.window);
   auto look = [&](int u) {
-    const int t0 = span.at(min(u + lane, count - 1)) * TK;
+    const int t0 = span.at(share.first + min(u + lane, count - 1)) * TK;
     const bool there_a = ok(page_at(t0)), there_b = ok(page_at(t0 + 16));
     const bool all = there_a & there_b & (t0 + TK - 1 <= i0) & ((t0 >= hi) | (t0 + TK <= a.sinks));
     infos = (uint32_t)t0 | (there_a ? THERE_A : 0u) | (there_b ? THERE_B : 0u) | (all ? WHOLE : 0u);
@@ -477,6 +509,17 @@ __device__ __forceinline__ bool ap_rows(const ApArgs &a, const KvItem &f, char *
   }
   if (idle) return true;
   l = lane_sum<32>(l);
+  if (share.parts > 1) {
+    const int row = wave * 32 + n;                                 // of the tile
+    float *part = a.part + ((int64_t)blockIdx.x * a.splits + blockIdx.y) * TM * (D + 2);
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        *reinterpret_cast<f32x4 *>(part + row * D + 32 * d + 8 * c + 4 * half) = f32x4{o[d][4 * c], o[d][4 * c + 1], o[d][4 * c + 2], o[d][4 * c + 3]};
+    if (half == 0) { part[TM * D + row] = m; part[TM * (D + 1) + row] = l; }
+    return true;
+  }
   const float by = l == 0.f ? 0.f : 1.f / l;
   // the lane halves hold columns 8 c + 0..3 and 8 c + 4..7 of a row: they swap, so that each has eight of them, of every other c
   T *out = reinterpret_cast<T *>(a.out) + (int64_t)(row0 + token) * a.out_stride + (int64_t)head * D + 8 * half;
@@ -505,29 +548,84 @@ __global__ __launch_bounds__(AP_WAVES * 64, DT <= 4 ? 2 : 1) void attend_prefill
   if (!ap_rows<DT, false>(a, f, smem)) ap_rows<DT, true>(a, f, smem);
 }
 
-template <int DT>
-static int ap_launch_bf16(const ApArgs &a, hipStream_t s) {
-  // a prompt's last tile may be begun only: rows / tile + prompts in all
-  const int64_t tiles = ((int64_t)a.rows * a.group) / AP_ROWS + min(a.P, a.rows);
-  if (tiles * a.kv.n_kv > INT32_MAX) return PARSE_ESHAPE;
-  const size_t lds = ap_lds_bytes(DT) + (3 + AP_WAVES + (a.P > 64 ? a.P + 1 : 0)) * 4;
-  PARSE_ALLOW_LDS((attend_prefill_bf16<DT>), 0, lds);
-  attend_prefill_bf16<DT><<<dim3((uint32_t)(tiles * a.kv.n_kv)), AP_WAVES * 64, lds, s>>>(a);
-  PARSE_LAUNCH_CHECK();
-  return PARSE_OK;
+// Joins the parts of a tile of rows; workgroup (x, y) has eight of the rows of tile and kv head x, a wavefront two of them, four columns a lane.
+constexpr int AP_JOIN = 8;
+template <class T>
+__global__ __launch_bounds__(AP_WAVES * 64) void ap_join(ApArgs a) {
+  extern __shared__ int pre[];
+  const int D = a.kv.d, group = a.group, kvh = blockIdx.x % a.kv.n_kv, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const KvItem f = kv_item<AP_WAVES * 64>(a.kv, a.tok_offsets, a.seqs, a.P, a.rows, blockIdx.x / a.kv.n_kv, pre + AP_WAVES, pre,
+                                          [&](const KvRows &r, const KvSeq &) { return ap_tiles(r.n, a.group, AP_ROWS); });
+  if (f.item < 0) return;
+  const int r0 = (ap_tiles(f.n, group, AP_ROWS) - 1 - f.item) * AP_ROWS, r_end = f.n * group, base = f.len - f.n;
+  const int i0 = base + r0 / group, i1 = base + (min(r0 + AP_ROWS, r_end) - 1) / group;
+  const KvSpan span = i1 < 0 ? KvSpan{0, 0, 0} : kv_span(max(i0, 0), i1, a.window, a.sinks, AP_TILE);
+  const int parts = ap_share(span.count, a.splits, 0).parts;
+  if (parts == 1) return;
+  const float *first = a.part + (int64_t)blockIdx.x * a.splits * AP_ROWS * (D + 2);
+  const int64_t next = (int64_t)AP_ROWS * (D + 2);
+  for (int k = wave; k < AP_JOIN; k += AP_WAVES) {
+    const int row = blockIdx.y * AP_JOIN + k, r = r0 + row;
+    if (r >= r_end) return;
+    // lane x: part x; there are 64 at most
+    const float m = lane < parts ? first[lane * next + AP_ROWS * D + row] : -INFINITY, l = lane < parts ? first[lane * next + AP_ROWS * (D + 1) + row] : 0.f;
+    float top = m;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+    const float by = at_exp2((m - finite_or_0(top)) * a.scale), total = wave_sum(lane < parts ? l * by : 0.f);
+    const float over = total == 0.f ? 0.f : 1.f / total;
+    const int token = r / group, head = kvh * group + r - token * group;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    if (4 * lane < D) {
+#pragma unroll 8
+      for (int x = 0; x < parts; ++x)
+        o += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(by), x)) * *reinterpret_cast<const f32x4 *>(first + x * next + row * D + 4 * lane);
+      Op<T>::store4(reinterpret_cast<T *>(a.out) + (int64_t)(f.first + token) * a.out_stride + (int64_t)head * D + 4 * lane, o[0] * over, o[1] * over, o[2] * over,
+                    o[3] * over);
+    }
+    if (a.lse && lane == 0) a.lse[(int64_t)(f.first + token) * a.n_q + head] = (finite_or_0(top) * a.scale + log2f(total)) * 0.6931471805599453f;
+  }
 }
 
-template <class T, int DT, int NW, int TK, int ST>
-static int ap_launch(const ApArgs &a, hipStream_t s) {
-  // a prompt's last tile may be begun only: rows / tile + prompts in all
-  const int64_t tiles = ((int64_t)a.rows * a.group) / (NW * 32) + min(a.P, a.rows);
-  if (tiles * a.kv.n_kv > INT32_MAX) return PARSE_ESHAPE;
-  const size_t lds = (size_t)ST * 2 * TK * DT * 32 * sizeof(T) + (NW + a.P + 1) * 4;
-  PARSE_ALLOW_LDS((attend_prefill<T, DT, NW, TK, ST>), 0, lds);
-  attend_prefill<T, DT, NW, TK, ST><<<dim3((uint32_t)(tiles * a.kv.n_kv)), NW * 64, lds, s>>>(a);
+// tiles of rows, times kv heads: a prompt's last tile may be begun only, rows / tile + prompts in all
+static int64_t ap_items(const parse_kv *kv, int n_q, int rows, int P) {
+  return ((int64_t)rows * (n_q / kv->n_kv) / AP_ROWS + std::min(P, rows)) * kv->n_kv;
+}
+// Few rows over caches that may be long: the tokens are cut, so that the workgroups fill the card.  Known are the tiles and how much the table can hold.
+static int ap_splits(const parse_kv *kv, int n_q, int rows, int P) {
+  const int64_t items = ap_items(kv, n_q, rows, P), tiles = (int64_t)kv->max_pages * kv->page / AP_TILE;
+  if (items * 2 > AP_GROUPS || tiles < 2 * AP_LEAST) return 1;
+  return (int)std::min<int64_t>({AP_GROUPS / items, tiles / AP_LEAST, 64});
+}
+static size_t ap_bytes(const parse_kv *kv, int n_q, int rows, int P) {
+  const int splits = ap_splits(kv, n_q, rows, P);
+  return splits == 1 ? 0 : (size_t)ap_items(kv, n_q, rows, P) * splits * AP_ROWS * (kv->d + 2) * 4;
+}
+
+template <class T, class K>
+static int ap_launch(const ApArgs &a, K kernel, size_t lds, hipStream_t s) {
+  const int64_t items = ap_items(&a.kv, a.n_q, a.rows, a.P);
+  if (items > INT32_MAX) return PARSE_ESHAPE;
+  const size_t scan = (AP_WAVES + (a.P > 64 ? a.P + 1 : 0)) * 4;
+  lds += scan;
+  PARSE_ALLOW_LDS(kernel, 0, lds);
+  kernel<<<dim3((uint32_t)items, a.splits), AP_WAVES * 64, lds, s>>>(a);
   PARSE_LAUNCH_CHECK();
+  if (a.splits > 1) {
+    ap_join<T><<<dim3((uint32_t)items, AP_ROWS / AP_JOIN), AP_WAVES * 64, scan, s>>>(a);
+    PARSE_LAUNCH_CHECK();
+  }
   return PARSE_OK;
 }
+template <int DT>
+static int ap_launch_bf16(const ApArgs &a, hipStream_t s) {
+  return ap_launch<uint16_t>(a, attend_prefill_bf16<DT>, ap_lds_bytes(DT) + 3 * 4, s);
+}
+template <int DT>
+static int ap_launch_f32(const ApArgs &a, hipStream_t s) {
+  return ap_launch<float>(a, attend_prefill_f32<DT>, (size_t)2 * 2 * AP_TILE * DT * 32 * 4, s);
+}
+
 static int ap_bf16(const ApArgs &a, hipStream_t s) {
   switch (a.kv.d / 32) {
     case 1: return ap_launch_bf16<1>(a, s);
@@ -542,14 +640,14 @@ static int ap_bf16(const ApArgs &a, hipStream_t s) {
 }
 static int ap_f32(const ApArgs &a, hipStream_t s) {
   switch (a.kv.d / 32) {
-    case 1: return ap_launch<float, 1, 4, 32, 2>(a, s);
-    case 2: return ap_launch<float, 2, 4, 32, 2>(a, s);
-    case 3: return ap_launch<float, 3, 4, 32, 2>(a, s);
-    case 4: return ap_launch<float, 4, 4, 32, 2>(a, s);
-    case 5: return ap_launch<float, 5, 4, 32, 2>(a, s);
-    case 6: return ap_launch<float, 6, 4, 32, 2>(a, s);
-    case 7: return ap_launch<float, 7, 4, 32, 2>(a, s);
-    default: return ap_launch<float, 8, 4, 32, 2>(a, s);
+    case 1: return ap_launch_f32<1>(a, s);
+    case 2: return ap_launch_f32<2>(a, s);
+    case 3: return ap_launch_f32<3>(a, s);
+    case 4: return ap_launch_f32<4>(a, s);
+    case 5: return ap_launch_f32<5>(a, s);
+    case 6: return ap_launch_f32<6>(a, s);
+    case 7: return ap_launch_f32<7>(a, s);
+    default: return ap_launch_f32<8>(a, s);
   }
 }
 
@@ -559,18 +657,20 @@ extern "C" {
 
 size_t parse_attend_prefill_workspace_bytes(const parse_kv *kv, int32_t n_q, int32_t rows, int32_t P) {
   if (parse::check_kv(kv, false) != PARSE_OK || n_q <= 0 || n_q % kv->n_kv != 0 || rows <= 0 || P <= 0) return 0;
-  return 0;
+  return parse::ap_bytes(kv, n_q, rows, P);
 }
 
 int parse_attend_prefill(const parse_kv *kv, int32_t layer, const void *q, int64_t q_stride, int32_t n_q, int32_t rows, const int32_t *tok_offsets,
                          const int32_t *seqs, int32_t P, float scale, int32_t window, int32_t sinks, void *out, int64_t out_stride, float *lse,
                          void *workspace, size_t workspace_bytes, parse_stream stream) {
   using namespace parse;
-  (void)workspace; (void)workspace_bytes;
   const int st = check_attend(kv, layer, q, q_stride, n_q, rows, tok_offsets, seqs, scale, window, sinks, out, out_stride, lse);
   if (st != PARSE_OK) return st;
   if (P <= 0) return PARSE_EINVAL;
   if ((int64_t)rows * (n_q / kv->n_kv) > KV_MAXROWS || P > KV_MAXSEQ || (!seqs && P > kv->n_seqs) || (!tok_offsets && rows != P)) return PARSE_ESHAPE;
+  const size_t need = ap_bytes(kv, n_q, rows, P);
+  if (need && (!workspace || workspace_bytes < need)) return PARSE_EWORKSPACE;
+  if (need && !aligned16(workspace)) return PARSE_EALIGN;
   const size_t at = (size_t)layer * kv->n_pages * kv->n_kv * kv->page * kv->d * elem_size(kv->dtype);
   ApArgs a{};
   a.kv = *kv;
@@ -578,6 +678,8 @@ int parse_attend_prefill(const parse_kv *kv, int32_t layer, const void *q, int64
   a.q = q; a.out = out; a.lse = lse; a.tok_offsets = tok_offsets; a.seqs = seqs;
   a.q_stride = q_stride; a.out_stride = out_stride;
   a.n_q = n_q; a.group = n_q / kv->n_kv; a.rows = rows; a.P = P; a.window = window; a.sinks = sinks;
+  a.splits = ap_splits(kv, n_q, rows, P);
+  a.part = (float *)workspace;
   at_scale(scale, a.scale, a.lag, a.q_sign);
   return kv->dtype == PARSE_BF16 ? ap_bf16(a, (hipStream_t)stream) : ap_f32(a, (hipStream_t)stream);
 }

@@ -310,6 +310,32 @@ def test_prefill_few_rows_over_a_long_cache():
     run_prefill(Case("fp32", 1, 32, 16, [3000], seed=17), 2, [9], 2500, 4)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (700, 40), (256, 4)])
+def test_prefill_splits_of_long_caches(dtype, window, sinks):
+    """Tokens cut over several workgroups: caches of which one, some and all cuts are used, rows that see nothing, many prompts."""
+    assert int(pa.lib().parse_attend_prefill_workspace_bytes(Case(dtype, 2, 64, 16, [2100], seed=1).kv.c(), 4, 40, 1)) > 0
+    run_prefill(Case(dtype, 2, 64, 16, [2100, 250, 20, 700], lambda s, c: s == 3, seed=19), 4, [40, 64, 30, 3], window, sinks)
+    run_prefill(Case(dtype, 1, 160, 64, [1500], seed=20), 1, [130], window, sinks)
+    lens = [1 + 37 * i % 600 for i in range(70)]
+    run_prefill(Case(dtype, 1, 32, 32, lens, seed=21), 2, [1 + i % 2 if n > 1 else 1 for i, n in enumerate(lens)], window, sinks)
+
+
+def test_prefill_split_rows_meet_infinities():
+    """A row tile whose cut is worked on twice (values that are infinite for some of its rows only) beside cuts that are not."""
+    case = Case("bf16", 1, 64, 16, [1000], seed=22)
+    val = case.v[0][990].copy(); val[0, 3] = np.inf
+    case.write(0, 990, v=val)
+    q = rounded(np.random.default_rng(2).standard_normal((20, 2, 64)), "bf16")
+    out = pa.attend_prefill(case.kv, 1, upload(q, "bf16"), i32(np.array([0, 20]))).double().cpu().numpy()
+    for t in range(20):
+        o, _, mag, big = ko.attend_row(q[t], case.k[0], case.v[0], ko.visible(980 + t, case.there[0], 0, 0), 0.125)
+        assert np.array_equal(np.isinf(out[t]), np.isinf(o)) and not np.isnan(out[t]).any(), t
+        fine = np.isfinite(o)
+        tol, _ = bounds("bf16", 64, 1000, np.where(fine, o, 0), np.zeros(2), np.where(np.isfinite(mag), mag, 0), big)
+        assert np.all(np.abs(out[t][fine] - o[fine]) <= tol[fine]), t
+
+
 def test_prefill_of_single_tokens_equals_decode():
     case = Case("bf16", 2, 64, 16, [100, 5, 333], seed=18)
     q = upload(rounded(np.random.default_rng(3).standard_normal((3, 4, 64)), "bf16"), "bf16")
