@@ -101,92 +101,94 @@ static KvWork kv_work(const parse_kv *kv, void *ws) {
   return KvWork{(int32_t *)p, (int2 *)(p + 16), (int32_t *)(p + 16 + round_up((size_t)kv->n_pages * 8, 16))};
 }
 
-// exclusive sum over the threads of a workgroup alone; `sums`: one int per wavefront, LDS.  Returns this thread's, and the total.
-__device__ __forceinline__ int sum_before(int mine, int *sums, int &total) {
+// Exclusive sums over the threads of a workgroup alone, N of them at once; `sums`: [N][wavefronts], LDS that nobody reads any more.  `mine` becomes this thread's.
+template <int N>
+__device__ __forceinline__ void sums_before(int (&mine)[N], int (&total)[N], int (*sums)[KV_ONE / 64]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int inc = wave_scan(mine);
-  __syncthreads();
-  if (lane == 63) sums[wave] = inc;
-  __syncthreads();
-  int base = 0, all = 0;
-  for (int w = 0; w < KV_ONE / 64; ++w) {
-    if (w < wave) base += sums[w];
-    all += sums[w];
+  int inc[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    inc[k] = wave_scan(mine[k]);
+    if (lane == 63) sums[k][wave] = inc[k];
   }
-  total = all;
-  return base + inc - mine;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const int of_wave = wave_scan(lane < KV_ONE / 64 ? sums[k][lane] : 0);
+    total[k] = __builtin_amdgcn_readlane(of_wave, KV_ONE / 64 - 1);
+    mine[k] = inc[k] - mine[k] + (wave ? __builtin_amdgcn_readlane(of_wave, wave - 1) : 0);
+  }
 }
 
-// One workgroup.  A thread has `per` consecutive sequences, then `words` consecutive words of the free pages.
+// One workgroup.  A thread has PER consecutive sequences and `words` consecutive words of the free pages.
+template <int PER>
 __global__ __launch_bounds__(KV_ONE) void kv_reserve(parse_kv kv, const int32_t *__restrict__ n_new, int32_t *__restrict__ served, KvWork ws) {
-  __shared__ int begun[KV_MAXSEQ], last[KV_MAXSEQ], sums[KV_ONE / 64];
-  const int tid = threadIdx.x, per = (kv.n_seqs + KV_ONE - 1) / KV_ONE, page = kv.page, most = kv.max_pages * page;
-  constexpr int PER = KV_MAXSEQ / KV_ONE;
-  int len[PER], more[PER], need[PER], mine = 0, total;
-  // begun[s]: the page that the next token of s goes to, if it has other users
+  __shared__ int begun[PER * KV_ONE], last[PER * KV_ONE], sums[3][KV_ONE / 64], copied;
+  const int tid = threadIdx.x, page = kv.page, most = kv.max_pages * page;
+  const int n_words = (kv.n_pages + 31) / 32, words = (n_words + KV_ONE - 1) / KV_ONE, w0 = tid * words, w1 = min(w0 + words, n_words);
+  int found = 0;
+  for (int w = w0; w < w1; ++w) found += __popc(free_word(kv, w));
+  if (tid == 0) copied = 0;
+  // begun[s]: the page that the next token of s goes to, if it has other users; -2: there is none where one should be
+  int len[PER], more[PER], need[PER], users[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    const int s = tid * per + i;
-    len[i] = more[i] = need[i] = 0;
-    if (i >= per || s >= kv.n_seqs) continue;
+    const int s = tid * PER + i;
+    len[i] = more[i] = need[i] = users[i] = 0;
+    begun[s] = -1;
+    if (s >= kv.n_seqs) continue;
     len[i] = min(max(kv.len[s], 0), most);
     more[i] = max(n_new[s], 0);
     if (more[i] > most - len[i]) more[i] = 0;
-    begun[s] = -1;
     if (more[i] > 0) {
       need[i] = (len[i] + more[i] + page - 1) / page - (len[i] + page - 1) / page;
       if (len[i] % page != 0) {
         const int id = kv.table[(int64_t)s * kv.max_pages + len[i] / page];
-        if (!page_ok(kv, id)) begun[s] = -2;                       // no page where one should be: a new one, nothing to copy
-        else if (kv.refs[id] > 1) begun[s] = id;
+        if (!page_ok(kv, id)) { begun[s] = -2; need[i] += 1; }
+        else if ((users[i] = kv.refs[id]) > 1) begun[s] = id;
       }
     }
   }
   __syncthreads();
   bool copy[PER];
+  int part[3] = {0, found, 0}, total[3];                           // pages that are needed, free pages, copies
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    const int s = tid * per + i;
+    const int s = tid * PER + i, id = begun[s];
     copy[i] = false;
-    if (i >= per || s >= kv.n_seqs) continue;
-    const int id = begun[s];
     if (id >= 0) {                                                 // the users before it have taken their copies
       int before = 0;
       for (int e = 0; e < s; ++e) before += begun[e] == id ? 1 : 0;
-      copy[i] = kv.refs[id] - before > 1;
+      copy[i] = users[i] - before > 1;
+      need[i] += copy[i] ? 1 : 0;
     }
-    need[i] += copy[i] || id == -2 ? 1 : 0;
-    mine += need[i];
+    part[0] += need[i];
+    part[2] += copy[i] ? 1 : 0;
   }
-  int at = sum_before(mine, sums, total);
+  sums_before(part, total, sums);
+  const int free_pages = total[1];
+  int at = part[0], rank = part[1], slot = part[2];
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    const int s = tid * per + i;
-    if (i >= per || s >= kv.n_seqs) continue;
     at += need[i];
-    last[s] = at;                                                  // pages that the sequences up to s take
+    last[tid * PER + i] = at;                                      // pages that the sequences up to this one take
   }
-  __syncthreads();                                                 // users are counted no more: they may change
-  // the free pages in ascending order
-  const int n_words = (kv.n_pages + 31) / 32, words = (n_words + KV_ONE - 1) / KV_ONE;
-  int found = 0, free_pages;
-  for (int w = tid * words; w < min((tid + 1) * words, n_words); ++w) found += __popc(free_word(kv, w));
-  int rank = sum_before(found, sums, free_pages);
-  // what is taken: the needs of the sequences before the first one that does not fit
-  int taken;
-  {
-    int lo = 0, hi = kv.n_seqs;                                    // first s with last[s] > free_pages
+  __syncthreads();                                                 // users and begun pages are looked at no more: they may change
+  auto first_over = [&](int v) {                                   // first s with last[s] > v
+    int lo = 0, hi = kv.n_seqs;
     while (lo < hi) {
       const int mid = (lo + hi) >> 1;
-      if (last[mid] > free_pages) hi = mid; else lo = mid + 1;
+      if (last[mid] > v) hi = mid; else lo = mid + 1;
     }
-    taken = lo > 0 ? last[lo - 1] : 0;
-  }
-  for (int w = tid * words; w < min((tid + 1) * words, n_words) && rank < taken; ++w) {
+    return lo;
+  };
+  // taken are the pages of the sequences before the first one that does not fit: the free ones of the lowest ids
+  const int fit = first_over(free_pages), taken = fit > 0 ? last[fit - 1] : 0;
+  for (int w = w0; w < w1 && rank < taken; ++w) {
     const uint32_t bits = free_word(kv, w);
     uint32_t left = bits;
     while (left && rank < taken) {
-      const int b = __builtin_ctz(left), id = w * 32 + b;
+      const int id = w * 32 + __builtin_ctz(left);
       left &= left - 1;
       ws.ids[rank++] = id;
       kv.refs[id] = 1;
@@ -194,54 +196,48 @@ __global__ __launch_bounds__(KV_ONE) void kv_reserve(parse_kv kv, const int32_t 
     if (left != bits) kv.free_bits[w] = left;
   }
   __syncthreads();
-  int copies = 0;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) copies += copy[i] && last[tid * per + i] <= free_pages ? 1 : 0;
-  int n_copies, slot = sum_before(copies, sums, n_copies);
-  if (tid == 0) *ws.count = n_copies;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    const int s = tid * per + i;
-    if (i >= per || s >= kv.n_seqs) continue;
-    const bool ok = more[i] > 0 && last[s] <= free_pages;
+    const int s = tid * PER + i;
+    if (s >= kv.n_seqs) continue;
+    const bool ok = more[i] > 0 && s < fit;
     if (served) served[s] = ok ? 1 : 0;
     if (!ok) continue;
     kv.len[s] = len[i] + more[i];
+    const int id = begun[s];
     if (copy[i]) {
-      ws.copies[slot++] = int2{begun[s], ws.ids[last[s] - need[i]]};
-      atomicSub(&kv.refs[begun[s]], 1);                            // one user is left at least
+      ws.copies[slot++] = int2{id, ws.ids[last[s] - need[i]]};     // copies of those that fit come first
+      atomicSub(&kv.refs[id], 1);                                  // one user is left at least
+      atomicAdd(&copied, 1);
     }
-    begun[s] = copy[i] || begun[s] == -2 ? len[i] / page : (len[i] + page - 1) / page;   // from now on: column of its first new page
+    begun[s] = copy[i] || id == -2 ? len[i] / page : (len[i] + page - 1) / page;   // from now on: column of its first new page
   }
   __syncthreads();
+  if (tid == 0) *ws.count = copied;
   for (int r = tid; r < taken; r += KV_ONE) {
-    int lo = 0, hi = kv.n_seqs - 1;                                // first s with last[s] > r
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (last[mid] > r) hi = mid; else lo = mid + 1;
-    }
-    const int column = begun[lo] + r - (lo > 0 ? last[lo - 1] : 0);
-    kv.table[(int64_t)lo * kv.max_pages + column] = ws.ids[r];
+    const int s = first_over(r);
+    kv.table[(int64_t)s * kv.max_pages + begun[s] + r - (s > 0 ? last[s - 1] : 0)] = ws.ids[r];
   }
 }
 
 // One workgroup: which pages in use move where.
 __global__ __launch_bounds__(KV_ONE) void kv_compact(parse_kv kv, int32_t *__restrict__ n_live, KvWork ws) {
-  __shared__ int sums[KV_ONE / 64];
+  __shared__ int sums[3][KV_ONE / 64];
   const int tid = threadIdx.x, n_words = (kv.n_pages + 31) / 32, words = (n_words + KV_ONE - 1) / KV_ONE;
   const int w0 = tid * words, w1 = min((tid + 1) * words, n_words);
   auto used_word = [&](int w) { return ~kv.free_bits[w] & page_bits(kv, w); };
   auto below = [&](int w, int n) { return n >= (w + 1) * 32 ? 0xffffffffu : n <= w * 32 ? 0u : (1u << (n - w * 32)) - 1u; };   // bits of the ids under n
-  int used = 0, live;
-  for (int w = w0; w < w1; ++w) used += __popc(used_word(w));
-  sum_before(used, sums, live);
-  int holes = 0, movers = 0, n_holes, n_movers;
+  int used[1] = {0}, all[1], moving[2] = {0, 0}, n_moving[2];       // holes, movers: as many
+  for (int w = w0; w < w1; ++w) used[0] += __popc(used_word(w));
+  sums_before(used, all, sums + 2);
+  const int live = all[0];
   for (int w = w0; w < w1; ++w) {
     const uint32_t under = below(w, live);
-    holes += __popc(free_word(kv, w) & under);
-    movers += __popc(used_word(w) & ~under);
+    moving[0] += __popc(free_word(kv, w) & under);
+    moving[1] += __popc(used_word(w) & ~under);
   }
-  int hole = sum_before(holes, sums, n_holes), mover = sum_before(movers, sums, n_movers);
+  sums_before(moving, n_moving, sums);
+  int hole = moving[0], mover = moving[1];
   for (int w = w0; w < w1; ++w)
     for (uint32_t f = free_word(kv, w) & below(w, live); f; f &= f - 1) ws.copies[hole++].y = w * 32 + __builtin_ctz(f);
   __syncthreads();
@@ -256,7 +252,7 @@ __global__ __launch_bounds__(KV_ONE) void kv_compact(parse_kv kv, int32_t *__res
   }
   for (int w = w0; w < w1; ++w) kv.free_bits[w] = page_bits(kv, w) & ~below(w, live);
   if (tid == 0) {
-    *ws.count = n_movers;
+    *ws.count = n_moving[1];
     ws.count[1] = live;
     if (n_live) *n_live = live;
   }
@@ -490,7 +486,8 @@ int parse_kv_reserve(const parse_kv *kv, const int32_t *n_new, int32_t *served, 
   if (!workspace || workspace_bytes < kv_work_bytes(kv)) return PARSE_EWORKSPACE;
   if (!aligned4(n_new) || !aligned4(served) || !aligned16(workspace)) return PARSE_EALIGN;
   const KvWork ws = kv_work(kv, workspace);
-  kv_reserve<<<dim3(1), KV_ONE, 0, (hipStream_t)stream>>>(*kv, n_new, served, ws);
+  if (kv->n_seqs <= KV_ONE) kv_reserve<1><<<dim3(1), KV_ONE, 0, (hipStream_t)stream>>>(*kv, n_new, served, ws);
+  else kv_reserve<KV_MAXSEQ / KV_ONE><<<dim3(1), KV_ONE, 0, (hipStream_t)stream>>>(*kv, n_new, served, ws);
   PARSE_LAUNCH_CHECK();
   kv_copy<false><<<dim3(2048), KV_THREADS, 0, (hipStream_t)stream>>>(*kv, ws, kv_page_bytes(kv));
   PARSE_LAUNCH_CHECK();
