@@ -606,3 +606,17 @@ def test_long_cache_past_32_bits():
     kv.free_bits.fill_(-1); kv.free_bits[-1] = 2 ** 31 - 1
     assert int(pa.kv_compact(kv)) == 1
     assert torch.equal(kv.K[1, 0], kv.K[1, n_pages - 1]) and int(kv.table[1, 0]) == 0
+
+
+def test_the_example_serves_a_block():
+    """Projections, cache and attention together: prompts, samples that share pages, a recorded step; every step's attention against a plain one."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "serve_block.py")
+    spec = importlib.util.spec_from_file_location("serve_block", path)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    r = m.run(hidden=512, heads=8, kv_heads=4, prompts=2, length=70, samples=3, steps=40, groups=8, gs=32, k=4, window=48, sinks=4, check=True)
+    # weights rounded as two halves, the result once (2^-8); the plain form in 32 bits
+    assert r["worst"] <= 2.0 ** -7 and r["steps"] == 40 and bool(torch.isfinite(r["x"].float()).all())
+    assert r["lengths"] == [0, 0] + [110] * 3 + [73] * 3
