@@ -552,7 +552,8 @@ int parse_kv_append(const parse_kv *kv, int32_t layer, const void *k, int64_t k_
  *     o = sum_j softmax_j(scale * q . k_j) v_j,     lse = ln sum_j exp(scale * q . k_j)
  * with k and v of head h / (n_q / n_kv) (shared heads; n_q % n_kv == 0).  What stands in positions that a row does not see has
  * no influence on it, whatever it holds (also infinities and NaN).  A row that sees nothing gives o = 0 and lse = -inf.
- * Sums and the softmax's statistics are held in 32 bits; bf16: the weights are rounded to bf16 for the second product.
+ * Sums and the softmax's statistics are held in 32 bits.  bf16: for the second product a weight is rounded to bf16 (prefill) or multiplied as two bf16
+ * halves (decode, where it costs no time).
  *   q, out        device [rows][n_q][d], rows q_stride / out_stride elements apart, 16-byte aligned; out is not q
  *   lse           device float [rows][n_q] or NULL
  *   window >= 0 (0: none), sinks >= 0 (read only with a window)
