@@ -47,6 +47,12 @@ __device__ __forceinline__ KvRows kv_rows(const int32_t *__restrict__ tok_offset
 __device__ __forceinline__ int kv_window_begin(int i, int window) { return window > 0 ? max(i - window + 1, 0) : 0; }
 __device__ __forceinline__ bool kv_sees(int i, int lo, int sinks, int j) { return (j <= i) & ((j >= lo) | (j < sinks)); }
 
+// ... of positions j0 .. j0 + 7, a bit each
+__device__ __forceinline__ uint32_t kv_first_bits(int n) { return (1u << min(max(n, 0), 8)) - 1u; }
+__device__ __forceinline__ uint32_t kv_sees8(int i, int lo, int sinks, int j0) {
+  return kv_first_bits(i + 1 - j0) & (~kv_first_bits(lo - j0) | kv_first_bits(sinks - j0));
+}
+
 // The positions that rows at [i0, i1] see, in tiles of `tile` tokens: the tiles of the sinks, then those from the first
 // row's window (all, without one) to i1.  Tile number t of them begins at token at(t) * tile.
 struct KvSpan {
@@ -117,6 +123,13 @@ static inline void at_scale(float given, float &scale, float &lag, uint32_t &q_s
   if (scale == 0.f) scale = 1.f;
   lag = fminf(AT_LAG / scale, 3e38f);
 }
+
+// x / by for x < 2^24 and by <= 2^16: x * ceil(2^40 / by) >> 40 (x times what the quotient was rounded up by stays below 2^40)
+struct KvDivisor {
+  uint64_t times;
+};
+static inline KvDivisor kv_divisor(int by) { return KvDivisor{(((uint64_t)1 << 40) + by - 1) / by}; }
+__device__ __forceinline__ int kv_divide(int x, KvDivisor by) { return (int)(((uint64_t)(uint32_t)x * by.times) >> 40); }
 
 // Which prompt an item belongs to, where prompt p has count(rows, sequence) of them, numbered through.
 struct KvItem {

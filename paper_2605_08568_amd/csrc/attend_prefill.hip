@@ -14,6 +14,7 @@ struct ApArgs {
   const int32_t *tok_offsets, *seqs;
   int64_t q_stride, out_stride;
   int n_q, group, rows, P, window, sinks;
+  KvDivisor by_group;
   int splits;                                        // workgroups that share the tokens of a tile of rows
   float *part;                                       // [tile of rows and kv head][split] of AP_ROWS * (d + 2): sums, maxima, totals
   float scale, lag;                                  // |scale| times log2(e); AT_LAG in products of q and k
@@ -21,15 +22,17 @@ struct ApArgs {
 };
 
 constexpr int AP_WAVES = 4, AP_ROWS = AP_WAVES * 32, AP_TILE = 32;
-constexpr int AP_LEAST = 8;                          // tiles of tokens that a split has at least
+// Tiles of tokens that a split has at least: about 8 us of them.  13 rows over 8192 tokens of 8 heads, bf16, 8 / 16 tiles: 33 / 24 us; fp32 tiles take four times as
+// long: over 4000 tokens of 16 heads, 8 / 16 tiles: 58 / 88 us
+__device__ __host__ __forceinline__ int ap_least(int dtype) { return dtype == PARSE_BF16 ? 16 : 4; }
 constexpr int AP_GROUPS = 512;                       // workgroups that fill the card, two a compute unit
 
 // The tiles of tokens [first, last) that a workgroup has of the `count` that its rows see, and how many share them
 struct ApShare {
   int first, last, parts;
 };
-__device__ __forceinline__ ApShare ap_share(int count, int splits, int split) {
-  const int each = max((count + splits - 1) / splits, AP_LEAST), parts = max((count + each - 1) / each, 1);
+__device__ __forceinline__ ApShare ap_share(int count, int splits, int split, int least) {
+  const int each = max((count + splits - 1) / splits, least), parts = max((count + each - 1) / each, 1);
   return ApShare{min(split * each, count), min((split + 1) * each, count), parts};
 }
 // tiles of rows of a prompt
@@ -58,9 +61,9 @@ __global__ __launch_bounds__(AP_WAVES * 64) void attend_prefill_f32(ApArgs a) {
   const int32_t *table = a.kv.table + (int64_t)f.row * a.kv.max_pages;
   const int r0 = (ap_tiles(n_rows, group, TM) - 1 - f.item) * TM;     // the rows that see most come first
   const int r_end = n_rows * group, base = len - n_rows;
-  const int i0 = base + r0 / group, i1 = base + (min(r0 + TM, r_end) - 1) / group;
+  const int i0 = base + kv_divide(r0, a.by_group), i1 = base + kv_divide(min(r0 + TM, r_end) - 1, a.by_group);
   const KvSpan span = i1 < 0 ? KvSpan{0, 0, 0} : kv_span(max(i0, 0), i1, a.window, a.sinks, TK);
-  const ApShare share = ap_share(span.count, a.splits, blockIdx.y);
+  const ApShare share = ap_share(span.count, a.splits, blockIdx.y, ap_least(a.kv.dtype));
   if ((int)blockIdx.y >= share.parts) return;
 
   // the pages of a tile's blocks of sixteen tokens, -1 for none; asked for a tile before they are used
@@ -94,9 +97,9 @@ __global__ __launch_bounds__(AP_WAVES * 64) void attend_prefill_f32(ApArgs a) {
   if (share.first + 1 < share.last) next = ids_of(share.first + 1);
 
   // this lane's row, and the positions of the wavefront's rows
-  const int r = r0 + wave * 32 + n, token = min(r, r_end - 1) / group, head = kvh * group + (min(r, r_end - 1) - token * group);
+  const int r = r0 + wave * 32 + n, token = kv_divide(min(r, r_end - 1), a.by_group), head = kvh * group + (min(r, r_end - 1) - token * group);
   const int i = base + token;
-  const int wi0 = base + min(r0 + wave * 32, r_end - 1) / group, wi1 = base + min(r0 + wave * 32 + 31, r_end - 1) / group;
+  const int wi0 = base + kv_divide(min(r0 + wave * 32, r_end - 1), a.by_group), wi1 = base + kv_divide(min(r0 + wave * 32 + 31, r_end - 1), a.by_group);
   const int lo = kv_window_begin(i, a.window), wlo = kv_window_begin(wi0, a.window), whi = kv_window_begin(wi1, a.window);
   const bool idle = r0 + wave * 32 >= r_end;
   frag qf[KB];
@@ -268,9 +271,9 @@ __device__ __forceinline__ bool ap_rows(const ApArgs &a, const KvItem &f, char *
   const int32_t *table = a.kv.table + (int64_t)f.row * a.kv.max_pages;
   const int r0 = (ap_tiles(n_rows, group, TM) - 1 - f.item) * TM;     // the rows that see most come first
   const int r_end = n_rows * group, base = len - n_rows;
-  const int i0 = base + r0 / group, i1 = base + (min(r0 + TM, r_end) - 1) / group;
+  const int i0 = base + kv_divide(r0, a.by_group), i1 = base + kv_divide(min(r0 + TM, r_end) - 1, a.by_group);
   const KvSpan span = i1 < 0 ? KvSpan{0, 0, 0} : kv_span(max(i0, 0), i1, a.window, a.sinks, TK);
-  const ApShare share = ap_share(span.count, a.splits, blockIdx.y);
+  const ApShare share = ap_share(span.count, a.splits, blockIdx.y, ap_least(a.kv.dtype));
   if ((int)blockIdx.y >= share.parts) return true;
   const int count = share.last - share.first, groups = count > 0 ? count + 2 : 0;   // tiles are numbered from the share's first
 
@@ -315,9 +318,9 @@ __device__ __forceinline__ bool ap_rows(const ApArgs &a, const KvItem &f, char *
   };
 
   // this lane's row, and the positions of the wavefront's rows
-  const int r = r0 + wave * 32 + n, token = min(r, r_end - 1) / group, head = kvh * group + (min(r, r_end - 1) - token * group);
+  const int r = r0 + wave * 32 + n, token = kv_divide(min(r, r_end - 1), a.by_group), head = kvh * group + (min(r, r_end - 1) - token * group);
   const int i = base + token;
-  const int wi0 = base + min(r0 + wave * 32, r_end - 1) / group, wi1 = base + min(r0 + wave * 32 + 31, r_end - 1) / group;
+  const int wi0 = base + kv_divide(min(r0 + wave * 32, r_end - 1), a.by_group), wi1 = base + kv_divide(min(r0 + wave * 32 + 31, r_end - 1), a.by_group);
   const int lo = kv_window_begin(i, a.window), wlo = kv_window_begin(wi0, a.window);
   const bool idle = r0 + wave * 32 >= r_end;
   frag qf[KB];
@@ -419,9 +422,7 @@ __device__ __forceinline__ bool ap_rows(const ApArgs &a, const KvItem &f, char *
     uint32_t most = 0;
     for (int e = tid; e < TILE / 16; e += THREADS) {
       const int side = e / D;                                      // eight tokens
-      uint32_t keep = 0;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) keep |= ((bool)(info & (side < 2 ? THERE_A : THERE_B)) & kv_sees(i1, wglo, a.sinks, t0 + 8 * side + k) ? 1u : 0u) << k;
+      const uint32_t keep = info & (side < 2 ? THERE_A : THERE_B) ? kv_sees8(i1, wglo, a.sinks, t0 + 8 * side) : 0u;
       T *at = reinterpret_cast<T *>(smem + ST * TILE + slot * TILE) + e * 8;
       const frag v = O::finite_only(O::only(O::load(at), keep), most);
       *reinterpret_cast<frag *>(at) = v;
@@ -468,12 +469,10 @@ __device__ __forceinline__ bool ap_rows(const ApArgs &a, const KvItem &f, char *
     if (!(info & WHOLE) && (CAREFUL || t0 + TK > len || (info & (THERE_A | THERE_B)) != (THERE_A | THERE_B))) bad = clean(info);
     if (t0 <= last) {
       if (!(info & WHOLE)) {
-        const bool there_a = info & THERE_A, there_b = info & THERE_B;
+        // register 8 b + e holds token 16 b + 8 half + e
+        const uint32_t bits = (info & THERE_A ? kv_sees8(i, lo, a.sinks, t0 + 8 * half) : 0u) | (info & THERE_B ? kv_sees8(i, lo, a.sinks, t0 + 16 + 8 * half) << 8 : 0u);
 #pragma unroll
-        for (int x = 0; x < 16; ++x) {                             // register 8 b + e holds token 16 b + 8 half + e
-          const bool sees = (x < 8 ? there_a : there_b) & kv_sees(i, lo, a.sinks, t0 + 16 * (x / 8) + 8 * half + x % 8);
-          sc[x] = sees ? sc[x] : -INFINITY;
-        }
+        for (int x = 0; x < 16; ++x) sc[x] = bits & (1u << x) ? sc[x] : -INFINITY;
       }
       lag(sc);
       read_v();
@@ -548,8 +547,8 @@ __global__ __launch_bounds__(AP_WAVES * 64, DT <= 4 ? 2 : 1) void attend_prefill
   if (!ap_rows<DT, false>(a, f, smem)) ap_rows<DT, true>(a, f, smem);
 }
 
-// Joins the parts of a tile of rows; workgroup (x, y) has eight of the rows of tile and kv head x, a wavefront two of them, four columns a lane.
-constexpr int AP_JOIN = 8;
+// Joins the parts of a tile of rows; workgroup (x, y) has four of the rows of tile and kv head x, a wavefront one of them, four columns a lane.
+constexpr int AP_JOIN = AP_WAVES;
 template <class T>
 __global__ __launch_bounds__(AP_WAVES * 64) void ap_join(ApArgs a) {
   extern __shared__ int pre[];
@@ -558,14 +557,14 @@ __global__ __launch_bounds__(AP_WAVES * 64) void ap_join(ApArgs a) {
                                           [&](const KvRows &r, const KvSeq &) { return ap_tiles(r.n, a.group, AP_ROWS); });
   if (f.item < 0) return;
   const int r0 = (ap_tiles(f.n, group, AP_ROWS) - 1 - f.item) * AP_ROWS, r_end = f.n * group, base = f.len - f.n;
-  const int i0 = base + r0 / group, i1 = base + (min(r0 + AP_ROWS, r_end) - 1) / group;
+  const int i0 = base + kv_divide(r0, a.by_group), i1 = base + kv_divide(min(r0 + AP_ROWS, r_end) - 1, a.by_group);
   const KvSpan span = i1 < 0 ? KvSpan{0, 0, 0} : kv_span(max(i0, 0), i1, a.window, a.sinks, AP_TILE);
-  const int parts = ap_share(span.count, a.splits, 0).parts;
+  const int parts = ap_share(span.count, a.splits, 0, ap_least(a.kv.dtype)).parts;
   if (parts == 1) return;
   const float *first = a.part + (int64_t)blockIdx.x * a.splits * AP_ROWS * (D + 2);
   const int64_t next = (int64_t)AP_ROWS * (D + 2);
-  for (int k = wave; k < AP_JOIN; k += AP_WAVES) {
-    const int row = blockIdx.y * AP_JOIN + k, r = r0 + row;
+  {
+    const int row = blockIdx.y * AP_JOIN + wave, r = r0 + row;
     if (r >= r_end) return;
     // lane x: part x; there are 64 at most
     const float m = lane < parts ? first[lane * next + AP_ROWS * D + row] : -INFINITY, l = lane < parts ? first[lane * next + AP_ROWS * (D + 1) + row] : 0.f;
@@ -574,10 +573,10 @@ __global__ __launch_bounds__(AP_WAVES * 64) void ap_join(ApArgs a) {
     for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
     const float by = at_exp2((m - finite_or_0(top)) * a.scale), total = wave_sum(lane < parts ? l * by : 0.f);
     const float over = total == 0.f ? 0.f : 1.f / total;
-    const int token = r / group, head = kvh * group + r - token * group;
+    const int token = kv_divide(r, a.by_group), head = kvh * group + r - token * group;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     if (4 * lane < D) {
-#pragma unroll 8
+#pragma unroll 16
       for (int x = 0; x < parts; ++x)
         o += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(by), x)) * *reinterpret_cast<const f32x4 *>(first + x * next + row * D + 4 * lane);
       Op<T>::store4(reinterpret_cast<T *>(a.out) + (int64_t)(f.first + token) * a.out_stride + (int64_t)head * D + 4 * lane, o[0] * over, o[1] * over, o[2] * over,
@@ -594,8 +593,9 @@ static int64_t ap_items(const parse_kv *kv, int n_q, int rows, int P) {
 // Few rows over caches that may be long: the tokens are cut, so that the workgroups fill the card.  Known are the tiles and how much the table can hold.
 static int ap_splits(const parse_kv *kv, int n_q, int rows, int P) {
   const int64_t items = ap_items(kv, n_q, rows, P), tiles = (int64_t)kv->max_pages * kv->page / AP_TILE;
-  if (items * 2 > AP_GROUPS || tiles < 2 * AP_LEAST) return 1;
-  return (int)std::min<int64_t>({AP_GROUPS / items, tiles / AP_LEAST, 64});
+  const int least = ap_least(kv->dtype);
+  if (items * 2 > AP_GROUPS || tiles < 2 * least) return 1;
+  return (int)std::min<int64_t>({AP_GROUPS / items, tiles / least, 64});
 }
 static size_t ap_bytes(const parse_kv *kv, int n_q, int rows, int P) {
   const int splits = ap_splits(kv, n_q, rows, P);
@@ -678,6 +678,7 @@ int parse_attend_prefill(const parse_kv *kv, int32_t layer, const void *q, int64
   a.q = q; a.out = out; a.lse = lse; a.tok_offsets = tok_offsets; a.seqs = seqs;
   a.q_stride = q_stride; a.out_stride = out_stride;
   a.n_q = n_q; a.group = n_q / kv->n_kv; a.rows = rows; a.P = P; a.window = window; a.sinks = sinks;
+  a.by_group = kv_divisor(a.group);
   a.splits = ap_splits(kv, n_q, rows, P);
   a.part = (float *)workspace;
   at_scale(scale, a.scale, a.lag, a.q_sign);
