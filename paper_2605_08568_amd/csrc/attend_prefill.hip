@@ -38,10 +38,12 @@ __device__ __forceinline__ ApShare ap_share(int count, int splits, int split, in
 // tiles of rows of a prompt
 __device__ __forceinline__ int ap_tiles(int n, int group, int tile) { return (int)(((int64_t)n * group + tile - 1) / tile); }
 
-// A workgroup has NW * 32 rows of one kv head: row r of a prompt is head r % group of token r / group, so that shared
-// heads read a tile of K and V once.  Tiles of TK tokens are staged in LDS as they stand in the pages, one while the one before it is worked on.  Both
-// products have the cache's side as operand A and the rows as columns: a lane holds weights of one row only, the softmax needs
-// one exchange between lane halves, and what comes out of the first product is what the second takes.
+// fp32.  A workgroup has 128 rows of one kv head: row r of a prompt is head r % group of token r / group, so that shared heads read a tile of K and V once.
+// Tiles of 32 tokens are staged in LDS as they stand in the pages, one while the one before it is worked on.  Both products have the cache's side as
+// operand A and the rows as columns: a lane holds weights of one row only, the softmax needs one exchange between lane halves, and what comes out of
+// the first product is what the second takes (K's rows are read in the order that makes it so).
+// Bound: the fp32 matrix instructions, 64 cycles each, 32 a tile and product at 64 columns: 1024 tokens of 16 heads of 128 44 TFLOP/s of 154 (one wavefront a SIMD:
+// nothing covers its waits), small batches by latency: 4 x 64 tokens of 16 heads of 64 11.5 us, of which two tiles are 4 and what comes before the first 4.
 template <int DT>
 __global__ __launch_bounds__(AP_WAVES * 64) void attend_prefill_f32(ApArgs a) {
   typedef float T;
@@ -248,10 +250,15 @@ __global__ __launch_bounds__(AP_WAVES * 64) void attend_prefill_f32(ApArgs a) {
   if (a.lse && half == 0) a.lse[(int64_t)(row0 + token) * a.n_q + head] = (finite_or_0(m) * a.scale + log2f(l)) * 0.6931471805599453f;
 }
 
-// The same for bf16, with the products of one tile under the softmax of the tile before it: in an iteration a wavefront has the
+// bf16: the same, with the products of one tile under the softmax of the tile before it: in an iteration a wavefront has the
 // scores of tile u and the operands of K of tile u + 1 in registers, multiplies the latter between the exponentials of the former, and reads the
 // operands of K of tile u + 2 between the products with V of tile u.  K is staged two tiles ahead of V; group j of loads is K of
 // tile j and V of tile j - 2 (at the ends a tile that is there stands for the one that is not, so that all groups are alike).
+// Of a tile (16 matrix instructions of 32 cycles a wavefront) the softmax takes 45 vector instructions and 16 exponentials, about as long; scalar work was a hundred
+// instructions more before the places of 64 tiles were worked out at once (648 -> 574 us below).  Two wavefronts a SIMD, 128 rows a workgroup and two of them
+// a unit: with 256 rows the eight wavefronts of a unit wait for each other at every tile (650 us and, 8 x 512 tokens, 81 against 607 and 63).
+// Bound: large calls by power (one prompt of 8192 tokens, 32 heads over 8: 519 to 560 us = 0.98 to 1.06 PFLOP/s at 1.67 GHz; with zeros for data 394 us at the full clock; a large
+// library product reaches 1.28), small ones by what a workgroup waits for before its first tile, 4 us: lengths, table, K (8 x 512 tokens of 32 heads 45 us for 135 MB).
 // CAREFUL: infinities and NaN of V in places that some rows of the workgroup see and others do not reach only the former (0 times infinity would
 // reach the others).  Without, something that is not finite comes out where they are met: then nothing is stored and the answer is false.
 constexpr int AP_STAGES = 4;                 // tiles of K, and of V, in LDS
