@@ -223,6 +223,16 @@ def test_decode_splits(lens):
     run_decode(Case("bf16", 1, 32, 64, lens, seed=len(lens)), 2)
 
 
+@pytest.mark.parametrize("dtype,kv,d", [("bf16", 32, 32), ("fp32", 16, 64), ("bf16", 64, 128)])
+@pytest.mark.parametrize("rows", [5, 23, 64, 65, 130])
+def test_decode_many_short_rows(dtype, kv, d, rows):
+    """Rows of a step or a few, several to a share: whole ones, ones that a share's end cuts, empty ones between them."""
+    rng = np.random.default_rng(rows)
+    lens = [int(n) for n in rng.choice([0, 1, 17, 31, 32, 33, 64, 90, 150], rows)]
+    lens[0], lens[-1] = max(lens[0], 1), 40
+    run_decode(Case(dtype, kv, d, 32, lens, seed=rows), kv, *((0, 0) if rows % 2 else (50, 4)))
+
+
 def test_decode_large_scores_and_scale():
     """Scores of +-300 in order and against it: the running maximum lags and grows."""
     for order in (1, -1):
