@@ -132,7 +132,7 @@ __device__ __forceinline__ void ad_join(const AdArgs &a, int b, int kvh, int hg,
 // on; a unit has 32 KiB on their way whatever is asked for, so that two workgroups a unit are enough, and more of them only cut the caches finer: 512 / 768 / 1024
 // workgroups, 32 ragged caches of 32 heads 108 / 121 / 114 us, 192 windows 162 / 182 / 175.  Shares are equal in steps, not in rows: a batch of unlike lengths needs no plan.
 // Measured, reads of the cache against 6.1 to 6.4 TB/s of a read-only stream of 2 GiB: 32 caches of 32 to 2048 tokens, 32 heads 5.9 TB/s (96 us), 100003 tokens of 8 heads
-// 5.4 (75 us), 192 windows of 1024 5.6 (142 us), 256 caches of 300 tokens, 8 heads 4.6 (68 us); 40 heads-wide rows of 17 tokens are bound by latency.
+// 5.4 (75 us), 192 windows of 1024 5.6 (142 us), 256 caches of 300 tokens, 8 heads 4.6 (68 us); single short caches by latency (77 tokens 7.3 us).
 template <class T, int DT, bool NT, bool TICKETS>
 __global__ __launch_bounds__(AD_THREADS, DT * sizeof(T) <= 16 ? 2 : 1) void attend_decode(AdArgs a) {
   constexpr int D = DT * 32, KB = D / 32, VB = D / 16;
