@@ -62,6 +62,20 @@ __device__ __forceinline__ AdDeal ad_lanes(const AdArgs &a, AdLane &w) {
   return ad_deal(a, __builtin_amdgcn_readlane(inc, 63));
 }
 
+// Row x is share x, whole, and nothing has to be joined, where no row has many more steps than an equal share would: three more a wavefront take about as long as
+// a join, two where rows are few and none of them begins inside a share.  32 heads over 8, equal shares / rows: 16 caches of 100 to 200 tokens 16.8 / 9.2 us, of 30 to 500 18.1 /
+// 11.8, 64 of 300 to 330 25.0 / 18.3, 64 of 2000 to 2300 99 / 90, 40 windows of 1000 40.9 / 34.8; 4 caches of 510 tokens 10.8 / 11.9, 1 of 250 10.3 / 8.5.
+__device__ __host__ __forceinline__ int ad_slack(int rows) { return rows <= 4 ? 8 : 12; }
+__device__ __forceinline__ bool ad_by_rows(const AdArgs &a, const AdDeal &deal, const AdLane &w) {
+  return a.rows <= a.shares && !__any((int)(threadIdx.x & 63) < a.rows && w.span.count > deal.per + ad_slack(a.rows));
+}
+__device__ __forceinline__ bool ad_by_rows(const AdArgs &a, const AdDeal &deal, const int *pre) {
+  if (a.rows > a.shares) return false;
+  bool longer = false;
+  for (int p = threadIdx.x; p < a.rows; p += AD_THREADS) longer |= pre[p + 1] - pre[p] > deal.per + ad_slack(a.rows);
+  return !__syncthreads_or(longer);
+}
+
 template <bool SHARED>
 __device__ __forceinline__ void ad_part(float *p, float v) {
   if (SHARED) __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -163,9 +177,12 @@ __global__ __launch_bounds__(AD_THREADS, DT * sizeof(T) <= 16 ? 2 : 1) void atte
       if (a.lse && v % D == 0) a.lse[(int64_t)e * a.n_q + h] = -INFINITY;
     }
   }
-  const int64_t begin = (int64_t)share * deal.per;
-  if (begin >= deal.total) return;
-  const int end = (int)min(begin + deal.per, (int64_t)deal.total);
+  const bool by_rows = few ? ad_by_rows(a, deal, w) : ad_by_rows(a, deal, pre);
+  if (by_rows && share >= a.rows) return;
+  const int64_t begin = by_rows ? (few ? __builtin_amdgcn_readlane(w.before, share) : __builtin_amdgcn_readfirstlane(pre[share])) : (int64_t)share * deal.per;
+  const int64_t behind = by_rows ? begin + (few ? __builtin_amdgcn_readlane(w.span.count, share) : __builtin_amdgcn_readfirstlane(pre[share + 1] - pre[share])) : begin + deal.per;
+  const int end = (int)min(behind, (int64_t)deal.total);
+  if (begin >= end) return;
   const int64_t page_elems = (int64_t)a.kv.n_kv * a.kv.page * D, head0 = (int64_t)kvh * a.kv.page * D;
   const int tok = 8 * (n >> 2) + (n & 3);                          // the first instruction's row n: tokens 8 quad + 0..3 of a step come back to a lane
   const int page_bits = 31 - __builtin_clz(a.kv.page);
@@ -358,36 +375,44 @@ __global__ __launch_bounds__(AD_THREADS, DT * sizeof(T) <= 16 ? 2 : 1) void atte
   }
 }
 
-// The parts of a row that more than one share had; workgroup (x, head) has the row that begins in share x and goes on behind it.  The weights of all
+// The parts of a row that more than one share had; workgroup (x, head) has row x or, where there are fewer shares, the row that begins in share x and goes on behind it.  The weights of all
 // parts first, then four columns a thread of every so many parts, none of which waits for another.
 template <class T>
 __global__ __launch_bounds__(AD_THREADS) void attend_join(AdArgs a) {
   extern __shared__ char smem[];
   float *weight = reinterpret_cast<float *>(smem), *sums = weight + AD_GROUPS;       // [parts]; [part group][D] and two numbers a wavefront
-  const int D = a.kv.d, tid = threadIdx.x, x0 = blockIdx.x, head = blockIdx.y, kvh = head / a.group, hg = head % a.group / AD_HEADS, h = head % a.group % AD_HEADS;
+  const int D = a.kv.d, tid = threadIdx.x, head = blockIdx.y, kvh = head / a.group, hg = head % a.group / AD_HEADS, h = head % a.group % AD_HEADS;
   const int zs = (a.group + AD_HEADS - 1) / AD_HEADS;
   int *wave_sums = reinterpret_cast<int *>(sums + AD_THREADS * 4 + 2 * AD_WAVES), *pre = wave_sums + AD_WAVES;
-  int b, before, count;
+  const bool of_row = a.rows < a.shares;
+  int b = blockIdx.x, before, count;
   AdDeal deal;
   if (a.rows <= 64) {
     AdLane w;
     deal = ad_lanes(a, w);
-    const int64_t end = (int64_t)(x0 + 1) * deal.per;              // of the share
-    if (end >= deal.total) return;
-    b = 63 - __builtin_clzll(__ballot((int)(threadIdx.x & 63) < a.rows && w.before < (int)end && w.span.count > 0));
+    if (ad_by_rows(a, deal, w)) return;
+    if (!of_row) {
+      const int64_t end = (int64_t)(blockIdx.x + 1) * deal.per;    // of the share
+      if (end >= deal.total) return;
+      b = 63 - __builtin_clzll(__ballot((int)(threadIdx.x & 63) < a.rows && w.before < (int)end && w.span.count > 0));
+    }
     before = __builtin_amdgcn_readlane(w.before, b);
     count = __builtin_amdgcn_readlane(w.span.count, b);
   } else {
     kv_prefix<AD_THREADS>(a.rows, pre, wave_sums, [&](int p) { return ad_span(a, kv_seq(a.kv, a.seqs, p).len).count; });
     deal = ad_deal(a, pre[a.rows]);
-    const int64_t end = (int64_t)(x0 + 1) * deal.per;
-    if (end >= deal.total) return;
-    b = kv_find(pre, a.rows, (int)end - 1);
+    if (ad_by_rows(a, deal, pre)) return;
+    if (!of_row) {
+      const int64_t end = (int64_t)(blockIdx.x + 1) * deal.per;
+      if (end >= deal.total) return;
+      b = kv_find(pre, a.rows, (int)end - 1);
+    }
     before = pre[b];
     count = pre[b + 1] - before;
   }
-  const int x1 = (before + count - 1) / deal.per, parts = x1 - x0 + 1;
-  if (parts == 1 || before / deal.per != x0) return;
+  if (count == 0) return;
+  const int x0 = before / deal.per, x1 = (before + count - 1) / deal.per, parts = x1 - x0 + 1;
+  if (parts == 1 || (!of_row && x0 != (int)blockIdx.x)) return;
   const float *base = a.part + ((int64_t)kvh * zs + hg) * a.shares * 2 * AD_HEADS * (D + 2);
   auto part_of = [&](int x) { return base + ((int64_t)(x0 + x) * 2 + ((int64_t)(x0 + x) * deal.per <= before ? 1 : 0)) * AD_HEADS * (D + 2); };
   float top = -INFINITY;
@@ -443,6 +468,13 @@ static bool ad_tickets(const parse_kv *kv, int n_q) {
   return weights * kv->d <= 65536 && 2 * weights <= AD_WAVES * AD_HEADS * kv->d;    // ... in the LDS that the sums left
 }
 
+// Whether table and window alone say that every row is a share's (ad_by_rows), whatever the lengths
+static bool ad_sure(const AdArgs &a) {
+  int64_t steps = ((int64_t)a.kv.max_pages * a.kv.page + AD_STEP - 1) / AD_STEP;
+  if (a.window > 0) steps = std::min(steps, ((int64_t)a.window + AD_STEP - 1) / AD_STEP + 1 + ((int64_t)a.sinks + AD_STEP - 1) / AD_STEP);
+  return a.rows <= a.shares && steps <= AD_WAVES + ad_slack(a.rows);
+}
+
 template <class T, int DT, bool NT, bool TICKETS>
 static int ad_launch(const AdArgs &a, hipStream_t s) {
   const int zs = (a.group + AD_HEADS - 1) / AD_HEADS, scan = a.rows > 64 ? a.rows + 1 : 0;
@@ -450,8 +482,8 @@ static int ad_launch(const AdArgs &a, hipStream_t s) {
   PARSE_ALLOW_LDS((attend_decode<T, DT, NT, TICKETS>), 0, lds);
   attend_decode<T, DT, NT, TICKETS><<<dim3(a.shares, a.kv.n_kv, zs), AD_THREADS, lds, s>>>(a);
   PARSE_LAUNCH_CHECK();
-  if (!TICKETS && a.shares > 1) {
-    attend_join<T><<<dim3(a.shares - 1, a.n_q), AD_THREADS, (AD_GROUPS + AD_THREADS * 4 + 3 * AD_WAVES + scan) * 4, s>>>(a);
+  if (!TICKETS && a.shares > 1 && !ad_sure(a)) {
+    attend_join<T><<<dim3(std::min(a.shares - 1, a.rows), a.n_q), AD_THREADS, (AD_GROUPS + AD_THREADS * 4 + 3 * AD_WAVES + scan) * 4, s>>>(a);
     PARSE_LAUNCH_CHECK();
   }
   return PARSE_OK;

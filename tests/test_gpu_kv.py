@@ -233,6 +233,16 @@ def test_decode_many_short_rows(dtype, kv, d, rows):
     run_decode(Case(dtype, kv, d, 32, lens, seed=rows), kv, *((0, 0) if rows % 2 else (50, 4)))
 
 
+@pytest.mark.parametrize("dtype,kv,n_q,d,lens", [
+    ("bf16", 2, 8, 64, [512, 0, 40, 1, 300]), ("bf16", 2, 8, 64, [513, 0, 40, 1, 300]), ("fp32", 2, 8, 64, [384, 1, 5]), ("fp32", 2, 8, 64, [385, 1, 5]),
+    ("bf16", 1, 16, 128, [512, 0, 33, 1, 512]), ("bf16", 1, 16, 128, [0, 513, 33, 1, 512]), ("bf16", 1, 16, 64, [1, 33, 65, 0, 512] * 14),
+    ("bf16", 1, 16, 64, [1, 33, 65, 0, 512] * 13 + [2000]), ("fp32", 1, 32, 32, [1, 2, 33, 0, 64] * 103 + [3000]),
+    ("bf16", 32, 32, 32, [640, 300, 310, 0, 320, 64, 290, 333, 1, 30]), ("bf16", 32, 32, 32, [300, 673, 310, 0, 320, 64, 290, 333, 1, 30])])
+def test_decode_rows_whole_and_cut(dtype, kv, n_q, d, lens):
+    """Batches whose rows are a workgroup's each, and such that have one row too long for it; joins by rows and by shares."""
+    run_decode(Case(dtype, kv, d, 32, lens, seed=len(lens)), n_q)
+
+
 def test_decode_large_scores_and_scale():
     """Scores of +-300 in order and against it: the running maximum lags and grows."""
     for order in (1, -1):
