@@ -42,10 +42,12 @@ __device__ __forceinline__ int ap_tiles(int n, int group, int tile) { return (in
 // Tiles of 32 tokens are staged in LDS as they stand in the pages, one while the one before it is worked on.  Both products have the cache's side as
 // operand A and the rows as columns: a lane holds weights of one row only, the softmax needs one exchange between lane halves, and what comes out of
 // the first product is what the second takes (K's rows are read in the order that makes it so).
-// Bound: the fp32 matrix instructions, 64 cycles each, 32 a tile and product at 64 columns: 1024 tokens of 16 heads of 128 44 TFLOP/s of 154 (one wavefront a SIMD:
-// nothing covers its waits), small batches by latency: 4 x 64 tokens of 16 heads of 64 11.5 us, of which two tiles are 4 and what comes before the first 4.
+// Bound: the fp32 matrix instructions, 64 cycles each, 32 a tile and product at 64 columns: 4 x 897 tokens of 16 heads of 128, window 284, 53 TFLOP/s of 154 (133 us; with the
+// one wavefront a SIMD that the compiler takes if left alone 176, 19 x 124 tokens of 32 heads 103 -> 72; 96 columns 183 -> 230, so only at 128), small batches by latency: 4 x 64 tokens of
+// 16 heads of 64 11.2 us, of which two tiles are 4 and what comes before the first 4.  Not kept: twice and four times as many cuts, for the longest row tiles of a causal prompt (2 x 1805
+// tokens of 16 heads of 64 272 -> 238 and 213 us, 1 x 1024 of 128 101 -> 86 and 84, but 4 x 897 133 -> 165, 2000 of 96 183 -> 197 and 218: parts are written and read again).
 template <int DT>
-__global__ __launch_bounds__(AP_WAVES * 64) void attend_prefill_f32(ApArgs a) {
+__global__ __launch_bounds__(AP_WAVES * 64, DT == 4 ? 2 : 1) void attend_prefill_f32(ApArgs a) {
   typedef float T;
   constexpr int NW = AP_WAVES, TK = AP_TILE, ST = 2;
   constexpr int D = DT * 32, KB = D / 16, TB = TK / 16, TS = TK / 32, TM = NW * 32, THREADS = NW * 64;
