@@ -640,3 +640,34 @@ def test_the_example_serves_a_block():
     # weights rounded as two halves, the result once (2^-8); the plain form in 32 bits
     assert r["worst"] <= 2.0 ** -7 and r["steps"] == 40 and bool(torch.isfinite(r["x"].float()).all())
     assert r["lengths"] == [0, 0] + [110] * 3 + [73] * 3
+
+
+SEEN = [("bf16", 2, 8, 64, [1, 3, 40, 77, 200]), ("fp32", 2, 8, 64, [1, 3, 40, 77, 200]),          # a workgroup a row
+        ("bf16", 32, 32, 32, [33, 1, 64, 90, 17, 150, 40, 31] * 9), ("fp32", 16, 16, 64, [33, 1, 64, 90, 17, 150, 40, 31] * 9),      # a wavefront a row
+        ("bf16", 2, 8, 64, [5000, 7]), ("fp32", 2, 8, 64, [5000, 7]),                              # joined by the workgroup that comes last
+        ("bf16", 1, 16, 128, [5000, 900]), ("bf16", 2, 8, 256, [600, 40])]                         # joined by a second launch; wide heads
+
+
+@pytest.mark.parametrize("dtype,kv,n_q,d,lens", SEEN)
+@pytest.mark.parametrize("window,sinks", [(0, 0), (30, 4)])
+def test_decode_infinities_and_nan_that_are_seen(dtype, kv, n_q, d, lens, window, sinks):
+    """An infinity of V that a row sees comes out as it is, whatever its weight's rounding left; both signs in a column, and NaN, give NaN; the other
+    columns stay finite.  Some of the tokens lie outside the window: those reach nothing."""
+    case = Case(dtype, kv, d, 16, lens, seed=len(lens) + d)
+    for s, n in enumerate(lens):
+        for j, columns in ((n // 3, {3: np.inf, 9: np.inf}), (2 * n // 3, {7: -np.inf, 9: -np.inf}), (n // 2, {5: np.nan}), (n - 1, {11: np.inf, d - 1: -np.inf})):
+            v = case.v[s][j].copy()
+            for c, x in columns.items():
+                v[:, c] = x
+            case.write(s, j, v=v)
+    q = rounded(np.random.default_rng(2).standard_normal((len(lens), n_q, d)), dtype)
+    out, lse = pa.attend_decode(case.kv, 1, upload(q, dtype), window=window, sinks=sinks, with_lse=True)
+    out, lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    for s, n in enumerate(lens):
+        with np.errstate(invalid="ignore"):
+            o, l, mag, big = ko.attend_row(q[s], case.k[s], case.v[s], ko.visible(n - 1, case.there[s], window, sinks), d ** -0.5)
+        assert np.array_equal(np.isnan(out[s]), np.isnan(o)), s
+        assert np.array_equal(np.isinf(out[s]), np.isinf(o)) and np.array_equal(out[s][np.isinf(o)], o[np.isinf(o)]), s
+        fine = np.isfinite(o)
+        tol, ltol = bounds(dtype, d, n, np.where(fine, o, 0), l, np.where(np.isfinite(mag), mag, 0), big)
+        assert np.all(np.abs(out[s][fine] - o[fine]) <= tol[fine]) and np.all(np.abs(lse[s] - l) <= ltol), s
