@@ -43,8 +43,8 @@ __device__ __forceinline__ KvRows kv_rows(const int32_t *__restrict__ tok_offset
 }
 
 // Whether a row sees position j: j <= i and j >= lo or j < sinks, with lo the first position of its window.  Without branches: one
-// select per score.
-__device__ __forceinline__ int kv_window_begin(int i, int window) { return window > 0 ? max(i - window + 1, 0) : 0; }
+// select per score.  i < 0 (a prompt with more rows than its sequence has tokens): a window as long as an int goes would begin below what an int holds
+__device__ __forceinline__ int kv_window_begin(int i, int window) { return window > 0 ? max(max(i, 0) - window + 1, 0) : 0; }
 __device__ __forceinline__ bool kv_sees(int i, int lo, int sinks, int j) { return (j <= i) & ((j >= lo) | (j < sinks)); }
 
 // ... of positions j0 .. j0 + 7, a bit each

@@ -671,3 +671,11 @@ def test_decode_infinities_and_nan_that_are_seen(dtype, kv, n_q, d, lens, window
         fine = np.isfinite(o)
         tol, ltol = bounds(dtype, d, n, np.where(fine, o, 0), l, np.where(np.isfinite(mag), mag, 0), big)
         assert np.all(np.abs(out[s][fine] - o[fine]) <= tol[fine]) and np.all(np.abs(lse[s] - l) <= ltol), s
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("window,sinks", [(2 ** 31 - 1, 0), (2 ** 31 - 1, 4), (2 ** 31 - 12, 0)])
+def test_prefill_rows_before_the_first_token_with_a_window_without_end(dtype, window, sinks):
+    """More rows than tokens: the first rows' positions lie below 0, and their window's begin below what 32 bits hold."""
+    run_prefill(Case(dtype, 2, 64, 16, [10, 33], seed=7), 4, [25, 3], window, sinks)
+    run_prefill(Case(dtype, 1, 64, 16, [700, 5], seed=8), 1, [760, 5], window, sinks)
