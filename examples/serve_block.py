@@ -74,10 +74,11 @@ def run(hidden=4096, heads=32, kv_heads=32, prompts=4, length=512, samples=4, st
     pid, _, _, n_patterns, rep = pa.bucket_patterns(subsets, k)
     packed = [pa.Patterns(k, prompts, *pa.pack_patterns(l, subsets, k, k, rep, n_patterns, prompts)) for l in qkv + [o]]
     q, key, value = pa.lowrank_prefill_multi(qkv, packed[:3], X, off, pid)
-    pa.kv_reserve(cache, i32(lengths + [0] * (seqs - prompts)), workspace=room)
+    placed = torch.empty(prompts, dtype=torch.int32, device=DEV)
+    pa.kv_reserve(cache, i32(lengths + [0] * (seqs - prompts)), workspace=room, seqs_served=placed)
     q, key, value = q.view(rows, heads, d), key.view(rows, kv_heads, d), value.view(rows, kv_heads, d)
-    pa.kv_append(cache, 0, key, value, off, q=q, q_out=q, rope=rope)
-    attn = pa.attend_prefill(cache, 0, q, off)
+    pa.kv_append(cache, 0, key, value, off, placed, q=q, q_out=q, rope=rope)
+    attn = pa.attend_prefill(cache, 0, q, off, placed)
     y = pa.lowrank_forward(pa.PARSE_PREFILL, o, packed[3], attn.view(rows, hidden), off, pid)
 
     # ---- every prompt's samples share its pages; each starts from the prompt's last row and a little noise
@@ -107,12 +108,13 @@ def run(hidden=4096, heads=32, kv_heads=32, prompts=4, length=512, samples=4, st
     out = [torch.empty((n, m), dtype=torch.bfloat16, device=DEV) for m in (hidden, kv_heads * d, kv_heads * d, hidden)]
     turned_q, attn = torch.empty((n, heads, d), dtype=torch.bfloat16, device=DEV), torch.empty((n, heads, d), dtype=torch.bfloat16, device=DEV)
     one, served, seq = i32([0] * prompts + [1] * n), torch.empty(seqs, dtype=torch.int32, device=DEV), i32(children)
+    room_for = torch.empty_like(seq)                               # the samples that got room for their token, -1 for the others: those are passed over
 
     def step():
         pa.lowrank_decode_planned(qkv, x, plan_qkv, out[:3], scratch)
-        pa.kv_reserve(cache, one, served, room)
-        pa.kv_append(cache, 0, out[1].view(n, kv_heads, d), out[2].view(n, kv_heads, d), seqs=seq, q=out[0].view(n, heads, d), q_out=turned_q, rope=rope)
-        pa.attend_decode(cache, 0, turned_q, seq, window=window, sinks=sinks, out=attn, workspace=ws)
+        pa.kv_reserve(cache, one, served, room, seq, room_for)
+        pa.kv_append(cache, 0, out[1].view(n, kv_heads, d), out[2].view(n, kv_heads, d), seqs=room_for, q=out[0].view(n, heads, d), q_out=turned_q, rope=rope)
+        pa.attend_decode(cache, 0, turned_q, room_for, window=window, sinks=sinks, out=attn, workspace=ws)
         pa.lowrank_decode_planned([o], attn.view(n, hidden), plan_o, out[3:], scratch)
         pa.kv_trim(cache, None, window, sinks)
         torch.mul(out[3], 4.0, out=x)

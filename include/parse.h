@@ -508,12 +508,22 @@ int parse_kv_fork(const parse_kv *kv, const int32_t *src, const int32_t *dst, in
  * The sequences are served in the order of their numbers, each as if the calls were made one after another (of
  * several users of a begun page the last one keeps it).  A sequence that would outgrow max_pages, or asks for no token, is
  * left as it is; from the first one that the free pages do not suffice for on, all are.
+ * A sequence that is not served keeps its length, so that its last tokens are the ones it had: a parse_kv_append behind
+ * the call that names it writes its row over a token that it has, in a page that other sequences may share.  What is recorded
+ * behind the call takes its list of sequences from parse_kv_reserve_seqs.
  *   n_new      device int32 [n_seqs] (negative: 0)
  *   served     device int32 [n_seqs] or NULL: 1 where the sequence has its new tokens, else 0
  *   workspace  device, >= parse_kv_workspace_bytes(kv) */
 size_t parse_kv_workspace_bytes(const parse_kv *kv);
 int parse_kv_reserve(const parse_kv *kv, const int32_t *n_new, int32_t *served, void *workspace, size_t workspace_bytes,
                      parse_stream stream);
+
+/* The same, and the list of sequences for the calls behind it: seqs_served[p] = seqs[p] where that sequence has its new
+ * tokens, else -1, which parse_kv_append and the attention calls pass over (no row is stored, o = 0, lse = -inf).
+ *   seqs         device int32 [P], 1 <= P <= 4096, or NULL: p (P <= n_seqs)
+ *   seqs_served  device int32 [P]; may be seqs */
+int parse_kv_reserve_seqs(const parse_kv *kv, const int32_t *n_new, int32_t *served, const int32_t *seqs, int32_t P,
+                          int32_t *seqs_served, void *workspace, size_t workspace_bytes, parse_stream stream);
 
 /* Gives up pages: len[s] becomes min(len[s], max(keep[s], 0)) (keep NULL: lengths stay) and the pages past it are given
  * up; with window > 0 also those that no later token sees, which are the pages whose tokens are all at or past
@@ -529,8 +539,8 @@ int parse_kv_compact(const parse_kv *kv, int32_t *n_live, void *workspace, size_
 
 /* The rows of new tokens on their way from the projections to the attention: k and v into their pages, q and k rotated
  * by their positions on the way.  The tokens of prompt p are the LAST ones of its sequence: rows [tok_offsets[p],
- * tok_offsets[p+1]) stand at positions len - n_p .. len - 1 (parse_kv_reserve has counted them).  A token whose page is
- * missing or that has no position is not stored.
+ * tok_offsets[p+1]) stand at positions len - n_p .. len - 1 (parse_kv_reserve has counted them; a sequence that it did not
+ * serve must not be named, parse_kv_reserve_seqs).  A token whose page is missing or that has no position is not stored.
  *   layer        0 <= layer < n_layers
  *   k, v         device [rows][n_kv][d], rows k_stride / v_stride elements apart (so that they may be slices of one
  *                fused projection), strides and pointers on 16 bytes

@@ -142,7 +142,7 @@ def lib():
     L.parse_kv_workspace_bytes.restype = sz; L.parse_kv_workspace_bytes.argtypes = [kvp]
     L.parse_attend_decode_workspace_bytes.restype = sz; L.parse_attend_decode_workspace_bytes.argtypes = [kvp, i32, i32]
     L.parse_attend_prefill_workspace_bytes.restype = sz; L.parse_attend_prefill_workspace_bytes.argtypes = [kvp, i32, i32, i32]
-    for name, args in [("clear", [vp]), ("fork", [vp, vp, i32, vp]), ("reserve", [vp, vp, vp, sz, vp]), ("trim", [vp, i32, i32, vp]),
+    for name, args in [("clear", [vp]), ("fork", [vp, vp, i32, vp]), ("reserve", [vp, vp, vp, sz, vp]), ("reserve_seqs", [vp, vp, vp, i32, vp, vp, sz, vp]), ("trim", [vp, i32, i32, vp]),
                        ("compact", [vp, vp, sz, vp]),
                        ("append", [i32, vp, i64, vp, i64, vp, i64, vp, i64, i32, i32, vp, vp, i32, vp, i32, vp])]:
         f = getattr(L, "parse_kv_" + name)
@@ -723,14 +723,22 @@ def kv_fork(kv: KV, src, dst):
     _check(_calls.parse_kv_fork(kv, _ints(src, n, "src"), _ints(dst, n, "dst"), n, _stream()), "parse_kv_fork")
 
 
-def kv_reserve(kv: KV, n_new, served=None, workspace=None):
-    """parse_kv_reserve: room for n_new[s] more tokens of every sequence -> served [n_seqs]."""
+def kv_reserve(kv: KV, n_new, served=None, workspace=None, seqs=None, seqs_served=None):
+    """parse_kv_reserve: room for n_new[s] more tokens of every sequence -> served [n_seqs].  With seqs_served [P]
+    (parse_kv_reserve_seqs): it becomes seqs [P] (None: 0 .. P-1) with -1 where a sequence was not served, the list for the calls behind."""
     if served is None:
         served = torch.empty(kv.n_seqs, dtype=torch.int32, device=kv.K.device)
     if workspace is None:
         workspace = kv_workspace(kv)
-    _check(_calls.parse_kv_reserve(kv, _ints(n_new, kv.n_seqs, "n_new"), _ints(served, kv.n_seqs, "served"), workspace, workspace.numel(),
-                                   _stream()), "parse_kv_reserve")
+    _ints(n_new, kv.n_seqs, "n_new"), _ints(served, kv.n_seqs, "served")
+    if seqs_served is None:
+        if seqs is not None:
+            raise ValueError("seqs goes with seqs_served")
+        _check(_calls.parse_kv_reserve(kv, n_new, served, workspace, workspace.numel(), _stream()), "parse_kv_reserve")
+    else:
+        P = seqs_served.numel()
+        _check(_calls.parse_kv_reserve_seqs(kv, n_new, served, _ints(seqs, P, "seqs"), P, _ints(seqs_served, P, "seqs_served"), workspace,
+                                            workspace.numel(), _stream()), "parse_kv_reserve_seqs")
     return served
 
 

@@ -191,7 +191,7 @@ PyMethodDef methods[] = {
     CALL(parse_bucket_patterns), CALL(parse_bucket_and_plan), CALL(parse_prefill_plan), CALL(parse_pack_patterns), CALL(parse_pack_new_entries),
     CALL(parse_pack_ranks), CALL(parse_lowrank_forward), CALL(parse_lowrank_prefill_planned), CALL_SEVERAL(parse_lowrank_prefill_multi),
     CALL_SEVERAL(parse_lowrank_decode_planned), CALL_SEVERAL(parse_lowrank_decode_multi), CALL(parse_router_grad),
-    CALL(parse_kv_clear), CALL(parse_kv_fork), CALL(parse_kv_reserve), CALL(parse_kv_trim), CALL(parse_kv_compact), CALL(parse_kv_append),
+    CALL(parse_kv_clear), CALL(parse_kv_fork), CALL(parse_kv_reserve), CALL(parse_kv_reserve_seqs), CALL(parse_kv_trim), CALL(parse_kv_compact), CALL(parse_kv_append),
     CALL(parse_attend_decode), CALL(parse_attend_prefill),
     {nullptr, nullptr, 0, nullptr}};
 

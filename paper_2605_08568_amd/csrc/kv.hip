@@ -123,7 +123,8 @@ __device__ __forceinline__ void sums_before(int (&mine)[N], int (&total)[N], int
 // One workgroup: what a sequence gets depends on all before it, and a batch's tables are small.  A thread has PER consecutive sequences and `words` consecutive words of
 // the free pages.  Bound: latency, five dependent trips to memory (7.8 us for 48 sequences and 300 pages).
 template <int PER>
-__global__ __launch_bounds__(KV_ONE) void kv_reserve(parse_kv kv, const int32_t *__restrict__ n_new, int32_t *__restrict__ served, KvWork ws) {
+__global__ __launch_bounds__(KV_ONE) void kv_reserve(parse_kv kv, const int32_t *__restrict__ n_new, int32_t *__restrict__ served, const int32_t *seqs, int P,
+                                                     int32_t *seqs_served, KvWork ws) {
   __shared__ int begun[PER * KV_ONE], last[PER * KV_ONE], sums[3][KV_ONE / 64], copied;
   const int tid = threadIdx.x, page = kv.page, most = kv.max_pages * page;
   const int n_words = (kv.n_pages + 31) / 32, words = (n_words + KV_ONE - 1) / KV_ONE, w0 = tid * words, w1 = min(w0 + words, n_words);
@@ -203,7 +204,7 @@ __global__ __launch_bounds__(KV_ONE) void kv_reserve(parse_kv kv, const int32_t 
     if (s >= kv.n_seqs) continue;
     const bool ok = more[i] > 0 && s < fit;
     if (served) served[s] = ok ? 1 : 0;
-    if (!ok) continue;
+    if (!ok) { begun[s] = -1; continue; }
     kv.len[s] = len[i] + more[i];
     const int id = begun[s];
     if (copy[i]) {
@@ -211,10 +212,14 @@ __global__ __launch_bounds__(KV_ONE) void kv_reserve(parse_kv kv, const int32_t 
       atomicSub(&kv.refs[id], 1);                                  // one user is left at least
       atomicAdd(&copied, 1);
     }
-    begun[s] = copy[i] || id == -2 ? len[i] / page : (len[i] + page - 1) / page;   // from now on: column of its first new page
+    begun[s] = copy[i] || id == -2 ? len[i] / page : (len[i] + page - 1) / page;   // from now on: column of its first new page, -1: not served
   }
   __syncthreads();
   if (tid == 0) *ws.count = copied;
+  for (int p = tid; p < P; p += KV_ONE) {
+    const int s = seqs ? seqs[p] : p;
+    seqs_served[p] = s >= 0 && s < kv.n_seqs && begun[s] >= 0 ? s : -1;
+  }
   for (int r = tid; r < taken; r += KV_ONE) {
     const int s = first_over(r);
     kv.table[(int64_t)s * kv.max_pages + begun[s] + r - (s > 0 ? last[s - 1] : 0)] = ws.ids[r];
@@ -483,19 +488,34 @@ size_t parse_kv_workspace_bytes(const parse_kv *kv) { return check_kv(kv, false)
 
 static int64_t kv_page_bytes(const parse_kv *kv) { return (int64_t)kv->n_kv * kv->page * kv->d * elem_size(kv->dtype); }
 
-int parse_kv_reserve(const parse_kv *kv, const int32_t *n_new, int32_t *served, void *workspace, size_t workspace_bytes, parse_stream stream) {
-  const int st = check_kv(kv, true);
-  if (st != PARSE_OK) return st;
-  if (!n_new) return PARSE_EINVAL;
+static int kv_reserve_call(const parse_kv *kv, const int32_t *n_new, int32_t *served, const int32_t *seqs, int32_t P, int32_t *seqs_served, void *workspace,
+                           size_t workspace_bytes, parse_stream stream) {
   if (!workspace || workspace_bytes < kv_work_bytes(kv)) return PARSE_EWORKSPACE;
   if (!aligned4(n_new) || !aligned4(served) || !aligned16(workspace)) return PARSE_EALIGN;
   const KvWork ws = kv_work(kv, workspace);
-  if (kv->n_seqs <= KV_ONE) kv_reserve<1><<<dim3(1), KV_ONE, 0, (hipStream_t)stream>>>(*kv, n_new, served, ws);
-  else kv_reserve<KV_MAXSEQ / KV_ONE><<<dim3(1), KV_ONE, 0, (hipStream_t)stream>>>(*kv, n_new, served, ws);
+  if (kv->n_seqs <= KV_ONE) kv_reserve<1><<<dim3(1), KV_ONE, 0, (hipStream_t)stream>>>(*kv, n_new, served, seqs, P, seqs_served, ws);
+  else kv_reserve<KV_MAXSEQ / KV_ONE><<<dim3(1), KV_ONE, 0, (hipStream_t)stream>>>(*kv, n_new, served, seqs, P, seqs_served, ws);
   PARSE_LAUNCH_CHECK();
   kv_copy<false><<<dim3(2048), KV_THREADS, 0, (hipStream_t)stream>>>(*kv, ws, kv_page_bytes(kv));
   PARSE_LAUNCH_CHECK();
   return PARSE_OK;
+}
+
+int parse_kv_reserve(const parse_kv *kv, const int32_t *n_new, int32_t *served, void *workspace, size_t workspace_bytes, parse_stream stream) {
+  const int st = check_kv(kv, true);
+  if (st != PARSE_OK) return st;
+  if (!n_new) return PARSE_EINVAL;
+  return kv_reserve_call(kv, n_new, served, nullptr, 0, nullptr, workspace, workspace_bytes, stream);
+}
+
+int parse_kv_reserve_seqs(const parse_kv *kv, const int32_t *n_new, int32_t *served, const int32_t *seqs, int32_t P, int32_t *seqs_served, void *workspace,
+                          size_t workspace_bytes, parse_stream stream) {
+  const int st = check_kv(kv, true);
+  if (st != PARSE_OK) return st;
+  if (!n_new || !seqs_served || P <= 0) return PARSE_EINVAL;
+  if (P > KV_MAXSEQ || (!seqs && P > kv->n_seqs)) return PARSE_ESHAPE;
+  if (!aligned4(seqs) || !aligned4(seqs_served)) return PARSE_EALIGN;
+  return kv_reserve_call(kv, n_new, served, seqs, P, seqs_served, workspace, workspace_bytes, stream);
 }
 
 int parse_kv_compact(const parse_kv *kv, int32_t *n_live, void *workspace, size_t workspace_bytes, parse_stream stream) {

@@ -679,3 +679,39 @@ def test_prefill_rows_before_the_first_token_with_a_window_without_end(dtype, wi
     """More rows than tokens: the first rows' positions lie below 0, and their window's begin below what 32 bits hold."""
     run_prefill(Case(dtype, 2, 64, 16, [10, 33], seed=7), 4, [25, 3], window, sinks)
     run_prefill(Case(dtype, 1, 64, 16, [700, 5], seed=8), 1, [760, 5], window, sinks)
+
+
+@pytest.mark.parametrize("n_seqs", [4, 1500])
+def test_a_sequence_without_room_leaves_its_pages_as_they_are(n_seqs):
+    """Forks of a begun page in a pool that runs out: the list that reserve gives keeps append and attention away from the sequences that got nothing."""
+    n_kv, d, page = 2, 32, 16
+    kv = pa.KV.empty(1, 3, page, n_kv, d, n_seqs, 4)
+    kv.K.zero_(); kv.V.zero_()
+    want = np.zeros(n_seqs, np.int32); want[[0, 1]] = [5, 16]
+    placed = i32(np.array([7, 7]))
+    pa.kv_reserve(kv, i32(want), seqs_served=placed)
+    assert placed.tolist() == [0, 1]
+    rows = torch.randn((21, n_kv, d), device=DEV).bfloat16()
+    pa.kv_append(kv, 0, rows, rows, i32(np.array([0, 5, 21])), placed)
+    pa.kv_fork(kv, i32(np.array([0, 0])), i32(np.array([2, n_seqs - 1])))      # one free page: the first of the three gets a copy, the second nothing
+    one = np.zeros(n_seqs, np.int32); one[[0, 2, n_seqs - 1]] = 1
+    K, V = kv.K.clone(), kv.V.clone()
+    served = torch.empty(n_seqs, dtype=torch.int32, device=DEV)
+    seqs = i32(np.array([n_seqs - 1, 2, 0, 1, -5, n_seqs, 2]))
+    room = torch.full_like(seqs, 9)
+    pa.kv_reserve(kv, i32(one), served, seqs=seqs, seqs_served=room)
+    assert np.flatnonzero(served.cpu().numpy()).tolist() == [0] and room.tolist() == [-1, -1, 0, -1, -1, -1, -1] and seqs.tolist()[0] == n_seqs - 1
+    q = torch.randn((7, 4, d), device=DEV).bfloat16()
+    new = torch.randn((7, n_kv, d), device=DEV).bfloat16()
+    pa.kv_append(kv, 0, new, new, seqs=room)
+    out, lse = pa.attend_decode(kv, 0, q, room, with_lse=True)
+    mine, shared = int(kv.table[0, 0]), int(kv.table[2, 0])
+    assert mine == 2 and shared == 0 and kv.len[[0, 2, n_seqs - 1]].tolist() == [6, 5, 5]
+    assert torch.equal(kv.K[:, :2], K[:, :2]) and torch.equal(kv.V[:, :2], V[:, :2]), "a page of others was written"
+    assert np.array_equal(ko.k_from_pages(kv.K[0, mine].float().cpu().numpy())[5], new[2].float().cpu().numpy())
+    empty = [0, 1, 3, 4, 5, 6]
+    assert not bool(out[empty].any()) and bool(torch.isneginf(lse[empty]).all()) and bool(torch.isfinite(lse[2]).all())
+    # the list over the one that it is made of
+    pa.kv_trim(kv, i32(np.where(np.arange(n_seqs) == 1, 0, 100)))
+    pa.kv_reserve(kv, i32(one - (np.arange(n_seqs) == 0)), seqs=seqs, seqs_served=seqs)
+    assert seqs.tolist() == [n_seqs - 1, 2, -1, -1, -1, -1, 2]

@@ -200,3 +200,22 @@ def test_bookkeeping_by_hand():
     q.reserve([100])
     q.trim(None, 40, 4)                                                  # tokens 61.. are seen by the next one: pages 1 and 2 go, 0 has the sinks
     assert q.table[0].tolist() == [0, -1, -1, 3, 4, 5, 6, -1, -1, -1] and q.len[0] == 100
+
+
+def test_reserve_with_a_list_refuses_bad_arguments():
+    L = pa.lib()
+
+    def call(kv=None, new=FAKE, served=FAKE, seqs=FAKE, P=3, out=FAKE, ws=FAKE, wsb=1 << 40):
+        return L.parse_kv_reserve_seqs(kv if kv is not None else cache(), new, served, seqs, P, out, ws, wsb, None)
+    for bad, status in BAD_CACHES + [(dict(refs=None), EINVAL), (dict(free_bits=ODD), EALIGN)]:
+        assert call(cache(**bad)) == status, bad
+    assert call(new=None) == EINVAL and call(out=None) == EINVAL and call(P=0) == EINVAL and call(P=-1) == EINVAL
+    assert call(P=4097) == ESHAPE and call(seqs=None, P=4) == ESHAPE
+    assert call(new=ODD) == EALIGN and call(served=ODD) == EALIGN and call(seqs=ODD) == EALIGN and call(out=ODD) == EALIGN and call(ws=ODD) == EALIGN
+    assert call(ws=None) == EWORKSPACE and call(wsb=L.parse_kv_workspace_bytes(cache()) - 1) == EWORKSPACE
+    kv = pa.KV(torch.zeros(2, 4, 3, 1, 4, 16, 8).bfloat16(), torch.zeros(2, 4, 3, 2, 32, 8).bfloat16(), torch.zeros(5, 6, dtype=torch.int32),
+               torch.zeros(5, dtype=torch.int32))
+    i = torch.zeros(5, dtype=torch.int32)
+    for bad in (dict(seqs=i), dict(seqs=i[:3], seqs_served=i), dict(seqs=i, seqs_served=i.long()), dict(seqs_served=i.float())):
+        with pytest.raises(ValueError):
+            pa.kv_reserve(kv, i, i, torch.zeros(1, dtype=torch.uint8), **bad)
