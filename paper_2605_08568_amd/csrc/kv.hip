@@ -101,6 +101,17 @@ static KvWork kv_work(const parse_kv *kv, void *ws) {
   return KvWork{(int32_t *)p, (int2 *)(p + 16), (int32_t *)(p + 16 + round_up((size_t)kv->n_pages * 8, 16))};
 }
 
+// Sums that stop at the largest int: what 4096 sequences may ask for is more (2^33 pages), and more than any pool has in either case.  A wavefront's own sums
+// stay below 2^30 (four sequences a lane).
+__device__ __forceinline__ int add_capped(int a, int b) { return (int)min((uint32_t)a + (uint32_t)b, 0x7fffffffu); }
+// ... over the lanes up to this one of the first sixteen
+__device__ __forceinline__ int scan16_capped(int v) {
+  v = add_capped(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false));  // row_shr:1
+  v = add_capped(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false));  // row_shr:2
+  v = add_capped(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false));  // row_shr:4
+  return add_capped(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false));  // row_shr:8
+}
+
 // Exclusive sums over the threads of a workgroup alone, N of them at once; `sums`: [N][wavefronts], LDS that nobody reads any more.  `mine` becomes this thread's.
 template <int N>
 __device__ __forceinline__ void sums_before(int (&mine)[N], int (&total)[N], int (*sums)[KV_ONE / 64]) {
@@ -114,9 +125,10 @@ __device__ __forceinline__ void sums_before(int (&mine)[N], int (&total)[N], int
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < N; ++k) {
-    const int of_wave = wave_scan(lane < KV_ONE / 64 ? sums[k][lane] : 0);
+    static_assert(KV_ONE / 64 == 16, "a wavefront a lane of one row of sixteen");
+    const int of_wave = scan16_capped(sums[k][lane & 15]);
     total[k] = __builtin_amdgcn_readlane(of_wave, KV_ONE / 64 - 1);
-    mine[k] = inc[k] - mine[k] + (wave ? __builtin_amdgcn_readlane(of_wave, wave - 1) : 0);
+    mine[k] = add_capped(inc[k] - mine[k], wave ? __builtin_amdgcn_readlane(of_wave, wave - 1) : 0);
   }
 }
 
@@ -172,7 +184,7 @@ __global__ __launch_bounds__(KV_ONE) void kv_reserve(parse_kv kv, const int32_t 
   int at = part[0], rank = part[1], slot = part[2];
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    at += need[i];
+    at = add_capped(at, need[i]);
     last[tid * PER + i] = at;                                      // pages that the sequences up to this one take
   }
   __syncthreads();                                                 // users and begun pages are looked at no more: they may change

@@ -715,3 +715,25 @@ def test_a_sequence_without_room_leaves_its_pages_as_they_are(n_seqs):
     pa.kv_trim(kv, i32(np.where(np.arange(n_seqs) == 1, 0, 100)))
     pa.kv_reserve(kv, i32(one - (np.arange(n_seqs) == 0)), seqs=seqs, seqs_served=seqs)
     assert seqs.tolist() == [n_seqs - 1, 2, -1, -1, -1, -1, 2]
+
+
+@pytest.mark.parametrize("first", [0, 16])
+def test_reserve_of_more_pages_than_32_bits_count(first):
+    """4096 sequences that ask for whole rows of a table of 2^25 tokens: 2^33 pages of sixteen.  (The table's 34 GB are not touched: nobody has a token.)"""
+    n_seqs, columns = 4096, 1 << 21
+    kv = pa.KV(torch.zeros((1, 64, 1, 1, 4, 16, 8), dtype=torch.bfloat16, device=DEV), torch.zeros((1, 64, 1, 2, 32, 8), dtype=torch.bfloat16, device=DEV),
+               torch.empty((n_seqs, columns), dtype=torch.int32, device=DEV), torch.zeros(n_seqs, dtype=torch.int32, device=DEV),
+               torch.zeros(64, dtype=torch.int32, device=DEV), torch.full((2,), -1, dtype=torch.int32, device=DEV))
+    want = np.full(n_seqs, 1 << 25, np.int32)
+    want[0] = first                                                # one page, or no token
+    want[4000:] = 1
+    room = torch.empty(n_seqs, dtype=torch.int32, device=DEV)
+    wbuf, ws = guarded_bytes(int(pa.lib().parse_kv_workspace_bytes(kv.c())))
+    served = pa.kv_reserve(kv, i32(want), workspace=ws, seqs_served=room)
+    check_guards(wbuf, "workspace")
+    got = [0] if first else []
+    assert np.flatnonzero(served.cpu().numpy()).tolist() == got and np.flatnonzero(room.cpu().numpy() >= 0).tolist() == got
+    assert int(kv.len[0]) == first and not bool(kv.len[1:].any())
+    assert kv.refs.tolist() == [len(got)] + [0] * 63 and kv.free_bits.tolist() == [-1 - len(got), -1]
+    del kv
+    torch.cuda.empty_cache()
