@@ -571,7 +571,9 @@ int parse_kv_append(const parse_kv *kv, int32_t layer, const void *k, int64_t k_
 
 /* One new token per sequence (its last: i = len - 1), over caches of any lengths; the caches' tokens are dealt out evenly
  * over the card and the parts of a cache joined.
- *   rows = number of sequences, 1..4096; seqs device int32 [rows], the table's row of each, or NULL: the row itself
+ *   rows = number of sequences, 1..4096, and rows times the tokens that a row may see (max_pages*page; with a window
+ *   window + sinks + 96, if that is less) at most 2^36 - 2^16: their blocks of 32 are counted in 31 bits;
+ *   seqs device int32 [rows], the table's row of each, or NULL: the row itself
  *   workspace  its first PARSE_ATTEND_DECODE_ZERO_BYTES are tickets with which the workgroups that share a cache find out
  *              which of them joins its parts: ZERO before the first call, zero again after every call.  The rest may hold anything.  A workspace serves one call at
  *              a time: calls that overlap need one each. */

@@ -7,9 +7,11 @@
 namespace parse {
 
 constexpr int KV_MAXSEQ = 4096;              // sequences of a table, prompts or sequences of a call
-constexpr int KV_MAXTOKENS = 1 << 25;        // tokens that a table's row can name: counts of tiles over 4096 rows stay in 31 bits
+constexpr int KV_MAXTOKENS = 1 << 25;        // tokens that a table's row can name.  Tiles of them over 4096 rows are more than an int counts: whoever adds those up has a limit of its own
 
-constexpr int KV_MAXROWS = 1 << 24;          // rows times the heads that share a kv head: their tiles stay countable also where offsets go back and forth
+// rows times the heads that share a kv head: tiles of 128 of them stay countable also where offsets go back and forth (2^17 * 4096).  Blocks of 16 that go back and
+// forth are not from 2^24 rows and 4095 prompts on: their sum is negative, and such a batch is passed over
+constexpr int KV_MAXROWS = 1 << 24;
 
 static inline bool aligned4(const void *p) { return (((uintptr_t)p) & 3u) == 0; }
 

@@ -494,12 +494,17 @@ static bool ad_tickets(const parse_kv *kv, int n_q) {
   return weights * kv->d <= 65536 && 2 * weights <= AD_WAVES * AD_HEADS * kv->d;    // ... in the LDS that the sums left
 }
 
-// Whether table and window alone say that every row is a share's (ad_by_rows), whatever the lengths
-static bool ad_sure(const AdArgs &a) {
-  int64_t steps = ((int64_t)a.kv.max_pages * a.kv.page + AD_STEP - 1) / AD_STEP;
-  if (a.window > 0) steps = std::min(steps, ((int64_t)a.window + AD_STEP - 1) / AD_STEP + 1 + ((int64_t)a.sinks + AD_STEP - 1) / AD_STEP);
-  return a.rows <= a.shares && steps <= AD_WAVES + ad_slack(a.rows);
+// Steps that a row has at most, by table and window alone
+static int64_t ad_most_steps(const parse_kv *kv, int window, int sinks) {
+  const int64_t steps = ((int64_t)kv->max_pages * kv->page + AD_STEP - 1) / AD_STEP;
+  if (window == 0) return steps;
+  return std::min(steps, ((int64_t)window + AD_STEP - 1) / AD_STEP + 1 + ((int64_t)sinks + AD_STEP - 1) / AD_STEP);
 }
+// The steps of all rows are added up and dealt out in an int; room for what rounding a share's number up adds (4 * AD_WAVES) and for the shares
+constexpr int64_t AD_MAXSTEPS = INT32_MAX - 2 * AD_GROUPS;
+
+// Whether table and window alone say that every row is a share's (ad_by_rows), whatever the lengths
+static bool ad_sure(const AdArgs &a) { return a.rows <= a.shares && ad_most_steps(&a.kv, a.window, a.sinks) <= AD_WAVES + ad_slack(a.rows); }
 
 template <class T, int DT, bool NT, bool TICKETS>
 static int ad_launch(const AdArgs &a, hipStream_t s) {
@@ -563,7 +568,7 @@ int parse_attend_decode(const parse_kv *kv, int32_t layer, const void *q, int64_
   using namespace parse;
   const int st = check_attend(kv, layer, q, q_stride, n_q, rows, nullptr, seqs, scale, window, sinks, out, out_stride, lse);
   if (st != PARSE_OK) return st;
-  if (rows > KV_MAXSEQ || (!seqs && rows > kv->n_seqs)) return PARSE_ESHAPE;
+  if (rows > KV_MAXSEQ || (!seqs && rows > kv->n_seqs) || rows * ad_most_steps(kv, window, sinks) > AD_MAXSTEPS) return PARSE_ESHAPE;
   if (!workspace || workspace_bytes < ad_bytes(kv, n_q)) return PARSE_EWORKSPACE;
   if (!aligned16(workspace)) return PARSE_EALIGN;
   const size_t at = (size_t)layer * kv->n_pages * kv->n_kv * kv->page * kv->d * elem_size(kv->dtype);

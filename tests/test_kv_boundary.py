@@ -219,3 +219,17 @@ def test_reserve_with_a_list_refuses_bad_arguments():
     for bad in (dict(seqs=i), dict(seqs=i[:3], seqs_served=i), dict(seqs=i, seqs_served=i.long()), dict(seqs_served=i.float())):
         with pytest.raises(ValueError):
             pa.kv_reserve(kv, i, i, torch.zeros(1, dtype=torch.uint8), **bad)
+
+
+def test_decode_refuses_more_steps_than_it_can_count():
+    """Blocks of 32 tokens over all rows are added up in 31 bits: the table says how many there may be, or the window where that is less.  A call that is
+    let through stops at the missing workspace here."""
+    L = pa.lib()
+
+    def call(rows, columns, page=16, window=0, sinks=0):
+        return L.parse_attend_decode(cache(n_seqs=4096, max_pages=columns, page=page), 0, FAKE, 512, 8, rows, FAKE, 1.0, window, sinks, FAKE, 512, None, None, 0, None)
+    whole = 1 << 21                                                 # 2^25 tokens, 2^20 blocks
+    assert call(4096, whole) == ESHAPE and call(2048, whole) == ESHAPE and call(4096, 1 << 17, 256) == ESHAPE
+    assert call(2047, whole) == EWORKSPACE and call(4096, whole // 2 - 2) == EWORKSPACE and call(1, whole) == EWORKSPACE
+    assert call(4096, whole, window=4096, sinks=4) == EWORKSPACE
+    assert call(4096, whole, window=1 << 24, sinks=1 << 10) == ESHAPE and call(4096, whole, window=2 ** 31 - 1, sinks=2 ** 31 - 1) == ESHAPE
