@@ -113,8 +113,9 @@ __device__ __forceinline__ int kv_find(const int *pre, int P, int v) {
   return lo;
 }
 
-// The running maximum of a softmax may lag behind by this much, in powers of two: weights stay below 2^8, and the sums are
-// multiplied over only where a maximum grows by more (the first tile of a row, then hardly ever).
+// The running maximum of a softmax may lag behind by this much, in powers of two: the sums are multiplied over only where a maximum grows
+// by more (the first tile of a row, then hardly ever).  Weights are taken so much below the maximum that they are 1 at most however far it lags: sums reach as
+// far as those of a softmax whose maximum is exact, and what falls below the smallest number is 2^-118 of the largest weight.
 constexpr float AT_LAG = 8.f;
 // Maxima are taken of the products q.k themselves; a weight is then one fused multiply-add and a 2^x.  That needs a positive scale: its
 // sign goes to q, and a scale of zero makes q zero (so that a masked score of -inf is never multiplied by 0).
@@ -189,13 +190,13 @@ template <> struct Op<uint16_t> {
   static __device__ __forceinline__ f32x16 mma32(frag a, frag b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
   }
-  // q for a scale of either sign (AtScale): the scores' sign turned, or zeros
+  // q for a scale of either sign (at_scale): the scores' sign turned, or zeros
   static __device__ __forceinline__ frag sign(frag a, uint32_t s) {
 #pragma unroll
     for (int w = 0; w < 4; ++w) a[w] = s == AT_ZERO ? 0u : a[w] ^ (s == AT_TURNED ? 0x80008000u : 0u);
     return a;
   }
-  // weights in [0, 2^8]: rounded to bf16, 2^-8 relative at most, independent from token to token
+  // weights in [0, 1]: rounded to bf16, 2^-8 relative at most, independent from token to token
   static __device__ __forceinline__ frag pack(const float *p) {
     return u32x4{cvt_pk_bf16(p[0], p[1]), cvt_pk_bf16(p[2], p[3]), cvt_pk_bf16(p[4], p[5]), cvt_pk_bf16(p[6], p[7])};
   }
@@ -303,5 +304,8 @@ template <int N> __device__ __forceinline__ float lane_sum(float v) {
 // 2^x of the vector unit: one rounding; below 2^-126 it is 0
 __device__ __forceinline__ float at_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float finite_or_0(float m) { return m == -INFINITY ? 0.f : m; }
+// what is taken off scale * score (a weight is 2 to what is left), and the log-sum of weights that add up to l
+__device__ __forceinline__ float at_base(float m, float scale) { return fmaf(finite_or_0(m), scale, AT_LAG); }
+__device__ __forceinline__ float at_lse(float m, float scale, float l) { return (at_base(m, scale) + log2f(l)) * 0.6931471805599453f; }
 
 }  // namespace parse

@@ -34,7 +34,7 @@ __device__ __forceinline__ void ad_store(const AdArgs &a, int row, int head, int
   T *out = reinterpret_cast<T *>(a.out) + (int64_t)row * a.out_stride + (int64_t)head * D + i;
   if constexpr (sizeof(T) == 2) *out = (uint16_t)cvt_pk_bf16(y, 0.f);
   else *out = y;
-  if (a.lse && i == 0) a.lse[(int64_t)row * a.n_q + head] = (finite_or_0(top) * a.scale + log2f(ls)) * 0.6931471805599453f;
+  if (a.lse && i == 0) a.lse[(int64_t)row * a.n_q + head] = at_lse(top, a.scale, ls);
 }
 
 // How the batch's steps are dealt out: sequence b has the steps [before, before + its count) of `total`, a workgroup `per` of them.
@@ -288,7 +288,7 @@ __global__ __launch_bounds__(AD_THREADS, DT * sizeof(T) <= 16 ? 2 : 1) void atte
         for (int v = 0; v < VB; ++v) o[v] *= by;
         m = grown;
       }
-      const float base = finite_or_0(m) * a.scale;
+      const float base = at_base(m, a.scale);
       float p[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) { p[e] = at_exp2(fmaf(s[e], a.scale, -base)); l += p[e]; }
@@ -354,7 +354,7 @@ __global__ __launch_bounds__(AD_THREADS, DT * sizeof(T) <= 16 ? 2 : 1) void atte
         T *out = reinterpret_cast<T *>(a.out) + (int64_t)b * a.out_stride + (int64_t)head * D + 4 * quad;
 #pragma unroll
         for (int v = 0; v < VB; ++v) Op<T>::store4(out + 16 * v, o[v][0] * by, o[v][1] * by, o[v][2] * by, o[v][3] * by);
-        if (a.lse && quad == 0) a.lse[(int64_t)b * a.n_q + head] = (finite_or_0(m) * a.scale + log2f(l)) * 0.6931471805599453f;
+        if (a.lse && quad == 0) a.lse[(int64_t)b * a.n_q + head] = at_lse(m, a.scale, l);
       }
       continue;
     }

@@ -172,7 +172,7 @@ __global__ __launch_bounds__(AP_WAVES * 64, DT == 4 ? 2 : 1) void attend_prefill
       for (int d = 0; d < DT; ++d) o[d] *= by;
       m = grown;
     }
-    const float low = finite_or_0(m) * a.scale;
+    const float low = at_base(m, a.scale);
     frag pf[TB];
 #pragma unroll
     for (int b = 0; b < TB; ++b) {
@@ -249,7 +249,7 @@ __global__ __launch_bounds__(AP_WAVES * 64, DT == 4 ? 2 : 1) void attend_prefill
 #pragma unroll
     for (int c = 0; c < 4; ++c)
       Op<T>::store4(out + 32 * d + 8 * c + 4 * half, o[d][4 * c] * by, o[d][4 * c + 1] * by, o[d][4 * c + 2] * by, o[d][4 * c + 3] * by);
-  if (a.lse && half == 0) a.lse[(int64_t)(row0 + token) * a.n_q + head] = (finite_or_0(m) * a.scale + log2f(l)) * 0.6931471805599453f;
+  if (a.lse && half == 0) a.lse[(int64_t)(row0 + token) * a.n_q + head] = at_lse(m, a.scale, l);
 }
 
 // bf16: the same, with the products of one tile under the softmax of the tile before it: in an iteration a wavefront has the
@@ -410,7 +410,7 @@ __device__ __forceinline__ bool ap_rows(const ApArgs &a, const KvItem &f, char *
       for (int d = 0; d < DT; ++d) vf[b * DT + d] = O::load(vs + b * 16 * D + d * 256);
   };
   auto weigh = [&](const f32x16 &sc) {
-    const float low = finite_or_0(m) * a.scale;
+    const float low = at_base(m, a.scale);
     float w[16];
 #pragma unroll
     for (int x = 0; x < 16; ++x) { w[x] = at_exp2(fmaf(sc[x], a.scale, -low)); l += w[x]; }
@@ -541,7 +541,7 @@ __device__ __forceinline__ bool ap_rows(const ApArgs &a, const KvItem &f, char *
       if (r < r_end) *reinterpret_cast<u32x4 *>(out + 32 * d + 8 * c) = u32x4{x[0], y[0], x[1], y[1]};
     }
   if (r >= r_end) return true;
-  if (a.lse && half == 0) a.lse[(int64_t)(row0 + token) * a.n_q + head] = (finite_or_0(m) * a.scale + log2f(l)) * 0.6931471805599453f;
+  if (a.lse && half == 0) a.lse[(int64_t)(row0 + token) * a.n_q + head] = at_lse(m, a.scale, l);
   return true;
 }
 
@@ -591,7 +591,7 @@ __global__ __launch_bounds__(AP_WAVES * 64) void ap_join(ApArgs a) {
       Op<T>::store4(reinterpret_cast<T *>(a.out) + (int64_t)(f.first + token) * a.out_stride + (int64_t)head * D + 4 * lane, o[0] * over, o[1] * over, o[2] * over,
                     o[3] * over);
     }
-    if (a.lse && lane == 0) a.lse[(int64_t)(f.first + token) * a.n_q + head] = (finite_or_0(top) * a.scale + log2f(total)) * 0.6931471805599453f;
+    if (a.lse && lane == 0) a.lse[(int64_t)(f.first + token) * a.n_q + head] = at_lse(top, a.scale, total);
   }
 }
 

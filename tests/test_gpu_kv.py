@@ -737,3 +737,21 @@ def test_reserve_of_more_pages_than_32_bits_count(first):
     assert kv.refs.tolist() == [len(got)] + [0] * 63 and kv.free_bits.tolist() == [-1 - len(got), -1]
     del kv
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_values_near_the_type_s_largest(dtype, sign):
+    """Scores of 0, then of 7.5 in powers of two, which is less than the running maximum may lag by: the sums hold 8 values of 1e37 and
+    128 of 2^-7.5 of that, as they do with weights of at most 1."""
+    n, d = 136, 32
+    k, v = np.zeros((n, 1, d)), np.full((n, 1, d), sign * 1e37)
+    k[128:, 0, 0] = 7.5
+    case = Case(dtype, 1, d, 16, [n], seed=1)
+    for j in range(n):
+        case.write(0, j, k[j], rounded(v[j], dtype))
+    q = np.zeros((1, 1, d)); q[0, 0, 0] = 1
+    want = ko.attend_row(q[0], case.k[0], case.v[0], np.ones(n, bool), np.log(2.0))
+    for out, lse in (pa.attend_decode(case.kv, 1, upload(q, dtype), scale=np.log(2.0), with_lse=True),
+                     pa.attend_prefill(case.kv, 1, upload(q, dtype), scale=np.log(2.0), with_lse=True)):
+        compare(case, out, lse, [(*want, n)], d)
