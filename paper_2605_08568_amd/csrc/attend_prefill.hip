@@ -49,11 +49,11 @@ __device__ __forceinline__ int ap_tiles(int n, int group, int tile) { return (in
 template <int DT>
 __global__ __launch_bounds__(AP_WAVES * 64, DT == 4 ? 2 : 1) void attend_prefill_f32(ApArgs a) {
   typedef float T;
-  constexpr int NW = AP_WAVES, TK = AP_TILE, ST = 2;
+  constexpr int NW = AP_WAVES, TK = AP_TILE, ST = 2;               // two stages: a tile is worked on, the next one is on its way
   constexpr int D = DT * 32, KB = D / 16, TB = TK / 16, TS = TK / 32, TM = NW * 32, THREADS = NW * 64;
   constexpr int BLOCK = 16 * D * (int)sizeof(T);                   // bytes of sixteen tokens of K, and of V
   constexpr int STAGE = 2 * TB * BLOCK, PIECES = STAGE / 1024, LOADS = PIECES / NW;
-  static_assert(PIECES % NW == 0 && ST >= 2 && ST <= 3, "every wavefront stages as much");
+  static_assert(PIECES % NW == 0, "every wavefront stages as much");
   typedef typename Op<T>::frag frag;
   extern __shared__ char smem[];
   int *wave_sums = reinterpret_cast<int *>(smem + ST * STAGE), *pre = wave_sums + NW;
@@ -115,7 +115,6 @@ __global__ __launch_bounds__(AP_WAVES * 64, DT == 4 ? 2 : 1) void attend_prefill
   // q comes first: whoever waits for a tile has it
   asm volatile("" ::: "memory");
   if (share.first < share.last) stage(share.first, now, 0);
-  if (ST == 3 && share.first + 1 < share.last) stage(share.first + 1, next, 1);
   float m = -INFINITY, l = 0.f;
   f32x16 o[DT];
 #pragma unroll
@@ -126,13 +125,13 @@ __global__ __launch_bounds__(AP_WAVES * 64, DT == 4 ? 2 : 1) void attend_prefill
   const int ktok = 16 * (n >> 4) + 8 * ((n >> 2) & 1) + 4 * ((n >> 3) & 1) + (n & 3);
 
   int buf = 0;
-  for (int u = share.first; u < share.last; ++u, buf = buf + 1 == ST ? 0 : buf + 1) {
+  for (int u = share.first; u < share.last; ++u, buf ^= 1) {
     const int t0 = span.at(u) * TK;
     if (u + 2 < share.last) later = ids_of(u + 2);
-    if (ST == 3 && u + 1 < share.last) wait_vm<LOADS>(); else wait_vm<0>();
+    wait_vm<0>();
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     wg_barrier();                                                  // this tile has landed for everybody, the one before it is read by everybody
-    if (u + ST - 1 < share.last) stage(u + ST - 1, ST == 3 ? later : next, buf == 0 ? ST - 1 : buf - 1);
+    if (u + 1 < share.last) stage(u + 1, next, buf ^ 1);
     const Ids ids = now;
     now = next; next = later;
     if (idle || t0 > wi1 || (t0 + TK <= wlo && t0 >= a.sinks)) continue;
@@ -215,7 +214,6 @@ __global__ __launch_bounds__(AP_WAVES * 64, DT == 4 ? 2 : 1) void attend_prefill
 #pragma unroll
           for (int e = 0; e < 8; ++e) w = ((c == b) & (e == (j & 7))) ? sc[c / 2][8 * (c % 2) + e] : w;
         w = __shfl(w, n + 32 * h, 64);
-        if constexpr (sizeof(T) == 2) w = __uint_as_float(cvt_pk_bf16(w, 0.f) << 16);
         const bool mine = (bool)(blocks >> b & 1) & kv_sees(i, lo, a.sinks, t0 + j);
         const T *vr = vs + b * 16 * D + h * D * 8 + (j & 7);
 #pragma unroll
