@@ -755,3 +755,78 @@ def test_values_near_the_type_s_largest(dtype, sign):
     for out, lse in (pa.attend_decode(case.kv, 1, upload(q, dtype), scale=np.log(2.0), with_lse=True),
                      pa.attend_prefill(case.kv, 1, upload(q, dtype), scale=np.log(2.0), with_lse=True)):
         compare(case, out, lse, [(*want, n)], d)
+
+
+@pytest.mark.parametrize("dtype,P,offsets", [("bf16", 64, True), ("bf16", 65, True), ("fp32", 65, True), ("bf16", 130, True), ("fp32", 300, True), ("bf16", 300, False),
+                                             ("fp32", 70, False), ("bf16", 1000, True)])
+def test_append_of_many_prompts(dtype, P, offsets):
+    """Prompts that a workgroup finds by sums in LDS: empty ones, missing pages, sequences that the table does not have, several blocks a workgroup."""
+    rng = np.random.default_rng(P)
+    n_kv, n_q, d, page = 2, 3, 32, 16
+    lens = rng.integers(1, 90, P)
+    new = np.minimum(rng.choice([0, 1, 2, 15, 16, 17, 40], P), lens) if offsets else np.ones(P, np.int64)
+    seqs = rng.permutation(P)                                      # prompt p is the table's row seqs[p]
+    counts = -(-lens // page)
+    ids = rng.permutation(int(counts.sum()))
+    table, n, at = np.full((P, int(counts.max()) + 1), -1, np.int32), np.zeros(P, np.int32), 0
+    for p in range(P):
+        table[seqs[p], :counts[p]] = ids[at:at + counts[p]]; at += counts[p]
+        n[seqs[p]] = lens[p]
+    table[seqs[P // 2], counts[P // 2] - 1] = -1                   # the page of a prompt's last tokens is not there
+    named = seqs.astype(np.int32); named[3], named[P - 5] = -1, P   # two prompts of no sequence
+    off = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    rows = int(off[-1])
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    kv = pa.KV(torch.full((1, at, n_kv, 1, d // 8, 16, 8), 7.0, device=DEV, dtype=dt), torch.full((1, at, n_kv, 2, d, 8), 7.0, device=DEV, dtype=dt), i32(table), i32(n))
+    x = rounded(rng.standard_normal((rows, n_q + 2 * n_kv, d)), dtype)
+    fused, turn = upload(x, dtype), rope_table(90, d)
+    buf, _, q_out = guarded(rows, n_q, d, fused, 16)
+    pa.kv_append(kv, 0, fused[:, n_q:n_q + n_kv], fused[:, n_q + n_kv:], i32(off) if offsets else None, i32(named), q=fused[:, :n_q], q_out=q_out,
+                 rope=torch.from_numpy(turn).to(DEV))
+    check_guards(buf, "q_out")
+    known = (named >= 0) & (named < P)
+    pos = np.concatenate([np.where(known[p], lens[p] - new[p] + np.arange(new[p]), 0) for p in range(P)]).astype(int)
+    angles = turn[pos].astype(np.float64)
+    qk = ko.rotate(x[:, :n_q + n_kv], angles)
+    # two products and a sum in 32 bits, the result rounded to the type
+    tol = 2.0 ** -23 * np.concatenate([np.abs(x[:, :n_q + n_kv, :d // 2]) + np.abs(x[:, :n_q + n_kv, d // 2:])] * 2, 2) + (1.01 * 2.0 ** -8 * np.abs(qk) if dtype == "bf16" else 0)
+    assert np.all(np.abs(q_out.double().cpu().numpy() - qk[:, :n_q]) <= tol[:, :n_q])
+    K, V = ko.k_from_pages(kv.K[0].double().cpu().numpy()), ko.v_from_pages(kv.V[0].double().cpu().numpy())
+    touched = np.zeros((at, page), bool)
+    for p in np.flatnonzero(known):
+        for t in range(new[p]):
+            j, r = lens[p] - new[p] + t, off[p] + t
+            id_ = table[seqs[p], j // page]
+            if id_ < 0:
+                continue
+            touched[id_, j % page] = True
+            assert np.all(np.abs(K[id_, j % page] - qk[r, n_q:]) <= tol[r, n_q:]) and np.array_equal(V[id_, j % page], x[r, n_q + n_kv:]), (p, t)
+    assert np.all(K[~touched] == 7) and np.all(V[~touched] == 7), "a place of no new token was written"
+
+
+@pytest.mark.parametrize("kv,n_q,d,lens,short", [(2, 8, 64, [300, 1, 77], True), (8, 8, 128, [40, 90, 33, 64] * 16, True), (1, 4, 32, [9000], False),
+                                                 (1, 16, 128, [3000], False), (1, 2, 256, [500], False)])
+def test_decode_keeps_what_the_rounding_of_a_weight_leaves(kv, n_q, d, lens, short):
+    """bf16: a weight is multiplied as two bf16 numbers, 2^-16 of it lost at most; only the result is rounded to 2^-8.  Values whose mean is near 0 show the
+    difference: with weights of one bf16 number the oracle itself is outside this bound, where rows are short (the bound grows with their number of sums)."""
+    case = Case("bf16", kv, d, 16, lens, seed=n_q)
+    q = rounded(np.random.default_rng(4).standard_normal((len(lens), n_q, d)), "bf16")
+    out = pa.attend_decode(case.kv, 1, upload(q, "bf16")).double().cpu().numpy()
+    over = 0
+    for s, n in enumerate(lens):
+        o, l, mag, big = ko.attend_row(q[s], case.k[s], case.v[s], case.there[s], d ** -0.5)
+        tol, _ = bounds("fp32", d, n, o, l, mag, big)
+        tol = tol + 1.01 * 2.0 ** -16 * mag + 1.01 * 2.0 ** -8 * (np.abs(o) + tol + 1.01 * 2.0 ** -16 * mag)
+        assert np.all(np.abs(out[s] - o) <= tol), s
+        for h in range(n_q):
+            g = h // (n_q // kv)
+            score = d ** -0.5 * (case.k[s][:, g] @ q[s, h])
+            p = np.exp(score - score.max())
+            over += int((np.abs(rounded(p, "bf16") @ case.v[s][:, g] / p.sum() - o[h]) > tol[h] - 1.01 * 2.0 ** -8 * np.abs(o[h])).sum())
+    assert over > 0 or not short
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("window,sinks", [(2 ** 31 - 1, 0), (2 ** 31 - 1, 2 ** 31 - 1), (33, 2 ** 31 - 1)])
+def test_decode_with_the_largest_window_and_sinks(dtype, window, sinks):
+    run_decode(Case(dtype, 2, 64, 16, [1, 31, 32, 33, 40, 500, 1025], seed=3), 4, window, sinks)
