@@ -143,10 +143,12 @@ __device__ __forceinline__ void ad_join(const AdArgs &a, int b, int kvh, int hg,
 // maximum grows by more than 2^8, that maximum.  The matrix units are used for their operand form: fifteen of sixteen columns may be empty, and still
 // they take 1 / 20 of the time of the loads.
 // Bound: reads.  Operands go straight from the pages into registers in pieces of 1 KiB (a page's layout is theirs), one step ahead of the one that is worked
-// on; a unit has 32 KiB on their way whatever is asked for, so that two workgroups a unit are enough, and more of them only cut the caches finer: 512 / 768 / 1024
+// on where two steps fit the registers (bf16 up to 128 columns, fp32 up to 64; wider heads load a step, wait and work on it, while another wavefront's loads are on their way); a unit has 32 KiB on their way whatever is asked for, so that two workgroups a unit are enough, and more of them only cut the caches finer: 512 / 768 / 1024
 // workgroups, 32 ragged caches of 32 heads 108 / 121 / 114 us, 192 windows 162 / 182 / 175.  Shares are equal in steps, not in rows: a batch of unlike lengths needs no plan.
 // Measured, reads of the cache against 6.1 to 6.4 TB/s of a read-only stream of 2 GiB: 32 caches of 32 to 2048 tokens, 32 heads 5.9 TB/s (96 us), 100003 tokens of 8 heads
-// 5.4 (75 us), 192 windows of 1024 5.6 (142 us), 256 caches of 300 tokens, 8 heads 4.6 (68 us); single short caches by latency (77 tokens 7.3 us).
+// 5.4 (76 us), 192 windows of 1024 5.6 (143 us), 256 caches of 300 tokens, 8 heads 5.4 (59 us); single short caches by latency (77 tokens 7.3 us).
+// By width, 32 caches of 32 to 2048 tokens, 16 heads: bf16 128 / 160 / 256 columns 5.1 / 5.3 / 5.4 TB/s, fp32 64 / 96 / 128 columns 4.5 / 4.4 / 4.1, and 2.7 at 256, where one
+// wavefront a SIMD has a step's 64 KiB on their way or none.
 template <class T, int DT, bool NT, bool TICKETS>
 __global__ __launch_bounds__(AD_THREADS, DT * sizeof(T) <= 16 ? 2 : 1) void attend_decode(AdArgs a) {
   constexpr int D = DT * 32, KB = D / 32, VB = D / 16;
@@ -519,8 +521,9 @@ static int ad_launch(const AdArgs &a, hipStream_t s) {
   }
   return PARSE_OK;
 }
-// A cache larger than the last-level cache is new to it in every step: loads that do not stay there (100003 tokens of 8 heads 81.5 -> 77.8 us, 192 windows 162 -> 153); a
-// smaller one may be found there again (four caches of 3000 to 4000 tokens, 16 heads of 64 columns: 18.1 us, 20.2 with such loads)
+// A pool larger than the last-level cache is taken to be new to it in every step: loads that do not stay there (100003 tokens of 8 heads 81.5 -> 77.8 us, 192 windows 162 -> 153); a
+// smaller one may be found there again (four caches of 3000 to 4000 tokens, 16 heads of 64 columns: 18.1 us, 20.2 with such loads).  How much of a pool a call reads only the
+// device knows, and between two calls for a layer stand those for the others.
 template <class T, int DT>
 static int ad_form(const AdArgs &a, hipStream_t s) {
   const bool nt = (size_t)a.kv.n_layers * a.kv.n_pages * a.kv.n_kv * a.kv.page * a.kv.d * sizeof(T) * 2 > ((size_t)192 << 20), tickets = ad_tickets(&a.kv, a.n_q);

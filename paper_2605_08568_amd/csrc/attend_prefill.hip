@@ -42,9 +42,12 @@ __device__ __forceinline__ int ap_tiles(int n, int group, int tile) { return (in
 // Tiles of 32 tokens are staged in LDS as they stand in the pages, one while the one before it is worked on.  Both products have the cache's side as
 // operand A and the rows as columns: a lane holds weights of one row only, the softmax needs one exchange between lane halves, and what comes out of
 // the first product is what the second takes (K's rows are read in the order that makes it so).
-// Bound: the fp32 matrix instructions, 64 cycles each, 32 a tile and product at 64 columns: 4 x 897 tokens of 16 heads of 128, window 284, 53 TFLOP/s of 154 (133 us; with the
-// one wavefront a SIMD that the compiler takes if left alone 176, 19 x 124 tokens of 32 heads 103 -> 72; 96 columns 183 -> 230, so only at 128), small batches by latency: 4 x 64 tokens of
-// 16 heads of 64 11.2 us, of which two tiles are 4 and what comes before the first 4.  Not kept: twice and four times as many cuts, for the longest row tiles of a causal prompt (2 x 1805
+// Bound: not by a unit.  The matrix units are busy for 31 to 47 % of the time at 64 to 128 columns (4 x 897 tokens of 16 heads of 128, window 284, 126 us, 55 TFLOP/s of 154; 2 x 1805 of
+// 16 heads of 64 272 us, 49; 1 x 2000 of 16 heads of 96 181 us, 68): units run dry while the longest row tile of a causal prompt is worked on (of two wavefronts that a SIMD has room for
+// at 64 and at 128 columns 0.9 and 1.3 are there on average, of the one at 96 0.9), and a wavefront has wait, barrier, first product, softmax and second product of a tile one after another (it waits 23
+// to 39 % of its time).  Wider heads have one wavefront a SIMD; from 192 columns on registers go to memory (256: 596 bytes a lane, the matrix units busy 10 %, 1 x 1500 of 8 heads 492 us, 19 TFLOP/s).
+// Small batches: latency, 4 x 64 tokens of 16 heads of 64 11.3 us, of which two tiles are 4 and what comes before the first 4.  Two wavefronts a SIMD at 128 columns: with the one that the compiler
+// takes if left alone 176 us instead of 133, 19 x 124 tokens of 32 heads 103 -> 72; 96 columns 183 -> 230, so only at 128.  Not kept: twice and four times as many cuts, for the longest row tiles (2 x 1805
 // tokens of 16 heads of 64 272 -> 238 and 213 us, 1 x 1024 of 128 101 -> 86 and 84, but 4 x 897 133 -> 165, 2000 of 96 183 -> 197 and 218: parts are written and read again).
 template <int DT>
 __global__ __launch_bounds__(AP_WAVES * 64, DT == 4 ? 2 : 1) void attend_prefill_f32(ApArgs a) {
@@ -257,8 +260,11 @@ __global__ __launch_bounds__(AP_WAVES * 64, DT == 4 ? 2 : 1) void attend_prefill
 // Of a tile (16 matrix instructions of 32 cycles a wavefront) the softmax takes 45 vector instructions and 16 exponentials, about as long; scalar work was a hundred
 // instructions more before the places of 64 tiles were worked out at once (648 -> 574 us below).  Two wavefronts a SIMD, 128 rows a workgroup and two of them
 // a unit: with 256 rows the eight wavefronts of a unit wait for each other at every tile (650 us and, 8 x 512 tokens, 81 against 607 and 63).
-// Bound: large calls by power (one prompt of 8192 tokens, 32 heads over 8: 519 to 560 us = 0.98 to 1.06 PFLOP/s at 1.67 GHz; with zeros for data 394 us at the full clock; a large
-// library product reaches 1.28), small ones by what a workgroup waits for before its first tile, 4 us: lengths, table, K (8 x 512 tokens of 32 heads 45 us for 135 MB).
+// Bound: large calls by power (one prompt of 8192 tokens, 32 heads over 8: 512 to 560 us = 0.98 to 1.07 PFLOP/s at 1.67 GHz; with zeros for data 394 us at the full clock; a large
+// library product reaches 1.28).  Small ones by what is not a tile: of the time that workgroups have on their units, 8 x 512 tokens of 32 heads (44 us for 135 MB, 16 tiles at most), 35 % go before the
+// first tile (6 us: lengths, then table and q, then K), 51 % on tiles (0.9 us each), 14 % on the stores, and for the last quarter of the call units run dry.  20 ragged prompts
+// with a window: 14, 80 and 5 %, 0.97 us a tile.  One prompt of 2048 tokens, 32 heads over 8 (50 us): every workgroup has its place at once, and the longest row tile, 64 tiles of
+// 0.84 us, is the call.  Wider heads: one workgroup a unit, and from 192 columns on registers go to memory (256: 1032 bytes a lane; 4 x 1000 of 16 heads over 4, 90 us, 363 TFLOP/s).
 // CAREFUL: infinities and NaN of V in places that some rows of the workgroup see and others do not reach only the former (0 times infinity would
 // reach the others).  Without, something that is not finite comes out where they are met: then nothing is stored and the answer is false.
 constexpr int AP_STAGES = 4;                 // tiles of K, and of V, in LDS
