@@ -298,9 +298,9 @@ def _run_own(st):
         if "ws" not in st:
             st["ws"] = pa.attend_shared_workspace(kv, c["heads"], st["q"].shape[0])
         if "shares" not in st:
-            st["shares"] = pa.shared_plan(kv, c["heads"], st["q"].shape[0])
+            st["shares"] = pa.shared_plan(kv, c["heads"], st["q"].shape[0], window=c["window"], sinks=c["sinks"])
         elif c["plan"] == "pass":
-            pa.shared_plan(kv, c["heads"], st["q"].shape[0], plan=st["shares"])
+            pa.shared_plan(kv, c["heads"], st["q"].shape[0], window=c["window"], sinks=c["sinks"], plan=st["shares"])
         return pa.attend_shared(kv, 0, st["q"], st["shares"], window=c["window"], sinks=c["sinks"], with_lse=True, workspace=st["ws"])
     if c["kind"] == "bounds":
         pa.kv_bounds(kv, st["bounds"], 0, st["off"])
