@@ -592,6 +592,86 @@ int parse_attend_prefill(const parse_kv *kv, int32_t layer, const void *q, int64
                          int32_t sinks, void *out, int64_t out_stride, float *lse, void *workspace, size_t workspace_bytes,
                          parse_stream stream);
 
+/* ---- attention of batches that begin alike ----------------------------------------------------------------------------
+ * One new token per sequence as in parse_attend_decode, the same formula, for batches whose sequences hold the same pages at
+ * their front (parse_kv_fork: samples of a prompt, prompts behind one common text): such pages are read once for all of them.
+ * Which pages those are is found out on the device, once for a batch, for all layers and steps:
+ * parse_shared_plan looks at the table's rows.  Up to three runs of pages one behind another (a common text, a prompt, a fork of a
+ * fork), of at least 128 tokens each, may be shared with ever fewer rows; what is behind them a row has for itself.  Any table is
+ * right: rows that do not hold the same pages share nothing.
+ * A plan holds for the rows, n_q, window and sinks that it was made with (a call with others reads every cache for itself) and for every layer,
+ * while sequences grow (parse_kv_reserve, parse_kv_append) and pages behind that window and sinks are given up (parse_kv_trim without keep).  After any other
+ * change of the table or the lengths it is made anew.  The call may be given -1 for sequences that were not served
+ * (parse_kv_reserve_seqs) where the plan had their number.
+ *   seqs       device int32 [rows], the table's row of each, or NULL: the row itself
+ *   plan       device, >= parse_shared_plan_bytes, 16-byte aligned; any contents before.  Read only in parse_attend_shared
+ *   workspace  any contents; one call at a time has it
+ * Limits: rows 1..4096; 3 * (rows * n_q / n_kv / 64 + rows / 2 + 1) + rows * ceil(n_q / n_kv / 64) <= 16384 (with 32 or 16 in the place of 64 for heads wider than
+ * 128 / 256 columns of bf16, 64 / 128 of fp32), and that number times max_pages*page/32 below 2^31 - 2^16; the queries give 0 otherwise, the calls PARSE_ESHAPE.
+ * Other arguments as in parse_attend_decode.  Same inputs and plan, same bits. */
+size_t parse_shared_plan_bytes(const parse_kv *kv, int32_t n_q, int32_t rows);
+int parse_shared_plan(const parse_kv *kv, int32_t n_q, int32_t rows, const int32_t *seqs, int32_t window, int32_t sinks, void *plan, size_t plan_bytes,
+                      parse_stream stream);
+size_t parse_attend_shared_workspace_bytes(const parse_kv *kv, int32_t n_q, int32_t rows);
+int parse_attend_shared(const parse_kv *kv, int32_t layer, const void *q, int64_t q_stride, int32_t n_q, int32_t rows, const int32_t *seqs, const void *plan,
+                        float scale, int32_t window, int32_t sinks, void *out, int64_t out_stride, float *lse, void *workspace, size_t workspace_bytes,
+                        parse_stream stream);
+
+/* ---- attention over selected pages -------------------------------------------------------------------------------------
+ * A long cache is read in part: every new token and kv head takes the pages whose keys may fit its queries best.
+ * parse_kv_bounds keeps, beside the cache, the least and the largest key of every complete page, column by column:
+ *     bounds [n_layers][n_pages][n_kv][2][d] in the cache's dtype (16-byte aligned), least first; NaN where one of the keys is NaN
+ * for the pages that the last tokens of the named sequences complete (tokens as in parse_kv_append, appended before; a page with a place that
+ * holds no token yet is left as it is, it is among the last ones that every token reads).  A page that moves leaves its bounds behind: after parse_kv_compact the call is
+ * made for whole sequences.
+ *   layer        0 <= layer < n_layers, or -1: all layers
+ *   tok_offsets  device int32 [P+1]: tok_offsets[p+1] - tok_offsets[p] last tokens of prompt p's sequence (more than it has: all), or NULL: one each
+ *   seqs         device int32 [P], the table's row of each, or NULL: p;  1 <= P <= 4096, with tok_offsets P * max_pages < 2^31 */
+size_t parse_kv_bounds_bytes(const parse_kv *kv);
+int parse_kv_bounds(const parse_kv *kv, void *bounds, int32_t layer, const int32_t *tok_offsets, const int32_t *seqs, int32_t P, parse_stream stream);
+
+/* The pages that one new token per sequence (its last, as in parse_attend_decode) reads, for every kv head: columns of the table, ascending, -1 behind
+ * the last.  The first `first` and the last `last` pages that the sequence has are always among them (the last one, which may be begun, has no bounds yet); of the others
+ * those with the largest
+ *     score = sum over the kv head's query heads h and columns i of max(q_hi * least_i, q_hi * largest_i),
+ * which no key of the page exceeds, taken over the head's queries together (a column where no q is positive, or none negative, does not look at the largest, or the least);
+ * sums in 64 bits, the lower column first among equals, NaN before all.  A sequence of no more than `top`
+ * pages takes all.  Columns without a page are not taken.
+ *   bounds     as written by parse_kv_bounds;  layer 0 <= layer < n_layers
+ *   q          device [rows][n_q][d], rows q_stride elements apart, 16-byte aligned, as it goes to parse_attend_pages
+ *   top, first, last   first >= 0, last >= 1, first + last <= top
+ *   pages      device int32 [rows][n_kv][top] (rows * n_kv * top < 2^31)
+ *   workspace  any contents; one call at a time has it */
+size_t parse_select_pages_workspace_bytes(const parse_kv *kv, int32_t n_q, int32_t rows);
+int parse_select_pages(const parse_kv *kv, const void *bounds, int32_t layer, const void *q, int64_t q_stride, int32_t n_q, int32_t rows, const int32_t *seqs,
+                       int32_t top, int32_t first, int32_t last, int32_t *pages, void *workspace, size_t workspace_bytes, parse_stream stream);
+
+/* The attention of parse_attend_decode over the listed pages only: a row and kv head see the tokens of the columns in pages[row][kv head][0..top) that the sequence has
+ * (j <= len - 1) and whose page is there.  Columns may stand in any order; -1 and others outside the table are passed over; one that stands twice counts twice.
+ *   pages      device int32 [rows][n_kv][top], 1 <= top, rows * n_kv * top < 2^31, and rows * ceil(n_q / n_kv / 16) * top * page / 32 below 2^31 - 2^16
+ *   workspace  any contents; one call at a time has it
+ * Other arguments as in parse_attend_decode.  Same inputs, same bits. */
+size_t parse_attend_pages_workspace_bytes(const parse_kv *kv, int32_t n_q, int32_t rows, int32_t top);
+int parse_attend_pages(const parse_kv *kv, int32_t layer, const void *q, int64_t q_stride, int32_t n_q, int32_t rows, const int32_t *seqs, const int32_t *pages,
+                       int32_t top, float scale, void *out, int64_t out_stride, float *lse, void *workspace, size_t workspace_bytes, parse_stream stream);
+
+/* ---- norm --------------------------------------------------------------------------------------------------------------
+ * What stands between the residual stream and the projections that read it (and the pooling of the router): for every row
+ *     s = x + residual (in 32 bits),   residual_out = s rounded,   y = s / sqrt(mean of s^2 + eps) * weight
+ * with out = y rounded (scales NULL), or y in 8 bits with a scale for every `block` columns:
+ *     scales[row][b] = max(largest |y| of the block / 448, 2^-120),   out = y / scale rounded to e4m3 (1 sign, 4 exponent, 3 significand bits, no infinity)
+ * so that out times its scale stands for y.  s is not rounded before it is used; squares are summed in 32 bits.  A row that holds a NaN gives NaN.
+ *   x, residual, residual_out  device [rows][d] of dtype, rows *_stride elements apart, pointers and strides on 16 bytes; residual and residual_out may be NULL each, and may be
+ *                              one array; residual_out may be x
+ *   weight      device [d] of weight_dtype, 16-byte aligned
+ *   d           a multiple of 8 up to 65536
+ *   out         scales NULL: dtype, pointer and stride on 16 bytes, may be x.  Otherwise bytes, pointer and stride (in bytes) on 8
+ *   scales      device float [rows][d / block] or NULL;  block: 32, 64, 128, 256 (a divisor of d) or d;  0 without scales
+ *   eps         >= 0 */
+int parse_rmsnorm(const void *x, int64_t x_stride, const void *residual, int64_t residual_stride, void *residual_out, int64_t residual_out_stride, int32_t dtype,
+                  const void *weight, int32_t weight_dtype, int32_t rows, int32_t d, float eps, void *out, int64_t out_stride, float *scales, int32_t block,
+                  parse_stream stream);
+
 /* ---- achievable-peak probes (measurement only) ---------------------------------------------------------------
  * Kernels with nothing but the resource a roofline prices: the caller times them with HIP events on its stream and
  * reports the rates beside the nominal peaks (MI355X: 2.5 PFLOP/s dense bf16, 8 TB/s HBM).  They only enqueue.

@@ -15,4 +15,6 @@ from .binding import (  # noqa: F401
     decode_plan, lowrank_decode_planned, lowrank_decode_planned_workspace_bytes,
     KV, kv_append, kv_clear, kv_compact, kv_fork, kv_reserve, kv_trim, kv_workspace,
     attend_decode, attend_decode_workspace, attend_prefill, attend_prefill_workspace,
+    attend_shared, attend_shared_workspace, shared_plan, shared_plan_bytes,
+    kv_bounds, kv_bounds_empty, select_pages, select_pages_workspace, attend_pages, attend_pages_workspace, rmsnorm,
 )

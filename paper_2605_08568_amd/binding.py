@@ -151,6 +151,18 @@ def lib():
     L.parse_attend_decode.argtypes = [kvp, i32, vp, i64, i32, i32, vp, f32, i32, i32, vp, i64, vp, vp, sz, vp]
     L.parse_attend_prefill.restype = C.c_int
     L.parse_attend_prefill.argtypes = [kvp, i32, vp, i64, i32, i32, vp, vp, i32, f32, i32, i32, vp, i64, vp, vp, sz, vp]
+    for name, args in [("shared_plan_bytes", [kvp, i32, i32]), ("attend_shared_workspace_bytes", [kvp, i32, i32]), ("kv_bounds_bytes", [kvp]),
+                       ("select_pages_workspace_bytes", [kvp, i32, i32]), ("attend_pages_workspace_bytes", [kvp, i32, i32, i32])]:
+        f = getattr(L, "parse_" + name)
+        f.restype = sz; f.argtypes = args
+    for name, args in [("shared_plan", [kvp, i32, i32, vp, i32, i32, vp, sz, vp]),
+                       ("attend_shared", [kvp, i32, vp, i64, i32, i32, vp, vp, f32, i32, i32, vp, i64, vp, vp, sz, vp]),
+                       ("kv_bounds", [kvp, vp, i32, vp, vp, i32, vp]),
+                       ("select_pages", [kvp, vp, i32, vp, i64, i32, i32, vp, i32, i32, i32, vp, vp, sz, vp]),
+                       ("attend_pages", [kvp, i32, vp, i64, i32, i32, vp, vp, i32, f32, vp, i64, vp, vp, sz, vp]),
+                       ("rmsnorm", [vp, i64, vp, i64, vp, i64, i32, vp, i32, i32, i32, f32, vp, i64, vp, i32, vp])]:
+        f = getattr(L, "parse_" + name)
+        f.restype = C.c_int; f.argtypes = args
     _lib = L
     return L
 
@@ -841,3 +853,127 @@ def attend_prefill(kv: KV, layer: int, q, tok_offsets=None, seqs=None, scale=Non
                                        kv.d ** -0.5 if scale is None else scale, window, sinks, out, out_stride, lse, workspace,
                                        workspace.numel(), _stream()), "parse_attend_prefill")
     return (out, lse) if with_lse else out
+
+
+# ---- decoding of batches that begin alike ---------------------------------------------------------------------------
+def shared_plan_bytes(kv: KV, n_q: int, rows: int) -> int:
+    return int(lib().parse_shared_plan_bytes(C.byref(kv.c()), n_q, rows))
+
+
+def shared_plan(kv: KV, n_q: int, rows: int, seqs=None, window: int = 0, sinks: int = 0, plan=None):
+    """parse_shared_plan: which pages the sequences seqs [rows] (None: 0 .. rows-1) hold in common -> plan, for attend_shared with the same
+    rows, n_q, window and sinks, in all layers and steps until the table changes otherwise than by growth and that window's trimming."""
+    if plan is None:
+        plan = torch.empty(max(shared_plan_bytes(kv, n_q, rows), 256), dtype=torch.uint8, device=kv.K.device)
+    _check(_calls.parse_shared_plan(kv, n_q, rows, _ints(seqs, rows, "seqs"), window, sinks, plan, plan.numel(), _stream()), "parse_shared_plan")
+    return plan
+
+
+def attend_shared_workspace(kv: KV, n_q: int, rows: int):
+    """Workspace of attend_shared, any contents.  One call at a time has it."""
+    return torch.empty(max(int(lib().parse_attend_shared_workspace_bytes(C.byref(kv.c()), n_q, rows)), 256), dtype=torch.uint8, device=kv.K.device)
+
+
+def attend_shared(kv: KV, layer: int, q, plan, seqs=None, scale=None, window: int = 0, sinks: int = 0, out=None, lse=None, with_lse=False, workspace=None):
+    """parse_attend_shared: attend_decode for sequences that begin with the same pages, which are read once for all of them (plan: shared_plan)."""
+    rows, n_q = q.shape[:2]
+    q_stride = _rows_of(q, kv, n_q, "q")
+    if plan.numel() * plan.element_size() < shared_plan_bytes(kv, n_q, rows):
+        raise ValueError("the plan is smaller than shared_plan_bytes(kv, n_q, rows)")
+    out, out_stride, lse = _attend_out(kv, q, n_q, q_stride, out, lse, with_lse)
+    if workspace is None:
+        workspace = attend_shared_workspace(kv, n_q, rows)
+    _check(_calls.parse_attend_shared(kv, layer, q, q_stride, n_q, rows, _ints(seqs, rows, "seqs"), plan, kv.d ** -0.5 if scale is None else scale, window,
+                                      sinks, out, out_stride, lse, workspace, workspace.numel(), _stream()), "parse_attend_shared")
+    return (out, lse) if with_lse else out
+
+
+# ---- attention over selected pages ---------------------------------------------------------------------------------
+def _bounds(kv, bounds):
+    if bounds.dtype is not kv.K.dtype or tuple(bounds.shape) != (kv.n_layers, kv.n_pages, kv.n_kv, 2, kv.d) or not bounds.is_contiguous():
+        raise ValueError(f"bounds: contiguous [{kv.n_layers}][{kv.n_pages}][{kv.n_kv}][2][{kv.d}] of the cache's dtype is wanted, got {tuple(bounds.shape)} {bounds.dtype}")
+    return bounds
+
+
+def kv_bounds_empty(kv: KV):
+    """Room for the bounds of all pages, as they come."""
+    return torch.empty((kv.n_layers, kv.n_pages, kv.n_kv, 2, kv.d), dtype=kv.K.dtype, device=kv.K.device)
+
+
+def kv_bounds(kv: KV, bounds, layer: int, tok_offsets=None, seqs=None):
+    """parse_kv_bounds: least and largest keys of the pages that the sequences' last tokens complete (tok_offsets as in kv_append; None: one token
+    each), of a layer or (-1) of all.  Returns bounds."""
+    P = tok_offsets.numel() - 1 if tok_offsets is not None else kv.n_seqs if seqs is None else seqs.numel()
+    _check(_calls.parse_kv_bounds(kv, _bounds(kv, bounds), layer, _ints(tok_offsets, P + 1, "tok_offsets"), _ints(seqs, P, "seqs"), P, _stream()), "parse_kv_bounds")
+    return bounds
+
+
+def select_pages_workspace(kv: KV, n_q: int, rows: int):
+    return torch.empty(max(int(lib().parse_select_pages_workspace_bytes(C.byref(kv.c()), n_q, rows)), 256), dtype=torch.uint8, device=kv.K.device)
+
+
+def _pages(kv, pages, rows, top=None):
+    if pages.dtype is not torch.int32 or pages.dim() != 3 or pages.shape[:2] != (rows, kv.n_kv) or (top is not None and pages.shape[2] != top) or not pages.is_contiguous():
+        raise ValueError(f"pages: contiguous int32 [{rows}][{kv.n_kv}][{'top' if top is None else top}] is wanted, got {tuple(pages.shape)} {pages.dtype}")
+    return pages
+
+
+def select_pages(kv: KV, layer: int, bounds, q, top: int, first: int = 1, last: int = 1, seqs=None, pages=None, workspace=None):
+    """parse_select_pages: q [rows][n_q][d], the last token of each sequence -> pages int32 [rows][n_kv][top], the table's columns that attend_pages reads."""
+    rows, n_q = q.shape[:2]
+    q_stride = _rows_of(q, kv, n_q, "q")
+    if pages is None:
+        pages = torch.empty((rows, kv.n_kv, max(top, 0)), dtype=torch.int32, device=q.device)
+    if workspace is None:
+        workspace = select_pages_workspace(kv, n_q, rows)
+    _check(_calls.parse_select_pages(kv, _bounds(kv, bounds), layer, q, q_stride, n_q, rows, _ints(seqs, rows, "seqs"), top, first, last,
+                                     _pages(kv, pages, rows, max(top, 0)), workspace, workspace.numel(), _stream()), "parse_select_pages")
+    return pages
+
+
+def attend_pages_workspace(kv: KV, n_q: int, rows: int, top: int):
+    return torch.empty(max(int(lib().parse_attend_pages_workspace_bytes(C.byref(kv.c()), n_q, rows, top)), 256), dtype=torch.uint8, device=kv.K.device)
+
+
+def attend_pages(kv: KV, layer: int, q, pages, seqs=None, scale=None, out=None, lse=None, with_lse=False, workspace=None):
+    """parse_attend_pages: attend_decode over the columns pages [rows][n_kv][top] of each sequence's table alone."""
+    rows, n_q = q.shape[:2]
+    q_stride = _rows_of(q, kv, n_q, "q")
+    top = _pages(kv, pages, rows).shape[2]
+    out, out_stride, lse = _attend_out(kv, q, n_q, q_stride, out, lse, with_lse)
+    if workspace is None:
+        workspace = attend_pages_workspace(kv, n_q, rows, top)
+    _check(_calls.parse_attend_pages(kv, layer, q, q_stride, n_q, rows, _ints(seqs, rows, "seqs"), pages, top, kv.d ** -0.5 if scale is None else scale, out,
+                                     out_stride, lse, workspace, workspace.numel(), _stream()), "parse_attend_pages")
+    return (out, lse) if with_lse else out
+
+
+# ---- norm ------------------------------------------------------------------------------------------------------------
+def _row_stride(t, rows, d, what):
+    if t.dim() != 2 or tuple(t.shape) != (rows, d) or (t.stride(1) != 1 and d > 1):
+        raise ValueError(f"{what}: [{rows}][{d}] with adjacent columns is wanted, got {tuple(t.shape)}, strides {t.stride()}")
+    return t.stride(0) if rows > 1 else max(t.stride(0), d)
+
+
+def rmsnorm(x, weight, eps: float, residual=None, residual_out=None, out=None, scales=None):
+    """parse_rmsnorm: (x + residual) / root of its mean square, times weight -> out [rows][d]; residual_out takes x + residual.  With scales (float32
+    [rows][d / block]) out is torch.float8_e4m3fn, out * scales the values."""
+    rows, d = x.shape
+    dtype = _dtype_code(x)
+    block = 0
+    if scales is not None:
+        if scales.dtype is not torch.float32 or scales.dim() != 2 or scales.shape[0] != rows or not scales.is_contiguous() or scales.shape[1] < 1 or d % scales.shape[1]:
+            raise ValueError(f"scales: contiguous float32 [{rows}][blocks of the {d} columns] is wanted, got {tuple(scales.shape)} {scales.dtype}")
+        block = d // scales.shape[1]
+    wanted = x.dtype if scales is None else torch.float8_e4m3fn
+    if out is None:
+        out = torch.empty((rows, d), dtype=wanted, device=x.device)
+    for t, of, what in ((residual, x.dtype, "residual"), (residual_out, x.dtype, "residual_out"), (out, wanted, "out")):
+        if t is not None and t.dtype is not of:
+            raise TypeError(f"{what}: {of} is wanted, got {t.dtype}")
+    if weight.shape != (d,) or not weight.is_contiguous():
+        raise ValueError(f"weight: contiguous [{d}] is wanted, got {tuple(weight.shape)}")
+    _check(_calls.parse_rmsnorm(x, _row_stride(x, rows, d, "x"), residual, 0 if residual is None else _row_stride(residual, rows, d, "residual"), residual_out,
+                                0 if residual_out is None else _row_stride(residual_out, rows, d, "residual_out"), dtype, weight, _dtype_code(weight), rows, d, eps,
+                                out, _row_stride(out, rows, d, "out"), scales, block, _stream()), "parse_rmsnorm")
+    return out

@@ -1,0 +1,320 @@
+// Attention of one new token per sequence for batches that begin alike (parse_shared_plan, parse_attend_shared): pages that several sequences of a
+// call hold at their front are read once for all of them.
+#include <algorithm>
+#include <type_traits>
+
+#include "attend_parts.hpp"
+
+namespace parse {
+
+constexpr int SH_THREADS = 256, SH_ONE = 1024;
+constexpr int SH_LEAST = 128;                        // tokens of a run that is worth a tile: a step a wavefront
+
+// ---- the plan: which rows hold the same pages ------------------------------------------------------------------------
+// Only whole pages in front of a row's last token count (those stay as they are while the sequence grows), and of them what the row sees or a later token of it
+// will see.  owner[page]: the shortest of the rows that hold it (of equal ones the first); users[page]: how many do.
+struct ShRow {
+  KvSeq seq;
+  int columns, lo, page, sinks;
+  bool windowed;
+  __device__ __forceinline__ bool cares(int c) const { return !windowed || (int64_t)c * page < sinks || (c + 1) * page > lo; }
+};
+__device__ __forceinline__ ShRow sh_row(const parse_kv &kv, const int32_t *seqs, int row, int window, int sinks) {
+  ShRow r;
+  r.seq = kv_seq(kv, seqs, row);
+  r.columns = r.seq.len > 0 ? min((r.seq.len - 1) / kv.page, kv.max_pages) : 0;
+  r.lo = kv_window_begin(r.seq.len - 1, window);
+  r.page = kv.page; r.sinks = sinks; r.windowed = window > 0;
+  return r;
+}
+
+template <bool COUNT>
+__global__ __launch_bounds__(SH_THREADS) void shared_count(parse_kv kv, const int32_t *__restrict__ seqs, int window, int sinks, PtPlan plan) {
+  const int row = blockIdx.y;
+  const ShRow r = sh_row(kv, seqs, row, window, sinks);
+  const int32_t *table = kv.table + (int64_t)r.seq.row * kv.max_pages;
+  for (int c = blockIdx.x * SH_THREADS + threadIdx.x; c < r.columns; c += gridDim.x * SH_THREADS) {
+    if (!r.cares(c)) continue;
+    const int id = table[c];
+    if ((unsigned)id >= (unsigned)kv.n_pages) continue;
+    if (COUNT) {
+      atomicMin(&plan.owner[id], (unsigned long long)(uint32_t)r.seq.len << 32 | (uint32_t)row);
+      atomicAdd(&plan.users[id], 1);
+    } else {
+      plan.owner[id] = ~0ull;
+      plan.users[id] = 0;
+    }
+  }
+}
+
+// A wavefront walks a row's columns.  A run ends where the pages have another owner or fewer users; one of two users and more that is long enough (with what
+// shorter ones left before it: their rows hold that too) is the row's next level.  Then the columns are compared with the owner's: the row takes part as far as they agree.
+__global__ __launch_bounds__(SH_THREADS) void shared_walk(parse_kv kv, const int32_t *__restrict__ seqs, int rows, int window, int sinks, PtPlan plan) {
+  const int row = blockIdx.x * (SH_THREADS / 64) + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (row >= rows) return;
+  const ShRow r = sh_row(kv, seqs, row, window, sinks);
+  const int32_t *table = kv.table + (int64_t)r.seq.row * kv.max_pages;
+  int4 found[PT_LEVELS];
+#pragma unroll
+  for (int l = 0; l < PT_LEVELS; ++l) found[l] = int4{0, 0, -1, 0};
+  int level = 0, from = 0, have = 0, owner = -2, users = 0;        // from: tokens; have: columns since then that the row cares for
+  auto ends = [&](int c, int now) {                                // the run before column c, with `now` columns
+    const int to = c * kv.page & ~(PT_STEP - 1);
+    if (users < 2 || owner < 0 || (int64_t)now * kv.page < SH_LEAST || to <= from || level >= PT_LEVELS) return false;
+#pragma unroll
+    for (int l = 0; l < PT_LEVELS; ++l)
+      if (l == level) found[l] = int4{from, to, owner, 1};
+    ++level;
+    from = to;
+    return true;
+  };
+  for (int c0 = 0; c0 < r.columns; c0 += 64) {
+    const int c = c0 + lane;
+    const bool care = c < r.columns && r.cares(c);
+    int o = -1, k = 0;
+    if (care) {
+      const int id = table[c];
+      if ((unsigned)id < (unsigned)kv.n_pages) { o = (int)(uint32_t)plan.owner[id]; k = plan.users[id]; }
+    }
+    const uint64_t cared = __ballot(care), below = cared & ((1ull << lane) - 1);
+    const int prev = below ? 63 - __builtin_clzll(below) : 0;
+    int po = __shfl(o, prev, 64), pk = __shfl(k, prev, 64);
+    if (!below) { po = owner; pk = users; }
+    uint64_t breaks = __ballot(care && (o != po || k < pk));
+    int counted = 0;                                               // lanes before this one are in `have`
+    while (breaks) {
+      const int b = __builtin_ctzll(breaks);
+      breaks &= breaks - 1;
+      have += __popcll(cared & ((1ull << b) - 1) & ~((1ull << counted) - 1));
+      counted = b;
+      owner = __builtin_amdgcn_readlane(po, b);
+      users = __builtin_amdgcn_readlane(pk, b);
+      if (ends(c0 + b, have)) have = (c0 + b) * kv.page > from ? 1 : 0;
+    }
+    have += __popcll(cared & ~((1ull << counted) - 1));
+    if (cared) {
+      const int at = 63 - __builtin_clzll(cared);
+      owner = __builtin_amdgcn_readlane(o, at);
+      users = __builtin_amdgcn_readlane(k, at);
+    }
+  }
+  ends(r.columns, have);
+#pragma unroll
+  for (int l = 0; l < PT_LEVELS; ++l) {
+    if (l >= level) break;
+    const int lead = found[l].z;
+    if (lead == row) continue;
+    const ShRow of = sh_row(kv, seqs, (unsigned)lead < (unsigned)rows ? lead : row, window, sinks);
+    const int32_t *other = kv.table + (int64_t)of.seq.row * kv.max_pages;
+    bool same = true;
+    for (int c = found[l].x / kv.page + lane; c < found[l].y / kv.page; c += 64) {
+      if (!r.cares(c)) continue;
+      const int x = table[c], y = other[c];
+      same &= x == y || ((unsigned)x >= (unsigned)kv.n_pages && (unsigned)y >= (unsigned)kv.n_pages);
+    }
+    if (!__all(same)) level = l;
+  }
+  if (lane < PT_LEVELS) {
+    int4 w = found[0];
+#pragma unroll
+    for (int l = 1; l < PT_LEVELS; ++l)
+      if (lane == l) w = found[l];
+    if (lane >= level) w.w = 0;
+    plan.walk[(int64_t)row * PT_LEVELS + lane] = w;
+  }
+}
+
+// One workgroup: the rows that agree with their owner become its group, groups of two and more get tiles, level after level.  A thread has PER consecutive rows.
+__global__ __launch_bounds__(SH_ONE) void shared_tiles(parse_kv kv, const int32_t *__restrict__ seqs, int rows, int group, int TC, int window, int sinks, PtPlan plan) {
+  extern __shared__ int words[];
+  int *lead = words, *users = lead + rows, *tile0 = users + rows, *list0 = tile0 + rows, *base0 = list0 + rows, *chain = base0 + rows;
+  __shared__ int sums[3][SH_ONE / 64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, per = (rows + SH_ONE - 1) / SH_ONE;
+  const int r0 = tid * per, r1 = min(r0 + per, rows);
+  for (int r = r0; r < r1; ++r) {
+    chain[r] = 1;
+    plan.row[r] = PtRow{0, 0, {0, 0, 0}, {0, 0, 0}};
+  }
+  int tiles = 0, listed = 0, columns = 0;
+  for (int l = 0; l < PT_LEVELS; ++l) {
+    __syncthreads();
+    for (int r = r0; r < r1; ++r) {
+      const int4 w = plan.walk[(int64_t)r * PT_LEVELS + l];
+      int of = -1;
+      if (chain[r] && w.w && (unsigned)w.z < (unsigned)rows) {
+        const int4 o = plan.walk[(int64_t)w.z * PT_LEVELS + l];
+        if (chain[w.z] && o.w && o.z == w.z && o.x == w.x && o.y == w.y) of = w.z;
+      }
+      lead[r] = of;
+      users[r] = 0;
+    }
+    __syncthreads();
+    for (int r = r0; r < r1; ++r)
+      if (lead[r] >= 0) atomicAdd(&users[lead[r]], 1);
+    __syncthreads();
+    for (int r = r0; r < r1; ++r) {
+      const int of = lead[r];
+      if (of >= 0 && users[of] < 2) lead[r] = -1;                  // its owner alone: nobody else looks at this word before the barrier but as a rank's
+    }
+    __syncthreads();
+    int mine[3] = {0, 0, 0};
+    for (int r = r0; r < r1; ++r) {
+      chain[r] = lead[r] >= 0;
+      if (lead[r] == r) {
+        tile0[r] = mine[0]; list0[r] = mine[1]; base0[r] = mine[2];
+        mine[0] += (users[r] * group + TC - 1) / TC;
+        mine[1] += users[r];
+        mine[2] += users[r] * group;
+      }
+    }
+    int before[3], total[3];
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      before[k] = wave_scan(mine[k]);
+      if (lane == 63) sums[k][wave] = before[k];
+      before[k] -= mine[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      total[k] = 0;
+      for (int w = 0; w < SH_ONE / 64; ++w) { before[k] += w < wave ? sums[k][w] : 0; total[k] += sums[k][w]; }
+    }
+    for (int r = r0; r < r1; ++r)
+      if (lead[r] == r) { tile0[r] += tiles + before[0]; list0[r] += listed + before[1]; base0[r] += columns + before[2]; }
+    __syncthreads();
+    for (int r = r0; r < r1; ++r) {
+      const int of = lead[r];
+      if (of < 0) continue;
+      int rank = 0;
+      for (int i = 0; i < r; ++i) rank += lead[i] == of ? 1 : 0;
+      const int4 w = plan.walk[(int64_t)r * PT_LEVELS + l];
+      plan.list[list0[of] + rank] = r;
+      plan.row[r].from = w.y;
+      plan.row[r].levels = l + 1;
+      plan.row[r].tile[l] = tile0[of];
+      plan.row[r].column[l] = rank * group;
+      if (of == r) {
+        const int all = users[r] * group, pos = kv_seq(kv, seqs, r).len - 1;
+        for (int f = 0, t = tile0[r]; f < all; f += TC, ++t)
+          plan.tile[t] = PtTile{list0[r], users[r], f, min(TC, all - f), w.x, w.y, base0[r] + f, pos};
+      }
+    }
+    tiles += total[0]; listed += total[1]; columns += total[2];
+  }
+  if (tid == 0) {
+    PtHead h{};
+    h.rows = rows; h.group = group; h.columns = TC; h.window = window; h.sinks = sinks; h.n_pages = kv.n_pages; h.max_pages = kv.max_pages; h.page = kv.page;
+    h.tiles = tiles; h.tile_columns = columns;
+    *plan.head = h;
+  }
+}
+
+// ---- the call
+constexpr int AS_GROUPS = 256;                       // a workgroup for each compute unit
+
+template <class T, int DT> static int as_go(const PtArgs &a, int64_t entries, hipStream_t s) { return pt_launch<T, DT, pt_blocks<T, DT>(), false>(a, entries, s); }
+template <class T>
+static int as_width(const PtArgs &a, int64_t entries, hipStream_t s) {
+  switch (a.kv.d / 32) {
+    case 1: return as_go<T, 1>(a, entries, s);
+    case 2: return as_go<T, 2>(a, entries, s);
+    case 3: return as_go<T, 3>(a, entries, s);
+    case 4: return as_go<T, 4>(a, entries, s);
+    case 5: return as_go<T, 5>(a, entries, s);
+    case 6: return as_go<T, 6>(a, entries, s);
+    case 7: return as_go<T, 7>(a, entries, s);
+    default: return as_go<T, 8>(a, entries, s);
+  }
+}
+
+// Entries of a call at most; a kv head's columns of parts; 0 where the call is refused
+struct AsSize {
+  int64_t tiles, entries, columns;
+  size_t bytes;
+};
+static bool as_size(const parse_kv *kv, int n_q, int rows, AsSize &z) {
+  if (n_q <= 0 || n_q % kv->n_kv != 0 || n_q > 65536 || rows <= 0 || rows > KV_MAXSEQ || (int64_t)rows * n_q > INT32_MAX) return false;
+  const int group = n_q / kv->n_kv, TC = pt_columns(kv->d, kv->dtype);
+  z.tiles = pt_most_tiles(rows, group, TC);
+  z.entries = z.tiles + (int64_t)rows * ((group + TC - 1) / TC);
+  z.columns = (int64_t)pt_shares(kv->n_kv, AS_GROUPS) * TC + (int64_t)(PT_LEVELS + 1) * rows * group;
+  z.bytes = pt_deal_bytes(z.entries) + round_up((size_t)z.columns * kv->n_kv * (kv->d + 4) * 4, 256);
+  return z.entries <= PT_MAXENTRIES;
+}
+
+}  // namespace parse
+
+extern "C" {
+
+using namespace parse;
+
+size_t parse_shared_plan_bytes(const parse_kv *kv, int32_t n_q, int32_t rows) {
+  AsSize z;
+  if (check_kv(kv, false) != PARSE_OK || !as_size(kv, n_q, rows, z)) return 0;
+  return pt_plan(kv, rows, n_q / kv->n_kv, nullptr).bytes;
+}
+
+int parse_shared_plan(const parse_kv *kv, int32_t n_q, int32_t rows, const int32_t *seqs, int32_t window, int32_t sinks, void *plan, size_t plan_bytes,
+                      parse_stream stream) {
+  const int st = check_kv(kv, false);
+  if (st != PARSE_OK) return st;
+  if (n_q <= 0 || rows <= 0 || window < 0 || sinks < 0) return PARSE_EINVAL;
+  AsSize z;
+  if (!as_size(kv, n_q, rows, z) || (!seqs && rows > kv->n_seqs)) return PARSE_ESHAPE;
+  if (!aligned4(seqs)) return PARSE_EALIGN;
+  const int group = n_q / kv->n_kv;
+  if (!plan || plan_bytes < pt_plan(kv, rows, group, nullptr).bytes) return PARSE_EWORKSPACE;
+  if (!aligned16(plan)) return PARSE_EALIGN;
+  const PtPlan p = pt_plan(kv, rows, group, plan);
+  hipStream_t s = (hipStream_t)stream;
+  const dim3 grid((uint32_t)std::min<int64_t>((kv->max_pages + SH_THREADS - 1) / SH_THREADS, std::max(1, 4096 / rows)), rows);
+  shared_count<false><<<grid, SH_THREADS, 0, s>>>(*kv, seqs, window, sinks, p);
+  PARSE_LAUNCH_CHECK();
+  shared_count<true><<<grid, SH_THREADS, 0, s>>>(*kv, seqs, window, sinks, p);
+  PARSE_LAUNCH_CHECK();
+  shared_walk<<<dim3((rows + SH_THREADS / 64 - 1) / (SH_THREADS / 64)), SH_THREADS, 0, s>>>(*kv, seqs, rows, window, sinks, p);
+  PARSE_LAUNCH_CHECK();
+  const size_t lds = (size_t)rows * 6 * 4;
+  PARSE_ALLOW_LDS(shared_tiles, 3 * SH_ONE / 64 * 4, lds);
+  shared_tiles<<<dim3(1), SH_ONE, lds, s>>>(*kv, seqs, rows, group, pt_columns(kv->d, kv->dtype), window, sinks, p);
+  PARSE_LAUNCH_CHECK();
+  return PARSE_OK;
+}
+
+size_t parse_attend_shared_workspace_bytes(const parse_kv *kv, int32_t n_q, int32_t rows) {
+  AsSize z;
+  return check_kv(kv, false) == PARSE_OK && as_size(kv, n_q, rows, z) ? z.bytes : 0;
+}
+
+int parse_attend_shared(const parse_kv *kv, int32_t layer, const void *q, int64_t q_stride, int32_t n_q, int32_t rows, const int32_t *seqs, const void *plan,
+                        float scale, int32_t window, int32_t sinks, void *out, int64_t out_stride, float *lse, void *workspace, size_t workspace_bytes,
+                        parse_stream stream) {
+  const int st = check_attend(kv, layer, q, q_stride, n_q, rows, nullptr, seqs, scale, window, sinks, out, out_stride, lse);
+  if (st != PARSE_OK) return st;
+  if (!plan) return PARSE_EINVAL;
+  AsSize z;
+  if (!as_size(kv, n_q, rows, z) || (!seqs && rows > kv->n_seqs)) return PARSE_ESHAPE;
+  // the steps of all entries are added up in an int
+  if (z.entries * (((int64_t)kv->max_pages * kv->page + PT_STEP - 1) / PT_STEP) > INT32_MAX - 65536) return PARSE_ESHAPE;
+  if (!workspace || workspace_bytes < z.bytes) return PARSE_EWORKSPACE;
+  if (!aligned16(workspace) || !aligned16(plan)) return PARSE_EALIGN;
+  const size_t at = (size_t)layer * kv->n_pages * kv->n_kv * kv->page * kv->d * elem_size(kv->dtype);
+  const int TC = pt_columns(kv->d, kv->dtype);
+  PtArgs a{};
+  a.kv = *kv;
+  a.K = (const char *)kv->K + at; a.V = (const char *)kv->V + at;
+  a.q = q; a.out = out; a.lse = lse; a.seqs = seqs;
+  a.q_stride = q_stride; a.out_stride = out_stride;
+  a.n_q = n_q; a.group = n_q / kv->n_kv; a.rows = rows; a.window = window; a.sinks = sinks;
+  a.shares = pt_shares(kv->n_kv, AS_GROUPS);
+  a.per_row = (a.group + TC - 1) / TC;
+  at_scale(scale, a.scale, a.lag, a.q_sign);
+  a.plan = pt_plan(kv, rows, a.group, plan);
+  a.most_tiles = (int)z.tiles;
+  a.deal = (int32_t *)workspace;
+  a.part = (float *)((char *)workspace + pt_deal_bytes(z.entries));
+  return kv->dtype == PARSE_BF16 ? as_width<uint16_t>(a, z.entries, (hipStream_t)stream) : as_width<float>(a, z.entries, (hipStream_t)stream);
+}
+
+}  // extern "C"

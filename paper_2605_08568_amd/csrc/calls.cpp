@@ -192,7 +192,8 @@ PyMethodDef methods[] = {
     CALL(parse_pack_ranks), CALL(parse_lowrank_forward), CALL(parse_lowrank_prefill_planned), CALL_SEVERAL(parse_lowrank_prefill_multi),
     CALL_SEVERAL(parse_lowrank_decode_planned), CALL_SEVERAL(parse_lowrank_decode_multi), CALL(parse_router_grad),
     CALL(parse_kv_clear), CALL(parse_kv_fork), CALL(parse_kv_reserve), CALL(parse_kv_reserve_seqs), CALL(parse_kv_trim), CALL(parse_kv_compact), CALL(parse_kv_append),
-    CALL(parse_attend_decode), CALL(parse_attend_prefill),
+    CALL(parse_attend_decode), CALL(parse_attend_prefill), CALL(parse_shared_plan), CALL(parse_attend_shared), CALL(parse_kv_bounds), CALL(parse_select_pages),
+    CALL(parse_attend_pages), CALL(parse_rmsnorm),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
