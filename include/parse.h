@@ -606,8 +606,8 @@ int parse_attend_prefill(const parse_kv *kv, int32_t layer, const void *q, int64
  *   seqs       device int32 [rows], the table's row of each, or NULL: the row itself
  *   plan       device, >= parse_shared_plan_bytes, 16-byte aligned; any contents before.  Read only in parse_attend_shared
  *   workspace  any contents; one call at a time has it
- * Limits: rows 1..4096; 3 * (rows * n_q / n_kv / 64 + rows / 2 + 1) + rows * ceil(n_q / n_kv / 64) <= 16384 (with 32 or 16 in the place of 64 for heads wider than
- * 128 / 256 columns of bf16, 64 / 128 of fp32), and that number times max_pages*page/32 below 2^31 - 2^16; the queries give 0 otherwise, the calls PARSE_ESHAPE.
+ * Limits: rows 1..4096; 3 * (rows * n_q / n_kv / C + rows / 2 + 1) + rows * ceil(n_q / n_kv / C) <= 16384 with C = 128 (64 for heads wider than 128 columns of bf16, 64 of
+ * fp32), and that number times max_pages*page/32 below 2^31 - 2^16; the queries give 0 otherwise, the calls PARSE_ESHAPE.
  * Other arguments as in parse_attend_decode.  Same inputs and plan, same bits. */
 size_t parse_shared_plan_bytes(const parse_kv *kv, int32_t n_q, int32_t rows);
 int parse_shared_plan(const parse_kv *kv, int32_t n_q, int32_t rows, const int32_t *seqs, int32_t window, int32_t sinks, void *plan, size_t plan_bytes,
@@ -648,7 +648,7 @@ int parse_select_pages(const parse_kv *kv, const void *bounds, int32_t layer, co
 
 /* The attention of parse_attend_decode over the listed pages only: a row and kv head see the tokens of the columns in pages[row][kv head][0..top) that the sequence has
  * (j <= len - 1) and whose page is there.  Columns may stand in any order; -1 and others outside the table are passed over; one that stands twice counts twice.
- *   pages      device int32 [rows][n_kv][top], 1 <= top, rows * n_kv * top < 2^31, and rows * ceil(n_q / n_kv / 16) * top * page / 32 below 2^31 - 2^16
+ *   pages      device int32 [rows][n_kv][top], 1 <= top, rows * n_kv * top < 2^31, and rows * ceil(n_q / n_kv / 64) * top * page / 32 below 2^31 - 2^16
  *   workspace  any contents; one call at a time has it
  * Other arguments as in parse_attend_decode.  Same inputs, same bits. */
 size_t parse_attend_pages_workspace_bytes(const parse_kv *kv, int32_t n_q, int32_t rows, int32_t top);

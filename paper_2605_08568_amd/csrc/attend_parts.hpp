@@ -8,6 +8,8 @@
 // columns' running maximum, sum of weights and weighted sum of V over the tokens that the share has of it.  Parts stand at column x * TC + base[e] of the
 // workspace (base: columns of the entries before), which no two of them have in common.
 #pragma once
+#include <type_traits>
+
 #include "attend.hpp"
 
 namespace parse {
@@ -17,9 +19,14 @@ constexpr int PT_STEP = 32;
 constexpr int PT_LEVELS = 3;                         // runs of shared pages that a row may have one behind another
 constexpr int PT_MAXENTRIES = 16384;
 
-// Columns of a tile, in blocks of sixteen: what the registers hold of q and of the sums beside a step of K and V
-template <class T, int DT> constexpr int pt_blocks() { return DT * (int)sizeof(T) <= 8 ? 4 : DT * (int)sizeof(T) <= 16 ? 2 : 1; }
-static inline int pt_columns(int d, int dtype) { const int w = d / 32 * elem_size(dtype); return 16 * (w <= 8 ? 4 : w <= 16 ? 2 : 1); }
+// Blocks of sixteen columns that a wavefront has of a wide entry: what the registers hold of q and of the sums beside a step of K and V.  The four wavefronts make TC columns.
+template <class T, int DT> constexpr int pt_blocks() { return DT * (int)sizeof(T) <= 8 ? 2 : 1; }
+static inline int pt_columns(int d, int dtype) { return 64 * (d / 32 * elem_size(dtype) <= 8 ? 2 : 1); }
+// Steps in LDS, the one that is worked on and those on their way: 64 KiB of them where two fit
+template <class T, int DT> constexpr int pt_step_bytes() { return 2 * PT_STEP * DT * 32 * (int)sizeof(T); }
+template <class T, int DT> constexpr int pt_stages() { return pt_step_bytes<T, DT>() >= 32768 ? 2 : pt_step_bytes<T, DT>() > 16384 ? 3 : 4; }
+// Workgroups that a compute unit has at once
+template <class T, int DT> constexpr int pt_at_once() { return DT * (int)sizeof(T) <= 8 ? 2 : 1; }
 
 // ---- the plan's words
 struct PtTile {
@@ -105,13 +112,17 @@ __device__ __forceinline__ PtSpan pt_span(int i0, int from, int to, int window, 
 }
 
 // The shortest sequence of a tile's rows: its table's row (its window reaches back the furthest, and no other of them has given up pages that it still holds) and
-// position.  By a whole wavefront, a lane a row: a tile has no more rows than columns.
+// position.  By a whole wavefront, a lane one or two rows: a tile has no more rows than its (at most 128) columns.
 struct PtShortest {
   int row, pos;
 };
 __device__ __forceinline__ PtShortest pt_shortest(const PtArgs &a, const PtTile &t) {
   const int m0 = t.first / a.group, m1 = (t.first + t.columns - 1) / a.group, m = m0 + (int)(threadIdx.x & 63);
-  const KvSeq q = kv_seq(a.kv, a.seqs, a.plan.list[t.list + min(m, m1)]);
+  KvSeq q = kv_seq(a.kv, a.seqs, a.plan.list[t.list + min(m, m1)]);
+  if (m1 - m0 >= 64) {
+    const KvSeq r = kv_seq(a.kv, a.seqs, a.plan.list[t.list + min(m + 64, m1)]);
+    if (q.len <= 0 || (r.len > 0 && r.len < q.len)) q = r;
+  }
   const int len = q.len > 0 ? q.len : 0x7fffffff;
   int least = len;
 #pragma unroll
@@ -127,21 +138,30 @@ __device__ __forceinline__ bool pt_fits(const PtArgs &a, int columns) {
          h.max_pages == a.kv.max_pages && h.page == a.kv.page && h.tiles >= 0 && h.tiles <= a.most_tiles;
 }
 
+// LDS of a workgroup but the entries' sums: the ring, or the wavefronts' sums
+template <class T, int DT> constexpr int pt_lds_own() {
+  const int ring = pt_stages<T, DT>() * pt_step_bytes<T, DT>(), sums = (PT_WAVES * 16 * (DT * 32 + 4) + 2 * PT_WAVES * 16) * 4;
+  return ring > sums ? ring : sums;
+}
+
 // Entry x is share x, whole, where no entry has many more steps than an equal share would
 constexpr int PT_SLACK = 12;
 
 // A step of 32 tokens: s = K q (operand A = K, token rows; operand B = q, a column of the entry), weights 2^(scale s - base), o += V^T p.  K's rows are taken in the order in
 // which the scores come back as operand B: rows 4 q + 0..3 of the two instructions of a step are tokens 8 q + 0..3 and 8 q + 4..7, so that a lane's eight weights are
-// the eight tokens whose V it has loaded.  Operands go straight from the pages into registers, a step ahead of the one that is worked on where two steps fit; they are
-// multiplied with up to NB blocks of sixteen columns.  bf16: a weight is multiplied as two bf16 numbers, as in the decode attention.
-template <class T, int DT, int NB, bool LISTED>
-__global__ __launch_bounds__(PT_THREADS, NB == 1 && DT * sizeof(T) <= 8 ? 2 : 1) void attend_parts(PtArgs a) {
-  constexpr int D = DT * 32, KB = D / 32, VB = D / 16, TC = 16 * NB, RD = D + 4;
+// the eight tokens whose V it has loaded.  bf16: a weight is multiplied as two bf16 numbers, as in the decode attention.
+//   narrow entries, up to sixteen columns: operands go straight from the pages into registers, a step ahead of the one that is worked on where two fit; the four wavefronts
+//   take turns and their sums meet in LDS, or, where rows are many and short, a wavefront has a row alone
+//   wide ones: a wavefront has up to NW blocks of sixteen columns; the steps go through a ring in LDS, filled by loads that write LDS, and are read by all four
+template <class T, int DT, bool LISTED>
+__global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_parts(PtArgs a) {
+  constexpr int D = DT * 32, KB = D / 32, VB = D / 16, NW = pt_blocks<T, DT>(), TC = 64 * NW, RD = D + 4, ST = pt_stages<T, DT>();
+  constexpr int CHUNK = 16 * D * (int)sizeof(T), STAGE = 4 * CHUNK, LOADS = CHUNK / 1024;         // K and V of sixteen tokens each stand in one piece
   typedef typename Op<T>::frag frag;
   extern __shared__ char smem[];
-  float *red = reinterpret_cast<float *>(smem);                    // [wave][16][RD]
-  float *red_m = red + PT_WAVES * 16 * RD, *red_l = red_m + PT_WAVES * TC;       // [wave][TC]
-  int *wave_sums = reinterpret_cast<int *>(red_l + PT_WAVES * TC), *pre = wave_sums + PT_WAVES;
+  float *red = reinterpret_cast<float *>(smem);                    // [wave][16][RD], [wave][16] twice; or the ring
+  float *red_m = red + PT_WAVES * 16 * RD, *red_l = red_m + PT_WAVES * 16;
+  int *wave_sums = reinterpret_cast<int *>(smem + pt_lds_own<T, DT>()), *pre = wave_sums + PT_WAVES;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 15, quad = lane >> 4;
   const int share = blockIdx.x, kvh = blockIdx.y;
@@ -164,7 +184,6 @@ __global__ __launch_bounds__(PT_THREADS, NB == 1 && DT * sizeof(T) <= 8 ? 2 : 1)
     return own_span(row, kv_seq(a.kv, a.seqs, row)).count;
   };
   int total;
-  bool longer = false;
   if constexpr (LISTED) {
     total = list_steps * entries;
   } else {
@@ -175,6 +194,7 @@ __global__ __launch_bounds__(PT_THREADS, NB == 1 && DT * sizeof(T) <= 8 ? 2 : 1)
   const int per = max(((total + a.shares - 1) / a.shares + PT_WAVES - 1) / PT_WAVES, 1) * PT_WAVES;
   bool by_rows = entries <= a.shares;
   if (by_rows) {
+    bool longer = false;
     for (int e = tid; e < entries; e += PT_THREADS) longer |= before_of(e + 1) - before_of(e) > per + PT_SLACK;
     by_rows = !__syncthreads_or(longer);
   }
@@ -190,15 +210,25 @@ __global__ __launch_bounds__(PT_THREADS, NB == 1 && DT * sizeof(T) <= 8 ? 2 : 1)
   const int tok = 8 * (n >> 2) + (n & 3);
   const int page_bits = 31 - __builtin_clz(a.kv.page);
   const int k_in = quad * 128 + (tok & 15) * 8, v_in = ((quad & 1) * D + n) * 8;
-  const int e0 = LISTED ? (int)begin / list_steps : kv_find(pre, entries, (int)begin), e1 = LISTED ? (end - 1) / list_steps : kv_find(pre, entries, end - 1);
+  const int e0 = __builtin_amdgcn_readfirstlane(LISTED ? (int)begin / list_steps : kv_find(pre, entries, (int)begin));
+  const int e1 = __builtin_amdgcn_readfirstlane(LISTED ? (end - 1) / list_steps : kv_find(pre, entries, end - 1));
   float *parts = a.part + (int64_t)kvh * ((int64_t)a.shares * TC + (LISTED ? 0 : (int64_t)PT_LEVELS * a.rows * a.group) + (int64_t)a.rows * a.group) * RD;
-  for (int e = __builtin_amdgcn_readfirstlane(e0); e <= e1; ++e) {
+  // Rows of sixteen columns at most that a wavefront has alone: from `alone` on
+  const int rows0 = max(e0, tiles);
+  const bool many = a.group <= 16 && e1 - rows0 >= PT_WAVES - 1 && end - max((int)begin, before_of(rows0)) <= 12 * (e1 - rows0);
+  const int alone = many ? rows0 : e1 + 1;
+  int mine = alone + wave, common = e0;
+  for (;;) {
+    const bool by_all = common < alone;
+    if (!by_all && mine > e1) break;
+    const int e = __builtin_amdgcn_readfirstlane(by_all ? common : mine);
+    if (by_all) ++common; else mine += PT_WAVES;
     const int before = __builtin_amdgcn_readfirstlane(before_of(e)), count = __builtin_amdgcn_readfirstlane(before_of(e + 1)) - before;
     if (count == 0) continue;
     // ---- the entry
     PtTile t{};
     int row = 0, z = 0, seq, columns, base, pos_of = -1;
-    bool direct = false;
+    bool direct = LISTED;
     int passed = 0;                                                // steps that were in sight when the plan was made and are no more
     PtSpan span{};
     const bool tile = !LISTED && e < tiles;
@@ -209,7 +239,7 @@ __global__ __launch_bounds__(PT_THREADS, NB == 1 && DT * sizeof(T) <= 8 ? 2 : 1)
       span = pt_span(t.pos, t.from, t.to, a.window, a.sinks);
       passed = s.pos < 0 ? count : span.sink_tiles + max(pt_span(max(s.pos, t.pos), t.from, t.to, a.window, a.sinks).a - span.a, 0);
     } else {
-      row = (e - tiles) / a.per_row; z = (e - tiles) % a.per_row;
+      row = (e - tiles) / a.per_row; z = (e - tiles) - row * a.per_row;
       const KvSeq s = kv_seq(a.kv, a.seqs, row);
       seq = s.row; pos_of = s.len - 1;
       columns = min(a.group - z * TC, TC);
@@ -217,131 +247,97 @@ __global__ __launch_bounds__(PT_THREADS, NB == 1 && DT * sizeof(T) <= 8 ? 2 : 1)
       if constexpr (!LISTED) {
         span = own_span(row, s);
         direct = !fits || a.plan.row[row].levels == 0;
-      } else {
-        direct = true;
       }
     }
     seq = __builtin_amdgcn_readfirstlane(seq);
     columns = __builtin_amdgcn_readfirstlane(columns);
     base = __builtin_amdgcn_readfirstlane(base);
-    const int first = max((int)begin - before, 0), last = min(end - before, count);
-    const int start = (tile && first >= span.sink_tiles ? max(first, passed) : first) + wave;
-    const int blocks = (columns + 15) / 16;
+    span.f = __builtin_amdgcn_readfirstlane(span.f);
+    span.sink_tiles = __builtin_amdgcn_readfirstlane(span.sink_tiles);
+    span.a = __builtin_amdgcn_readfirstlane(span.a);
+    int first = max((int)begin - before, 0);
+    const int last = min(end - before, count);
+    const bool all = direct && first == 0 && last == count;
+    if (tile && first >= span.sink_tiles) first = __builtin_amdgcn_readfirstlane(min(max(first, passed), last));
+    const bool wide = columns > 16;
     const int32_t *table = a.kv.table + (int64_t)seq * a.kv.max_pages;
     const int32_t *list = LISTED ? a.pages + ((int64_t)row * a.kv.n_kv + kvh) * a.top : nullptr;
-    frag qf[NB][KB];
-    int pos[NB], lo[NB], least = 0x7fffffff, most = 0;
+    float *part = parts + ((int64_t)share * TC + base) * RD;
+    // NB: blocks of sixteen columns that this wavefront has, number wave + 4 b of a wide entry, the only one of a narrow one
+    auto entry = [&](auto is_wide, auto of) {
+      constexpr bool WIDE = decltype(is_wide)::value;
+      constexpr int NB = decltype(of)::value, NA = NB > 0 ? NB : 1;
+      auto column = [&](int b) { return WIDE ? 16 * (wave + PT_WAVES * b) + n : n; };
+      frag qf[NA][KB];
+      int pos[NA], lo[NA], least = 0x7fffffff, most = 0;
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const int c = min(16 * b + n, columns - 1);
-      int r = row, h = z * TC + c;
-      pos[b] = pos_of;
-      if (tile) {
-        const int f = t.first + c, m = f / a.group;
-        r = a.plan.list[t.list + m];
-        h = f - m * a.group;
-        pos[b] = kv_seq(a.kv, a.seqs, r).len - 1;
+      for (int b = 0; b < NA; ++b) {
+        const int c = min(column(b), columns - 1);
+        int r = row, h = z * TC + c;
+        pos[b] = pos_of;
+        if (tile) {
+          const int f = t.first + c, m = f / a.group;
+          r = a.plan.list[t.list + m];
+          h = f - m * a.group;
+          pos[b] = kv_seq(a.kv, a.seqs, r).len - 1;
+        }
+        lo[b] = LISTED ? 0 : kv_window_begin(pos[b], a.window);
+        least = min(least, pos[b]);
+        most = max(most, lo[b]);
+        const T *q = reinterpret_cast<const T *>(a.q) + (int64_t)r * a.q_stride + (int64_t)(kvh * a.group + h) * D;
+#pragma unroll
+        for (int k = 0; k < KB; ++k) qf[b][k] = Op<T>::sign(Op<T>::load(q + 32 * k + 8 * quad), a.q_sign);
       }
-      lo[b] = LISTED ? 0 : kv_window_begin(pos[b], a.window);
-      least = min(least, pos[b]);
-      most = max(most, lo[b]);
-      const T *q = reinterpret_cast<const T *>(a.q) + (int64_t)r * a.q_stride + (int64_t)(kvh * a.group + h) * D;
 #pragma unroll
-      for (int k = 0; k < KB; ++k) qf[b][k] = Op<T>::sign(Op<T>::load(q + 32 * k + 8 * quad), a.q_sign);
-    }
+      for (int o = 8; o > 0; o >>= 1) { least = min(least, __shfl_xor(least, o, 64)); most = max(most, __shfl_xor(most, o, 64)); }
+      least = __builtin_amdgcn_readfirstlane(least);
+      most = __builtin_amdgcn_readfirstlane(most);
+      float m[NA], l[NA];
+      f32x4 o[NA][VB];
+      auto clear = [&]() {
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) { least = min(least, __shfl_xor(least, o, 64)); most = max(most, __shfl_xor(most, o, 64)); }
-    least = __builtin_amdgcn_readfirstlane(least);
-    most = __builtin_amdgcn_readfirstlane(most);
-    float m[NB], l[NB];
-    f32x4 o[NB][VB];
-    auto clear = [&]() {
+        for (int b = 0; b < NA; ++b) {
+          m[b] = -INFINITY; l[b] = 0.f;
 #pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        m[b] = -INFINITY; l[b] = 0.f;
-#pragma unroll
-        for (int v = 0; v < VB; ++v) o[b][v] = f32x4{0.f, 0.f, 0.f, 0.f};
-      }
-    };
-    clear();
-    // the wavefront's next 64 steps, a lane each: page and first token of their two halves, -1 for none
-    int id_a = -1, id_b = -1, at_a = 0, at_b = 0;
-    struct Step {
-      frag k0[KB], k1[KB], v[VB];
-      int ta, tb;
-      bool there_a, there_b;
-    };
-    auto load = [&](Step &x, int j) {
-      const int u = start + j * PT_WAVES;
-      if ((j & 63) == 0) {
-        const int mine = min(u + lane * PT_WAVES, count - 1);
+          for (int v = 0; v < VB; ++v) o[b][v] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+      };
+      clear();
+      // Half (sixteen tokens) of a step: its page and first token; a page outside [0, n_pages): none
+      auto place = [&](int u, int half, int &id, int &at) {
         if constexpr (LISTED) {
-          auto half = [&](int block, int &id, int &at) {           // block of sixteen tokens of the listed pages
-            const int i = block >> (page_bits - 4);
-            const int c = i < a.top ? list[i] : -1;
-            const bool ok = (unsigned)c < (unsigned)a.kv.max_pages;
-            id = ok ? table[c] : -1;
-            at = (ok ? c : 0) * a.kv.page + (block & ((a.kv.page >> 4) - 1)) * 16;
-          };
-          half(2 * mine, id_a, at_a);
-          half(2 * mine + 1, id_b, at_b);
+          const int block = 2 * u + half, i = block >> (page_bits - 4);
+          const int c = i < a.top ? list[i] : -1;
+          const bool ok = (unsigned)c < (unsigned)a.kv.max_pages;
+          id = ok ? table[c] : -1;
+          at = (ok ? c : 0) * a.kv.page + (block & ((a.kv.page >> 4) - 1)) * 16;
         } else {
-          at_a = span.at(mine) * PT_STEP;
-          at_b = at_a + 16;
-          id_a = table[min(at_a >> page_bits, a.kv.max_pages - 1)];
-          id_b = table[min(at_b >> page_bits, a.kv.max_pages - 1)];
+          at = span.at(u) * PT_STEP + 16 * half;
+          id = table[min(at >> page_bits, a.kv.max_pages - 1)];
         }
-      }
-      const int ida = __builtin_amdgcn_readlane(id_a, j & 63), idb = __builtin_amdgcn_readlane(id_b, j & 63);
-      x.ta = __builtin_amdgcn_readlane(at_a, j & 63);
-      x.tb = LISTED ? __builtin_amdgcn_readlane(at_b, j & 63) : x.ta + 16;
-      x.there_a = (unsigned)ida < (unsigned)a.kv.n_pages;
-      x.there_b = (unsigned)idb < (unsigned)a.kv.n_pages;
-      const int64_t pa = (int64_t)(x.there_a ? ida : 0) * page_elems + head0 + (int64_t)(x.ta & (a.kv.page - 1)) * D;
-      const int64_t pb = (int64_t)(x.there_b ? idb : 0) * page_elems + head0 + (int64_t)(x.tb & (a.kv.page - 1)) * D;
-      const T *kp = reinterpret_cast<const T *>(a.K) + (n < 8 ? pa : pb) + k_in;
-      const T *vp = reinterpret_cast<const T *>(a.V) + (quad < 2 ? pa : pb) + v_in;
-#pragma unroll
-      for (int k = 0; k < KB; ++k) { x.k0[k] = Op<T>::load(kp + k * 512); x.k1[k] = Op<T>::load(kp + k * 512 + 32); }
-#pragma unroll
-      for (int v = 0; v < VB; ++v) x.v[v] = Op<T>::load(vp + v * 128);
-    };
-    // which of the lane's eight tokens a row at position i sees
-    auto seen = [&](const Step &x, int i, int from) -> uint32_t {
-      const bool there = quad < 2 ? x.there_a : x.there_b;
-      const int j0 = (quad < 2 ? x.ta : x.tb) + 8 * (quad & 1);
-      return there ? kv_sees8(i, from, LISTED ? 0 : a.sinks, j0) : 0u;
-    };
-    auto work = [&](Step &x, auto careful) {
-      constexpr bool CAREFUL = decltype(careful)::value;
-      const bool whole = x.there_a && x.there_b && x.ta + 15 <= least && x.tb + 15 <= least && (x.ta >= most || x.ta + PT_STEP <= a.sinks);
-      uint32_t keep[NB];
-      if (!whole) {                                                // what no column sees: nothing of V to multiply with
-        uint32_t any = 0;
-#pragma unroll
-        for (int b = 0; b < NB; ++b) { keep[b] = seen(x, pos[b], lo[b]); any |= keep[b]; }
-#pragma unroll
-        for (int s = 8; s > 0; s >>= 1) any |= __shfl_xor(any, s, 64);
-        if (!CAREFUL) {
-#pragma unroll
-          for (int v = 0; v < VB; ++v) x.v[v] = Op<T>::only(x.v[v], any);
-        }
-      } else {
-#pragma unroll
-        for (int b = 0; b < NB; ++b) keep[b] = 0xffu;
-      }
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        if (b >= blocks) break;
-        f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
-#pragma unroll
-        for (int k = 0; k < KB; ++k) { s0 = Op<T>::mma16(x.k0[k], qf[b][k], s0); s1 = Op<T>::mma16(x.k1[k], qf[b][k], s1); }
+      };
+      auto page_there = [&](int id) { return (unsigned)id < (unsigned)a.kv.n_pages; };
+      struct Where {                                                 // of a step
+        int ta, tb;
+        bool there_a, there_b;
+      };
+      // which of the lane's eight tokens a row at position i sees
+      auto seen = [&](const Where &x, int i, int from) -> uint32_t {
+        const bool there = quad < 2 ? x.there_a : x.there_b;
+        const int j0 = (quad < 2 ? x.ta : x.tb) + 8 * (quad & 1);
+        return there ? kv_sees8(i, from, LISTED ? 0 : a.sinks, j0) : 0u;
+      };
+      auto whole_of = [&](const Where &x) {
+        return x.there_a && x.there_b && x.ta + 15 <= least && x.tb + 15 <= least && (x.ta >= most || x.ta + PT_STEP <= a.sinks);
+      };
+      // weights of block b from the scores, the running maximum moved where it has to grow
+      auto weigh = [&](int b, f32x4 s0, f32x4 s1, bool whole, uint32_t keep, float *p) {
         float s[8];
 #pragma unroll
         for (int e = 0; e < 4; ++e) { s[e] = s0[e]; s[4 + e] = s1[e]; }
         if (!whole) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) s[e] = keep[b] >> e & 1 ? s[e] : -INFINITY;
+          for (int e = 0; e < 8; ++e) s[e] = keep >> e & 1 ? s[e] : -INFINITY;
         }
         float top = s[0];
 #pragma unroll
@@ -355,114 +351,271 @@ __global__ __launch_bounds__(PT_THREADS, NB == 1 && DT * sizeof(T) <= 8 ? 2 : 1)
           m[b] = grown;
         }
         const float off = at_base(m[b], a.scale);
-        float p[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) { p[e] = at_exp2(fmaf(s[e], a.scale, -off)); l[b] += p[e]; }
-        const frag pf = Op<T>::pack(p);
-        if constexpr (!CAREFUL) {
+      };
+      auto any_seen = [&](const Where &x, uint32_t *keep) {          // what no column of the wavefront sees: nothing of V to multiply with
+        uint32_t any = 0;
 #pragma unroll
-          for (int v = 0; v < VB; ++v) o[b][v] = Op<T>::mma16(x.v[v], pf, o[b][v]);
+        for (int b = 0; b < NA; ++b) { keep[b] = seen(x, pos[b], lo[b]); any |= keep[b]; }
+#pragma unroll
+        for (int s = 8; s > 0; s >>= 1) any |= __shfl_xor(any, s, 64);
+        return any;
+      };
+      // ---- from pages into registers: steps start, start + turn, ...
+      struct Step {
+        frag k0[KB], k1[KB], v[VB];
+        Where at;
+      };
+      int start = first, turn = 1, steps = max(last - first, 0);
+      if (!WIDE && by_all) { start = first + wave; turn = PT_WAVES; steps = last > start ? (last - start + PT_WAVES - 1) / PT_WAVES : 0; }
+      int id_a = -1, id_b = -1, at_a = 0, at_b = 0;                  // of the next 64 steps, a lane each
+      auto load = [&](Step &x, int j) {
+        if ((j & 63) == 0) {
+          const int u = min(start + (j + lane) * turn, last - 1);
+          place(u, 0, id_a, at_a);
+          place(u, 1, id_b, at_b);
+        }
+        const int ida = __builtin_amdgcn_readlane(id_a, j & 63), idb = __builtin_amdgcn_readlane(id_b, j & 63);
+        x.at.ta = __builtin_amdgcn_readlane(at_a, j & 63);
+        x.at.tb = __builtin_amdgcn_readlane(at_b, j & 63);
+        x.at.there_a = page_there(ida);
+        x.at.there_b = page_there(idb);
+        const int64_t pa = (int64_t)(x.at.there_a ? ida : 0) * page_elems + head0 + (int64_t)(x.at.ta & (a.kv.page - 1)) * D;
+        const int64_t pb = (int64_t)(x.at.there_b ? idb : 0) * page_elems + head0 + (int64_t)(x.at.tb & (a.kv.page - 1)) * D;
+        const T *kp = reinterpret_cast<const T *>(a.K) + (n < 8 ? pa : pb) + k_in;
+        const T *vp = reinterpret_cast<const T *>(a.V) + (quad < 2 ? pa : pb) + v_in;
+#pragma unroll
+        for (int k = 0; k < KB; ++k) { x.k0[k] = Op<T>::load(kp + k * 512); x.k1[k] = Op<T>::load(kp + k * 512 + 32); }
+#pragma unroll
+        for (int v = 0; v < VB; ++v) x.v[v] = Op<T>::load(vp + v * 128);
+      };
+      if constexpr (!WIDE) {
+        auto work = [&](Step &x) {
+          f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
+#pragma unroll
+          for (int k = 0; k < KB; ++k) { s0 = Op<T>::mma16(x.k0[k], qf[0][k], s0); s1 = Op<T>::mma16(x.k1[k], qf[0][k], s1); }
+          const bool whole = whole_of(x.at);
+          uint32_t keep[NA] = {};
+          if (!whole) {
+            const uint32_t any = any_seen(x.at, keep);
+#pragma unroll
+            for (int v = 0; v < VB; ++v) x.v[v] = Op<T>::only(x.v[v], any);
+          }
+          float p[8];
+          weigh(0, s0, s1, whole, keep[0], p);
+          const frag pf = Op<T>::pack(p);
+#pragma unroll
+          for (int v = 0; v < VB; ++v) o[0][v] = Op<T>::mma16(x.v[v], pf, o[0][v]);
           if constexpr (sizeof(T) == 2) {
             const frag rest = Op<T>::pack_rest(p, pf);
 #pragma unroll
-            for (int v = 0; v < VB; ++v) o[b][v] = Op<T>::mma16(x.v[v], rest, o[b][v]);
+            for (int v = 0; v < VB; ++v) o[0][v] = Op<T>::mma16(x.v[v], rest, o[0][v]);
           }
-        } else {                                                   // column after column, each with what it sees of V
-          for (int c = 0; c < 16; ++c) {
-            const uint32_t sees = whole ? 0xffu : seen(x, __builtin_amdgcn_readlane(pos[b], c), __builtin_amdgcn_readlane(lo[b], c));
+        };
+        Step even;
+        if constexpr (DT * sizeof(T) <= 8) {                         // two steps fit the registers
+          Step odd;
+          if (steps > 0) load(even, 0);
+          for (int j = 0; j < steps; j += 2) {
+            if (j + 1 < steps) load(odd, j + 1);
+            work(even);
+            if (j + 1 < steps) {
+              if (j + 2 < steps) load(even, j + 2);
+              work(odd);
+            }
+          }
+        } else {
+          for (int j = 0; j < steps; ++j) {
+            load(even, j);
+            work(even);
+          }
+        }
+      } else if (steps > 0) {
+        // ---- through LDS.  Wavefront w stages K (0, 1) or V (2, 3) of a step's first or second sixteen tokens.  In the second half's K tokens t and t ^ 4 change places, so that
+        // the sixteen rows of an operand (of a pair of quads four tokens of each half) stand in different banks.
+        const char *const pool = (const char *)(wave < 2 ? a.K : a.V) + head0 * (int64_t)sizeof(T);
+        const int from_lane = wave == 1 ? (sizeof(T) == 2 ? lane ^ 4 : lane ^ 8) : lane;
+        uint32_t place_lo = 0, place_hi = 0;                         // of the next 64 steps to stage, a lane each: where this wavefront's sixteen tokens stand
+        int there_ab = 0;                                            // of the next 64 steps to work on: there_a, there_b
+        int staged = 0;
+        auto stage = [&]() {
+          if ((staged & 63) == 0) {
+            int id, at;
+            place(min(first + staged + lane, last - 1), wave & 1, id, at);
+            const int64_t p = ((int64_t)(page_there(id) ? id : 0) * page_elems + (int64_t)(at & (a.kv.page - 1)) * D) * (int64_t)sizeof(T);
+            place_lo = (uint32_t)p;
+            place_hi = (uint32_t)(p >> 32);
+          }
+          const char *src = pool + ((uint64_t)(uint32_t)__builtin_amdgcn_readlane(place_hi, staged & 63) << 32 | (uint32_t)__builtin_amdgcn_readlane(place_lo, staged & 63)) + from_lane * 16;
+          char *dst = smem + (staged % ST) * STAGE + wave * CHUNK;
+#pragma unroll
+          for (int q = 0; q < LOADS; ++q) __builtin_amdgcn_global_load_lds(PARSE_GLB_PTR(src + q * 1024), PARSE_LDS_PTR(dst + q * 1024), 16, 0, 0);
+          ++staged;
+        };
+        auto look = [&](int j) {
+          const int u = min(first + j + lane, last - 1);
+          place(u, 0, id_a, at_a);
+          place(u, 1, id_b, at_b);
+          there_ab = (page_there(id_a) ? 1 : 0) | (page_there(id_b) ? 2 : 0);
+        };
+        look(0);
+        __syncthreads();                                             // the sums of the entry before are read
+#pragma unroll
+        for (int j = 0; j < ST - 1; ++j)
+          if (j < steps) stage();
+        // where this lane's pieces stand: rows 0..7 of an operand in the first half, 8..15 in the second
+        const int k_at = (n < 8 ? 0 : CHUNK) + (quad * 16 + (tok & 15)) * 8 * (int)sizeof(T), k_turn = n < 8 ? 0 : 4 * 8 * (int)sizeof(T);
+        const int v_at = 2 * CHUNK + (quad >> 1) * CHUNK + v_in * (int)sizeof(T);
+        for (int j = 0; j < steps; ++j) {
+          if (j > 0 && (j & 63) == 0) look(j);
+          wait_slices<ST - 2, LOADS>(steps - 1 - j);
+          wg_barrier();                                              // this step has landed for everybody, the one before it is read by everybody
+          if (staged < steps) stage();
+          if constexpr (NB > 0) {
+            const int flags = __builtin_amdgcn_readlane(there_ab, j & 63);
+            const Where x{__builtin_amdgcn_readlane(at_a, j & 63), __builtin_amdgcn_readlane(at_b, j & 63), (flags & 1) != 0, (flags & 2) != 0};
+            const char *buf = smem + (j % ST) * STAGE;
+            f32x4 s0[NB], s1[NB];
+#pragma unroll
+            for (int b = 0; b < NB; ++b) s0[b] = s1[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < KB; ++k) {
+              const frag k0 = Op<T>::load(reinterpret_cast<const T *>(buf + (k_at ^ k_turn)) + k * 512);
+              const frag k1 = Op<T>::load(reinterpret_cast<const T *>(buf + (k_at ^ k_turn ^ (4 * 8 * (int)sizeof(T)))) + k * 512);
+#pragma unroll
+              for (int b = 0; b < NB; ++b) { s0[b] = Op<T>::mma16(k0, qf[b][k], s0[b]); s1[b] = Op<T>::mma16(k1, qf[b][k], s1[b]); }
+            }
+            const bool whole = whole_of(x);
+            uint32_t keep[NA] = {}, any = 0xffu;
+            if (!whole) any = any_seen(x, keep);
+            frag pf[NB], rest[NB];
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+              float p[8];
+              weigh(b, s0[b], s1[b], whole, keep[b], p);
+              pf[b] = Op<T>::pack(p);
+              if constexpr (sizeof(T) == 2) rest[b] = Op<T>::pack_rest(p, pf[b]);
+            }
 #pragma unroll
             for (int v = 0; v < VB; ++v) {
-              const frag vc = Op<T>::only(x.v[v], sees);
-              const f32x4 add = Op<T>::mma16(vc, pf, f32x4{0.f, 0.f, 0.f, 0.f});
-              f32x4 more = {0.f, 0.f, 0.f, 0.f};
-              if constexpr (sizeof(T) == 2) more = Op<T>::mma16(vc, Op<T>::pack_rest(p, pf), more);
+              frag vf = Op<T>::load(reinterpret_cast<const T *>(buf + v_at) + v * 128);
+              if (!whole) vf = Op<T>::only(vf, any);
 #pragma unroll
-              for (int e = 0; e < 4; ++e) o[b][v][e] += n == c ? add[e] + (fabsf(more[e]) < INFINITY ? more[e] : 0.f) : 0.f;
+              for (int b = 0; b < NB; ++b) {
+                o[b][v] = Op<T>::mma16(vf, pf[b], o[b][v]);
+                if constexpr (sizeof(T) == 2) o[b][v] = Op<T>::mma16(vf, rest[b], o[b][v]);
+              }
             }
           }
         }
       }
+      if constexpr (NB > 0) {
+        // An infinity or NaN of V that some columns see and others do not makes NaN of a weight of zero, and so does what the rounding of a weight left.  Where
+        // something that is not finite came out, once more, from the pages, column by column, each with what it sees of V.
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};                            // NaN where one of them is not finite
+#pragma unroll
+        for (int b = 0; b < NA; ++b)
+#pragma unroll
+          for (int v = 0; v < VB; ++v)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[i] = fmaf(o[b][v][i], 0.f, sum[i]);
+        if (__any((sum[0] + sum[1]) + (sum[2] + sum[3]) != 0.f)) {
+          clear();
+#pragma unroll 1
+          for (int j = 0; j < steps; ++j) {
+            Step x;
+            load(x, j);
+            const bool whole = whole_of(x.at);
+#pragma unroll
+            for (int b = 0; b < NA; ++b) {
+              f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
+#pragma unroll
+              for (int k = 0; k < KB; ++k) { s0 = Op<T>::mma16(x.k0[k], qf[b][k], s0); s1 = Op<T>::mma16(x.k1[k], qf[b][k], s1); }
+              float p[8];
+              weigh(b, s0, s1, whole, whole ? 0xffu : seen(x.at, pos[b], lo[b]), p);
+              const frag pf = Op<T>::pack(p);
+              frag rest = pf;
+              if constexpr (sizeof(T) == 2) rest = Op<T>::pack_rest(p, pf);
+#pragma unroll 1
+              for (int c = 0; c < 16; ++c) {
+                const uint32_t sees = whole ? 0xffu : seen(x.at, __builtin_amdgcn_readlane(pos[b], c), __builtin_amdgcn_readlane(lo[b], c));
+#pragma unroll
+                for (int v = 0; v < VB; ++v) {
+                  const frag vc = Op<T>::only(x.v[v], sees);
+                  const f32x4 add = Op<T>::mma16(vc, pf, f32x4{0.f, 0.f, 0.f, 0.f});
+                  f32x4 more = {0.f, 0.f, 0.f, 0.f};
+                  if constexpr (sizeof(T) == 2) more = Op<T>::mma16(vc, rest, more);
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) o[b][v][i] += n == c ? add[i] + (fabsf(more[i]) < INFINITY ? more[i] : 0.f) : 0.f;
+                }
+              }
+            }
+          }
+        }
+      }
+#pragma unroll
+      for (int b = 0; b < NA; ++b) l[b] = lane_sum<32>(lane_sum<16>(l[b]));
+      if (WIDE || !by_all) {                                         // a column's sums are one wavefront's
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          const int c = column(b);
+          if (c >= columns) continue;
+          if (all) {
+            const int head = kvh * a.group + z * TC + c;
+            const float by = l[b] == 0.f ? 0.f : 1.f / l[b];
+            T *out = reinterpret_cast<T *>(a.out) + (int64_t)row * a.out_stride + (int64_t)head * D + 4 * quad;
+#pragma unroll
+            for (int v = 0; v < VB; ++v) Op<T>::store4(out + 16 * v, o[b][v][0] * by, o[b][v][1] * by, o[b][v][2] * by, o[b][v][3] * by);
+            if (a.lse && quad == 0) a.lse[(int64_t)row * a.n_q + head] = at_lse(m[b], a.scale, l[b]);
+          } else {
+            float *to = part + (int64_t)c * RD;
+#pragma unroll
+            for (int v = 0; v < VB; ++v) *reinterpret_cast<f32x4 *>(to + 16 * v + 4 * quad) = o[b][v];
+            if (quad == 0) { to[D] = m[b]; to[D + 1] = l[b]; }
+          }
+        }
+        return;
+      }
+      // ---- the wavefronts' sums meet
+      if constexpr (!WIDE) {
+        __syncthreads();
+        if (quad == 0) { red_m[wave * 16 + n] = m[0]; red_l[wave * 16 + n] = l[0]; }
+#pragma unroll
+        for (int v = 0; v < VB; ++v) *reinterpret_cast<f32x4 *>(red + (wave * 16 + n) * RD + 16 * v + 4 * quad) = o[0][v];
+        __syncthreads();
+        for (int w = tid; w < columns * D; w += PT_THREADS) {
+          const int c = w / D, i = w % D;
+          float top = -INFINITY, ls = 0.f, os = 0.f;
+#pragma unroll
+          for (int x = 0; x < PT_WAVES; ++x) top = fmaxf(top, red_m[x * 16 + c]);
+#pragma unroll
+          for (int x = 0; x < PT_WAVES; ++x) {
+            const float by = at_exp2((red_m[x * 16 + c] - finite_or_0(top)) * a.scale);
+            ls += by * red_l[x * 16 + c];
+            os += by * red[(x * 16 + c) * RD + i];
+          }
+          if (all) {
+            const int head = kvh * a.group + z * TC + c;
+            const float y = ls == 0.f ? 0.f : os / ls;
+            T *out = reinterpret_cast<T *>(a.out) + (int64_t)row * a.out_stride + (int64_t)head * D + i;
+            if constexpr (sizeof(T) == 2) *out = (uint16_t)cvt_pk_bf16(y, 0.f);
+            else *out = y;
+            if (a.lse && i == 0) a.lse[(int64_t)row * a.n_q + head] = at_lse(top, a.scale, ls);
+          } else {
+            part[(int64_t)c * RD + i] = os;
+            if (i == 0) { part[(int64_t)c * RD + D] = top; part[(int64_t)c * RD + D + 1] = ls; }
+          }
+        }
+        __syncthreads();
+      }
     };
-    const int steps = last > start ? (last - start + PT_WAVES - 1) / PT_WAVES : 0;
-    Step even;
-    if constexpr (DT * sizeof(T) <= 8) {                           // two steps fit the registers
-      Step odd;
-      if (steps > 0) load(even, 0);
-      for (int j = 0; j < steps; j += 2) {
-        if (j + 1 < steps) load(odd, j + 1);
-        work(even, std::false_type{});
-        if (j + 1 < steps) {
-          if (j + 2 < steps) load(even, j + 2);
-          work(odd, std::false_type{});
-        }
-      }
-    } else {
-      for (int j = 0; j < steps; ++j) {
-        load(even, j);
-        work(even, std::false_type{});
-      }
-    }
-    {
-      // An infinity or NaN of V that some columns see and others do not makes NaN of a weight of zero, and so does what the rounding of a weight left.  Where
-      // something that is not finite came out, once more column by column.
-      f32x4 sum = {0.f, 0.f, 0.f, 0.f};                            // NaN where one of them is not finite
-#pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int v = 0; v < VB; ++v)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) sum[i] = fmaf(o[b][v][i], 0.f, sum[i]);
-      if (__any((sum[0] + sum[1]) + (sum[2] + sum[3]) != 0.f)) {
-        clear();
-        for (int j = 0; j < steps; ++j) {
-          load(even, j);
-          work(even, std::true_type{});
-        }
-      }
-    }
-    // ---- the wavefronts' sums meet, sixteen columns after another
-#pragma unroll
-    for (int b = 0; b < NB; ++b) l[b] = lane_sum<32>(lane_sum<16>(l[b]));
-    __syncthreads();
-    if (quad == 0) {
-#pragma unroll
-      for (int b = 0; b < NB; ++b) { red_m[wave * TC + 16 * b + n] = m[b]; red_l[wave * TC + 16 * b + n] = l[b]; }
-    }
-    const bool all = direct && first == 0 && last == count;
-    float *part = parts + ((int64_t)share * TC + base) * RD;
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      if (b >= blocks) break;
-      if (b) __syncthreads();
-#pragma unroll
-      for (int v = 0; v < VB; ++v) *reinterpret_cast<f32x4 *>(red + (wave * 16 + n) * RD + 16 * v + 4 * quad) = o[b][v];
-      __syncthreads();
-      const int here = min(columns - 16 * b, 16);
-      for (int w = tid; w < here * D; w += PT_THREADS) {
-        const int h = w / D, i = w % D, c = 16 * b + h;
-        float top = -INFINITY, ls = 0.f, os = 0.f;
-#pragma unroll
-        for (int x = 0; x < PT_WAVES; ++x) top = fmaxf(top, red_m[x * TC + c]);
-#pragma unroll
-        for (int x = 0; x < PT_WAVES; ++x) {
-          const float by = at_exp2((red_m[x * TC + c] - finite_or_0(top)) * a.scale);
-          ls += by * red_l[x * TC + c];
-          os += by * red[(x * 16 + h) * RD + i];
-        }
-        if (all) {
-          const int head = kvh * a.group + z * TC + c;
-          const float y = ls == 0.f ? 0.f : os / ls;
-          T *out = reinterpret_cast<T *>(a.out) + (int64_t)row * a.out_stride + (int64_t)head * D + i;
-          if constexpr (sizeof(T) == 2) *out = (uint16_t)cvt_pk_bf16(y, 0.f);
-          else *out = y;
-          if (a.lse && i == 0) a.lse[(int64_t)row * a.n_q + head] = at_lse(top, a.scale, ls);
-        } else {
-          part[(int64_t)c * RD + i] = os;
-          if (i == 0) { part[(int64_t)c * RD + D] = top; part[(int64_t)c * RD + D + 1] = ls; }
-        }
-      }
-    }
-    __syncthreads();
+    // blocks of a wide entry that are this wavefront's
+    const int blocks = ((columns + 15) / 16 - wave + PT_WAVES - 1) / PT_WAVES;
+    if (!wide) entry(std::false_type{}, std::integral_constant<int, 1>{});
+    else if (blocks <= 0) entry(std::true_type{}, std::integral_constant<int, 0>{});
+    else if (blocks == 1) entry(std::true_type{}, std::integral_constant<int, 1>{});
+    else entry(std::true_type{}, std::integral_constant<int, NW>{});
   }
 }
 
@@ -551,9 +704,11 @@ __global__ __launch_bounds__(PT_THREADS) void attend_parts_join(PtArgs a, int TC
 }
 
 // ---- host
-static inline int pt_shares(int n_kv, int workgroups) { return n_kv >= workgroups ? 1 : workgroups / n_kv; }
+static inline int pt_shares(const parse_kv *kv) {
+  const int workgroups = kv->d / 32 * elem_size(kv->dtype) <= 8 ? 512 : 256;         // what the card has at once (pt_at_once)
+  return kv->n_kv >= workgroups ? 1 : workgroups / kv->n_kv;
+}
 static inline size_t pt_deal_bytes(int64_t entries) { return round_up((PT_DEAL + (size_t)entries + 1) * 4, 256); }
-static inline size_t pt_lds(int d, int TC, int64_t entries) { return (size_t)(PT_WAVES * 16 * (d + 4) + 2 * PT_WAVES * TC) * 4 + (PT_WAVES + (size_t)entries + 1) * 4; }
 
 template <class T, bool LISTED>
 static int pt_join_launch(const PtArgs &a, int TC, hipStream_t s) {
@@ -561,13 +716,26 @@ static int pt_join_launch(const PtArgs &a, int TC, hipStream_t s) {
   PARSE_LAUNCH_CHECK();
   return PARSE_OK;
 }
-template <class T, int DT, int NB, bool LISTED>
+template <class T, int DT, bool LISTED>
 static int pt_launch(const PtArgs &a, int64_t entries, hipStream_t s) {
-  const size_t lds = pt_lds(DT * 32, 16 * NB, LISTED ? 0 : entries);
-  PARSE_ALLOW_LDS((attend_parts<T, DT, NB, LISTED>), 0, lds);
-  attend_parts<T, DT, NB, LISTED><<<dim3(a.shares, a.kv.n_kv), PT_THREADS, lds, s>>>(a);
+  const size_t lds = pt_lds_own<T, DT>() + (PT_WAVES + (LISTED ? 0 : (size_t)entries + 1)) * 4;
+  PARSE_ALLOW_LDS((attend_parts<T, DT, LISTED>), 0, lds);
+  attend_parts<T, DT, LISTED><<<dim3(a.shares, a.kv.n_kv), PT_THREADS, lds, s>>>(a);
   PARSE_LAUNCH_CHECK();
-  return pt_join_launch<T, LISTED>(a, 16 * NB, s);
+  return pt_join_launch<T, LISTED>(a, 64 * pt_blocks<T, DT>(), s);
+}
+template <class T, bool LISTED>
+static int pt_width(const PtArgs &a, int64_t entries, hipStream_t s) {
+  switch (a.kv.d / 32) {
+    case 1: return pt_launch<T, 1, LISTED>(a, entries, s);
+    case 2: return pt_launch<T, 2, LISTED>(a, entries, s);
+    case 3: return pt_launch<T, 3, LISTED>(a, entries, s);
+    case 4: return pt_launch<T, 4, LISTED>(a, entries, s);
+    case 5: return pt_launch<T, 5, LISTED>(a, entries, s);
+    case 6: return pt_launch<T, 6, LISTED>(a, entries, s);
+    case 7: return pt_launch<T, 7, LISTED>(a, entries, s);
+    default: return pt_launch<T, 8, LISTED>(a, entries, s);
+  }
 }
 
 }  // namespace parse

@@ -211,23 +211,6 @@ __global__ __launch_bounds__(SH_ONE) void shared_tiles(parse_kv kv, const int32_
 }
 
 // ---- the call
-constexpr int AS_GROUPS = 256;                       // a workgroup for each compute unit
-
-template <class T, int DT> static int as_go(const PtArgs &a, int64_t entries, hipStream_t s) { return pt_launch<T, DT, pt_blocks<T, DT>(), false>(a, entries, s); }
-template <class T>
-static int as_width(const PtArgs &a, int64_t entries, hipStream_t s) {
-  switch (a.kv.d / 32) {
-    case 1: return as_go<T, 1>(a, entries, s);
-    case 2: return as_go<T, 2>(a, entries, s);
-    case 3: return as_go<T, 3>(a, entries, s);
-    case 4: return as_go<T, 4>(a, entries, s);
-    case 5: return as_go<T, 5>(a, entries, s);
-    case 6: return as_go<T, 6>(a, entries, s);
-    case 7: return as_go<T, 7>(a, entries, s);
-    default: return as_go<T, 8>(a, entries, s);
-  }
-}
-
 // Entries of a call at most; a kv head's columns of parts; 0 where the call is refused
 struct AsSize {
   int64_t tiles, entries, columns;
@@ -238,7 +221,7 @@ static bool as_size(const parse_kv *kv, int n_q, int rows, AsSize &z) {
   const int group = n_q / kv->n_kv, TC = pt_columns(kv->d, kv->dtype);
   z.tiles = pt_most_tiles(rows, group, TC);
   z.entries = z.tiles + (int64_t)rows * ((group + TC - 1) / TC);
-  z.columns = (int64_t)pt_shares(kv->n_kv, AS_GROUPS) * TC + (int64_t)(PT_LEVELS + 1) * rows * group;
+  z.columns = (int64_t)pt_shares(kv) * TC + (int64_t)(PT_LEVELS + 1) * rows * group;
   z.bytes = pt_deal_bytes(z.entries) + round_up((size_t)z.columns * kv->n_kv * (kv->d + 4) * 4, 256);
   return z.entries <= PT_MAXENTRIES;
 }
@@ -307,14 +290,14 @@ int parse_attend_shared(const parse_kv *kv, int32_t layer, const void *q, int64_
   a.q = q; a.out = out; a.lse = lse; a.seqs = seqs;
   a.q_stride = q_stride; a.out_stride = out_stride;
   a.n_q = n_q; a.group = n_q / kv->n_kv; a.rows = rows; a.window = window; a.sinks = sinks;
-  a.shares = pt_shares(kv->n_kv, AS_GROUPS);
+  a.shares = pt_shares(kv);
   a.per_row = (a.group + TC - 1) / TC;
   at_scale(scale, a.scale, a.lag, a.q_sign);
   a.plan = pt_plan(kv, rows, a.group, plan);
   a.most_tiles = (int)z.tiles;
   a.deal = (int32_t *)workspace;
   a.part = (float *)((char *)workspace + pt_deal_bytes(z.entries));
-  return kv->dtype == PARSE_BF16 ? as_width<uint16_t>(a, z.entries, (hipStream_t)stream) : as_width<float>(a, z.entries, (hipStream_t)stream);
+  return kv->dtype == PARSE_BF16 ? pt_width<uint16_t, false>(a, z.entries, (hipStream_t)stream) : pt_width<float, false>(a, z.entries, (hipStream_t)stream);
 }
 
 }  // extern "C"

@@ -152,7 +152,7 @@ def test_pages_outside_the_windows_are_gone(page, window, sinks):
 
 @pytest.mark.parametrize("rows", [1, 2, 64, 65, 200])
 def test_numbers_of_rows(rows):
-    """One prompt for all, every head with its own keys: 64 columns and more a tile."""
+    """One prompt for all, every head with its own keys: up to 128 columns a tile."""
     family = [([("p", 10)], 1 + s % 19) for s in range(rows)]
     run(Family("bf16", 2, 32, 16, family, seed=rows), 2, shares=rows > 1)
 
@@ -162,7 +162,7 @@ def test_many_groups_in_any_order():
     family = [([("s", 9), (f"g{g}", 8 + g % 3), (f"g{g}.{c}", 12)], int(rng.integers(1, 60))) for g in range(11) for c in range(2) for _ in range(3)]
     rng.shuffle(family)
     _, _, plan, _ = run(Family("bf16", 1, 64, 16, family, seed=6), 4, shares=True)
-    assert tiles_of(plan) == 5 + 11 + 22                           # the text: 66 rows of four heads, the prompts: 24 columns each, their forks: 12
+    assert tiles_of(plan) == 3 + 11 + 22                           # the text: 66 rows of four heads in tiles of 128 columns, the prompts: 24 columns each, their forks: 12
 
 
 def test_a_short_text_before_the_prompts_goes_with_them():
