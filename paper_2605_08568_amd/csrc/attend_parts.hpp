@@ -30,7 +30,7 @@ template <class T, int DT> constexpr int pt_at_once() { return DT * (int)sizeof(
 
 // ---- the plan's words
 struct PtTile {
-  int list, members, first, columns;                 // members of the run from `list` on; the tile's first column among theirs (member * group + head), how many
+  int list, seq, first, columns;                     // members of the run from `list` on; the shortest row's row of the table; the tile's first column among the members' (member * group + head), how many
   int from, to, base, pos;                           // tokens [from, to), multiples of PT_STEP; columns of the tiles before; the shortest row's position
 };
 struct PtRow {
@@ -88,7 +88,7 @@ struct PtArgs {
   int most_tiles;
   const int32_t *pages;                              // LISTED: [row][kv head][top]
   int top;
-  int32_t *deal;                                     // {share, by rows, entries, 0, steps before entry 0 .. entries}
+  int32_t *deal;                                     // {steps of a share, entry x is share x, entries, columns of the tiles, steps before entry 0 .. entries}
   float *part;
 };
 constexpr int PT_DEAL = 4;
@@ -144,6 +144,8 @@ template <class T, int DT> constexpr int pt_lds_own() {
   return ring > sums ? ring : sums;
 }
 
+constexpr int PT_WIDE_STEPS = 8;
+
 // Entry x is share x, whole, where no entry has many more steps than an equal share would
 constexpr int PT_SLACK = 12;
 
@@ -191,7 +193,8 @@ __global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_part
     total = pre[entries];
   }
   auto before_of = [&](int e) { return LISTED ? e * list_steps : pre[e]; };
-  const int per = max(((total + a.shares - 1) / a.shares + PT_WAVES - 1) / PT_WAVES, 1) * PT_WAVES;
+  // Tiles are cut in shares of PT_WIDE_STEPS at least: a part of them is as many bytes as four steps, written and read again
+  const int per = max(((total + a.shares - 1) / a.shares + PT_WAVES - 1) / PT_WAVES * PT_WAVES, tiles > 0 ? PT_WIDE_STEPS : PT_WAVES);
   bool by_rows = entries <= a.shares;
   if (by_rows) {
     bool longer = false;
@@ -199,7 +202,7 @@ __global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_part
     by_rows = !__syncthreads_or(longer);
   }
   if (share == 0 && kvh == 0) {                                    // for the kernel that joins
-    if (tid == 0) { a.deal[0] = per; a.deal[1] = by_rows; a.deal[2] = entries; }
+    if (tid == 0) *reinterpret_cast<int4 *>(a.deal) = int4{per, by_rows, entries, tile_columns};
     for (int e = tid; e <= entries; e += PT_THREADS) a.deal[PT_DEAL + e] = before_of(e);
   }
   if (by_rows && share >= entries) return;
@@ -234,10 +237,13 @@ __global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_part
     const bool tile = !LISTED && e < tiles;
     if (tile) {
       t = a.plan.tile[e];
-      const PtShortest s = pt_shortest(a, t);
-      seq = s.row; columns = t.columns; base = t.base;
+      seq = t.seq; columns = t.columns; base = t.base;
       span = pt_span(t.pos, t.from, t.to, a.window, a.sinks);
-      passed = s.pos < 0 ? count : span.sink_tiles + max(pt_span(max(s.pos, t.pos), t.from, t.to, a.window, a.sinks).a - span.a, 0);
+      if (a.window > 0) {                                          // pages behind the window may have been given up since, by some of the rows
+        const PtShortest s = pt_shortest(a, t);
+        if (s.pos >= 0) seq = s.row;
+        passed = s.pos < 0 ? count : span.sink_tiles + max(pt_span(max(s.pos, t.pos), t.from, t.to, a.window, a.sinks).a - span.a, 0);
+      }
     } else {
       row = (e - tiles) / a.per_row; z = (e - tiles) - row * a.per_row;
       const KvSeq s = kv_seq(a.kv, a.seqs, row);
@@ -619,17 +625,23 @@ __global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_part
   }
 }
 
-// The parts of one row's head, in the order of entries and shares.  Workgroup (head, row); a wavefront has every fourth part, a lane D / 64 columns of it and more.
-template <class T, bool LISTED>
-__global__ __launch_bounds__(PT_THREADS) void attend_parts_join(PtArgs a, int TC) {
-  extern __shared__ char smem[];
-  const int D = a.kv.d, RD = D + 4, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int row = blockIdx.y, head = blockIdx.x, kvh = head / a.group, g = head % a.group;
-  const int per = a.deal[0], by_rows = a.deal[1], entries = a.deal[2], tiles = entries - a.rows * a.per_row;
+// The parts of one row's head; workgroup (head, row).  Four columns a lane, so many parts at once as the workgroup has lanes for, four of them on their way each; a group of lanes
+// joins its parts one after another, then the groups are joined, both in a fixed order.  Bound: three dependent trips to memory, then the parts' reads.
+template <class T, int DT, bool LISTED>
+__global__ __launch_bounds__(PT_THREADS) void attend_parts_join(PtArgs a) {
+  constexpr int D = DT * 32, RD = D + 4, TC = 64 * pt_blocks<T, DT>(), LANES = D / 4, GROUPS = PT_THREADS / LANES, N = 4;
+  __shared__ float tops[GROUPS], totals[GROUPS], sums[GROUPS * D];
+  const int tid = threadIdx.x, g = tid / LANES, i = tid % LANES * 4;
+  const int row = blockIdx.y, head = blockIdx.x, kvh = head / a.group, h = head - kvh * a.group;
+  const int4 deal = *reinterpret_cast<const int4 *>(a.deal);
+  const int per = deal.x, tiles = deal.z - a.rows * a.per_row, tile_columns = deal.w;
+  const bool by_rows = deal.y != 0;
   const int32_t *pre = a.deal + PT_DEAL;
   PtRow rec{};
-  int tile_columns = 0;
-  if (!LISTED && tiles > 0) { rec = a.plan.row[row]; tile_columns = a.plan.head->tile_columns; }
+  if constexpr (!LISTED) {
+    const PtRow r = a.plan.row[row];
+    if (tiles > 0) rec = r;
+  }
   // up to PT_LEVELS tiles and the row's own entry: first share, parts, column of the first part
   int x0[PT_LEVELS + 1], count[PT_LEVELS + 1], col[PT_LEVELS + 1], parts = 0;
   const int levels = min(max(rec.levels, 0), PT_LEVELS);
@@ -638,10 +650,10 @@ __global__ __launch_bounds__(PT_THREADS) void attend_parts_join(PtArgs a, int TC
     x0[s] = count[s] = col[s] = 0;
     int e = -1, c = 0;
     if (s == PT_LEVELS) {
-      e = tiles + row * a.per_row + g / TC;
-      c = tile_columns + row * a.group + g;
+      e = tiles + row * a.per_row + h / TC;
+      c = tile_columns + row * a.group + h;
     } else if (s < levels) {
-      const int f = rec.column[s] + g;
+      const int f = rec.column[s] + h;
       e = rec.tile[s] + f / TC;
       if (e >= 0 && e < tiles) c = a.plan.tile[e].base + f % TC;
       else e = -1;
@@ -659,47 +671,63 @@ __global__ __launch_bounds__(PT_THREADS) void attend_parts_join(PtArgs a, int TC
   if (levels == 0 && parts == 1) return;                           // stored by the share that had it
   const float *base = a.part + (int64_t)kvh * ((int64_t)a.shares * TC + (LISTED ? 0 : (int64_t)PT_LEVELS * a.rows * a.group) + (int64_t)a.rows * a.group) * RD;
   auto part_of = [&](int x) {
-    int s = 0;
-#pragma unroll
-    for (int k = 0; k < PT_LEVELS; ++k)
-      if (s == k && x >= count[k]) { x -= count[k]; s = k + 1; }
     int at = x0[0], c = col[0];
+    bool found = x < count[0];
 #pragma unroll
-    for (int k = 1; k <= PT_LEVELS; ++k)
-      if (s == k) { at = x0[k]; c = col[k]; }
+    for (int k = 1; k <= PT_LEVELS; ++k) {
+      x -= found ? 0 : count[k - 1];
+      at = found ? at : x0[k];
+      c = found ? c : col[k];
+      found |= x < count[k];
+    }
     return base + ((int64_t)(at + x) * TC + c) * RD;
   };
-  float *tops = reinterpret_cast<float *>(smem), *sums = tops + PT_WAVES, *os = sums + PT_WAVES;       // [wave][D]
-  float top = -INFINITY;
-  for (int x = tid; x < parts; x += PT_THREADS) top = fmaxf(top, part_of(x)[D]);
+  float top = -INFINITY, total = 0.f;
+  f32x4 y = {0.f, 0.f, 0.f, 0.f};
+  if (g < GROUPS) {
+    for (int first = g; first < parts; first += N * GROUPS) {
+      f32x4 o[N];
+      float m[N], l[N];
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-  if (lane == 0) tops[wave] = top;
-  __syncthreads();
-  top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-  float ls = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int x = wave; x < parts; x += PT_WAVES) {
-    const float *p = part_of(x);
-    const float by = at_exp2((p[D] - finite_or_0(top)) * a.scale);
-    ls += by * p[D + 1];
+      for (int k = 0; k < N; ++k) {
+        const int x = first + k * GROUPS;
+        const float *p = part_of(min(x, parts - 1));
+        o[k] = *reinterpret_cast<const f32x4 *>(p + i);
+        m[k] = x < parts ? p[D] : -INFINITY;
+        l[k] = x < parts ? p[D + 1] : 0.f;
+      }
+      float grown = top;
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (lane + 64 * k < D) y[k] = fmaf(by, p[lane + 64 * k], y[k]);
+      for (int k = 0; k < N; ++k) grown = fmaxf(grown, m[k]);
+      const float by = at_exp2((top - finite_or_0(grown)) * a.scale);
+      total *= by;
+      y *= by;
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        const float w = at_exp2((m[k] - finite_or_0(grown)) * a.scale);
+        total = fmaf(w, l[k], total);
+        if (first + k * GROUPS < parts) y += w * o[k];
+      }
+      top = grown;
+    }
+    if (i == 0) { tops[g] = top; totals[g] = total; }
+    *reinterpret_cast<f32x4 *>(sums + g * D + i) = y;
   }
-#pragma unroll
-  for (int k = 0; k < 4; ++k)
-    if (lane + 64 * k < D) os[wave * D + lane + 64 * k] = y[k];
-  if (lane == 0) sums[wave] = ls;
   __syncthreads();
-  ls = (sums[0] + sums[1]) + (sums[2] + sums[3]);
-  for (int i = tid; i < D; i += PT_THREADS) {
-    const float v = (os[i] + os[D + i]) + (os[2 * D + i] + os[3 * D + i]);
-    const float r = ls == 0.f ? 0.f : v / ls;
-    T *out = reinterpret_cast<T *>(a.out) + (int64_t)row * a.out_stride + (int64_t)head * D + i;
-    if constexpr (sizeof(T) == 2) *out = (uint16_t)cvt_pk_bf16(r, 0.f);
-    else *out = r;
-    if (a.lse && i == 0) a.lse[(int64_t)row * a.n_q + head] = at_lse(top, a.scale, ls);
+  const int groups = min(GROUPS, parts);
+  if (tid < LANES) {
+    float most = -INFINITY, ls = 0.f;
+    for (int x = 0; x < groups; ++x) most = fmaxf(most, tops[x]);
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    for (int x = 0; x < groups; ++x) {
+      const float w = at_exp2((tops[x] - finite_or_0(most)) * a.scale);
+      ls = fmaf(w, totals[x], ls);
+      v += w * *reinterpret_cast<const f32x4 *>(sums + x * D + i);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = ls == 0.f ? 0.f : v[e] / ls;
+    Op<T>::store4(reinterpret_cast<T *>(a.out) + (int64_t)row * a.out_stride + (int64_t)head * D + i, v[0], v[1], v[2], v[3]);
+    if (a.lse && i == 0) a.lse[(int64_t)row * a.n_q + head] = at_lse(most, a.scale, ls);
   }
 }
 
@@ -710,19 +738,15 @@ static inline int pt_shares(const parse_kv *kv) {
 }
 static inline size_t pt_deal_bytes(int64_t entries) { return round_up((PT_DEAL + (size_t)entries + 1) * 4, 256); }
 
-template <class T, bool LISTED>
-static int pt_join_launch(const PtArgs &a, int TC, hipStream_t s) {
-  attend_parts_join<T, LISTED><<<dim3(a.n_q, a.rows), PT_THREADS, (2 * PT_WAVES + PT_WAVES * a.kv.d) * 4, s>>>(a, TC);
-  PARSE_LAUNCH_CHECK();
-  return PARSE_OK;
-}
 template <class T, int DT, bool LISTED>
 static int pt_launch(const PtArgs &a, int64_t entries, hipStream_t s) {
   const size_t lds = pt_lds_own<T, DT>() + (PT_WAVES + (LISTED ? 0 : (size_t)entries + 1)) * 4;
   PARSE_ALLOW_LDS((attend_parts<T, DT, LISTED>), 0, lds);
   attend_parts<T, DT, LISTED><<<dim3(a.shares, a.kv.n_kv), PT_THREADS, lds, s>>>(a);
   PARSE_LAUNCH_CHECK();
-  return pt_join_launch<T, LISTED>(a, 64 * pt_blocks<T, DT>(), s);
+  attend_parts_join<T, DT, LISTED><<<dim3(a.n_q, a.rows), PT_THREADS, 0, s>>>(a);
+  PARSE_LAUNCH_CHECK();
+  return PARSE_OK;
 }
 template <class T, bool LISTED>
 static int pt_width(const PtArgs &a, int64_t entries, hipStream_t s) {

@@ -195,9 +195,10 @@ __global__ __launch_bounds__(SH_ONE) void shared_tiles(parse_kv kv, const int32_
       plan.row[r].tile[l] = tile0[of];
       plan.row[r].column[l] = rank * group;
       if (of == r) {
-        const int all = users[r] * group, pos = kv_seq(kv, seqs, r).len - 1;
+        const int all = users[r] * group;
+        const KvSeq of_r = kv_seq(kv, seqs, r);
         for (int f = 0, t = tile0[r]; f < all; f += TC, ++t)
-          plan.tile[t] = PtTile{list0[r], users[r], f, min(TC, all - f), w.x, w.y, base0[r] + f, pos};
+          plan.tile[t] = PtTile{list0[r], of_r.row, f, min(TC, all - f), w.x, w.y, base0[r] + f, of_r.len - 1};
       }
     }
     tiles += total[0]; listed += total[1]; columns += total[2];
