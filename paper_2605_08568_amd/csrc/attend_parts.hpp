@@ -163,35 +163,53 @@ __global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_part
   extern __shared__ char smem[];
   float *red = reinterpret_cast<float *>(smem);                    // [wave][16][RD], [wave][16] twice; or the ring
   float *red_m = red + PT_WAVES * 16 * RD, *red_l = red_m + PT_WAVES * 16;
-  int *wave_sums = reinterpret_cast<int *>(smem + pt_lds_own<T, DT>()), *pre = wave_sums + PT_WAVES;
+  int *wave_sums = reinterpret_cast<int *>(smem + pt_lds_own<T, DT>()), *pre = wave_sums + 2 * PT_WAVES;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 15, quad = lane >> 4;
   const int share = blockIdx.x, kvh = blockIdx.y;
-  int tiles = 0, tile_columns = 0;
+  int tiles = 0, tile_columns = 0, total;
   bool fits = false;
-  if constexpr (!LISTED) {
+  const int list_steps = LISTED ? (int)(((int64_t)a.top * a.kv.page + PT_STEP - 1) / PT_STEP) : 0;
+  auto tile_span = [&](const PtTile &t) { return pt_span(t.pos, t.from, t.to, a.window, a.sinks); };
+  auto own_span = [&](int from, const KvSeq &s) { return pt_span(s.len - 1, min(from, s.len), s.len, a.window, a.sinks); };
+  auto from_of = [&](int row) { return fits ? a.plan.row[row].from : 0; };
+  if constexpr (LISTED) {
+    total = list_steps * a.rows * a.per_row;
+  } else {
+    // a thread's first tile and row are asked for before it is known how many there are, and whether the plan is this call's
+    const PtTile t = a.plan.tile[min(tid, a.most_tiles - 1)];
+    const int r = min(tid, a.rows - 1), from = a.plan.row[r].from;
+    const KvSeq seq = kv_seq(a.kv, a.seqs, r);
     fits = pt_fits(a, TC);
     if (fits) { tiles = a.plan.head->tiles; tile_columns = a.plan.head->tile_columns; }
+    if (tiles <= PT_THREADS && a.rows <= PT_THREADS) {
+      const int of_tile = tid < tiles ? tile_span(t).count : 0, of_row = tid < a.rows ? own_span(fits ? from : 0, seq).count : 0;
+      const int up_tile = wave_scan(of_tile), up_row = wave_scan(of_row * a.per_row);
+      if (lane == 63) { wave_sums[wave] = up_tile; wave_sums[PT_WAVES + wave] = up_row; }
+      __syncthreads();
+      int before = up_tile - of_tile, behind = up_row - of_row * a.per_row;
+      total = 0;
+#pragma unroll
+      for (int w = 0; w < PT_WAVES; ++w) {
+        before += w < wave ? wave_sums[w] : 0;
+        behind += wave_sums[w] + (w < wave ? wave_sums[PT_WAVES + w] : 0);
+        total += wave_sums[w] + wave_sums[PT_WAVES + w];
+      }
+      if (tid < tiles) pre[tid] = before;
+      if (tid < a.rows)
+        for (int z = 0; z < a.per_row; ++z) pre[tiles + tid * a.per_row + z] = behind + z * of_row;
+      if (tid == 0) pre[tiles + a.rows * a.per_row] = total;
+      __syncthreads();
+    } else {
+      kv_prefix<PT_THREADS>(tiles + a.rows * a.per_row, pre, wave_sums, [&](int e) {
+        if (e < tiles) return tile_span(a.plan.tile[e]).count;
+        const int row = (e - tiles) / a.per_row;
+        return own_span(from_of(row), kv_seq(a.kv, a.seqs, row)).count;
+      });
+      total = pre[tiles + a.rows * a.per_row];
+    }
   }
   const int entries = tiles + a.rows * a.per_row;
-  const int list_steps = LISTED ? (int)(((int64_t)a.top * a.kv.page + PT_STEP - 1) / PT_STEP) : 0;
-  auto own_span = [&](int row, const KvSeq &s) { return pt_span(s.len - 1, fits ? min(a.plan.row[row].from, s.len) : 0, s.len, a.window, a.sinks); };
-  auto count_of = [&](int e) {
-    if constexpr (LISTED) return list_steps;
-    if (e < tiles) {
-      const PtTile t = a.plan.tile[e];
-      return pt_span(t.pos, t.from, t.to, a.window, a.sinks).count;
-    }
-    const int row = (e - tiles) / a.per_row;
-    return own_span(row, kv_seq(a.kv, a.seqs, row)).count;
-  };
-  int total;
-  if constexpr (LISTED) {
-    total = list_steps * entries;
-  } else {
-    kv_prefix<PT_THREADS>(entries, pre, wave_sums, count_of);
-    total = pre[entries];
-  }
   auto before_of = [&](int e) { return LISTED ? e * list_steps : pre[e]; };
   // Tiles are cut in shares of PT_WIDE_STEPS at least: a part of them is as many bytes as four steps, written and read again
   const int per = max(((total + a.shares - 1) / a.shares + PT_WAVES - 1) / PT_WAVES * PT_WAVES, tiles > 0 ? PT_WIDE_STEPS : PT_WAVES);
@@ -213,8 +231,23 @@ __global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_part
   const int tok = 8 * (n >> 2) + (n & 3);
   const int page_bits = 31 - __builtin_clz(a.kv.page);
   const int k_in = quad * 128 + (tok & 15) * 8, v_in = ((quad & 1) * D + n) * 8;
-  const int e0 = __builtin_amdgcn_readfirstlane(LISTED ? (int)begin / list_steps : kv_find(pre, entries, (int)begin));
-  const int e1 = __builtin_amdgcn_readfirstlane(LISTED ? (end - 1) / list_steps : kv_find(pre, entries, end - 1));
+  int e0, e1;                                                      // first and last entry of the share
+  if constexpr (LISTED) {
+    e0 = (int)begin / list_steps;
+    e1 = (end - 1) / list_steps;
+  } else if (entries <= 512) {
+    e0 = e1 = -1;
+    for (int e = 0; e < entries; e += 64) {
+      const int v = pre[min(e + lane, entries)];
+      e0 += __popcll(__ballot(e + lane < entries && v <= (int)begin));
+      e1 += __popcll(__ballot(e + lane < entries && v < end));
+    }
+  } else {
+    e0 = kv_find(pre, entries, (int)begin);
+    e1 = kv_find(pre, entries, end - 1);
+  }
+  e0 = __builtin_amdgcn_readfirstlane(e0);
+  e1 = __builtin_amdgcn_readfirstlane(e1);
   float *parts = a.part + (int64_t)kvh * ((int64_t)a.shares * TC + (LISTED ? 0 : (int64_t)PT_LEVELS * a.rows * a.group) + (int64_t)a.rows * a.group) * RD;
   // Rows of sixteen columns at most that a wavefront has alone: from `alone` on
   const int rows0 = max(e0, tiles);
@@ -238,7 +271,7 @@ __global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_part
     if (tile) {
       t = a.plan.tile[e];
       seq = t.seq; columns = t.columns; base = t.base;
-      span = pt_span(t.pos, t.from, t.to, a.window, a.sinks);
+      span = tile_span(t);
       if (a.window > 0) {                                          // pages behind the window may have been given up since, by some of the rows
         const PtShortest s = pt_shortest(a, t);
         if (s.pos >= 0) seq = s.row;
@@ -251,7 +284,7 @@ __global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_part
       columns = min(a.group - z * TC, TC);
       base = tile_columns + row * a.group + z * TC;
       if constexpr (!LISTED) {
-        span = own_span(row, s);
+        span = own_span(from_of(row), s);
         direct = !fits || a.plan.row[row].levels == 0;
       }
     }
@@ -276,28 +309,42 @@ __global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_part
       auto column = [&](int b) { return WIDE ? 16 * (wave + PT_WAVES * b) + n : n; };
       frag qf[NA][KB];
       int pos[NA], lo[NA], least = 0x7fffffff, most = 0;
+      // q and what the columns see: asked for behind the first steps
+      auto ask = [&]() {
+        int r[NA], h[NA];
 #pragma unroll
-      for (int b = 0; b < NA; ++b) {
-        const int c = min(column(b), columns - 1);
-        int r = row, h = z * TC + c;
-        pos[b] = pos_of;
-        if (tile) {
-          const int f = t.first + c, m = f / a.group;
-          r = a.plan.list[t.list + m];
-          h = f - m * a.group;
-          pos[b] = kv_seq(a.kv, a.seqs, r).len - 1;
+        for (int b = 0; b < NA; ++b) {
+          const int c = min(column(b), columns - 1);
+          r[b] = row; h[b] = z * TC + c;
+          pos[b] = pos_of;
+          if (tile) {
+            const int f = t.first + c, m = f / a.group;
+            r[b] = a.plan.list[t.list + m];
+            h[b] = f - m * a.group;
+          }
         }
-        lo[b] = LISTED ? 0 : kv_window_begin(pos[b], a.window);
-        least = min(least, pos[b]);
-        most = max(most, lo[b]);
-        const T *q = reinterpret_cast<const T *>(a.q) + (int64_t)r * a.q_stride + (int64_t)(kvh * a.group + h) * D;
 #pragma unroll
-        for (int k = 0; k < KB; ++k) qf[b][k] = Op<T>::sign(Op<T>::load(q + 32 * k + 8 * quad), a.q_sign);
-      }
+        for (int b = 0; b < NA; ++b) {
+          const T *q = reinterpret_cast<const T *>(a.q) + (int64_t)r[b] * a.q_stride + (int64_t)(kvh * a.group + h[b]) * D;
 #pragma unroll
-      for (int o = 8; o > 0; o >>= 1) { least = min(least, __shfl_xor(least, o, 64)); most = max(most, __shfl_xor(most, o, 64)); }
-      least = __builtin_amdgcn_readfirstlane(least);
-      most = __builtin_amdgcn_readfirstlane(most);
+          for (int k = 0; k < KB; ++k) qf[b][k] = Op<T>::load(q + 32 * k + 8 * quad);
+          if (tile) pos[b] = kv_seq(a.kv, a.seqs, r[b]).len - 1;
+        }
+#pragma unroll
+        for (int b = 0; b < NA; ++b) {
+          lo[b] = LISTED ? 0 : kv_window_begin(pos[b], a.window);
+          least = min(least, pos[b]);
+          most = max(most, lo[b]);
+        }
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) { least = min(least, __shfl_xor(least, o, 64)); most = max(most, __shfl_xor(most, o, 64)); }
+        least = __builtin_amdgcn_readfirstlane(least);
+        most = __builtin_amdgcn_readfirstlane(most);
+#pragma unroll
+        for (int b = 0; b < NA; ++b)
+#pragma unroll
+          for (int k = 0; k < KB; ++k) qf[b][k] = Op<T>::sign(qf[b][k], a.q_sign);
+      };
       float m[NA], l[NA];
       f32x4 o[NA][VB];
       auto clear = [&]() {
@@ -423,6 +470,7 @@ __global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_part
         if constexpr (DT * sizeof(T) <= 8) {                         // two steps fit the registers
           Step odd;
           if (steps > 0) load(even, 0);
+          ask();
           for (int j = 0; j < steps; j += 2) {
             if (j + 1 < steps) load(odd, j + 1);
             work(even);
@@ -432,6 +480,7 @@ __global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_part
             }
           }
         } else {
+          ask();
           for (int j = 0; j < steps; ++j) {
             load(even, j);
             work(even);
@@ -466,10 +515,11 @@ __global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_part
           there_ab = (page_there(id_a) ? 1 : 0) | (page_there(id_b) ? 2 : 0);
         };
         look(0);
-        __syncthreads();                                             // the sums of the entry before are read
+        if (e > e0) __syncthreads();                                 // the sums of the entry before are read
 #pragma unroll
         for (int j = 0; j < ST - 1; ++j)
           if (j < steps) stage();
+        ask();
         // where this lane's pieces stand: rows 0..7 of an operand in the first half, 8..15 in the second
         const int k_at = (n < 8 ? 0 : CHUNK) + (quad * 16 + (tok & 15)) * 8 * (int)sizeof(T), k_turn = n < 8 ? 0 : 4 * 8 * (int)sizeof(T);
         const int v_at = 2 * CHUNK + (quad >> 1) * CHUNK + v_in * (int)sizeof(T);
@@ -495,6 +545,9 @@ __global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_part
             const bool whole = whole_of(x);
             uint32_t keep[NA] = {}, any = 0xffu;
             if (!whole) any = any_seen(x, keep);
+            frag vf[VB];                                             // before the weights: a branch stands among those
+#pragma unroll
+            for (int v = 0; v < VB; ++v) vf[v] = Op<T>::load(reinterpret_cast<const T *>(buf + v_at) + v * 128);
             frag pf[NB], rest[NB];
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
@@ -505,12 +558,11 @@ __global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_part
             }
 #pragma unroll
             for (int v = 0; v < VB; ++v) {
-              frag vf = Op<T>::load(reinterpret_cast<const T *>(buf + v_at) + v * 128);
-              if (!whole) vf = Op<T>::only(vf, any);
+              if (!whole) vf[v] = Op<T>::only(vf[v], any);
 #pragma unroll
               for (int b = 0; b < NB; ++b) {
-                o[b][v] = Op<T>::mma16(vf, pf[b], o[b][v]);
-                if constexpr (sizeof(T) == 2) o[b][v] = Op<T>::mma16(vf, rest[b], o[b][v]);
+                o[b][v] = Op<T>::mma16(vf[v], pf[b], o[b][v]);
+                if constexpr (sizeof(T) == 2) o[b][v] = Op<T>::mma16(vf[v], rest[b], o[b][v]);
               }
             }
           }
@@ -740,7 +792,7 @@ static inline size_t pt_deal_bytes(int64_t entries) { return round_up((PT_DEAL +
 
 template <class T, int DT, bool LISTED>
 static int pt_launch(const PtArgs &a, int64_t entries, hipStream_t s) {
-  const size_t lds = pt_lds_own<T, DT>() + (PT_WAVES + (LISTED ? 0 : (size_t)entries + 1)) * 4;
+  const size_t lds = pt_lds_own<T, DT>() + (2 * PT_WAVES + (LISTED ? 0 : (size_t)entries + 1)) * 4;
   PARSE_ALLOW_LDS((attend_parts<T, DT, LISTED>), 0, lds);
   attend_parts<T, DT, LISTED><<<dim3(a.shares, a.kv.n_kv), PT_THREADS, lds, s>>>(a);
   PARSE_LAUNCH_CHECK();
