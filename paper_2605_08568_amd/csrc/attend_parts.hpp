@@ -309,27 +309,31 @@ __global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_part
       auto column = [&](int b) { return WIDE ? 16 * (wave + PT_WAVES * b) + n : n; };
       frag qf[NA][KB];
       int pos[NA], lo[NA], least = 0x7fffffff, most = 0;
-      // q and what the columns see: asked for behind the first steps
-      auto ask = [&]() {
-        int r[NA], h[NA];
+      // q and what the columns see.  Three trips to memory one behind another: the rows go with the pages' numbers, q and the lengths with the first steps.
+      int r[NA], h[NA];
+      auto ask_rows = [&]() {
 #pragma unroll
         for (int b = 0; b < NA; ++b) {
           const int c = min(column(b), columns - 1);
           r[b] = row; h[b] = z * TC + c;
-          pos[b] = pos_of;
           if (tile) {
             const int f = t.first + c, m = f / a.group;
             r[b] = a.plan.list[t.list + m];
             h[b] = f - m * a.group;
           }
         }
+      };
+      auto ask = [&]() {
 #pragma unroll
         for (int b = 0; b < NA; ++b) {
           const T *q = reinterpret_cast<const T *>(a.q) + (int64_t)r[b] * a.q_stride + (int64_t)(kvh * a.group + h[b]) * D;
+          pos[b] = pos_of;
+          if (tile) pos[b] = kv_seq(a.kv, a.seqs, r[b]).len - 1;
 #pragma unroll
           for (int k = 0; k < KB; ++k) qf[b][k] = Op<T>::load(q + 32 * k + 8 * quad);
-          if (tile) pos[b] = kv_seq(a.kv, a.seqs, r[b]).len - 1;
         }
+      };
+      auto asked = [&]() {
 #pragma unroll
         for (int b = 0; b < NA; ++b) {
           lo[b] = LISTED ? 0 : kv_window_begin(pos[b], a.window);
@@ -469,8 +473,10 @@ __global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_part
         Step even;
         if constexpr (DT * sizeof(T) <= 8) {                         // two steps fit the registers
           Step odd;
+          ask_rows();
           if (steps > 0) load(even, 0);
           ask();
+          asked();
           for (int j = 0; j < steps; j += 2) {
             if (j + 1 < steps) load(odd, j + 1);
             work(even);
@@ -480,7 +486,9 @@ __global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_part
             }
           }
         } else {
+          ask_rows();
           ask();
+          asked();
           for (int j = 0; j < steps; ++j) {
             load(even, j);
             work(even);
@@ -514,17 +522,19 @@ __global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_part
           place(u, 1, id_b, at_b);
           there_ab = (page_there(id_a) ? 1 : 0) | (page_there(id_b) ? 2 : 0);
         };
+        ask_rows();
         look(0);
         if (e > e0) __syncthreads();                                 // the sums of the entry before are read
 #pragma unroll
         for (int j = 0; j < ST - 1; ++j)
           if (j < steps) stage();
         ask();
+        asked();
         // where this lane's pieces stand: rows 0..7 of an operand in the first half, 8..15 in the second
         const int k_at = (n < 8 ? 0 : CHUNK) + (quad * 16 + (tok & 15)) * 8 * (int)sizeof(T), k_turn = n < 8 ? 0 : 4 * 8 * (int)sizeof(T);
         const int v_at = 2 * CHUNK + (quad >> 1) * CHUNK + v_in * (int)sizeof(T);
+#pragma unroll 1
         for (int j = 0; j < steps; ++j) {
-          if (j > 0 && (j & 63) == 0) look(j);
           wait_slices<ST - 2, LOADS>(steps - 1 - j);
           wg_barrier();                                              // this step has landed for everybody, the one before it is read by everybody
           if (staged < steps) stage();
@@ -566,6 +576,7 @@ __global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_part
               }
             }
           }
+          if (((j + 1) & 63) == 0) look(j + 1);
         }
       }
       if constexpr (NB > 0) {
