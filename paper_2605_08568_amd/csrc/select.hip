@@ -13,71 +13,97 @@ struct KbArgs {
   const void *K;
   void *bounds;                                      // of the first layer: [page][head][2][d]
   const int32_t *tok_offsets, *seqs;
-  int P, layers;
+  int P, layers, at_once;                            // at_once: heads that a wavefront has one after another
   int64_t k_layer, b_layer;                          // elements
 };
 
-// smaller / larger of two, NaN if one of them is
+// smaller of two, NaN if one of them is
 __device__ __forceinline__ float kb_min(float a, float b) { return __builtin_elementwise_minimum(a, b); }
-__device__ __forceinline__ float kb_max(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
-// A wavefront has a page of one head: a load brings 64 pieces of eight columns, lane % 16 the token, so that the block's 16 tokens are the lanes of a row.
+// Smaller of two over lanes that stand opposite each other: N values a lane become N / 2, the lower ones where `upper` is clear, the upper ones where it is set
+template <int CTRL, int N>
+__device__ __forceinline__ void kb_fold(float *v, bool upper) {
+#pragma unroll
+  for (int k = 0; k < N / 2; ++k) {
+    const float keep = upper ? v[k + N / 2] : v[k], give = upper ? v[k] : v[k + N / 2];
+    v[k] = kb_min(keep, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(give), CTRL, 0xf, 0xf, false)));
+  }
+}
+
+// A wavefront has pages of single heads: a load brings 64 pieces of eight columns, lane % 16 the token, so that a block's sixteen tokens are a row of lanes; the rows fold
+// to one value a lane in 60 exchanges (values and negated values side by side: the largest is the least of the negated).  The next head's first block is asked for before this
+// one's lanes fold.  Bound: reads; pages of 16 tokens by the vector unit as much (bf16 to fp32, two comparisons a value, the folding).
 template <class T, int DT>
 __global__ __launch_bounds__(SP_THREADS) void kv_bounds(KbArgs a) {
   constexpr int D = DT * 32;
+  typedef typename Op<T>::frag frag;
   extern __shared__ int pre[];
   int *wave_sums = pre + a.P + 1;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, page = a.kv.page;
-  const int heads = a.kv.n_kv * a.layers, per = (heads + SP_WAVES - 1) / SP_WAVES;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, page = a.kv.page, blocks = page / 16;
+  const int heads = a.kv.n_kv * a.layers, per = (heads + SP_WAVES * a.at_once - 1) / (SP_WAVES * a.at_once);
   for (int64_t w = blockIdx.x;; w += gridDim.x) {
     const int64_t number = w / per;
     if (number > 0x7fffffff) return;
     const KvItem f = kv_item<SP_THREADS>(a.kv, a.tok_offsets, a.seqs, a.P, 0x7fffffff, (int)number, pre, wave_sums,
                                          [&](const KvRows &r, const KvSeq &s) { return s.len / page - max(s.len - r.n, 0) / page; });
     if (f.item < 0) return;
-    const int c = max(f.len - f.n, 0) / page + f.item, lh = (int)(w % per) * SP_WAVES + wave;
+    const int c = max(f.len - f.n, 0) / page + f.item;
     const int id = a.kv.table[(int64_t)f.row * a.kv.max_pages + c];
-    if (lh < heads && id >= 0 && id < a.kv.n_pages) {
-      const int layer = lh / a.kv.n_kv, head = lh % a.kv.n_kv;
-      const T *k = reinterpret_cast<const T *>(a.K) + layer * a.k_layer + ((int64_t)id * a.kv.n_kv + head) * page * D + lane * 8;
-      float lo[DT][8], hi[DT][8];
+    int lh = (int)(w % per) * SP_WAVES * a.at_once + wave;
+    const int behind = min(lh - wave + SP_WAVES * a.at_once, heads);
+    if (id >= 0 && id < a.kv.n_pages && lh < behind) {
+      auto keys = [&](int of) {
+        const int layer = of / a.kv.n_kv, head = of - layer * a.kv.n_kv;
+        return reinterpret_cast<const T *>(a.K) + layer * a.k_layer + ((int64_t)id * a.kv.n_kv + head) * page * D + lane * 8;
+      };
+      frag x[DT];
+      const T *k = keys(lh);
 #pragma unroll
-      for (int p = 0; p < DT; ++p)
+      for (int p = 0; p < DT; ++p) x[p] = Op<T>::load_nt(k + p * 512);
+      for (; lh < behind; lh += SP_WAVES) {
+        float v[16 * DT];                                          // [least, largest negated][column of the piece][piece]
 #pragma unroll
-        for (int e = 0; e < 8; ++e) { lo[p][e] = INFINITY; hi[p][e] = -INFINITY; }
-      for (int b = 0; b < page / 16; ++b) {
-        float v[DT][8];
-#pragma unroll
-        for (int p = 0; p < DT; ++p) {
-          const typename Op<T>::frag x = Op<T>::load(k + b * 16 * D + p * 512);
+        for (int i = 0; i < 16 * DT; ++i) v[i] = INFINITY;
+        auto take = [&](const frag &y, int p) {
+          float z[8];
           if constexpr (sizeof(T) == 2) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) { v[p][2 * e] = __uint_as_float(x[e] << 16); v[p][2 * e + 1] = __uint_as_float(x[e] & 0xffff0000u); }
+            for (int e = 0; e < 4; ++e) { z[2 * e] = __uint_as_float(y[e] << 16); z[2 * e + 1] = __uint_as_float(y[e] & 0xffff0000u); }
           } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) { v[p][e] = x.lo[e]; v[p][4 + e] = x.hi[e]; }
+            for (int e = 0; e < 4; ++e) { z[e] = y.lo[e]; z[4 + e] = y.hi[e]; }
           }
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            v[e * DT + p] = kb_min(v[e * DT + p], z[e]);
+            v[(8 + e) * DT + p] = kb_min(v[(8 + e) * DT + p], -z[e]);
+          }
+        };
+        for (int b = 1; b < blocks; ++b) {
+          frag y[DT];
+#pragma unroll
+          for (int p = 0; p < DT; ++p) y[p] = Op<T>::load_nt(k + b * 16 * D + p * 512);
+#pragma unroll
+          for (int p = 0; p < DT; ++p) { take(x[p], p); x[p] = y[p]; }
         }
 #pragma unroll
-        for (int p = 0; p < DT; ++p)
+        for (int p = 0; p < DT; ++p) take(x[p], p);
+        const int layer = lh / a.kv.n_kv, head = lh - layer * a.kv.n_kv;
+        if (lh + SP_WAVES < behind) {
+          k = keys(lh + SP_WAVES);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) { lo[p][e] = kb_min(lo[p][e], v[p][e]); hi[p][e] = kb_max(hi[p][e], v[p][e]); }
-      }
-#pragma unroll
-      for (int o = 8; o > 0; o >>= 1)
-#pragma unroll
-        for (int p = 0; p < DT; ++p)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) { lo[p][e] = kb_min(lo[p][e], __shfl_xor(lo[p][e], o, 64)); hi[p][e] = kb_max(hi[p][e], __shfl_xor(hi[p][e], o, 64)); }
-      T *to = reinterpret_cast<T *>(a.bounds) + layer * a.b_layer + ((int64_t)id * a.kv.n_kv + head) * 2 * D;
-      if ((lane & 15) == 0) {
+          for (int p = 0; p < DT; ++p) x[p] = Op<T>::load_nt(k + p * 512);
+        }
+        kb_fold<0x140, 16 * DT>(v, lane & 8);                      // row_mirror: lane ^ 15
+        kb_fold<0x141, 8 * DT>(v, lane & 4);                       // row_half_mirror: lane ^ 7
+        kb_fold<0x1b, 4 * DT>(v, lane & 2);                        // quad_perm 3 2 1 0
+        kb_fold<0xb1, 2 * DT>(v, lane & 1);                        // quad_perm 1 0 3 2
+        T *to = reinterpret_cast<T *>(a.bounds) + layer * a.b_layer + ((int64_t)id * a.kv.n_kv + head) * 2 * D + (lane & 8 ? D : 0) + (lane >> 4) * 8 + (lane & 7);
 #pragma unroll
         for (int p = 0; p < DT; ++p) {
-          T *t = to + (p * 4 + (lane >> 4)) * 8;
-          Op<T>::store4(t, lo[p][0], lo[p][1], lo[p][2], lo[p][3]);
-          Op<T>::store4(t + 4, lo[p][4], lo[p][5], lo[p][6], lo[p][7]);
-          Op<T>::store4(t + D, hi[p][0], hi[p][1], hi[p][2], hi[p][3]);
-          Op<T>::store4(t + D + 4, hi[p][4], hi[p][5], hi[p][6], hi[p][7]);
+          const float r = lane & 8 ? -v[p] : v[p];
+          if constexpr (sizeof(T) == 2) to[p * 32] = (T)(__float_as_uint(r) >> 16);        // it is one of the keys
+          else to[p * 32] = r;
         }
       }
     }
@@ -95,6 +121,9 @@ struct SpArgs {
   uint64_t *keys;                                    // [row][head][max_pages]
   int32_t *sel;
 };
+
+// Lanes for a page's bounds of one head, eight columns of one of the two each
+constexpr int sp_lanes(int d) { return d <= 32 ? 8 : d <= 64 ? 16 : d <= 128 ? 32 : 64; }
 
 // Doubles in their order as unsigned numbers; NaN is the largest, whatever its sign
 __device__ __forceinline__ uint64_t sp_key(double v) {
@@ -114,166 +143,251 @@ __device__ __forceinline__ SpCols sp_cols(const SpArgs &a, int len) {
   return c;
 }
 
+// Sum over LP lanes of eight values a lane, LP >= 8: lane l of a group ends with that of value l % 8 (moves in the vector unit).
+template <int CTRL> __device__ __forceinline__ double sp_move(double v) {
+  const uint64_t u = (uint64_t)__double_as_longlong(v);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, 0xf, 0xf, false), hi = __builtin_amdgcn_update_dpp(0, (int)(u >> 32), CTRL, 0xf, 0xf, false);
+  return __longlong_as_double((int64_t)((uint64_t)hi << 32 | lo));
+}
+template <int CTRL, int N> __device__ __forceinline__ void sp_fold(double *v, bool upper) {
+#pragma unroll
+  for (int k = 0; k < N / 2; ++k) {
+    const double keep = upper ? v[2 * k + 1] : v[2 * k], give = upper ? v[2 * k] : v[2 * k + 1];
+    v[k] = keep + sp_move<CTRL>(give);
+  }
+}
+template <int LP> __device__ __forceinline__ double sp_sum8(double *v) {
+  const int lane = threadIdx.x & 63;
+  sp_fold<0xb1, 8>(v, lane & 1);                                   // lane ^ 1
+  sp_fold<0x4e, 4>(v, lane & 2);                                   // lane ^ 2
+  // lane ^ 7 would turn the lowest two bits as well: a quarter round each, then lane ^ 4
+  const double give = lane & 4 ? v[0] : v[1], keep = lane & 4 ? v[1] : v[0];
+  double s = keep + __shfl_xor(give, 4, 64);
+  if constexpr (LP > 8) s += __shfl_xor(s, 8, 64);
+  if constexpr (LP > 16) s += __shfl_xor(s, 16, 64);
+  if constexpr (LP > 32) s += __shfl_xor(s, 32, 64);
+  return s;
+}
+
 // LP lanes have a page's bounds of one head, eight columns of one of the two each, and what of q they are multiplied with in 64 bits: the sum over the group's heads
-// of what is positive goes with the largest, of what is negative with the least.  Sums in 64 bits because a choice hangs on neighbours in the order.
+// of what is positive goes with the largest, of what is negative with the least.  Sums in 64 bits because a choice hangs on neighbours in the order.  Eight pages a lane on their way.
 template <class T, int DT>
 __global__ __launch_bounds__(SP_THREADS) void page_scores(SpArgs a) {
-  constexpr int D = DT * 32, LP = DT <= 2 ? 8 * DT : DT <= 4 ? 32 : 64, PAGES = 64 / LP, AT_ONCE = 4;
+  constexpr int D = DT * 32, LP = sp_lanes(D), PAGES = 64 / LP, AT_ONCE = 8;
+  typedef typename Op<T>::frag frag;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, piece = lane % LP, slot = lane / LP;
   const int head = blockIdx.y, row = blockIdx.z;
+  const bool has = piece < D / 4;
+  const int half = piece >= D / 8 ? 1 : 0, col = has ? (piece - half * (D / 8)) * 8 : 0;
+  auto values = [](const frag &x, float *v) {
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { v[2 * e] = __uint_as_float(x[e] << 16); v[2 * e + 1] = __uint_as_float(x[e] & 0xffff0000u); }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { v[e] = x.lo[e]; v[4 + e] = x.hi[e]; }
+    }
+  };
+  double q[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  {
+    const T *p = reinterpret_cast<const T *>(a.q) + (int64_t)row * a.q_stride + (int64_t)head * a.group * D + col;
+    for (int h0 = 0; h0 < a.group; h0 += 4) {
+      frag x[4];
+#pragma unroll
+      for (int h = 0; h < 4; ++h) x[h] = Op<T>::load(p + (int64_t)min(h0 + h, a.group - 1) * D);
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        float v[8];
+        values(x[h], v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float part = half ? (v[e] < 0.f ? 0.f : v[e]) : (v[e] > 0.f ? 0.f : v[e]);      // a NaN stays in both
+          q[e] += h0 + h < a.group && has ? part : 0.f;
+        }
+      }
+    }
+  }
   const KvSeq sq = kv_seq(a.kv, a.seqs, row);
   const SpCols cols = sp_cols(a, sq.len);
   if (cols.n <= a.top) return;                                     // all of them are taken
-  const bool has = piece < D / 4;
-  const int half = piece >= D / 8 ? 1 : 0, col = has ? (piece - half * (D / 8)) * 8 : 0;
-  double q[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  if (has) {
-    const T *p = reinterpret_cast<const T *>(a.q) + (int64_t)row * a.q_stride + (int64_t)head * a.group * D + col;
-    for (int h = 0; h < a.group; ++h)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float v = Op<T>::value(p[(int64_t)h * D + e]);
-        q[e] += half ? (v > 0.f || v != v ? v : 0.f) : (v < 0.f || v != v ? v : 0.f);
-      }
-  }
   const int32_t *table = a.kv.table + (int64_t)sq.row * a.kv.max_pages;
   const T *bounds = reinterpret_cast<const T *>(a.bounds) + (int64_t)head * 2 * D + half * D + col;
+  const int64_t page_elems = (int64_t)a.kv.n_kv * 2 * D;
   uint64_t *keys = a.keys + ((int64_t)row * a.kv.n_kv + head) * a.kv.max_pages;
   constexpr int STEP = SP_WAVES * PAGES * AT_ONCE;
-  for (int64_t c0 = cols.begin + (int64_t)blockIdx.x * STEP; c0 < cols.end; c0 += (int64_t)gridDim.x * STEP) {
-    typename Op<T>::frag x[AT_ONCE];
+  for (int64_t c0 = cols.begin + (int64_t)blockIdx.x * STEP + wave * PAGES * AT_ONCE; c0 < cols.end; c0 += (int64_t)gridDim.x * STEP) {
+    frag x[AT_ONCE];
 #pragma unroll
     for (int k = 0; k < AT_ONCE; ++k) {
-      const int c = (int)min(c0 + (k * SP_WAVES + wave) * PAGES + slot, (int64_t)cols.end - 1), id = table[c];
-      x[k] = Op<T>::load(bounds + (int64_t)(id >= 0 && id < a.kv.n_pages ? id : 0) * a.kv.n_kv * 2 * D);
+      const int id = table[(int)min(c0 + slot * AT_ONCE + k, (int64_t)cols.end - 1)];
+      x[k] = Op<T>::load(bounds + ((unsigned)id < (unsigned)a.kv.n_pages ? id : 0) * page_elems);
     }
+    double s[AT_ONCE];
+    bool odd = false;
 #pragma unroll
     for (int k = 0; k < AT_ONCE; ++k) {
-      double s = 0.0;
-      if (has) {
+      float v[8];
+      values(x[k], v);
+      s[k] = 0.0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[k] = fma(q[e], (double)v[e], s[k]);
+      odd |= s[k] != s[k];
+    }
+    if (__any(odd)) {                                              // nothing of q times an infinity is nothing
+#pragma unroll
+      for (int k = 0; k < AT_ONCE; ++k) {
         float v[8];
-        if constexpr (sizeof(T) == 2) {
+        values(x[k], v);
+        s[k] = 0.0;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) { v[2 * e] = __uint_as_float(x[k][e] << 16); v[2 * e + 1] = __uint_as_float(x[k][e] & 0xffff0000u); }
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) { v[e] = x[k].lo[e]; v[4 + e] = x[k].hi[e]; }
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s = fma(q[e], (double)(q[e] == 0.0 ? 0.f : v[e]), s);      // nothing of q times an infinity is nothing
+        for (int e = 0; e < 8; ++e) s[k] = fma(q[e], (double)(q[e] == 0.0 ? 0.f : v[e]), s[k]);
       }
-#pragma unroll
-      for (int o = LP / 2; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-      const int64_t c = c0 + (k * SP_WAVES + wave) * PAGES + slot;
-      if (piece == 0 && c < cols.end) keys[c] = sp_key(s);
     }
+    const double sum = sp_sum8<LP>(s);
+    const int64_t c = c0 + slot * AT_ONCE + (lane & 7);
+    if (piece < 8 && c < cols.end) keys[c] = sp_key(sum);
   }
 }
 
 // ---- choice ----------------------------------------------------------------------------------------------------------
-// Sum over the threads before this one, and over all
-__device__ __forceinline__ int sp_before(int v, int *sums, int &total) {
+constexpr int SC_THREADS = 1024, SC_WAVES = SC_THREADS / 64, SC_PER = 8, SC_CHUNK = SC_THREADS * SC_PER, SC_BITS = 11;
+
+// Sums over the threads before this one, and over all; `sums`: LDS that nobody reads any more
+__device__ __forceinline__ int sc_before(int v, int *sums, int &total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, inc = wave_scan(v);
-  __syncthreads();
   if (lane == 63) sums[wave] = inc;
   __syncthreads();
-  int base = 0;
-  total = 0;
-#pragma unroll
-  for (int w = 0; w < SP_WAVES; ++w) { base += w < wave ? sums[w] : 0; total += sums[w]; }
-  return base + inc - v;
+  const int of_wave = wave_scan(lane < SC_WAVES ? sums[lane] : 0);
+  total = __builtin_amdgcn_readlane(of_wave, SC_WAVES - 1);
+  return inc - v + (wave ? __builtin_amdgcn_readlane(of_wave, wave - 1) : 0);
 }
 
-// A workgroup has a row's head: the key of the last page that is taken, eight bits after another from the first in which the keys differ, then the columns in order.
-__global__ __launch_bounds__(SP_THREADS) void page_choice(SpArgs a) {
-  __shared__ int hist[256], sums[SP_WAVES];
-  __shared__ uint64_t wide[SP_WAVES];
-  __shared__ int found[2];
-  const int tid = threadIdx.x, head = blockIdx.x, row = blockIdx.y;
+// A workgroup has a row's head: the key of the last page that is taken, SC_BITS after another from the first bit in which the keys differ, then the columns in order.  A thread has
+// SC_PER columns side by side; up to SC_CHUNK of them their keys are read once, of more once for each step.  Bound: latency, two trips to memory and about ten barriers.
+__global__ __launch_bounds__(SC_THREADS) void page_choice(SpArgs a) {
+  __shared__ int hist[1 << SC_BITS], sums[4][SC_WAVES], found[2];
+  __shared__ uint64_t wide[2][SC_WAVES];
+  static_assert((1 << SC_BITS) == 2 * SC_THREADS, "two bins a thread");
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, head = blockIdx.x, row = blockIdx.y;
   const KvSeq sq = kv_seq(a.kv, a.seqs, row);
   const SpCols cols = sp_cols(a, sq.len);
   const int32_t *table = a.kv.table + (int64_t)sq.row * a.kv.max_pages;
   int32_t *sel = a.sel + ((int64_t)row * a.kv.n_kv + head) * a.top;
   const uint64_t *keys = a.keys + ((int64_t)row * a.kv.n_kv + head) * a.kv.max_pages;
-  auto there = [&](int c) { const int id = table[c]; return id >= 0 && id < a.kv.n_pages; };
-  uint64_t prefix = 0, mask = 0;                                   // the keys that are taken are those above prefix, and `ties` of those that agree with it
-  int ties = 0;
-  if (cols.n > a.top) {
-    int mine = 0, always;
-    for (int c = tid; c < cols.begin; c += SP_THREADS) mine += there(c);
-    for (int c = cols.end + tid; c < cols.n; c += SP_THREADS) mine += there(c);
-    sp_before(mine, sums, always);
-    int want = a.top - always;                                     // of the scored ones
-    uint64_t all_or = 0, all_and = ~0ull;
-    int held = 0;
-    for (int c = cols.begin + tid; c < cols.end; c += SP_THREADS)
-      if (there(c)) { all_or |= keys[c]; all_and &= keys[c]; ++held; }
-    int total;
-    sp_before(held, sums, total);
-    if (total <= want) ties = total;                               // all of them
-    else if (want <= 0) prefix = mask = ~0ull;                     // none
-    else {
-      uint64_t differ[2] = {all_or, all_and};
+  const int chunks = (cols.n + SC_CHUNK - 1) / SC_CHUNK;
+  const bool every = cols.n <= a.top;
+  uint64_t key[SC_PER];
+  uint32_t scored = 0, always = 0;                                 // of the thread's columns of a chunk, a bit each
+  auto fetch = [&](int chunk) {
+    int id[SC_PER];
 #pragma unroll
-      for (int o = 32; o > 0; o >>= 1) { differ[0] |= __shfl_xor(differ[0], o, 64); differ[1] &= __shfl_xor(differ[1], o, 64); }
-      __syncthreads();
-      if ((tid & 63) == 0) wide[tid >> 6] = differ[0];
-      __syncthreads();
-      all_or = wide[0] | wide[1] | wide[2] | wide[3];
-      __syncthreads();
-      if ((tid & 63) == 0) wide[tid >> 6] = differ[1];
-      __syncthreads();
-      all_and = wide[0] & wide[1] & wide[2] & wide[3];
-      const uint64_t other = all_or ^ all_and;
+    for (int i = 0; i < SC_PER; ++i) {
+      const int c = chunk * SC_CHUNK + tid * SC_PER + i;
+      id[i] = c < cols.n ? table[c] : -1;
+      key[i] = !every && c >= cols.begin && c < cols.end ? keys[c] : 0;
+    }
+    scored = always = 0;
+#pragma unroll
+    for (int i = 0; i < SC_PER; ++i) {
+      const int c = chunk * SC_CHUNK + tid * SC_PER + i;
+      const uint32_t there = (unsigned)id[i] < (unsigned)a.kv.n_pages ? 1u << i : 0u;
+      if (every || c < cols.begin || c >= cols.end) always |= there; else scored |= there;
+    }
+  };
+  if (chunks == 1) fetch(0);
+  uint64_t prefix = ~0ull, mask = ~0ull;                           // the keys that are taken are those above prefix, and `ties` of those that agree with it
+  int ties = 0;
+  if (!every) {
+    int held = 0;
+    uint64_t any = 0, all = ~0ull;
+    int firm = 0;
+    for (int k = 0; k < chunks; ++k) {
+      if (chunks > 1) fetch(k);
+      firm += __popc(always);
+      held += __popc(scored);
+#pragma unroll
+      for (int i = 0; i < SC_PER; ++i)
+        if (scored >> i & 1) { any |= key[i]; all &= key[i]; }
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) { any |= __shfl_xor(any, o, 64); all &= __shfl_xor(all, o, 64); }
+    firm = __builtin_amdgcn_readlane(wave_scan(firm), 63);
+    held = __builtin_amdgcn_readlane(wave_scan(held), 63);
+    if (lane == 0) { wide[0][wave] = any; wide[1][wave] = all; sums[0][wave] = firm; sums[1][wave] = held; }
+    __syncthreads();
+    firm = held = 0;
+    for (int w = 0; w < SC_WAVES; ++w) { any |= wide[0][w]; all &= wide[1][w]; firm += sums[0][w]; held += sums[1][w]; }
+    const int want = a.top - firm;                                 // of the scored ones
+    if (held <= want) {                                            // all of them
+      prefix = mask = 0;
+      ties = held;
+    } else if (want > 0) {
+      const uint64_t other = any ^ all;
       int shift = other ? 64 - __builtin_clzll(other) : 0;         // bits below this one differ
       mask = shift == 64 ? 0 : ~0ull << shift;
-      prefix = all_and & mask;
+      prefix = all & mask;
       ties = want;
-      int left = total;
+      int left = held;
       while (shift > 0 && left > ties) {
-        const int bits = min(shift, 8), s = shift - bits;
-        hist[tid] = 0;
+        const int bits = min(shift, SC_BITS), s = shift - bits;
+        *reinterpret_cast<u32x2 *>(hist + 2 * tid) = u32x2{0, 0};
         __syncthreads();
-        for (int c = cols.begin + tid; c < cols.end; c += SP_THREADS)
-          if (there(c) && (keys[c] & mask) == prefix) atomicAdd(&hist[(keys[c] >> s) & ((1u << bits) - 1)], 1);
+        for (int k = 0; k < chunks; ++k) {
+          if (chunks > 1) fetch(k);
+#pragma unroll
+          for (int i = 0; i < SC_PER; ++i)
+            if ((scored >> i & 1) && (key[i] & mask) == prefix) atomicAdd(&hist[(key[i] >> s) & ((1u << bits) - 1)], 1);
+        }
         __syncthreads();
-        // bins from the largest on: thread t has bin 255 - t
-        const int n = hist[255 - tid];
+        // bins from the largest on, two a thread
+        const int top_bin = (1 << SC_BITS) - 1 - 2 * tid, n0 = hist[top_bin], n1 = hist[top_bin - 1];
         int sum;
-        const int before = sp_before(n, sums, sum);
-        if (before < ties && before + n >= ties) { found[0] = 255 - tid; found[1] = before; }
+        const int before = sc_before(n0 + n1, sums[2], sum);
+        if (before < ties && before + n0 >= ties) { found[0] = top_bin; found[1] = before; }
+        else if (before + n0 < ties && before + n0 + n1 >= ties) { found[0] = top_bin - 1; found[1] = before + n0; }
         __syncthreads();
         const int bin = found[0];
         left = hist[bin];
         ties -= found[1];
         prefix |= (uint64_t)bin << s;
         shift = s;
-        mask = s == 64 ? 0 : ~0ull << s;
-        __syncthreads();
+        mask = ~0ull << s;
+        __syncthreads();                                           // hist, found and sums are read
       }
     }
   }
   int at = 0;
-  for (int c0 = 0; c0 < cols.n; c0 += SP_THREADS) {
-    const int c = c0 + tid;
-    bool take = false, tie = false;
-    if (c < cols.n && there(c)) {
-      if (cols.n <= a.top || c < cols.begin || c >= cols.end) take = true;
-      else {
-        const uint64_t k = keys[c] & mask;
-        take = k > prefix;
-        tie = k == prefix;
+  for (int k = 0; k < chunks; ++k) {
+    if (chunks > 1) fetch(k);
+    uint32_t take = always, tie = 0;
+#pragma unroll
+    for (int i = 0; i < SC_PER; ++i) {
+      const uint64_t v = key[i] & mask;
+      if (scored >> i & 1) {
+        take |= v > prefix ? 1u << i : 0u;
+        tie |= v == prefix ? 1u << i : 0u;
       }
     }
     int total;
-    const int earlier = sp_before(tie ? 1 : 0, sums, total);
-    take |= tie && earlier < ties;
+    int room = ties - sc_before(__popc(tie), sums[2], total);      // equal keys: the lowest columns
+#pragma unroll
+    for (int i = 0; i < SC_PER; ++i)
+      if (tie >> i & 1) {
+        if (room > 0) take |= 1u << i;
+        --room;
+      }
     ties -= min(ties, total);
-    const int place = at + sp_before(take ? 1 : 0, sums, total);
-    if (take && place < a.top) sel[place] = c;
+    int place = at + sc_before(__popc(take), sums[3], total);
+#pragma unroll
+    for (int i = 0; i < SC_PER; ++i)
+      if (take >> i & 1) {
+        if (place < a.top) sel[place] = k * SC_CHUNK + tid * SC_PER + i;
+        ++place;
+      }
     at += total;
+    if (chunks > 1) __syncthreads();
   }
-  for (int v = at + tid; v < a.top; v += SP_THREADS) sel[v] = -1;
+  for (int v = at + tid; v < a.top; v += SC_THREADS) sel[v] = -1;
 }
 
 template <class T>
@@ -331,9 +445,11 @@ int parse_kv_bounds(const parse_kv *kv, void *bounds, int32_t layer, const int32
   a.tok_offsets = tok_offsets; a.seqs = seqs; a.P = P;
   if ((int64_t)kv->n_kv * a.layers > INT32_MAX) return PARSE_ESHAPE;
   if (tok_offsets && (int64_t)P * kv->max_pages > INT32_MAX) return PARSE_ESHAPE;              // their pages are counted in an int
-  const int64_t per = ((int64_t)kv->n_kv * a.layers + SP_WAVES - 1) / SP_WAVES;
-  const int64_t most = per * P * (tok_offsets ? (int64_t)kv->max_pages : 1);
-  const dim3 grid((uint32_t)std::min<int64_t>(most, 2048));
+  // a prompt's whole pages are no more than the pool has; heads by fours where that still makes 2048 workgroups
+  const int64_t heads = (int64_t)kv->n_kv * a.layers, items = (int64_t)P * (tok_offsets ? std::min(kv->max_pages, kv->n_pages) : 1);
+  a.at_once = items * heads >= 2048 * SP_WAVES * 4 ? 4 : 1;
+  const int64_t per = (heads + SP_WAVES * a.at_once - 1) / (SP_WAVES * a.at_once);
+  const dim3 grid((uint32_t)std::min<int64_t>(per * items, 2048));
   const size_t lds = (P + 1 + SP_WAVES) * 4;
   if (kv->dtype == PARSE_BF16) kb_launch<uint16_t>(a, grid, lds, (hipStream_t)stream);
   else kb_launch<float>(a, grid, lds, (hipStream_t)stream);
@@ -364,12 +480,13 @@ int parse_select_pages(const parse_kv *kv, const void *bounds, int32_t layer, co
   a.keys = (uint64_t *)workspace; a.sel = pages;
   if (kv->max_pages > top) {
     const int64_t pairs = (int64_t)rows * kv->n_kv;
-    const dim3 grid((uint32_t)std::min<int64_t>((kv->max_pages + 15) / 16, std::max<int64_t>(1, 4096 / pairs)), kv->n_kv, rows);
+    const int64_t step = (int64_t)SP_WAVES * 8 * (64 / sp_lanes(kv->d));
+    const dim3 grid((uint32_t)std::min<int64_t>((kv->max_pages + step - 1) / step, std::max<int64_t>(1, 4096 / pairs)), kv->n_kv, rows);
     if (kv->dtype == PARSE_BF16) sp_launch<uint16_t>(a, grid, (hipStream_t)stream);
     else sp_launch<float>(a, grid, (hipStream_t)stream);
     PARSE_LAUNCH_CHECK();
   }
-  page_choice<<<dim3(kv->n_kv, rows), SP_THREADS, 0, (hipStream_t)stream>>>(a);
+  page_choice<<<dim3(kv->n_kv, rows), SC_THREADS, 0, (hipStream_t)stream>>>(a);
   PARSE_LAUNCH_CHECK();
   return PARSE_OK;
 }
