@@ -125,11 +125,12 @@ struct SpArgs {
 // Lanes for a page's bounds of one head, eight columns of one of the two each
 constexpr int sp_lanes(int d) { return d <= 32 ? 8 : d <= 64 ? 16 : d <= 128 ? 32 : 64; }
 
-// Doubles in their order as unsigned numbers; NaN is the largest, whatever its sign
+// Doubles in their order as unsigned numbers, NaN the largest, whatever its sign; below them a column without a page, above them one that is always taken
+constexpr uint64_t SP_NONE = 0, SP_ALWAYS = ~0ull, SP_NAN = ~0ull - 1;
 __device__ __forceinline__ uint64_t sp_key(double v) {
   const int64_t b = __double_as_longlong(v);
-  if (v != v) return ~0ull;
-  return v == 0.0 ? 1ull << 63 : (uint64_t)(b ^ ((b >> 63) | (int64_t)(1ull << 63)));
+  const uint64_t k = v == 0.0 ? 1ull << 63 : (uint64_t)(b ^ ((b >> 63) | (int64_t)(1ull << 63)));
+  return v != v ? SP_NAN : k;
 }
 
 // Columns of the table that are scored: [first, n - last) of n
@@ -169,14 +170,14 @@ template <int LP> __device__ __forceinline__ double sp_sum8(double *v) {
   return s;
 }
 
-// LP lanes have a page's bounds of one head, eight columns of one of the two each, and what of q they are multiplied with in 64 bits: the sum over the group's heads
-// of what is positive goes with the largest, of what is negative with the least.  Sums in 64 bits because a choice hangs on neighbours in the order.  Eight pages a lane on their way.
-template <class T, int DT>
-__global__ __launch_bounds__(SP_THREADS) void page_scores(SpArgs a) {
-  constexpr int D = DT * 32, LP = sp_lanes(D), PAGES = 64 / LP, AT_ONCE = 8;
+// Scores of the pages from column c0 on, `step` further each time, by a wavefront: store(column, key).  LP lanes have a page's bounds of one head, eight columns of one of the
+// two each, and what of q they are multiplied with in 64 bits: the sum over the group's heads of what is positive goes with the largest, of what is negative with the
+// least.  Sums in 64 bits because a choice hangs on neighbours in the order.  Eight pages a lane on their way, the first of them before q.
+template <class T, int DT, class F>
+__device__ __forceinline__ void score_pages(const SpArgs &a, int row, int head, const KvSeq &sq, const SpCols &cols, int64_t c0, int64_t step, F store) {
+  constexpr int D = DT * 32, LP = sp_lanes(D), AT_ONCE = 8;
   typedef typename Op<T>::frag frag;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, piece = lane % LP, slot = lane / LP;
-  const int head = blockIdx.y, row = blockIdx.z;
+  const int lane = threadIdx.x & 63, piece = lane % LP, slot = lane / LP;
   const bool has = piece < D / 4;
   const int half = piece >= D / 8 ? 1 : 0, col = has ? (piece - half * (D / 8)) * 8 : 0;
   auto values = [](const frag &x, float *v) {
@@ -188,17 +189,35 @@ __global__ __launch_bounds__(SP_THREADS) void page_scores(SpArgs a) {
       for (int e = 0; e < 4; ++e) { v[e] = x.lo[e]; v[4 + e] = x.hi[e]; }
     }
   };
+  const int32_t *table = a.kv.table + (int64_t)sq.row * a.kv.max_pages;
+  const T *bounds = reinterpret_cast<const T *>(a.bounds) + (int64_t)head * 2 * D + half * D + col;
+  const int64_t page_elems = (int64_t)a.kv.n_kv * 2 * D;
+  if (c0 >= cols.end) return;
+  frag x[AT_ONCE];
+  uint32_t there = 0;                                              // bit k: page k is there
+  auto ask = [&](int64_t c) {
+    int id[AT_ONCE];
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; ++k) id[k] = table[(int)min(c + slot * AT_ONCE + k, (int64_t)cols.end - 1)];
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; ++k) x[k] = Op<T>::load(bounds + ((unsigned)id[k] < (unsigned)a.kv.n_pages ? id[k] : 0) * page_elems);
+    there = 0;
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; ++k) there |= (unsigned)id[k] < (unsigned)a.kv.n_pages ? 1u << k : 0u;
+  };
+  ask(c0);
   double q[8] = {0, 0, 0, 0, 0, 0, 0, 0};
   {
     const T *p = reinterpret_cast<const T *>(a.q) + (int64_t)row * a.q_stride + (int64_t)head * a.group * D + col;
+#pragma unroll 1
     for (int h0 = 0; h0 < a.group; h0 += 4) {
-      frag x[4];
+      frag y[4];
 #pragma unroll
-      for (int h = 0; h < 4; ++h) x[h] = Op<T>::load(p + (int64_t)min(h0 + h, a.group - 1) * D);
+      for (int h = 0; h < 4; ++h) y[h] = Op<T>::load(p + (int64_t)min(h0 + h, a.group - 1) * D);
 #pragma unroll
       for (int h = 0; h < 4; ++h) {
         float v[8];
-        values(x[h], v);
+        values(y[h], v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float part = half ? (v[e] < 0.f ? 0.f : v[e]) : (v[e] > 0.f ? 0.f : v[e]);      // a NaN stays in both
@@ -207,21 +226,8 @@ __global__ __launch_bounds__(SP_THREADS) void page_scores(SpArgs a) {
       }
     }
   }
-  const KvSeq sq = kv_seq(a.kv, a.seqs, row);
-  const SpCols cols = sp_cols(a, sq.len);
-  if (cols.n <= a.top) return;                                     // all of them are taken
-  const int32_t *table = a.kv.table + (int64_t)sq.row * a.kv.max_pages;
-  const T *bounds = reinterpret_cast<const T *>(a.bounds) + (int64_t)head * 2 * D + half * D + col;
-  const int64_t page_elems = (int64_t)a.kv.n_kv * 2 * D;
-  uint64_t *keys = a.keys + ((int64_t)row * a.kv.n_kv + head) * a.kv.max_pages;
-  constexpr int STEP = SP_WAVES * PAGES * AT_ONCE;
-  for (int64_t c0 = cols.begin + (int64_t)blockIdx.x * STEP + wave * PAGES * AT_ONCE; c0 < cols.end; c0 += (int64_t)gridDim.x * STEP) {
-    frag x[AT_ONCE];
-#pragma unroll
-    for (int k = 0; k < AT_ONCE; ++k) {
-      const int id = table[(int)min(c0 + slot * AT_ONCE + k, (int64_t)cols.end - 1)];
-      x[k] = Op<T>::load(bounds + ((unsigned)id < (unsigned)a.kv.n_pages ? id : 0) * page_elems);
-    }
+#pragma unroll 1
+  for (;;) {
     double s[AT_ONCE];
     bool odd = false;
 #pragma unroll
@@ -233,7 +239,8 @@ __global__ __launch_bounds__(SP_THREADS) void page_scores(SpArgs a) {
       for (int e = 0; e < 8; ++e) s[k] = fma(q[e], (double)v[e], s[k]);
       odd |= s[k] != s[k];
     }
-    if (__any(odd)) {                                              // nothing of q times an infinity is nothing
+    if (__any(odd)) {                                              // nothing of q times an infinity is nothing: once more (read again, so that no register waits for it)
+      ask(c0);
 #pragma unroll
       for (int k = 0; k < AT_ONCE; ++k) {
         float v[8];
@@ -243,151 +250,202 @@ __global__ __launch_bounds__(SP_THREADS) void page_scores(SpArgs a) {
         for (int e = 0; e < 8; ++e) s[k] = fma(q[e], (double)(q[e] == 0.0 ? 0.f : v[e]), s[k]);
       }
     }
-    const double sum = sp_sum8<LP>(s);
     const int64_t c = c0 + slot * AT_ONCE + (lane & 7);
-    if (piece < 8 && c < cols.end) keys[c] = sp_key(sum);
+    const bool of_page = there >> (lane & 7) & 1;
+    c0 += step;
+    const bool more = c0 < cols.end;
+    if (more) ask(c0);
+    const double sum = sp_sum8<LP>(s);
+    if (piece < 8 && c < cols.end) store((int)c, of_page ? sp_key(sum) : SP_NONE);
+    if (!more) return;
   }
+}
+template <int DT> constexpr int sp_pages() { return 8 * (64 / sp_lanes(DT * 32)); }      // of a wavefront at once
+
+template <class T, int DT>
+__global__ __launch_bounds__(SP_THREADS, 2) void page_scores(SpArgs a) {
+  const int head = blockIdx.y, row = blockIdx.z;
+  const KvSeq sq = kv_seq(a.kv, a.seqs, row);
+  const SpCols cols = sp_cols(a, sq.len);
+  if (cols.n <= a.top) return;                                     // all of them are taken
+  uint64_t *keys = a.keys + ((int64_t)row * a.kv.n_kv + head) * a.kv.max_pages;
+  constexpr int STEP = SP_WAVES * sp_pages<DT>();
+  score_pages<T, DT>(a, row, head, sq, cols, cols.begin + (int64_t)blockIdx.x * STEP + (threadIdx.x >> 6) * sp_pages<DT>(), (int64_t)gridDim.x * STEP,
+                     [&](int c, uint64_t key) { keys[c] = key; });
 }
 
 // ---- choice ----------------------------------------------------------------------------------------------------------
-constexpr int SC_THREADS = 1024, SC_WAVES = SC_THREADS / 64, SC_PER = 8, SC_CHUNK = SC_THREADS * SC_PER, SC_BITS = 11;
+constexpr int SC_THREADS = 1024, SC_FUSED = 512, SC_BITS = 11;
+constexpr int SC_MOST = 4096;                        // columns whose keys stay in LDS
 
-// Sums over the threads before this one, and over all; `sums`: LDS that nobody reads any more
-__device__ __forceinline__ int sc_before(int v, int *sums, int &total) {
+template <int THREADS> struct ScShared {
+  uint64_t keys[SC_MOST];
+  int hist[1 << SC_BITS], count[2][THREADS / 64], found[2], columns[SC_MOST / 64];
+};
+
+// Sums over the lanes before this one of the workgroup's, and over all; `sums`: LDS that nobody reads any more
+template <int WAVES> __device__ __forceinline__ int sc_before(int v, int *sums, int &total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, inc = wave_scan(v);
   if (lane == 63) sums[wave] = inc;
   __syncthreads();
-  const int of_wave = wave_scan(lane < SC_WAVES ? sums[lane] : 0);
-  total = __builtin_amdgcn_readlane(of_wave, SC_WAVES - 1);
+  const int of_wave = wave_scan(lane < WAVES ? sums[lane] : 0);
+  total = __builtin_amdgcn_readlane(of_wave, WAVES - 1);
   return inc - v + (wave ? __builtin_amdgcn_readlane(of_wave, wave - 1) : 0);
 }
 
-// A workgroup has a row's head: the key of the last page that is taken, SC_BITS after another from the first bit in which the keys differ, then the columns in order.  A thread has
-// SC_PER columns side by side; up to SC_CHUNK of them their keys are read once, of more once for each step.  Bound: latency, two trips to memory and about ten barriers.
-__global__ __launch_bounds__(SC_THREADS) void page_choice(SpArgs a) {
-  __shared__ int hist[1 << SC_BITS], sums[4][SC_WAVES], found[2];
-  __shared__ uint64_t wide[2][SC_WAVES];
-  static_assert((1 << SC_BITS) == 2 * SC_THREADS, "two bins a thread");
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, head = blockIdx.x, row = blockIdx.y;
-  const KvSeq sq = kv_seq(a.kv, a.seqs, row);
-  const SpCols cols = sp_cols(a, sq.len);
-  const int32_t *table = a.kv.table + (int64_t)sq.row * a.kv.max_pages;
-  int32_t *sel = a.sel + ((int64_t)row * a.kv.n_kv + head) * a.top;
-  const uint64_t *keys = a.keys + ((int64_t)row * a.kv.n_kv + head) * a.kv.max_pages;
-  const int chunks = (cols.n + SC_CHUNK - 1) / SC_CHUNK;
-  const bool every = cols.n <= a.top;
-  uint64_t key[SC_PER];
-  uint32_t scored = 0, always = 0;                                 // of the thread's columns of a chunk, a bit each
-  auto fetch = [&](int chunk) {
-    int id[SC_PER];
-#pragma unroll
-    for (int i = 0; i < SC_PER; ++i) {
-      const int c = chunk * SC_CHUNK + tid * SC_PER + i;
-      id[i] = c < cols.n ? table[c] : -1;
-      key[i] = !every && c >= cols.begin && c < cols.end ? keys[c] : 0;
-    }
-    scored = always = 0;
-#pragma unroll
-    for (int i = 0; i < SC_PER; ++i) {
-      const int c = chunk * SC_CHUNK + tid * SC_PER + i;
-      const uint32_t there = (unsigned)id[i] < (unsigned)a.kv.n_pages ? 1u << i : 0u;
-      if (every || c < cols.begin || c >= cols.end) always |= there; else scored |= there;
-    }
-  };
-  if (chunks == 1) fetch(0);
-  uint64_t prefix = ~0ull, mask = ~0ull;                           // the keys that are taken are those above prefix, and `ties` of those that agree with it
+// A workgroup has a row's head and n columns with their keys: the key of the last one that is taken, SC_BITS after another, then the columns in order, 64 after another.
+// Loops are short and not unrolled: a launch's first pass through its code costs more than what it does.  Bound: latency, two to three steps with three barriers each.
+template <int THREADS, class F>
+__device__ __forceinline__ void choose_pages(int n, int top, int32_t *__restrict__ sel, ScShared<THREADS> &sh, F key_of) {
+  constexpr int WAVES = THREADS / 64, BINS = (1 << SC_BITS) / THREADS;      // bins of a thread
+  typedef __attribute__((ext_vector_type(BINS))) int bins_t;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  uint64_t prefix = SP_NONE, mask = ~0ull;                         // keys above prefix are taken, and `ties` of those that agree with it
   int ties = 0;
-  if (!every) {
-    int held = 0;
-    uint64_t any = 0, all = ~0ull;
-    int firm = 0;
-    for (int k = 0; k < chunks; ++k) {
-      if (chunks > 1) fetch(k);
-      firm += __popc(always);
-      held += __popc(scored);
-#pragma unroll
-      for (int i = 0; i < SC_PER; ++i)
-        if (scored >> i & 1) { any |= key[i]; all &= key[i]; }
+  if (n > top) {
+    int firm = 0, held = 0;
+#pragma unroll 1
+    for (int c0 = 0; c0 < n; c0 += THREADS) {
+      const uint64_t k = c0 + tid < n ? key_of(c0 + tid) : SP_NONE;
+      firm += __popcll(__ballot(k == SP_ALWAYS));
+      held += __popcll(__ballot(k != SP_ALWAYS && k != SP_NONE));
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) { any |= __shfl_xor(any, o, 64); all &= __shfl_xor(all, o, 64); }
-    firm = __builtin_amdgcn_readlane(wave_scan(firm), 63);
-    held = __builtin_amdgcn_readlane(wave_scan(held), 63);
-    if (lane == 0) { wide[0][wave] = any; wide[1][wave] = all; sums[0][wave] = firm; sums[1][wave] = held; }
+    if (lane == 0) { sh.count[0][wave] = firm; sh.count[1][wave] = held; }
     __syncthreads();
-    firm = held = 0;
-    for (int w = 0; w < SC_WAVES; ++w) { any |= wide[0][w]; all &= wide[1][w]; firm += sums[0][w]; held += sums[1][w]; }
-    const int want = a.top - firm;                                 // of the scored ones
-    if (held <= want) {                                            // all of them
-      prefix = mask = 0;
-      ties = held;
-    } else if (want > 0) {
-      const uint64_t other = any ^ all;
-      int shift = other ? 64 - __builtin_clzll(other) : 0;         // bits below this one differ
-      mask = shift == 64 ? 0 : ~0ull << shift;
-      prefix = all & mask;
+    firm = __builtin_amdgcn_readlane(wave_scan(lane < WAVES ? sh.count[0][lane] : 0), WAVES - 1);
+    held = __builtin_amdgcn_readlane(wave_scan(lane < WAVES ? sh.count[1][lane] : 0), WAVES - 1);
+    const int want = top - firm;                                   // of the others
+    if (want <= 0) prefix = SP_ALWAYS - 1;
+    else if (held > want) {
+      mask = 0;
       ties = want;
       int left = held;
-      while (shift > 0 && left > ties) {
+#pragma unroll 1
+      for (int shift = 64; shift > 0 && left > ties;) {
         const int bits = min(shift, SC_BITS), s = shift - bits;
-        *reinterpret_cast<u32x2 *>(hist + 2 * tid) = u32x2{0, 0};
+        *reinterpret_cast<bins_t *>(sh.hist + BINS * tid) = bins_t(0);
         __syncthreads();
-        for (int k = 0; k < chunks; ++k) {
-          if (chunks > 1) fetch(k);
-#pragma unroll
-          for (int i = 0; i < SC_PER; ++i)
-            if ((scored >> i & 1) && (key[i] & mask) == prefix) atomicAdd(&hist[(key[i] >> s) & ((1u << bits) - 1)], 1);
+#pragma unroll 1
+        for (int c = tid; c < n; c += THREADS) {
+          const uint64_t k = key_of(c);
+          if (k != SP_NONE && k != SP_ALWAYS && (k & mask) == prefix) atomicAdd(&sh.hist[(k >> s) & ((1u << bits) - 1)], 1);
         }
         __syncthreads();
-        // bins from the largest on, two a thread
-        const int top_bin = (1 << SC_BITS) - 1 - 2 * tid, n0 = hist[top_bin], n1 = hist[top_bin - 1];
-        int sum;
-        const int before = sc_before(n0 + n1, sums[2], sum);
-        if (before < ties && before + n0 >= ties) { found[0] = top_bin; found[1] = before; }
-        else if (before + n0 < ties && before + n0 + n1 >= ties) { found[0] = top_bin - 1; found[1] = before + n0; }
+        // bins from the largest on, BINS a thread
+        const int bin0 = (1 << SC_BITS) - BINS * (tid + 1);
+        const bins_t in_bin = *reinterpret_cast<const bins_t *>(sh.hist + bin0);
+        int mine = 0, sum;
+#pragma unroll
+        for (int b = 0; b < BINS; ++b) mine += in_bin[b];
+        int before = sc_before<WAVES>(mine, sh.count[0], sum);
+        if (before < ties && before + mine >= ties) {              // one thread's
+          int b = BINS - 1, in = in_bin[BINS - 1];
+#pragma unroll
+          for (int x = BINS - 2; x >= 0; --x) {
+            const bool on = b == x + 1 && before + in < ties;
+            before += on ? in : 0;
+            b = on ? x : b;
+            in = on ? in_bin[x] : in;
+          }
+          sh.found[0] = bin0 + b;
+          sh.found[1] = before;
+        }
         __syncthreads();
-        const int bin = found[0];
-        left = hist[bin];
-        ties -= found[1];
+        const int bin = sh.found[0];
+        left = sh.hist[bin];
+        ties -= sh.found[1];
         prefix |= (uint64_t)bin << s;
         shift = s;
         mask = ~0ull << s;
-        __syncthreads();                                           // hist, found and sums are read
+        __syncthreads();                                           // hist, found and count are read
       }
     }
   }
+  auto judge = [&](int c, bool &take, bool &tie) {
+    const uint64_t k = c < n ? key_of(c) : SP_NONE;
+    const bool other = k != SP_NONE && k != SP_ALWAYS;
+    take = k == SP_ALWAYS || (other && (k & mask) > prefix);
+    tie = other && (k & mask) == prefix;
+  };
   int at = 0;
-  for (int k = 0; k < chunks; ++k) {
-    if (chunks > 1) fetch(k);
-    uint32_t take = always, tie = 0;
-#pragma unroll
-    for (int i = 0; i < SC_PER; ++i) {
-      const uint64_t v = key[i] & mask;
-      if (scored >> i & 1) {
-        take |= v > prefix ? 1u << i : 0u;
-        tie |= v == prefix ? 1u << i : 0u;
-      }
+#pragma unroll 1
+  for (int begin = 0; begin < n; begin += SC_MOST) {
+    const int end = min(begin + SC_MOST, n);
+    // taken for sure, and ties, of 64 columns side by side, counted together; then of those before
+#pragma unroll 1
+    for (int c0 = begin; c0 < end; c0 += THREADS) {
+      bool take, tie;
+      judge(c0 + tid, take, tie);
+      const int both = __popcll(__ballot(take)) | __popcll(__ballot(tie)) << 16;
+      if (lane == 0) sh.columns[(c0 - begin) / 64 + wave] = both;
     }
-    int total;
-    int room = ties - sc_before(__popc(tie), sums[2], total);      // equal keys: the lowest columns
-#pragma unroll
-    for (int i = 0; i < SC_PER; ++i)
-      if (tie >> i & 1) {
-        if (room > 0) take |= 1u << i;
-        --room;
-      }
-    ties -= min(ties, total);
-    int place = at + sc_before(__popc(take), sums[3], total);
-#pragma unroll
-    for (int i = 0; i < SC_PER; ++i)
-      if (take >> i & 1) {
-        if (place < a.top) sel[place] = k * SC_CHUNK + tid * SC_PER + i;
-        ++place;
-      }
-    at += total;
-    if (chunks > 1) __syncthreads();
+    __syncthreads();
+    const int groups = (end - begin + THREADS - 1) / THREADS * WAVES;
+    static_assert(SC_MOST / 64 == 64, "a lane a group");
+    const int mine = lane < groups ? sh.columns[lane] : 0, inc = wave_scan(mine), total = __builtin_amdgcn_readlane(inc, 63);
+#pragma unroll 1
+    for (int c0 = begin; c0 < end; c0 += THREADS) {
+      bool take, tie;
+      judge(c0 + tid, take, tie);
+      const int before = __builtin_amdgcn_readlane(inc - mine, (c0 - begin) / 64 + wave);
+      const uint64_t below = (1ull << lane) - 1, takes = __ballot(take), tied = __ballot(tie);
+      const int ties_before = (before >> 16) + __popcll(tied & below);
+      const int place = at + (before & 0xffff) + __popcll(takes & below) + min(ties, ties_before);
+      if ((take || (tie && ties_before < ties)) && place < top) sel[place] = c0 + tid;      // equal keys: the lowest columns
+    }
+    const int of_ties = min(ties, total >> 16);
+    at += (total & 0xffff) + of_ties;
+    ties -= of_ties;
+    __syncthreads();
   }
-  for (int v = at + tid; v < a.top; v += SC_THREADS) sel[v] = -1;
+  for (int v = at + tid; v < top; v += THREADS) sel[v] = -1;
+}
+
+// The keys of the columns that are not scored
+__device__ __forceinline__ uint64_t sp_unscored(const SpArgs &a, const int32_t *table, const SpCols &cols, int c) {
+  return (unsigned)table[c] < (unsigned)a.kv.n_pages ? SP_ALWAYS : SP_NONE;
+}
+__device__ __forceinline__ bool sp_scored(const SpArgs &a, const SpCols &cols, int c) { return cols.n > a.top && c >= cols.begin && c < cols.end; }
+
+__global__ __launch_bounds__(SC_THREADS) void page_choice(SpArgs a) {
+  __shared__ ScShared<SC_THREADS> sh;
+  const int head = blockIdx.x, row = blockIdx.y;
+  const KvSeq sq = kv_seq(a.kv, a.seqs, row);
+  const SpCols cols = sp_cols(a, sq.len);
+  const int32_t *table = a.kv.table + (int64_t)sq.row * a.kv.max_pages;
+  const uint64_t *keys = a.keys + ((int64_t)row * a.kv.n_kv + head) * a.kv.max_pages;
+  int32_t *sel = a.sel + ((int64_t)row * a.kv.n_kv + head) * a.top;
+  auto key = [&](int c) { return sp_scored(a, cols, c) ? keys[c] : sp_unscored(a, table, cols, c); };
+  if (cols.n <= SC_MOST) {
+#pragma unroll
+    for (int i = 0; i < SC_MOST / SC_THREADS; ++i) {
+      const int c = i * SC_THREADS + threadIdx.x;
+      if (c < cols.n) sh.keys[c] = key(c);
+    }
+    __syncthreads();
+    choose_pages<SC_THREADS>(cols.n, a.top, sel, sh, [&](int c) { return sh.keys[c]; });
+  } else {
+    choose_pages<SC_THREADS>(cols.n, a.top, sel, sh, key);
+  }
+}
+
+// Both, for tables of SC_MOST columns at most: the keys stay in LDS.
+template <class T, int DT>
+__global__ __launch_bounds__(SC_FUSED, 2) void page_select(SpArgs a) {
+  __shared__ ScShared<SC_FUSED> sh;
+  const int head = blockIdx.x, row = blockIdx.y;
+  const KvSeq sq = kv_seq(a.kv, a.seqs, row);
+  const SpCols cols = sp_cols(a, sq.len);
+  const int32_t *table = a.kv.table + (int64_t)sq.row * a.kv.max_pages;
+  if (cols.n > a.top) {
+    constexpr int STEP = SC_FUSED / 64 * sp_pages<DT>();
+    score_pages<T, DT>(a, row, head, sq, cols, cols.begin + (threadIdx.x >> 6) * sp_pages<DT>(), STEP, [&](int c, uint64_t key) { sh.keys[c] = key; });
+  }
+#pragma unroll 1
+  for (int c = threadIdx.x; c < cols.n; c += SC_FUSED)
+    if (!sp_scored(a, cols, c)) sh.keys[c] = sp_unscored(a, table, cols, c);
+  __syncthreads();
+  choose_pages<SC_FUSED>(cols.n, a.top, a.sel + ((int64_t)row * a.kv.n_kv + head) * a.top, sh, [&](int c) { return sh.keys[c]; });
 }
 
 template <class T>
@@ -403,17 +461,39 @@ static void kb_launch(const KbArgs &a, dim3 grid, size_t lds, hipStream_t s) {
     default: kv_bounds<T, 8><<<grid, SP_THREADS, lds, s>>>(a); break;
   }
 }
+// One launch where a workgroup a head fills the card about once, or there is little to score.  Two launches / one, us, 128 columns of bf16, heads of all rows x columns of the
+// table: 8 x 44 9.6 / 7.4, 8 x 512 10.2 / 13.8, 8 x 4000 16.8 / 65, 64 x 1000 17.8 / 23.8, 128 x 500 17.5 / 15.6, 256 x 300 19.9 / 14.3, 256 x 1500 54 / 39, 128 x 4000 61 / 75,
+// 2048 x 200 69 / 81.
+static bool sp_fused(const SpArgs &a) {
+  const int64_t pairs = (int64_t)a.rows * a.kv.n_kv;
+  return pairs <= 1024 && (a.kv.max_pages <= 256 || (a.kv.max_pages <= 2048 && pairs >= 128));
+}
+static_assert(SC_MOST >= 2048, "their keys stay in LDS");
+template <class T, int DT>
+static void sp_go(const SpArgs &a, hipStream_t s) {
+  const int64_t pairs = (int64_t)a.rows * a.kv.n_kv;
+  if (sp_fused(a)) {
+    page_select<T, DT><<<dim3(a.kv.n_kv, a.rows), SC_FUSED, 0, s>>>(a);
+    return;
+  }
+  if (a.kv.max_pages > a.top) {
+    const int64_t step = (int64_t)SP_WAVES * sp_pages<DT>();
+    const dim3 grid((uint32_t)std::min<int64_t>((a.kv.max_pages + step - 1) / step, std::max<int64_t>(1, 4096 / pairs)), a.kv.n_kv, a.rows);
+    page_scores<T, DT><<<grid, SP_THREADS, 0, s>>>(a);
+  }
+  page_choice<<<dim3(a.kv.n_kv, a.rows), SC_THREADS, 0, s>>>(a);
+}
 template <class T>
-static void sp_launch(const SpArgs &a, dim3 grid, hipStream_t s) {
+static void sp_launch(const SpArgs &a, hipStream_t s) {
   switch (a.kv.d / 32) {
-    case 1: page_scores<T, 1><<<grid, SP_THREADS, 0, s>>>(a); break;
-    case 2: page_scores<T, 2><<<grid, SP_THREADS, 0, s>>>(a); break;
-    case 3: page_scores<T, 3><<<grid, SP_THREADS, 0, s>>>(a); break;
-    case 4: page_scores<T, 4><<<grid, SP_THREADS, 0, s>>>(a); break;
-    case 5: page_scores<T, 5><<<grid, SP_THREADS, 0, s>>>(a); break;
-    case 6: page_scores<T, 6><<<grid, SP_THREADS, 0, s>>>(a); break;
-    case 7: page_scores<T, 7><<<grid, SP_THREADS, 0, s>>>(a); break;
-    default: page_scores<T, 8><<<grid, SP_THREADS, 0, s>>>(a); break;
+    case 1: sp_go<T, 1>(a, s); break;
+    case 2: sp_go<T, 2>(a, s); break;
+    case 3: sp_go<T, 3>(a, s); break;
+    case 4: sp_go<T, 4>(a, s); break;
+    case 5: sp_go<T, 5>(a, s); break;
+    case 6: sp_go<T, 6>(a, s); break;
+    case 7: sp_go<T, 7>(a, s); break;
+    default: sp_go<T, 8>(a, s); break;
   }
 }
 
@@ -478,15 +558,8 @@ int parse_select_pages(const parse_kv *kv, const void *bounds, int32_t layer, co
   a.bounds = (const char *)bounds + (size_t)layer * kv->n_pages * kv->n_kv * 2 * kv->d * elem_size(kv->dtype);
   a.q = q; a.seqs = seqs; a.q_stride = q_stride; a.n_q = n_q; a.group = n_q / kv->n_kv; a.rows = rows; a.top = top; a.first = first; a.last = last;
   a.keys = (uint64_t *)workspace; a.sel = pages;
-  if (kv->max_pages > top) {
-    const int64_t pairs = (int64_t)rows * kv->n_kv;
-    const int64_t step = (int64_t)SP_WAVES * 8 * (64 / sp_lanes(kv->d));
-    const dim3 grid((uint32_t)std::min<int64_t>((kv->max_pages + step - 1) / step, std::max<int64_t>(1, 4096 / pairs)), kv->n_kv, rows);
-    if (kv->dtype == PARSE_BF16) sp_launch<uint16_t>(a, grid, (hipStream_t)stream);
-    else sp_launch<float>(a, grid, (hipStream_t)stream);
-    PARSE_LAUNCH_CHECK();
-  }
-  page_choice<<<dim3(kv->n_kv, rows), SC_THREADS, 0, (hipStream_t)stream>>>(a);
+  if (kv->dtype == PARSE_BF16) sp_launch<uint16_t>(a, (hipStream_t)stream);
+  else sp_launch<float>(a, (hipStream_t)stream);
   PARSE_LAUNCH_CHECK();
   return PARSE_OK;
 }
