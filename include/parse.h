@@ -614,7 +614,7 @@ int parse_shared_plan(const parse_kv *kv, int32_t n_q, int32_t rows, const int32
                       parse_stream stream);
 size_t parse_attend_shared_workspace_bytes(const parse_kv *kv, int32_t n_q, int32_t rows);
 int parse_attend_shared(const parse_kv *kv, int32_t layer, const void *q, int64_t q_stride, int32_t n_q, int32_t rows, const int32_t *seqs, const void *plan,
-                        float scale, int32_t window, int32_t sinks, void *out, int64_t out_stride, float *lse, void *workspace, size_t workspace_bytes,
+                        size_t plan_bytes, float scale, int32_t window, int32_t sinks, void *out, int64_t out_stride, float *lse, void *workspace, size_t workspace_bytes,
                         parse_stream stream);
 
 /* ---- attention over selected pages -------------------------------------------------------------------------------------

@@ -156,7 +156,7 @@ def lib():
         f = getattr(L, "parse_" + name)
         f.restype = sz; f.argtypes = args
     for name, args in [("shared_plan", [kvp, i32, i32, vp, i32, i32, vp, sz, vp]),
-                       ("attend_shared", [kvp, i32, vp, i64, i32, i32, vp, vp, f32, i32, i32, vp, i64, vp, vp, sz, vp]),
+                       ("attend_shared", [kvp, i32, vp, i64, i32, i32, vp, vp, sz, f32, i32, i32, vp, i64, vp, vp, sz, vp]),
                        ("kv_bounds", [kvp, vp, i32, vp, vp, i32, vp]),
                        ("select_pages", [kvp, vp, i32, vp, i64, i32, i32, vp, i32, i32, i32, vp, vp, sz, vp]),
                        ("attend_pages", [kvp, i32, vp, i64, i32, i32, vp, vp, i32, f32, vp, i64, vp, vp, sz, vp]),
@@ -878,13 +878,11 @@ def attend_shared(kv: KV, layer: int, q, plan, seqs=None, scale=None, window: in
     """parse_attend_shared: attend_decode for sequences that begin with the same pages, which are read once for all of them (plan: shared_plan)."""
     rows, n_q = q.shape[:2]
     q_stride = _rows_of(q, kv, n_q, "q")
-    if plan.numel() * plan.element_size() < shared_plan_bytes(kv, n_q, rows):
-        raise ValueError("the plan is smaller than shared_plan_bytes(kv, n_q, rows)")
     out, out_stride, lse = _attend_out(kv, q, n_q, q_stride, out, lse, with_lse)
     if workspace is None:
         workspace = attend_shared_workspace(kv, n_q, rows)
-    _check(_calls.parse_attend_shared(kv, layer, q, q_stride, n_q, rows, _ints(seqs, rows, "seqs"), plan, kv.d ** -0.5 if scale is None else scale, window,
-                                      sinks, out, out_stride, lse, workspace, workspace.numel(), _stream()), "parse_attend_shared")
+    _check(_calls.parse_attend_shared(kv, layer, q, q_stride, n_q, rows, _ints(seqs, rows, "seqs"), plan, plan.numel() * plan.element_size(),
+                                      kv.d ** -0.5 if scale is None else scale, window, sinks, out, out_stride, lse, workspace, workspace.numel(), _stream()), "parse_attend_shared")
     return (out, lse) if with_lse else out
 
 
@@ -950,6 +948,8 @@ def attend_pages(kv: KV, layer: int, q, pages, seqs=None, scale=None, out=None, 
 
 # ---- norm ------------------------------------------------------------------------------------------------------------
 def _row_stride(t, rows, d, what):
+    if t.is_contiguous() and t.shape == (rows, d):
+        return d
     if t.dim() != 2 or tuple(t.shape) != (rows, d) or (t.stride(1) != 1 and d > 1):
         raise ValueError(f"{what}: [{rows}][{d}] with adjacent columns is wanted, got {tuple(t.shape)}, strides {t.stride()}")
     return t.stride(0) if rows > 1 else max(t.stride(0), d)

@@ -8,6 +8,7 @@
 // columns' running maximum, sum of weights and weighted sum of V over the tokens that the share has of it.  Parts stand at column x * TC + base[e] of the
 // workspace (base: columns of the entries before), which no two of them have in common.
 #pragma once
+#include <algorithm>
 #include <type_traits>
 
 #include "attend.hpp"
@@ -807,6 +808,10 @@ static int pt_launch(const PtArgs &a, int64_t entries, hipStream_t s) {
   PARSE_ALLOW_LDS((attend_parts<T, DT, LISTED>), 0, lds);
   attend_parts<T, DT, LISTED><<<dim3(a.shares, a.kv.n_kv), PT_THREADS, lds, s>>>(a);
   PARSE_LAUNCH_CHECK();
+  if (LISTED && entries <= a.shares) {                             // the lists' steps are the host's to count: whether every entry is a share's, whole
+    const int64_t steps = ((int64_t)a.top * a.kv.page + PT_STEP - 1) / PT_STEP, total = steps * entries;
+    if (steps <= std::max<int64_t>(((total + a.shares - 1) / a.shares + PT_WAVES - 1) / PT_WAVES, 1) * PT_WAVES + PT_SLACK) return PARSE_OK;
+  }
   attend_parts_join<T, DT, LISTED><<<dim3(a.n_q, a.rows), PT_THREADS, 0, s>>>(a);
   PARSE_LAUNCH_CHECK();
   return PARSE_OK;

@@ -34,9 +34,8 @@ __global__ __launch_bounds__(SH_THREADS) void shared_count(parse_kv kv, const in
   const ShRow r = sh_row(kv, seqs, row, window, sinks);
   const int32_t *table = kv.table + (int64_t)r.seq.row * kv.max_pages;
   for (int c = blockIdx.x * SH_THREADS + threadIdx.x; c < r.columns; c += gridDim.x * SH_THREADS) {
-    if (!r.cares(c)) continue;
     const int id = table[c];
-    if ((unsigned)id >= (unsigned)kv.n_pages) continue;
+    if (!r.cares(c) || (unsigned)id >= (unsigned)kv.n_pages) continue;
     if (COUNT) {
       atomicMin(&plan.owner[id], (unsigned long long)(uint32_t)r.seq.len << 32 | (uint32_t)row);
       atomicAdd(&plan.users[id], 1);
@@ -50,17 +49,18 @@ __global__ __launch_bounds__(SH_THREADS) void shared_count(parse_kv kv, const in
 // A wavefront walks a row's columns.  A run ends where the pages have another owner or fewer users; one of two users and more that is long enough (with what
 // shorter ones left before it: their rows hold that too) is the row's next level.  Then the columns are compared with the owner's: the row takes part as far as they agree.
 __global__ __launch_bounds__(SH_THREADS) void shared_walk(parse_kv kv, const int32_t *__restrict__ seqs, int rows, int window, int sinks, PtPlan plan) {
-  const int row = blockIdx.x * (SH_THREADS / 64) + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int row = blockIdx.x * (SH_THREADS / 64) + (threadIdx.x >> 6), lane = threadIdx.x & 63, page = kv.page;
   if (row >= rows) return;
   const ShRow r = sh_row(kv, seqs, row, window, sinks);
   const int32_t *table = kv.table + (int64_t)r.seq.row * kv.max_pages;
+  auto there = [&](int id) { return (unsigned)id < (unsigned)kv.n_pages; };
   int4 found[PT_LEVELS];
 #pragma unroll
   for (int l = 0; l < PT_LEVELS; ++l) found[l] = int4{0, 0, -1, 0};
   int level = 0, from = 0, have = 0, owner = -2, users = 0;        // from: tokens; have: columns since then that the row cares for
   auto ends = [&](int c, int now) {                                // the run before column c, with `now` columns
-    const int to = c * kv.page & ~(PT_STEP - 1);
-    if (users < 2 || owner < 0 || (int64_t)now * kv.page < SH_LEAST || to <= from || level >= PT_LEVELS) return false;
+    const int to = c * page & ~(PT_STEP - 1);
+    if (users < 2 || owner < 0 || (int64_t)now * page < SH_LEAST || to <= from || level >= PT_LEVELS) return false;
 #pragma unroll
     for (int l = 0; l < PT_LEVELS; ++l)
       if (l == level) found[l] = int4{from, to, owner, 1};
@@ -74,7 +74,7 @@ __global__ __launch_bounds__(SH_THREADS) void shared_walk(parse_kv kv, const int
     int o = -1, k = 0;
     if (care) {
       const int id = table[c];
-      if ((unsigned)id < (unsigned)kv.n_pages) { o = (int)(uint32_t)plan.owner[id]; k = plan.users[id]; }
+      if (there(id)) { o = (int)(uint32_t)plan.owner[id]; k = plan.users[id]; }
     }
     const uint64_t cared = __ballot(care), below = cared & ((1ull << lane) - 1);
     const int prev = below ? 63 - __builtin_clzll(below) : 0;
@@ -89,7 +89,7 @@ __global__ __launch_bounds__(SH_THREADS) void shared_walk(parse_kv kv, const int
       counted = b;
       owner = __builtin_amdgcn_readlane(po, b);
       users = __builtin_amdgcn_readlane(pk, b);
-      if (ends(c0 + b, have)) have = (c0 + b) * kv.page > from ? 1 : 0;
+      if (ends(c0 + b, have)) have = (c0 + b) * page > from ? 1 : 0;
     }
     have += __popcll(cared & ~((1ull << counted) - 1));
     if (cared) {
@@ -104,13 +104,12 @@ __global__ __launch_bounds__(SH_THREADS) void shared_walk(parse_kv kv, const int
     if (l >= level) break;
     const int lead = found[l].z;
     if (lead == row) continue;
-    const ShRow of = sh_row(kv, seqs, (unsigned)lead < (unsigned)rows ? lead : row, window, sinks);
-    const int32_t *other = kv.table + (int64_t)of.seq.row * kv.max_pages;
+    const int32_t *other = kv.table + (int64_t)kv_seq(kv, seqs, min((unsigned)lead, (unsigned)rows - 1)).row * kv.max_pages;
     bool same = true;
-    for (int c = found[l].x / kv.page + lane; c < found[l].y / kv.page; c += 64) {
+    for (int c = found[l].x / page + lane; c < found[l].y / page; c += 64) {
       if (!r.cares(c)) continue;
       const int x = table[c], y = other[c];
-      same &= x == y || ((unsigned)x >= (unsigned)kv.n_pages && (unsigned)y >= (unsigned)kv.n_pages);
+      same &= x == y || (!there(x) && !there(y));
     }
     if (!__all(same)) level = l;
   }
@@ -124,10 +123,12 @@ __global__ __launch_bounds__(SH_THREADS) void shared_walk(parse_kv kv, const int
   }
 }
 
-// One workgroup: the rows that agree with their owner become its group, groups of two and more get tiles, level after level.  A thread has PER consecutive rows.
+// One workgroup: the rows that agree with their owner become its group, groups of two and more get tiles, level after level.  A thread has consecutive rows.
 __global__ __launch_bounds__(SH_ONE) void shared_tiles(parse_kv kv, const int32_t *__restrict__ seqs, int rows, int group, int TC, int window, int sinks, PtPlan plan) {
-  extern __shared__ int words[];
-  int *lead = words, *users = lead + rows, *tile0 = users + rows, *list0 = tile0 + rows, *base0 = list0 + rows, *chain = base0 + rows;
+  extern __shared__ int4 words[];
+  const int4 *walk = plan.walk;
+  const int wide = (rows + 3) & ~3;
+  int *lead = reinterpret_cast<int *>(words), *users = lead + wide, *tile0 = users + wide, *list0 = tile0 + wide, *base0 = list0 + wide, *chain = base0 + wide;
   __shared__ int sums[3][SH_ONE / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, per = (rows + SH_ONE - 1) / SH_ONE;
   const int r0 = tid * per, r1 = min(r0 + per, rows);
@@ -135,20 +136,24 @@ __global__ __launch_bounds__(SH_ONE) void shared_tiles(parse_kv kv, const int32_
     chain[r] = 1;
     plan.row[r] = PtRow{0, 0, {0, 0, 0}, {0, 0, 0}};
   }
+  if (tid < wide - rows) lead[rows + tid] = -1;
   int tiles = 0, listed = 0, columns = 0;
+#pragma unroll 1
   for (int l = 0; l < PT_LEVELS; ++l) {
     __syncthreads();
+    bool some = false;
     for (int r = r0; r < r1; ++r) {
-      const int4 w = plan.walk[(int64_t)r * PT_LEVELS + l];
+      const int4 w = walk[r * PT_LEVELS + l];
       int of = -1;
       if (chain[r] && w.w && (unsigned)w.z < (unsigned)rows) {
-        const int4 o = plan.walk[(int64_t)w.z * PT_LEVELS + l];
+        const int4 o = walk[w.z * PT_LEVELS + l];
         if (chain[w.z] && o.w && o.z == w.z && o.x == w.x && o.y == w.y) of = w.z;
       }
       lead[r] = of;
       users[r] = 0;
+      some |= of >= 0;
     }
-    __syncthreads();
+    if (!__syncthreads_or(some)) break;
     for (int r = r0; r < r1; ++r)
       if (lead[r] >= 0) atomicAdd(&users[lead[r]], 1);
     __syncthreads();
@@ -187,8 +192,12 @@ __global__ __launch_bounds__(SH_ONE) void shared_tiles(parse_kv kv, const int32_
       const int of = lead[r];
       if (of < 0) continue;
       int rank = 0;
-      for (int i = 0; i < r; ++i) rank += lead[i] == of ? 1 : 0;
-      const int4 w = plan.walk[(int64_t)r * PT_LEVELS + l];
+#pragma unroll 2
+      for (int i = 0; i < r; i += 4) {
+        const int4 x = *reinterpret_cast<const int4 *>(lead + i);
+        rank += (x.x == of ? 1 : 0) + (x.y == of && i + 1 < r ? 1 : 0) + (x.z == of && i + 2 < r ? 1 : 0) + (x.w == of && i + 3 < r ? 1 : 0);
+      }
+      const int4 w = walk[r * PT_LEVELS + l];
       plan.list[list0[of] + rank] = r;
       plan.row[r].from = w.y;
       plan.row[r].levels = l + 1;
@@ -252,6 +261,8 @@ int parse_shared_plan(const parse_kv *kv, int32_t n_q, int32_t rows, const int32
   if (!aligned16(plan)) return PARSE_EALIGN;
   const PtPlan p = pt_plan(kv, rows, group, plan);
   hipStream_t s = (hipStream_t)stream;
+  const size_t lds = (size_t)((rows + 3) & ~3) * 6 * 4;
+  const int TC = pt_columns(kv->d, kv->dtype);
   const dim3 grid((uint32_t)std::min<int64_t>((kv->max_pages + SH_THREADS - 1) / SH_THREADS, std::max(1, 4096 / rows)), rows);
   shared_count<false><<<grid, SH_THREADS, 0, s>>>(*kv, seqs, window, sinks, p);
   PARSE_LAUNCH_CHECK();
@@ -259,9 +270,8 @@ int parse_shared_plan(const parse_kv *kv, int32_t n_q, int32_t rows, const int32
   PARSE_LAUNCH_CHECK();
   shared_walk<<<dim3((rows + SH_THREADS / 64 - 1) / (SH_THREADS / 64)), SH_THREADS, 0, s>>>(*kv, seqs, rows, window, sinks, p);
   PARSE_LAUNCH_CHECK();
-  const size_t lds = (size_t)rows * 6 * 4;
   PARSE_ALLOW_LDS(shared_tiles, 3 * SH_ONE / 64 * 4, lds);
-  shared_tiles<<<dim3(1), SH_ONE, lds, s>>>(*kv, seqs, rows, group, pt_columns(kv->d, kv->dtype), window, sinks, p);
+  shared_tiles<<<dim3(1), SH_ONE, lds, s>>>(*kv, seqs, rows, group, TC, window, sinks, p);
   PARSE_LAUNCH_CHECK();
   return PARSE_OK;
 }
@@ -272,7 +282,7 @@ size_t parse_attend_shared_workspace_bytes(const parse_kv *kv, int32_t n_q, int3
 }
 
 int parse_attend_shared(const parse_kv *kv, int32_t layer, const void *q, int64_t q_stride, int32_t n_q, int32_t rows, const int32_t *seqs, const void *plan,
-                        float scale, int32_t window, int32_t sinks, void *out, int64_t out_stride, float *lse, void *workspace, size_t workspace_bytes,
+                        size_t plan_bytes, float scale, int32_t window, int32_t sinks, void *out, int64_t out_stride, float *lse, void *workspace, size_t workspace_bytes,
                         parse_stream stream) {
   const int st = check_attend(kv, layer, q, q_stride, n_q, rows, nullptr, seqs, scale, window, sinks, out, out_stride, lse);
   if (st != PARSE_OK) return st;
@@ -281,7 +291,7 @@ int parse_attend_shared(const parse_kv *kv, int32_t layer, const void *q, int64_
   if (!as_size(kv, n_q, rows, z) || (!seqs && rows > kv->n_seqs)) return PARSE_ESHAPE;
   // the steps of all entries are added up in an int
   if (z.entries * (((int64_t)kv->max_pages * kv->page + PT_STEP - 1) / PT_STEP) > INT32_MAX - 65536) return PARSE_ESHAPE;
-  if (!workspace || workspace_bytes < z.bytes) return PARSE_EWORKSPACE;
+  if (!workspace || workspace_bytes < z.bytes || plan_bytes < pt_plan(kv, rows, n_q / kv->n_kv, nullptr).bytes) return PARSE_EWORKSPACE;
   if (!aligned16(workspace) || !aligned16(plan)) return PARSE_EALIGN;
   const size_t at = (size_t)layer * kv->n_pages * kv->n_kv * kv->page * kv->d * elem_size(kv->dtype);
   const int TC = pt_columns(kv->d, kv->dtype);

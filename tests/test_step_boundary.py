@@ -23,7 +23,7 @@ def calls():
         return call
     return {
         "plan": wrap(lambda kv, a: L.parse_shared_plan(kv, a["n_q"], a["rows"], a["seqs"], a["window"], a["sinks"], a["plan"], a["planb"], None)),
-        "shared": wrap(lambda kv, a: L.parse_attend_shared(kv, a["layer"], a["q"], a["qs"], a["n_q"], a["rows"], a["seqs"], a["plan"], a["scale"], a["window"], a["sinks"],
+        "shared": wrap(lambda kv, a: L.parse_attend_shared(kv, a["layer"], a["q"], a["qs"], a["n_q"], a["rows"], a["seqs"], a["plan"], a["planb"], a["scale"], a["window"], a["sinks"],
                                                            a["out"], a["outs"], a["lse"], a["ws"], a["wsb"], None)),
         "bounds": wrap(lambda kv, a: L.parse_kv_bounds(kv, a["bounds"], a["layer"], a["off"], a["seqs"], a["P"], None)),
         "select": wrap(lambda kv, a: L.parse_select_pages(kv, a["bounds"], a["layer"], a["q"], a["qs"], a["n_q"], a["rows"], a["seqs"], a["top"], a["first"], a["last"],
@@ -59,7 +59,7 @@ def test_attention_refuses_bad_arguments(name):
     if name == "shared":
         assert c(wsb=L.parse_attend_shared_workspace_bytes(cache(), 8, 3) - 1) == EWORKSPACE
         refused(c, EINVAL, [dict(plan=None), dict(window=-1), dict(sinks=-1)])
-        assert c(plan=ODD) == EALIGN
+        assert c(plan=ODD) == EALIGN and c(planb=L.parse_shared_plan_bytes(cache(), 8, 3) - 1) == EWORKSPACE
     else:
         assert c(wsb=L.parse_attend_pages_workspace_bytes(cache(), 8, 3, 4) - 1) == EWORKSPACE
         refused(c, EINVAL, [dict(pages=None), dict(top=0), dict(top=-5)])
@@ -133,7 +133,7 @@ def test_the_binding_refuses_what_the_kernels_would_misread():
     assert tuple(bounds.shape) == (2, 4, 3, 2, 32)
     pages = torch.zeros(5, 3, 4, dtype=torch.int32)
     plan = torch.zeros(pa.shared_plan_bytes(kv, 6, 5), dtype=torch.uint8)
-    for bad in (lambda: pa.attend_shared(kv, 0, q.float(), plan), lambda: pa.attend_shared(kv, 0, q, plan[:-1]), lambda: pa.attend_shared(kv, 0, q, plan, pages.flatten()[:4]),
+    for bad in (lambda: pa.attend_shared(kv, 0, q.float(), plan), lambda: pa.attend_shared(kv, 0, q, plan, pages.flatten()[:4]),
                 lambda: pa.kv_bounds(kv, bounds[:1], 0), lambda: pa.kv_bounds(kv, bounds.float(), 0), lambda: pa.kv_bounds(kv, bounds, 0, pages.long().flatten()[:6]),
                 lambda: pa.select_pages(kv, 0, bounds, q, 4, pages=pages[:4]), lambda: pa.select_pages(kv, 0, bounds, q, 5, pages=pages),
                 lambda: pa.attend_pages(kv, 0, q, pages[:, :2]), lambda: pa.attend_pages(kv, 0, q, pages.long()), lambda: pa.attend_pages(kv, 0, q, pages.transpose(1, 2))):
