@@ -156,7 +156,7 @@ constexpr int PT_SLACK = 12;
 //   narrow entries, up to sixteen columns: operands go straight from the pages into registers, a step ahead of the one that is worked on where two fit; the four wavefronts
 //   take turns and their sums meet in LDS, or, where rows are many and short, a wavefront has a row alone
 //   wide ones: a wavefront has up to NW blocks of sixteen columns; the steps go through a ring in LDS, filled by loads that write LDS, and are read by all four
-template <class T, int DT, bool LISTED>
+template <class T, int DT, bool NT, bool LISTED>
 __global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_parts(PtArgs a) {
   constexpr int D = DT * 32, KB = D / 32, VB = D / 16, NW = pt_blocks<T, DT>(), TC = 64 * NW, RD = D + 4, ST = pt_stages<T, DT>();
   constexpr int CHUNK = 16 * D * (int)sizeof(T), STAGE = 4 * CHUNK, LOADS = CHUNK / 1024;         // K and V of sixteen tokens each stand in one piece
@@ -441,12 +441,13 @@ __global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_part
         x.at.there_b = page_there(idb);
         const int64_t pa = (int64_t)(x.at.there_a ? ida : 0) * page_elems + head0 + (int64_t)(x.at.ta & (a.kv.page - 1)) * D;
         const int64_t pb = (int64_t)(x.at.there_b ? idb : 0) * page_elems + head0 + (int64_t)(x.at.tb & (a.kv.page - 1)) * D;
+        auto get = [](const T *p) { return NT ? Op<T>::load_nt(p) : Op<T>::load(p); };
         const T *kp = reinterpret_cast<const T *>(a.K) + (n < 8 ? pa : pb) + k_in;
         const T *vp = reinterpret_cast<const T *>(a.V) + (quad < 2 ? pa : pb) + v_in;
 #pragma unroll
-        for (int k = 0; k < KB; ++k) { x.k0[k] = Op<T>::load(kp + k * 512); x.k1[k] = Op<T>::load(kp + k * 512 + 32); }
+        for (int k = 0; k < KB; ++k) { x.k0[k] = get(kp + k * 512); x.k1[k] = get(kp + k * 512 + 32); }
 #pragma unroll
-        for (int v = 0; v < VB; ++v) x.v[v] = Op<T>::load(vp + v * 128);
+        for (int v = 0; v < VB; ++v) x.v[v] = get(vp + v * 128);
       };
       if constexpr (!WIDE) {
         auto work = [&](Step &x) {
@@ -802,11 +803,20 @@ static inline int pt_shares(const parse_kv *kv) {
 }
 static inline size_t pt_deal_bytes(int64_t entries) { return round_up((PT_DEAL + (size_t)entries + 1) * 4, 256); }
 
+// Loads of narrow entries past the caches where what they bring in does not stay there anyway, as in the decode attention: pools larger than the last-level cache, lists of
+// more than a third of it.  Without / with such loads, us: 32 caches of 2049 tokens of 8 heads (268 MB) 57.7 / 50.0, lists of 134 MB 29.3 / 27.0; pools of 95 MB (three in turn) 30.8 /
+// 32.3, lists of 17 MB 9.2 / 11.4.  Wide entries read a page once a tile, several tiles of a run the same one: through the caches.
 template <class T, int DT, bool LISTED>
 static int pt_launch(const PtArgs &a, int64_t entries, hipStream_t s) {
-  const size_t lds = pt_lds_own<T, DT>() + (2 * PT_WAVES + (LISTED ? 0 : (size_t)entries + 1)) * 4;
-  PARSE_ALLOW_LDS((attend_parts<T, DT, LISTED>), 0, lds);
-  attend_parts<T, DT, LISTED><<<dim3(a.shares, a.kv.n_kv), PT_THREADS, lds, s>>>(a);
+  const size_t lds = pt_lds_own<T, DT>() + (2 * PT_WAVES + (LISTED ? 0 : (size_t)entries + 1)) * 4, page = (size_t)a.kv.page * DT * 32 * sizeof(T) * 2;
+  const bool nt = LISTED ? (size_t)a.rows * a.kv.n_kv * a.top * page > ((size_t)96 << 20) : (size_t)a.kv.n_layers * a.kv.n_pages * a.kv.n_kv * page > ((size_t)192 << 20);
+  if (nt) {
+    PARSE_ALLOW_LDS((attend_parts<T, DT, true, LISTED>), 0, lds);
+    attend_parts<T, DT, true, LISTED><<<dim3(a.shares, a.kv.n_kv), PT_THREADS, lds, s>>>(a);
+  } else {
+    PARSE_ALLOW_LDS((attend_parts<T, DT, false, LISTED>), 0, lds);
+    attend_parts<T, DT, false, LISTED><<<dim3(a.shares, a.kv.n_kv), PT_THREADS, lds, s>>>(a);
+  }
   PARSE_LAUNCH_CHECK();
   if (LISTED && entries <= a.shares) {                             // the lists' steps are the host's to count: whether every entry is a share's, whole
     const int64_t steps = ((int64_t)a.top * a.kv.page + PT_STEP - 1) / PT_STEP, total = steps * entries;
