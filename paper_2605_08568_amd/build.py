@@ -11,7 +11,8 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libparse.so")
 CALLS = os.path.join(HERE, "_calls" + sysconfig.get_config_var("EXT_SUFFIX"))      # CPython module of the step's calls; another Python does not take it
-SOURCES = ["attend_shared.hip", "attend_pages.hip", "attend_decode.hip", "attend_prefill.hip", "api.hip", "route.hip", "cache.hip",
+SOURCES = ["attend_shared_bf16.hip", "attend_shared_f32.hip", "attend_pages_bf16.hip", "attend_pages_f32.hip", "attend_decode.hip", "attend_prefill.hip", "attend_shared.hip",
+           "attend_pages.hip", "api.hip", "route.hip", "cache.hip",
            "pack.hip", "bucket.hip", "forward_f32.hip", "prefill_bf16.hip", "prefill_split_bf16.hip", "prefill_lds_bf16.hip",
            "plan.hip", "decode_bf16.hip", "decode_wide_bf16.hip", "decode_static.hip", "forward.hip", "ranks.hip", "train.hip",
            "peaks.hip", "kv.hip", "select.hip", "norm.hip"]          # the ones that take longest first
