@@ -2,12 +2,13 @@
 
 Prompts are prefilled (pool and route, one plan for the batch, q/k/v fused, room in the cache, rotation and append, causal attention, o projection), every
 prompt is forked into samples that share its pages, and the samples are decoded step by step, one HIP graph replayed: q/k/v over a
-decode plan, room for a token (a page that is shared and begun is copied), append, attention over window and sinks, o projection, pages that no later token
-sees given up.  At the end half of the samples stop and the rest of the cache moves together.
+decode plan, room for a token (a page that is shared and begun is copied), append, attention over window and sinks (pages that samples share are read once for
+all of them), o projection, its output added to the residual stream and the stream's norm, pages that no later token sees given up.  At the end half of the samples
+stop and the rest of the cache moves together.
 
     python examples/serve_block.py [--hidden 4096 --heads 32 --kv 32 --prompts 4 --length 512 --samples 4 --steps 64 --check]
 
-Weights are random and there is no norm, MLP or vocabulary: a step's input is the o projection's output, bent back to unit size.
+Weights are random and there is no MLP or vocabulary: a step's input is the norm of the stream after the step before.
 """
 from __future__ import annotations
 
@@ -63,7 +64,7 @@ def run(hidden=4096, heads=32, kv_heads=32, prompts=4, length=512, samples=4, st
     off = i32([sum(lengths[:p]) for p in range(prompts + 1)])
     rows, seqs = sum(lengths), prompts * (1 + samples)
     columns = -(-(length + steps + 1) // page)
-    pages = sum(-(-n // page) for n in lengths) + prompts * samples * (2 + min(steps, window + 2 * page) // page) + 2
+    pages = sum(-(-n // page) for n in lengths) + prompts * samples * (2 + (min(steps, window + 2 * page) if window else steps) // page) + 2
     cache = pa.KV.empty(1, pages, page, kv_heads, d, seqs, columns)
     rope = rope_table(length + steps + 1, d)
     room = pa.kv_workspace(cache)
@@ -88,7 +89,9 @@ def run(hidden=4096, heads=32, kv_heads=32, prompts=4, length=512, samples=4, st
     pa.kv_trim(cache, i32([0] * prompts + [length + steps + 1] * len(children)))
     n = len(children)
     last = y[(off[1:] - 1).long()][parents].float()
-    x = (last / last.square().mean(1, keepdim=True).sqrt() + 0.1 * torch.randn((n, hidden), generator=gen, device=DEV)).bfloat16()
+    stream = (last / last.square().mean(1, keepdim=True).sqrt() + 0.1 * torch.randn((n, hidden), generator=gen, device=DEV)).bfloat16()
+    gain = torch.ones(hidden, dtype=torch.bfloat16, device=DEV)
+    x = pa.rmsnorm(stream, gain, 1e-6)
     log = {s: [] for s in range(n)}
     if check:                                                      # the prompts' rows as the cache has them
         turned = torch.empty_like(key)
@@ -104,21 +107,22 @@ def run(hidden=4096, heads=32, kv_heads=32, prompts=4, length=512, samples=4, st
     which = i32(parents)
     plan_qkv, plan_o = pa.decode_plan(qkv, [chosen] * 3, which), pa.decode_plan([o], [chosen], which)
     scratch = torch.empty(max(pa.lowrank_decode_planned_workspace_bytes(qkv), pa.lowrank_decode_planned_workspace_bytes([o])), dtype=torch.uint8, device=DEV)
-    ws = pa.attend_decode_workspace(cache, heads, n)
+    ws = pa.attend_shared_workspace(cache, heads, n)
     out = [torch.empty((n, m), dtype=torch.bfloat16, device=DEV) for m in (hidden, kv_heads * d, kv_heads * d, hidden)]
     turned_q, attn = torch.empty((n, heads, d), dtype=torch.bfloat16, device=DEV), torch.empty((n, heads, d), dtype=torch.bfloat16, device=DEV)
     one, served, seq = i32([0] * prompts + [1] * n), torch.empty(seqs, dtype=torch.int32, device=DEV), i32(children)
     room_for = torch.empty_like(seq)                               # the samples that got room for their token, -1 for the others: those are passed over
+    common = pa.shared_plan(cache, heads, n, seq, window, sinks)   # holds as long as the samples only grow and their windows move
 
     def step():
         pa.lowrank_decode_planned(qkv, x, plan_qkv, out[:3], scratch)
         pa.kv_reserve(cache, one, served, room, seq, room_for)
         pa.kv_append(cache, 0, out[1].view(n, kv_heads, d), out[2].view(n, kv_heads, d), seqs=room_for, q=out[0].view(n, heads, d), q_out=turned_q, rope=rope)
-        pa.attend_decode(cache, 0, turned_q, room_for, window=window, sinks=sinks, out=attn, workspace=ws)
+        pa.attend_shared(cache, 0, turned_q, common, room_for, window=window, sinks=sinks, out=attn, workspace=ws)
         pa.lowrank_decode_planned([o], attn.view(n, hidden), plan_o, out[3:], scratch)
-        pa.kv_trim(cache, None, window, sinks)
-        torch.mul(out[3], 4.0, out=x)
-        x.tanh_()
+        if window:
+            pa.kv_trim(cache, None, window, sinks)
+        pa.rmsnorm(out[3], gain, 1e-6, residual=stream, residual_out=stream, out=x)
 
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())

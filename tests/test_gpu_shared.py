@@ -329,3 +329,18 @@ def test_after_real_forks():
             pa.kv_reserve(kv, i32([0, 0, 9, 9, 9, 9, 9, 9, 9, 9, 0, 0]))
             if window:
                 pa.kv_trim(kv, None, window, sinks)
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (200, 4)])
+def test_the_example_serves_samples_that_share_their_prompts(window, sinks):
+    """Norm, projections, cache and attention together, prompts long enough to be shared, one recorded step; every step's attention against a plain one."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "serve_block.py")
+    spec = importlib.util.spec_from_file_location("serve_block", path)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    r = m.run(hidden=512, heads=8, kv_heads=4, prompts=2, length=300, samples=5, steps=30, groups=8, gs=32, k=4, window=window, sinks=sinks, check=True)
+    # weights rounded as two halves, the result once (2^-8); the plain form in 32 bits
+    assert r["worst"] <= 2.0 ** -7 and r["steps"] == 30 and bool(torch.isfinite(r["x"].float()).all())
+    assert r["lengths"] == [0, 0] + [330] * 5 + [293] * 5
