@@ -606,7 +606,7 @@ int parse_attend_prefill(const parse_kv *kv, int32_t layer, const void *q, int64
  *   seqs       device int32 [rows], the table's row of each, or NULL: the row itself
  *   plan       device, >= parse_shared_plan_bytes, 16-byte aligned; any contents before.  Read only in parse_attend_shared
  *   workspace  any contents; one call at a time has it
- * Limits: rows 1..4096; 3 * (rows * n_q / n_kv / C + rows / 2 + 1) + rows * ceil(n_q / n_kv / C) <= 16384 with C = 128 (64 for heads wider than 128 columns of bf16, 64 of
+ * Limits: rows 1..4096; 3 * (rows * n_q / n_kv / C + rows / 2 + 1) + rows * ceil(n_q / n_kv / C) <= 16384 (8176 for fp32 heads wider than 160 columns) with C = 128 (64 for heads wider than 128 columns of bf16, 64 of
  * fp32), and that number times max_pages*page/32 below 2^31 - 2^16; the queries give 0 otherwise, the calls PARSE_ESHAPE.
  * Other arguments as in parse_attend_decode.  Same inputs and plan, same bits. */
 size_t parse_shared_plan_bytes(const parse_kv *kv, int32_t n_q, int32_t rows);
@@ -667,6 +667,7 @@ int parse_attend_pages(const parse_kv *kv, int32_t layer, const void *q, int64_t
  *   d           a multiple of 8 up to 65536
  *   out         scales NULL: dtype, pointer and stride on 16 bytes, may be x.  Otherwise bytes, pointer and stride (in bytes) on 8
  *   scales      device float [rows][d / block] or NULL;  block: 32, 64, 128, 256 (a divisor of d) or d;  0 without scales
+ *   rows        up to 2^30
  *   eps         >= 0 */
 int parse_rmsnorm(const void *x, int64_t x_stride, const void *residual, int64_t residual_stride, void *residual_out, int64_t residual_out_stride, int32_t dtype,
                   const void *weight, int32_t weight_dtype, int32_t rows, int32_t d, float eps, void *out, int64_t out_stride, float *scales, int32_t block,

@@ -15,7 +15,7 @@ namespace parse {
 constexpr int PT_WAVES = 4, PT_THREADS = PT_WAVES * 64;
 constexpr int PT_STEP = 32;
 constexpr int PT_LEVELS = 3;                         // runs of shared pages that a row may have one behind another
-constexpr int PT_MAXENTRIES = 16384;
+constexpr int PT_MAXENTRIES = 16384, PT_MAXENTRIES_WIDE = 8176;     // their sums stand in LDS beside the ring, which is 128 KiB for fp32 heads wider than 160 columns
 
 // Blocks of sixteen columns that a wavefront has of a wide entry: what the registers hold of q and of the sums beside a step of K and V.  The four wavefronts make TC columns.
 template <class T, int DT> constexpr int pt_blocks() { return DT * (int)sizeof(T) <= 8 ? 2 : 1; }

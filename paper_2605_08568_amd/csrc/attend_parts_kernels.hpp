@@ -670,6 +670,8 @@ __global__ __launch_bounds__(PT_THREADS) void attend_parts_join(PtArgs a) {
 // 32.3, lists of 17 MB 9.2 / 11.4.  Wide entries read a page once a tile, several tiles of a run the same one: through the caches.
 template <class T, int DT, bool LISTED>
 static int pt_launch(const PtArgs &a, int64_t entries, hipStream_t s) {
+  constexpr int most = sizeof(T) == 4 && DT > 5 ? PT_MAXENTRIES_WIDE : PT_MAXENTRIES;
+  static_assert(pt_lds_own<T, DT>() + (2 * PT_WAVES + most + 1) * 4 <= 160 * 1024, "a unit's LDS");
   const size_t lds = pt_lds_own<T, DT>() + (2 * PT_WAVES + (LISTED ? 0 : (size_t)entries + 1)) * 4, page = (size_t)a.kv.page * DT * 32 * sizeof(T) * 2;
   const bool nt = LISTED ? (size_t)a.rows * a.kv.n_kv * a.top * page > ((size_t)96 << 20) : (size_t)a.kv.n_layers * a.kv.n_pages * a.kv.n_kv * page > ((size_t)192 << 20);
   if (nt) {

@@ -233,7 +233,7 @@ static bool as_size(const parse_kv *kv, int n_q, int rows, AsSize &z) {
   z.entries = z.tiles + (int64_t)rows * ((group + TC - 1) / TC);
   z.columns = (int64_t)pt_shares(kv) * TC + (int64_t)(PT_LEVELS + 1) * rows * group;
   z.bytes = pt_deal_bytes(z.entries) + round_up((size_t)z.columns * kv->n_kv * (kv->d + 4) * 4, 256);
-  return z.entries <= PT_MAXENTRIES;
+  return z.entries <= (kv->dtype == PARSE_F32 && kv->d > 160 ? PT_MAXENTRIES_WIDE : PT_MAXENTRIES);
 }
 
 }  // namespace parse

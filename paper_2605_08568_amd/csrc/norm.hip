@@ -170,7 +170,7 @@ extern "C" int parse_rmsnorm(const void *x, int64_t x_stride, const void *residu
   if (!x || !weight || !out || rows <= 0 || d <= 0 || !(eps >= 0.f && eps < 1e38f)) return PARSE_EINVAL;
   if ((dtype != PARSE_F32 && dtype != PARSE_BF16) || (weight_dtype != PARSE_F32 && weight_dtype != PARSE_BF16)) return PARSE_EINVAL;
   if (scales ? block <= 0 : block != 0) return PARSE_EINVAL;
-  if (d % 8 != 0 || d > RN_MAXD) return PARSE_ESHAPE;
+  if (d % 8 != 0 || d > RN_MAXD || rows > 1 << 30) return PARSE_ESHAPE;
   if (scales && block != d && ((block != 32 && block != 64 && block != 128 && block != 256) || d % block != 0)) return PARSE_ESHAPE;
   if (x_stride < d || out_stride < d || (residual && residual_stride < d) || (residual_out && residual_out_stride < d)) return PARSE_ESHAPE;
   const int per16 = 16 / elem_size(dtype);

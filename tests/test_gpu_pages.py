@@ -246,7 +246,7 @@ def test_attend_widths(dtype, d):
     run_attend(case, 6, some_pages(np.random.default_rng(d), case, 5, 7), pad=8)
 
 
-@pytest.mark.parametrize("heads,kv", [(1, 1), (4, 4), (16, 1), (17, 1), (40, 2), (28, 4), (80, 1), (130, 2)])
+@pytest.mark.parametrize("heads,kv", [(1, 1), (4, 4), (16, 1), (17, 1), (40, 2), (28, 4), (80, 1), (130, 2), (300, 1)])
 def test_attend_head_groups(heads, kv):
     case = Case("bf16", kv, 64, 32, [31, 32, 33, 130, 400], seed=heads)
     run_attend(case, heads, some_pages(np.random.default_rng(heads), case, 5, 5))

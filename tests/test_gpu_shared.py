@@ -129,7 +129,7 @@ def test_widths(dtype, d):
     run(Family(dtype, 2, d, 16, tree(16), seed=d), 6, pad=8, shares=True)
 
 
-@pytest.mark.parametrize("heads,kv", [(1, 1), (4, 4), (8, 1), (17, 1), (40, 2), (28, 4), (80, 1), (130, 2)])
+@pytest.mark.parametrize("heads,kv", [(1, 1), (4, 4), (8, 1), (17, 1), (40, 2), (28, 4), (80, 1), (130, 2), (300, 1)])
 def test_head_groups(heads, kv):
     run(Family("bf16", kv, 64, 32, tree(32), seed=heads), heads, shares=True)
 
@@ -155,6 +155,16 @@ def test_numbers_of_rows(rows):
     """One prompt for all, every head with its own keys: up to 128 columns a tile."""
     family = [([("p", 10)], 1 + s % 19) for s in range(rows)]
     run(Family("bf16", 2, 32, 16, family, seed=rows), 2, shares=rows > 1)
+
+
+@pytest.mark.parametrize("dtype,d,rows", [("bf16", 32, 300), ("bf16", 32, 1500), ("fp32", 256, 300)])
+def test_more_rows_than_a_workgroup_has_threads(dtype, d, rows):
+    """Many groups of two to five rows, their order shuffled: plans of more rows than the threads that make them, sums over entries in several rounds."""
+    rng = np.random.default_rng(rows)
+    family = [([(f"p{g}", 8 + g % 2)], int(rng.integers(1, 40))) for g in range(rows // 3) for _ in range(2 + g % 3)][:rows]
+    family = [family[i] for i in rng.permutation(len(family))]
+    _, _, plan, _ = run(Family(dtype, 1, d, 16, family, seed=rows), 2, shares=True)
+    assert tiles_of(plan) == len({sh[0][0] for sh, _ in family if sum(x[0][0][0] == sh[0][0] for x in family) > 1})
 
 
 def test_many_groups_in_any_order():

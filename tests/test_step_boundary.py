@@ -86,6 +86,9 @@ def test_shared_limits():
         wide = dict(kv=kv, n_q=n_q, rows=rows, qs=n_q * 64, outs=n_q * 64)
         if not good:
             assert calls()["shared"](**wide) == ESHAPE and calls()["plan"](**wide) == ESHAPE
+    for d, good in ((160, True), (192, False), (256, False)):
+        kv = cache(n_seqs=4096, n_kv=4, d=d, dtype=0)
+        assert (L.parse_shared_plan_bytes(kv, 4, 4096) > 0) == good and (L.parse_attend_shared_workspace_bytes(kv, 4, 3000) > 0), d
     long = cache(n_seqs=4096, max_pages=1 << 21)
     assert calls()["shared"](long, rows=4096, n_q=8) == ESHAPE
 
@@ -119,7 +122,7 @@ def test_norm_refuses_bad_arguments():
     nan = float("nan")
     refused(c, EINVAL, [dict(x=None), dict(w=None), dict(out=None), dict(rows=0), dict(d=0), dict(eps=-1.0), dict(eps=nan), dict(eps=float("inf")), dict(dtype=2), dict(wt=-1),
                         dict(block=32), dict(sc=FAKE, block=0), dict(sc=FAKE, block=-1)])
-    refused(c, ESHAPE, [dict(d=60), dict(d=65544, xs=1 << 20, rs=1 << 20, ros=1 << 20, outs=1 << 20), dict(xs=56), dict(rs=56), dict(ros=56), dict(outs=56),
+    refused(c, ESHAPE, [dict(rows=(1 << 30) + 1), dict(d=60), dict(d=65544, xs=1 << 20, rs=1 << 20, ros=1 << 20, outs=1 << 20), dict(xs=56), dict(rs=56), dict(ros=56), dict(outs=56),
                         dict(sc=FAKE, block=16), dict(sc=FAKE, block=48), dict(sc=FAKE, block=128), dict(sc=FAKE, block=512)])
     refused(c, EALIGN, [dict(x=ODD), dict(r=ODD), dict(ro=ODD), dict(w=ODD), dict(out=ODD), dict(out=FAKE + 8), dict(xs=68), dict(rs=68), dict(ros=68), dict(outs=68),
                         dict(sc=ODD, block=64), dict(sc=FAKE, block=64, out=FAKE + 4), dict(sc=FAKE, block=64, outs=68)])
