@@ -599,15 +599,16 @@ int parse_attend_prefill(const parse_kv *kv, int32_t layer, const void *q, int64
  * parse_shared_plan looks at the table's rows.  Up to three runs of pages one behind another (a common text, a prompt, a fork of a
  * fork), of at least 128 tokens each, may be shared with ever fewer rows; what is behind them a row has for itself.  Any table is
  * right: rows that do not hold the same pages share nothing.
- * A plan holds for the rows, n_q, window and sinks that it was made with (a call with others reads every cache for itself) and for every layer,
+ * A plan holds for the rows, n_q, window, sinks and sizes of the cache that it was made with (a call with others reads every cache for itself) and for every layer,
  * while sequences grow (parse_kv_reserve, parse_kv_append) and pages behind that window and sinks are given up (parse_kv_trim without keep).  After any other
  * change of the table or the lengths it is made anew.  The call may be given -1 for sequences that were not served
  * (parse_kv_reserve_seqs) where the plan had their number.
  *   seqs       device int32 [rows], the table's row of each, or NULL: the row itself
  *   plan       device, >= parse_shared_plan_bytes, 16-byte aligned; any contents before.  Read only in parse_attend_shared
  *   workspace  any contents; one call at a time has it
- * Limits: rows 1..4096; 3 * (rows * n_q / n_kv / C + rows / 2 + 1) + rows * ceil(n_q / n_kv / C) <= 16384 (8176 for fp32 heads wider than 160 columns) with C = 128 (64 for heads wider than 128 columns of bf16, 64 of
- * fp32), and that number times max_pages*page/32 below 2^31 - 2^16; the queries give 0 otherwise, the calls PARSE_ESHAPE.
+ * Limits: rows 1..4096; 3 * (rows * n_q / n_kv / C + rows / 2 + 1) + rows * ceil(n_q / n_kv / C) <= 16384 (8176 for fp32 heads wider than 160
+ * columns) with C = 128 (64 for heads wider than 128 columns of bf16, 64 of fp32), and that number times max_pages*page/32 below 2^31 - 2^16; the
+ * queries give 0 otherwise, the calls PARSE_ESHAPE.
  * Other arguments as in parse_attend_decode.  Same inputs and plan, same bits. */
 size_t parse_shared_plan_bytes(const parse_kv *kv, int32_t n_q, int32_t rows);
 int parse_shared_plan(const parse_kv *kv, int32_t n_q, int32_t rows, const int32_t *seqs, int32_t window, int32_t sinks, void *plan, size_t plan_bytes,
@@ -648,7 +649,8 @@ int parse_select_pages(const parse_kv *kv, const void *bounds, int32_t layer, co
 
 /* The attention of parse_attend_decode over the listed pages only: a row and kv head see the tokens of the columns in pages[row][kv head][0..top) that the sequence has
  * (j <= len - 1) and whose page is there.  Columns may stand in any order; -1 and others outside the table are passed over; one that stands twice counts twice.
- *   pages      device int32 [rows][n_kv][top], 1 <= top, rows * n_kv * top < 2^31, and rows * ceil(n_q / n_kv / 64) * top * page / 32 below 2^31 - 2^16
+ *   pages      device int32 [rows][n_kv][top], 1 <= top, top * page < 2^31, rows * n_kv * top < 2^31, and
+ *              rows * ceil(n_q / n_kv / 64) * top * page / 32 below 2^31 - 2^16
  *   workspace  any contents; one call at a time has it
  * Other arguments as in parse_attend_decode.  Same inputs, same bits. */
 size_t parse_attend_pages_workspace_bytes(const parse_kv *kv, int32_t n_q, int32_t rows, int32_t top);

@@ -20,7 +20,7 @@ static bool al_size(const parse_kv *kv, int n_q, int rows, int top, AlSize &z) {
   const int64_t columns = (int64_t)pt_shares(kv) * z.TC + (int64_t)rows * group;
   z.bytes = pt_deal_bytes(z.entries) + round_up((size_t)columns * kv->n_kv * (kv->d + 4) * 4, 256);
   return z.entries <= INT32_MAX && z.entries * (((int64_t)top * kv->page + PT_STEP - 1) / PT_STEP) <= INT32_MAX - 65536 &&
-         (int64_t)rows * kv->n_kv * top <= INT32_MAX;
+         (int64_t)top * kv->page <= INT32_MAX && (int64_t)rows * kv->n_kv * top <= INT32_MAX;
 }
 
 }  // namespace parse

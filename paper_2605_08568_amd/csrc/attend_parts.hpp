@@ -38,7 +38,7 @@ struct PtRow {
 static_assert(sizeof(PtTile) == 32 && sizeof(PtRow) == 32, "read as words");
 struct PtHead {
   int rows, group, columns, window, sinks, n_pages, max_pages, page;    // what the plan was made for
-  int tiles, tile_columns, pad[6];
+  int tiles, tile_columns, n_seqs, pad[5];
 };
 static_assert(sizeof(PtHead) == 64, "");
 struct PtPlan {
@@ -132,7 +132,7 @@ __device__ __forceinline__ PtShortest pt_shortest(const PtArgs &a, const PtTile 
 // Whether the plan was made for such a call; one that was not shares nothing
 __device__ __forceinline__ bool pt_fits(const PtArgs &a, int columns) {
   const PtHead &h = *a.plan.head;
-  return h.rows == a.rows && h.group == a.group && h.columns == columns && h.window == a.window && h.sinks == a.sinks && h.n_pages == a.kv.n_pages &&
+  return h.rows == a.rows && h.group == a.group && h.columns == columns && h.window == a.window && h.sinks == a.sinks && h.n_pages == a.kv.n_pages && h.n_seqs == a.kv.n_seqs &&
          h.max_pages == a.kv.max_pages && h.page == a.kv.page && h.tiles >= 0 && h.tiles <= a.most_tiles;
 }
 

@@ -215,7 +215,7 @@ __global__ __launch_bounds__(SH_ONE) void shared_tiles(parse_kv kv, const int32_
   if (tid == 0) {
     PtHead h{};
     h.rows = rows; h.group = group; h.columns = TC; h.window = window; h.sinks = sinks; h.n_pages = kv.n_pages; h.max_pages = kv.max_pages; h.page = kv.page;
-    h.tiles = tiles; h.tile_columns = columns;
+    h.tiles = tiles; h.tile_columns = columns; h.n_seqs = kv.n_seqs;
     *plan.head = h;
   }
 }

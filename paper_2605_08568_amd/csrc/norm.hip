@@ -145,7 +145,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rmsnorm(RnArgs a) {
 }
 
 template <class T, class W, bool E4M3>
-static int rn_launch(const RnArgs &a, hipStream_t s) {
+static int rn_piece(const RnArgs &a, hipStream_t s) {
   const int pieces = a.d / 8;
 #define RN_GO(LANES, PIECES) rmsnorm<T, W, LANES, PIECES, E4M3><<<dim3((a.rows + (LANES < 256 ? 256 / LANES : 1) - 1) / (LANES < 256 ? 256 / LANES : 1)), LANES < 256 ? 256 : LANES, 0, s>>>(a)
   if (pieces <= 64) RN_GO(64, 1);
@@ -158,6 +158,23 @@ static int rn_launch(const RnArgs &a, hipStream_t s) {
   else RN_GO(1024, 8);
 #undef RN_GO
   PARSE_LAUNCH_CHECK();
+  return PARSE_OK;
+}
+// A launch has fewer than 2^32 threads: rows by 2^21, of which only the largest calls have more
+template <class T, class W, bool E4M3>
+static int rn_launch(const RnArgs &a, hipStream_t s) {
+  constexpr int MOST = 1 << 21;
+  for (int r0 = 0; r0 < a.rows; r0 += MOST) {
+    RnArgs b = a;
+    b.rows = std::min(a.rows - r0, MOST);
+    b.x = (const T *)a.x + r0 * a.x_stride;
+    if (a.residual) b.residual = (const T *)a.residual + r0 * a.residual_stride;
+    if (a.residual_out) b.residual_out = (T *)a.residual_out + r0 * a.residual_out_stride;
+    b.out = (char *)a.out + r0 * a.out_stride * (E4M3 ? 1 : (int)sizeof(T));
+    if (a.scales) b.scales = a.scales + (int64_t)r0 * (a.d / a.block);
+    const int st = rn_piece<T, W, E4M3>(b, s);
+    if (st != PARSE_OK) return st;
+  }
   return PARSE_OK;
 }
 

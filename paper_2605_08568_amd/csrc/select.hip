@@ -402,7 +402,7 @@ __device__ __forceinline__ void choose_pages(int n, int top, int32_t *__restrict
 }
 
 // The keys of the columns that are not scored
-__device__ __forceinline__ uint64_t sp_unscored(const SpArgs &a, const int32_t *table, const SpCols &cols, int c) {
+__device__ __forceinline__ uint64_t sp_unscored(const SpArgs &a, const int32_t *table, int c) {
   return (unsigned)table[c] < (unsigned)a.kv.n_pages ? SP_ALWAYS : SP_NONE;
 }
 __device__ __forceinline__ bool sp_scored(const SpArgs &a, const SpCols &cols, int c) { return cols.n > a.top && c >= cols.begin && c < cols.end; }
@@ -415,7 +415,7 @@ __global__ __launch_bounds__(SC_THREADS) void page_choice(SpArgs a) {
   const int32_t *table = a.kv.table + (int64_t)sq.row * a.kv.max_pages;
   const uint64_t *keys = a.keys + ((int64_t)row * a.kv.n_kv + head) * a.kv.max_pages;
   int32_t *sel = a.sel + ((int64_t)row * a.kv.n_kv + head) * a.top;
-  auto key = [&](int c) { return sp_scored(a, cols, c) ? keys[c] : sp_unscored(a, table, cols, c); };
+  auto key = [&](int c) { return sp_scored(a, cols, c) ? keys[c] : sp_unscored(a, table, c); };
   if (cols.n <= SC_MOST) {
 #pragma unroll
     for (int i = 0; i < SC_MOST / SC_THREADS; ++i) {
@@ -443,7 +443,7 @@ __global__ __launch_bounds__(SC_FUSED, 2) void page_select(SpArgs a) {
   }
 #pragma unroll 1
   for (int c = threadIdx.x; c < cols.n; c += SC_FUSED)
-    if (!sp_scored(a, cols, c)) sh.keys[c] = sp_unscored(a, table, cols, c);
+    if (!sp_scored(a, cols, c)) sh.keys[c] = sp_unscored(a, table, c);
   __syncthreads();
   choose_pages<SC_FUSED>(cols.n, a.top, a.sel + ((int64_t)row * a.kv.n_kv + head) * a.top, sh, [&](int c) { return sh.keys[c]; });
 }

@@ -157,6 +157,26 @@ def test_small_weights_keep_their_scale():
     assert np.all(np.abs(q.double().cpu().numpy() * 2.0 ** -120 - y) <= np.maximum(np.abs(y) * 2.0 ** -4, 2.0 ** -130) * 1.01 + 2.0 ** -149)
 
 
+@pytest.mark.parametrize("block", [None, 8])
+def test_more_rows_than_a_launch_takes(block):
+    """The rows on both sides of the seam, at the end, and those between that repeat them."""
+    seam, d = 1 << 21, 8
+    some = torch.from_numpy(np.random.default_rng(3).standard_normal((64, d)).astype(np.float32)).bfloat16()
+    x = some.to(DEV).repeat(seam // 64 + 1, 1)[:seam + 37].contiguous()
+    w = torch.ones(d, device=DEV, dtype=torch.bfloat16)
+    res, scales = torch.empty_like(x), None if block is None else torch.full((len(x), d // block), np.nan, device=DEV)
+    out = pa.rmsnorm(x, w, 1e-5, x, res, None, scales)
+    s, y = so.rmsnorm(some.double().numpy(), some.double().numpy(), np.ones(d), 1e-5)
+    if block is None:
+        check(out[:64], y, "bf16", "out")
+    else:
+        check_e4m3(out[:64], scales[:64], y, block)
+    assert torch.equal(res, 2 * x), "twice a number of bf16 is one"
+    for t in (out.view(torch.uint8), scales):
+        if t is not None:
+            assert torch.equal(t[64:], t[:-64]), "equal rows, equal results"
+
+
 def test_graph_and_stream():
     torch.manual_seed(2)
     x, r, w = torch.randn(100, 4096, device=DEV).bfloat16(), torch.randn(100, 4096, device=DEV).bfloat16(), torch.rand(4096, device=DEV).bfloat16()

@@ -67,6 +67,12 @@ def test_bounds_of_many_sequences_and_missing_pages():
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_bounds_of_many_heads(dtype):
+    """Heads one after another in a wavefront, their number not a multiple of it."""
+    run_bounds(Case(dtype, 127, 32, 16, [16 * 100, 16 * 100 + 7, 16 * 99], seed=6), [1600] * 3)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_bounds_of_infinities_and_nan(dtype):
     case = Case(dtype, 1, 32, 16, [48], seed=2)
     case.write(0, 3, k=np.inf), case.write(0, 5, k=-np.inf), case.write(0, 20, k=np.nan)
@@ -134,6 +140,13 @@ def test_select_numbers(top, first, last):
     lens = [1, 16, 17, 16 * top, 16 * top + 1, 4500, 0]
     lens = [min(n, 9000) for n in lens]
     run_select(*table_cache(np.random.default_rng(top), "bf16", 2, 32, 16, lens), lens, 2, top, first, last)
+
+
+@pytest.mark.parametrize("rows,kv,cols", [(70, 2, 700), (3, 2, 700), (2, 520, 40), (40, 4, 2300)])
+def test_select_launches(rows, kv, cols):
+    """One launch for many heads with tables of middle length; two for few of them, for very many, and for longer tables."""
+    lens = [16 * cols - 5 - 3 * r for r in range(rows)]
+    run_select(*table_cache(np.random.default_rng(cols), "bf16", kv, 32, 16, lens), lens, kv, 9, 1, 1)
 
 
 def test_select_from_long_tables():
@@ -266,6 +279,24 @@ def test_attend_odd_lists(dtype):
     run_attend(case, 4, [[[3, 3, 0, -1]], [[6, 5, 100, 8]], [[-1, -1, -1, -7]], [[2 ** 31 - 1, 1, 2, -2 ** 31]]])
     run_attend(case, 4, [[[2, 1, 0]], [[2, 2, 2]], [[0, 1, 2]]], seqs=[0, -1, 99])
     run_attend(case, 4, [[[2, 1, 0]], [[2, 2, 2]], [[0, 1, 2]]], seqs=[3, 3, 1])
+
+
+@pytest.mark.parametrize("heads", [128, 2560])
+def test_attend_shares_of_more_steps_than_lanes(heads):
+    """Lists of mostly nothing, 400 steps for four shares a head: narrow and wide entries, pages behind a share's 64th step."""
+    case = Case("bf16", 128, 32, 256, [700, 600], seed=4)
+    pages = np.full((1, 128, 50), -1)
+    for i, c in ((0, 2), (9, 0), (10, 1), (37, 0), (49, 2)):
+        pages[0, :, i] = c
+    run_attend(case, heads, pages)
+
+
+def test_attend_lists_that_do_not_stay_in_the_caches():
+    """Over 96 MB as the list's length has it: loads past the caches."""
+    case = Case("bf16", 1, 256, 256, [2000, 513], seed=5)
+    pages = np.full((2, 1, 256), -1)
+    pages[0, 0, ::37], pages[1, 0, 250:253] = np.arange(7), (2, 0, 1)
+    run_attend(case, 3, pages)
 
 
 @pytest.mark.parametrize("rows", [1, 63, 65, 300])

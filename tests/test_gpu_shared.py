@@ -272,6 +272,28 @@ def test_scales(scale):
     run(Family("bf16", 2, 64, 16, tree(16), seed=16), 4, scale=scale, shares=True)
 
 
+@pytest.mark.parametrize("n_q", [128, 640])
+def test_shares_of_more_steps_than_lanes(n_q):
+    """Heads of so many caches that a share has over 64 steps: narrow (four columns) and wide tiles (twenty), and the first row's own tokens."""
+    run(Family("bf16", 128, 32, 64, [([("p", 150)], 30), ([("p", 150)], 1), ([("p", 150)], 64), ([("p", 150)], 5)], seed=18), n_q, shares=True)
+    run(Family("bf16", 128, 32, 64, [([], 9700), ([], 3)], seed=19), n_q, shares=False)
+
+
+def test_a_pool_that_does_not_stay_in_the_caches():
+    """Over 192 MB: loads of narrow entries past the caches; of tokens that only one row has, and of a prompt's."""
+    run(Family("bf16", 8, 128, 64, [([("p", 330)], 70), ([("p", 330)], 1), ([], 4000)], seed=20), 16, shares=True)
+
+
+def test_a_plan_for_a_larger_table_shares_nothing():
+    f = Family("bf16", 1, 64, 16, tree(16), seed=21)
+    n = len(f.lens)
+    first = list(range(3))
+    _, _, plan, _ = run(f, 2, seqs=[n - 1, n - 2, n - 3], shares=True)
+    f.table, f.lens = f.table[:3], f.lens[:3]
+    f.kv = pa.KV(f.kv.K, f.kv.V, i32(f.table), i32(np.array(f.lens)))
+    run(f, 2, seqs=first, plan=plan)
+
+
 def test_long_prompts_are_cut_over_the_card():
     run(Family("bf16", 1, 64, 64, [([("p", 160)], 50 + 100 * s) for s in range(6)], seed=17), 4, shares=True)
 

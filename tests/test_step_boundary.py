@@ -64,6 +64,7 @@ def test_attention_refuses_bad_arguments(name):
         assert c(wsb=L.parse_attend_pages_workspace_bytes(cache(), 8, 3, 4) - 1) == EWORKSPACE
         refused(c, EINVAL, [dict(pages=None), dict(top=0), dict(top=-5)])
         assert c(pages=ODD) == EALIGN and c(top=1 << 29) == ESHAPE
+        assert c(cache(n_kv=1, page=256), rows=1, n_q=1, top=1 << 23) == ESHAPE and c(cache(n_kv=1, page=16), rows=1, n_q=1, top=1 << 27) == ESHAPE
 
 
 def test_shared_plan_refuses_bad_arguments():
