@@ -13,9 +13,11 @@ template <class T, int DT> constexpr int pt_lds_own() {
   return ring > sums ? ring : sums;
 }
 
+// Steps of a share where there are tiles, at least.  8 / 12 / 16, us: 32 samples of 8192 tokens 39.5 / 42.4 / 46.9 with the join
 constexpr int PT_WIDE_STEPS = 8;
 
-// Entry x is share x, whole, where no entry has many more steps than an equal share would
+// Entry x is share x, whole, where no entry has more steps than an equal share would and these: it costs what the longest entry is longer, and saves parts and, where rows
+// share nothing, the join.  4 / 12 / 24, us with the join: 32 caches of 100 to 356 tokens 19.3 / 17.7 / 17.7, 32 lists of 32 pages of 32 30.9 / 31.1 / 36.0
 constexpr int PT_SLACK = 12;
 
 // A step of 32 tokens: s = K q (operand A = K, token rows; operand B = q, a column of the entry), weights 2^(scale s - base), o += V^T p.  K's rows are taken in the order in
@@ -23,7 +25,11 @@ constexpr int PT_SLACK = 12;
 // the eight tokens whose V it has loaded.  bf16: a weight is multiplied as two bf16 numbers, as in the decode attention.
 //   narrow entries, up to sixteen columns: operands go straight from the pages into registers, a step ahead of the one that is worked on where two fit; the four wavefronts
 //   take turns and their sums meet in LDS, or, where rows are many and short, a wavefront has a row alone
-//   wide ones: a wavefront has up to NW blocks of sixteen columns; the steps go through a ring in LDS, filled by loads that write LDS, and are read by all four
+//   wide ones: a wavefront has up to NW blocks of sixteen columns; the steps go through a ring in LDS, filled by loads that write LDS, and are read by all four (the same columns
+//     out of registers, every wavefront its own loads: 123 us where this takes 28)
+// Bound, bf16 of 128 columns: small calls by latency (lengths and the plan, the entry's columns and pages, first loads, the meeting: four trips, 8 to 10 us); wide entries by the
+// vector unit and by how few steps a share has: 32 samples of one text of 8192 tokens, 8 heads, 32/8, 27.5 us, 1.2 us a step of 128 columns; narrow entries by reads: 32 caches of 2049
+// tokens 50 us, 5.4 TB/s.
 template <class T, int DT, bool NT, bool LISTED>
 __global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_parts(PtArgs a) {
   constexpr int D = DT * 32, KB = D / 32, VB = D / 16, NW = pt_blocks<T, DT>(), TC = 64 * NW, RD = D + 4, ST = pt_stages<T, DT>();
@@ -559,7 +565,8 @@ __global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_part
 }
 
 // The parts of one row's head; workgroup (head, row).  Four columns a lane, so many parts at once as the workgroup has lanes for, four of them on their way each; a group of lanes
-// joins its parts one after another, then the groups are joined, both in a fixed order.  Bound: three dependent trips to memory, then the parts' reads.
+// joins its parts one after another, then the groups are joined, both in a fixed order.  Bound: three dependent trips to memory, then the parts' reads: 3.8 us (a part or two a
+// row) to 9.8 (96 rows of a window, up to 20 parts each); 8 where 32 rows have 64 parts each.
 template <class T, int DT, bool LISTED>
 __global__ __launch_bounds__(PT_THREADS) void attend_parts_join(PtArgs a) {
   constexpr int D = DT * 32, RD = D + 4, TC = 64 * pt_blocks<T, DT>(), LANES = D / 4, GROUPS = PT_THREADS / LANES, N = 4;

@@ -13,7 +13,7 @@ struct KbArgs {
   const void *K;
   void *bounds;                                      // of the first layer: [page][head][2][d]
   const int32_t *tok_offsets, *seqs;
-  int P, layers, at_once;                            // at_once: heads that a wavefront has one after another
+  int P, layers;
   int64_t k_layer, b_layer;                          // elements
 };
 
@@ -31,8 +31,9 @@ __device__ __forceinline__ void kb_fold(float *v, bool upper) {
 }
 
 // A wavefront has pages of single heads: a load brings 64 pieces of eight columns, lane % 16 the token, so that a block's sixteen tokens are a row of lanes; the rows fold
-// to one value a lane in 60 exchanges (values and negated values side by side: the largest is the least of the negated).  The next head's first block is asked for before this
-// one's lanes fold.  Bound: reads; pages of 16 tokens by the vector unit as much (bf16 to fp32, two comparisons a value, the folding).
+// to one value a lane in 60 exchanges (values and negated values side by side: the largest is the least of the negated).  Bound: reads; pages of 16 tokens by the vector unit as much (bf16 to fp32, two comparisons a value, the
+// folding).  A cache of 100003 tokens, 8 heads of 128 columns of bf16, 205 MB: 38 us, 5.4 TB/s; 8 prompts of 512 15 us.  Heads one after another in a wavefront, the next one's loads
+// before this one's folding: 39 and 15.6.
 template <class T, int DT>
 __global__ __launch_bounds__(SP_THREADS) void kv_bounds(KbArgs a) {
   constexpr int D = DT * 32;
@@ -40,7 +41,7 @@ __global__ __launch_bounds__(SP_THREADS) void kv_bounds(KbArgs a) {
   extern __shared__ int pre[];
   int *wave_sums = pre + a.P + 1;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, page = a.kv.page, blocks = page / 16;
-  const int heads = a.kv.n_kv * a.layers, per = (heads + SP_WAVES * a.at_once - 1) / (SP_WAVES * a.at_once);
+  const int heads = a.kv.n_kv * a.layers, per = (heads + SP_WAVES - 1) / SP_WAVES;
   for (int64_t w = blockIdx.x;; w += gridDim.x) {
     const int64_t number = w / per;
     if (number > 0x7fffffff) return;
@@ -49,62 +50,50 @@ __global__ __launch_bounds__(SP_THREADS) void kv_bounds(KbArgs a) {
     if (f.item < 0) return;
     const int c = max(f.len - f.n, 0) / page + f.item;
     const int id = a.kv.table[(int64_t)f.row * a.kv.max_pages + c];
-    int lh = (int)(w % per) * SP_WAVES * a.at_once + wave;
-    const int behind = min(lh - wave + SP_WAVES * a.at_once, heads);
-    if (id >= 0 && id < a.kv.n_pages && lh < behind) {
-      auto keys = [&](int of) {
-        const int layer = of / a.kv.n_kv, head = of - layer * a.kv.n_kv;
-        return reinterpret_cast<const T *>(a.K) + layer * a.k_layer + ((int64_t)id * a.kv.n_kv + head) * page * D + lane * 8;
-      };
+    const int lh = (int)(w % per) * SP_WAVES + wave;
+    if (id >= 0 && id < a.kv.n_pages && lh < heads) {
+      const int layer = lh / a.kv.n_kv, head = lh - layer * a.kv.n_kv;
+      const T *k = reinterpret_cast<const T *>(a.K) + layer * a.k_layer + ((int64_t)id * a.kv.n_kv + head) * page * D + lane * 8;
       frag x[DT];
-      const T *k = keys(lh);
 #pragma unroll
       for (int p = 0; p < DT; ++p) x[p] = Op<T>::load_nt(k + p * 512);
-      for (; lh < behind; lh += SP_WAVES) {
-        float v[16 * DT];                                          // [least, largest negated][column of the piece][piece]
+      float v[16 * DT];                                            // [least, largest negated][column of the piece][piece]
 #pragma unroll
-        for (int i = 0; i < 16 * DT; ++i) v[i] = INFINITY;
-        auto take = [&](const frag &y, int p) {
-          float z[8];
-          if constexpr (sizeof(T) == 2) {
+      for (int i = 0; i < 16 * DT; ++i) v[i] = INFINITY;
+      auto take = [&](const frag &y, int p) {
+        float z[8];
+        if constexpr (sizeof(T) == 2) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) { z[2 * e] = __uint_as_float(y[e] << 16); z[2 * e + 1] = __uint_as_float(y[e] & 0xffff0000u); }
-          } else {
+          for (int e = 0; e < 4; ++e) { z[2 * e] = __uint_as_float(y[e] << 16); z[2 * e + 1] = __uint_as_float(y[e] & 0xffff0000u); }
+        } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) { z[e] = y.lo[e]; z[4 + e] = y.hi[e]; }
-          }
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            v[e * DT + p] = kb_min(v[e * DT + p], z[e]);
-            v[(8 + e) * DT + p] = kb_min(v[(8 + e) * DT + p], -z[e]);
-          }
-        };
-        for (int b = 1; b < blocks; ++b) {
-          frag y[DT];
-#pragma unroll
-          for (int p = 0; p < DT; ++p) y[p] = Op<T>::load_nt(k + b * 16 * D + p * 512);
-#pragma unroll
-          for (int p = 0; p < DT; ++p) { take(x[p], p); x[p] = y[p]; }
+          for (int e = 0; e < 4; ++e) { z[e] = y.lo[e]; z[4 + e] = y.hi[e]; }
         }
 #pragma unroll
-        for (int p = 0; p < DT; ++p) take(x[p], p);
-        const int layer = lh / a.kv.n_kv, head = lh - layer * a.kv.n_kv;
-        if (lh + SP_WAVES < behind) {
-          k = keys(lh + SP_WAVES);
-#pragma unroll
-          for (int p = 0; p < DT; ++p) x[p] = Op<T>::load_nt(k + p * 512);
+        for (int e = 0; e < 8; ++e) {
+          v[e * DT + p] = kb_min(v[e * DT + p], z[e]);
+          v[(8 + e) * DT + p] = kb_min(v[(8 + e) * DT + p], -z[e]);
         }
-        kb_fold<0x140, 16 * DT>(v, lane & 8);                      // row_mirror: lane ^ 15
-        kb_fold<0x141, 8 * DT>(v, lane & 4);                       // row_half_mirror: lane ^ 7
-        kb_fold<0x1b, 4 * DT>(v, lane & 2);                        // quad_perm 3 2 1 0
-        kb_fold<0xb1, 2 * DT>(v, lane & 1);                        // quad_perm 1 0 3 2
-        T *to = reinterpret_cast<T *>(a.bounds) + layer * a.b_layer + ((int64_t)id * a.kv.n_kv + head) * 2 * D + (lane & 8 ? D : 0) + (lane >> 4) * 8 + (lane & 7);
+      };
+      for (int b = 1; b < blocks; ++b) {
+        frag y[DT];
 #pragma unroll
-        for (int p = 0; p < DT; ++p) {
-          const float r = lane & 8 ? -v[p] : v[p];
-          if constexpr (sizeof(T) == 2) to[p * 32] = (T)(__float_as_uint(r) >> 16);        // it is one of the keys
-          else to[p * 32] = r;
-        }
+        for (int p = 0; p < DT; ++p) y[p] = Op<T>::load_nt(k + b * 16 * D + p * 512);
+#pragma unroll
+        for (int p = 0; p < DT; ++p) { take(x[p], p); x[p] = y[p]; }
+      }
+#pragma unroll
+      for (int p = 0; p < DT; ++p) take(x[p], p);
+      kb_fold<0x140, 16 * DT>(v, lane & 8);                        // row_mirror: lane ^ 15
+      kb_fold<0x141, 8 * DT>(v, lane & 4);                         // row_half_mirror: lane ^ 7
+      kb_fold<0x1b, 4 * DT>(v, lane & 2);                          // quad_perm 3 2 1 0
+      kb_fold<0xb1, 2 * DT>(v, lane & 1);                          // quad_perm 1 0 3 2
+      T *to = reinterpret_cast<T *>(a.bounds) + layer * a.b_layer + ((int64_t)id * a.kv.n_kv + head) * 2 * D + (lane & 8 ? D : 0) + (lane >> 4) * 8 + (lane & 7);
+#pragma unroll
+      for (int p = 0; p < DT; ++p) {
+        const float r = lane & 8 ? -v[p] : v[p];
+        if constexpr (sizeof(T) == 2) to[p * 32] = (T)(__float_as_uint(r) >> 16);          // it is one of the keys
+        else to[p * 32] = r;
       }
     }
     if (a.P > 64) __syncthreads();                                 // the prompts' sums are made anew
@@ -173,6 +162,7 @@ template <int LP> __device__ __forceinline__ double sp_sum8(double *v) {
 // Scores of the pages from column c0 on, `step` further each time, by a wavefront: store(column, key).  LP lanes have a page's bounds of one head, eight columns of one of the
 // two each, and what of q they are multiplied with in 64 bits: the sum over the group's heads of what is positive goes with the largest, of what is negative with the
 // least.  Sums in 64 bits because a choice hangs on neighbours in the order.  Eight pages a lane on their way, the first of them before q.
+// Bound: latency and 64-bit products; 1563 pages of 8 heads (6.4 MB of bounds) 6.7 us.
 template <class T, int DT, class F>
 __device__ __forceinline__ void score_pages(const SpArgs &a, int row, int head, const KvSeq &sq, const SpCols &cols, int64_t c0, int64_t step, F store) {
   constexpr int D = DT * 32, LP = sp_lanes(D), AT_ONCE = 8;
@@ -294,7 +284,9 @@ template <int WAVES> __device__ __forceinline__ int sc_before(int v, int *sums, 
 }
 
 // A workgroup has a row's head and n columns with their keys: the key of the last one that is taken, SC_BITS after another, then the columns in order, 64 after another.
-// Loops are short and not unrolled: a launch's first pass through its code costs more than what it does.  Bound: latency, two to three steps with three barriers each.
+// Loops are short and not unrolled: a launch's first pass through its code costs more than what it does (unrolled 11.9 us, so 8.4).  Bound: latency, two to three steps with three
+// barriers each: 8.4 us for 64 of 1563 columns, 8 heads; with the scores in one launch 8.4 for 4 rows of 16
+// heads and up to 44 columns, 18 for 32 rows of 8 heads and up to 500.
 template <int THREADS, class F>
 __device__ __forceinline__ void choose_pages(int n, int top, int32_t *__restrict__ sel, ScShared<THREADS> &sh, F key_of) {
   constexpr int WAVES = THREADS / 64, BINS = (1 << SC_BITS) / THREADS;      // bins of a thread
@@ -525,10 +517,9 @@ int parse_kv_bounds(const parse_kv *kv, void *bounds, int32_t layer, const int32
   a.tok_offsets = tok_offsets; a.seqs = seqs; a.P = P;
   if ((int64_t)kv->n_kv * a.layers > INT32_MAX) return PARSE_ESHAPE;
   if (tok_offsets && (int64_t)P * kv->max_pages > INT32_MAX) return PARSE_ESHAPE;              // their pages are counted in an int
-  // a prompt's whole pages are no more than the pool has; heads by fours where that still makes 2048 workgroups
+  // a prompt's whole pages are no more than the pool has
   const int64_t heads = (int64_t)kv->n_kv * a.layers, items = (int64_t)P * (tok_offsets ? std::min(kv->max_pages, kv->n_pages) : 1);
-  a.at_once = items * heads >= 2048 * SP_WAVES * 4 ? 4 : 1;
-  const int64_t per = (heads + SP_WAVES * a.at_once - 1) / (SP_WAVES * a.at_once);
+  const int64_t per = (heads + SP_WAVES - 1) / SP_WAVES;
   const dim3 grid((uint32_t)std::min<int64_t>(per * items, 2048));
   const size_t lds = (P + 1 + SP_WAVES) * 4;
   if (kv->dtype == PARSE_BF16) kb_launch<uint16_t>(a, grid, lds, (hipStream_t)stream);
