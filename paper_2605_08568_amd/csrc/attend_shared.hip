@@ -8,6 +8,7 @@
 namespace parse {
 
 constexpr int SH_THREADS = 256, SH_ONE = 1024;
+constexpr int SH_NEAR_ROWS = 64;                    // a lane each
 // Tokens of a run that is worth a tile: a step a wavefront.  128 / 64, us with the join: 32 prompts of 100 tokens with 4 samples each of up to 200 more 33.5 / 53, 4 with 16 samples
 // 16.1 / 35, one of 77 with 4 samples 13.1 / 12.4
 constexpr int SH_LEAST = 128;
@@ -15,8 +16,8 @@ constexpr int SH_LEAST = 128;
 // ---- the plan: which rows hold the same pages ------------------------------------------------------------------------
 // Only whole pages in front of a row's last token count (those stay as they are while the sequence grows), and of them what the row sees or a later token of it
 // will see.  owner[page]: the shortest of the rows that hold it (of equal ones the first); users[page]: how many do.
-// Four launches, made once for all layers and steps; bound by their latency.  36 rows of three levels 20 us (4.0 + 2.5 + 5.1 + 8.7); one workgroup for small batches was
-// slower (24 us with its atomics in memory, 29 in LDS).
+// Four launches, or two (below), made once for all layers and steps; bound by their latency.  One workgroup for a small batch was slower than four launches of 18 to 23 us (24 with
+// its atomics in memory, 29 in LDS).
 struct ShRow {
   KvSeq seq;
   int columns, lo, page, sinks;
@@ -50,12 +51,51 @@ __global__ __launch_bounds__(SH_THREADS) void shared_count(parse_kv kv, const in
   }
 }
 
+// Where rows are few, a workgroup a row instead: owner and users of 256 columns at once from the rows' tables themselves, a thread a column, sixteen rows asked for together
+// (a page counts in the column that it stands in: another would not be shared anyway).  One launch instead of three; three / one, us without what lies between them: 4 rows of
+// 5 columns 8.5 / 5.4, 36 of 75 13.7 / 8.4, 32 of 132 13.1 / 7.8, 64 of 132 14.0 / 11.0, 48 of 470 21.5 / 16.4; 96 of 200 (two rows a lane, from LDS) 13.6 / 18.6.
+struct ShNear {
+  int owner[SH_THREADS], users[SH_THREADS];
+};
+struct ShOther {                                       // a lane a row
+  int at, columns, lo, len;                            // first word of the table's row; columns that it cares for are below `columns`, and from `lo` on or below the sinks' end
+};
+__device__ __forceinline__ void shared_near(const parse_kv &kv, const ShRow &r, const int32_t *table, int rows, int c, const ShOther &all, ShNear &sh) {
+  const bool care = c < r.columns && r.cares(c), sink = r.windowed && (int64_t)c * r.page < r.sinks;
+  const int cc = min(c, kv.max_pages - 1), id = care ? table[cc] : -1;
+  int least = 0x7fffffff, owner = -1, users = 0;
+#pragma unroll 1
+  for (int r0 = 0; r0 < rows; r0 += 16) {
+    int x[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) x[j] = (kv.table + __builtin_amdgcn_readlane(all.at, r0 + j))[cc];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      const int len = __builtin_amdgcn_readlane(all.len, r0 + j);
+      const bool has = (x[j] == id) & (c < __builtin_amdgcn_readlane(all.columns, r0 + j)) & (sink | (c >= __builtin_amdgcn_readlane(all.lo, r0 + j)));
+      users += has ? 1 : 0;
+      owner = has & (len < least) ? r0 + j : owner;
+      least = has ? min(least, len) : least;
+    }
+  }
+  const bool there = care && (unsigned)id < (unsigned)kv.n_pages;
+  sh.owner[threadIdx.x] = there ? owner : -1;
+  sh.users[threadIdx.x] = there ? users : 0;
+}
+
 // A wavefront walks a row's columns.  A run ends where the pages have another owner or fewer users; one of two users and more that is long enough (with what
 // shorter ones left before it: their rows hold that too) is the row's next level.  Then the columns are compared with the owner's: the row takes part as far as they agree.
+template <bool NEAR>
 __global__ __launch_bounds__(SH_THREADS) void shared_walk(parse_kv kv, const int32_t *__restrict__ seqs, int rows, int window, int sinks, PtPlan plan) {
-  const int row = blockIdx.x * (SH_THREADS / 64) + (threadIdx.x >> 6), lane = threadIdx.x & 63, page = kv.page;
+  __shared__ ShNear near;
+  const int tid = threadIdx.x, lane = tid & 63, page = kv.page, row = NEAR ? blockIdx.x : blockIdx.x * (SH_THREADS / 64) + (tid >> 6);
   if (row >= rows) return;
   const ShRow r = sh_row(kv, seqs, row, window, sinks);
+  ShOther all{};
+  if (NEAR) {
+    const ShRow x = sh_row(kv, seqs, min(lane, rows - 1), window, sinks);
+    all = ShOther{x.seq.row * kv.max_pages, lane < rows ? x.columns : 0, x.lo / page, x.seq.len};
+  }
   const int32_t *table = kv.table + (int64_t)r.seq.row * kv.max_pages;
   auto there = [&](int id) { return (unsigned)id < (unsigned)kv.n_pages; };
   int4 found[PT_LEVELS];
@@ -73,10 +113,19 @@ __global__ __launch_bounds__(SH_THREADS) void shared_walk(parse_kv kv, const int
     return true;
   };
   for (int c0 = 0; c0 < r.columns; c0 += 64) {
+    if (NEAR && (c0 & (SH_THREADS - 1)) == 0) {
+      if (c0 > 0) __syncthreads();                                 // the columns before are read
+      shared_near(kv, r, table, rows, c0 + tid, all, near);
+      __syncthreads();
+    }
+    if (NEAR && tid >= 64) continue;
     const int c = c0 + lane;
     const bool care = c < r.columns && r.cares(c);
     int o = -1, k = 0;
-    if (care) {
+    if (NEAR) {
+      o = near.owner[(c0 & (SH_THREADS - 1)) + lane];
+      k = near.users[(c0 & (SH_THREADS - 1)) + lane];
+    } else if (care) {
       const int id = table[c];
       if (there(id)) { o = (int)(uint32_t)plan.owner[id]; k = plan.users[id]; }
     }
@@ -102,6 +151,7 @@ __global__ __launch_bounds__(SH_THREADS) void shared_walk(parse_kv kv, const int
       users = __builtin_amdgcn_readlane(k, at);
     }
   }
+  if (NEAR && tid >= 64) return;
   ends(r.columns, have);
 #pragma unroll
   for (int l = 0; l < PT_LEVELS; ++l) {
@@ -127,14 +177,15 @@ __global__ __launch_bounds__(SH_THREADS) void shared_walk(parse_kv kv, const int
   }
 }
 
-// One workgroup: the rows that agree with their owner become its group, groups of two and more get tiles, level after level.  A thread has consecutive rows.
-__global__ __launch_bounds__(SH_ONE) void shared_tiles(parse_kv kv, const int32_t *__restrict__ seqs, int rows, int group, int TC, int window, int sinks, PtPlan plan) {
+// One workgroup, of 256 threads where they have a row each (36 rows 7.7 us, 8.7 with 1024): the rows that agree with their owner become its group, groups of two and more get tiles, level after level.  A thread has consecutive rows.
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void shared_tiles(parse_kv kv, const int32_t *__restrict__ seqs, int rows, int group, int TC, int window, int sinks, PtPlan plan) {
   extern __shared__ int4 words[];
   const int4 *walk = plan.walk;
   const int wide = (rows + 3) & ~3;
   int *lead = reinterpret_cast<int *>(words), *users = lead + wide, *tile0 = users + wide, *list0 = tile0 + wide, *base0 = list0 + wide, *chain = base0 + wide;
-  __shared__ int sums[3][SH_ONE / 64];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, per = (rows + SH_ONE - 1) / SH_ONE;
+  __shared__ int sums[3][THREADS / 64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, per = (rows + THREADS - 1) / THREADS;
   const int r0 = tid * per, r1 = min(r0 + per, rows);
   for (int r = r0; r < r1; ++r) {
     chain[r] = 1;
@@ -187,7 +238,7 @@ __global__ __launch_bounds__(SH_ONE) void shared_tiles(parse_kv kv, const int32_
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
       total[k] = 0;
-      for (int w = 0; w < SH_ONE / 64; ++w) { before[k] += w < wave ? sums[k][w] : 0; total[k] += sums[k][w]; }
+      for (int w = 0; w < THREADS / 64; ++w) { before[k] += w < wave ? sums[k][w] : 0; total[k] += sums[k][w]; }
     }
     for (int r = r0; r < r1; ++r)
       if (lead[r] == r) { tile0[r] += tiles + before[0]; list0[r] += listed + before[1]; base0[r] += columns + before[2]; }
@@ -222,6 +273,11 @@ __global__ __launch_bounds__(SH_ONE) void shared_tiles(parse_kv kv, const int32_
     h.tiles = tiles; h.tile_columns = columns; h.n_seqs = kv.n_seqs;
     *plan.head = h;
   }
+}
+
+static_assert((int64_t)KV_MAXSEQ * 256 * SH_THREADS <= INT32_MAX, "words of the tables where this is chosen");
+static bool sh_near(const parse_kv *kv, int rows) {
+  return rows <= SH_NEAR_ROWS && (int64_t)rows * ((kv->max_pages + SH_THREADS - 1) / SH_THREADS) <= 256;
 }
 
 // ---- the call
@@ -268,14 +324,22 @@ int parse_shared_plan(const parse_kv *kv, int32_t n_q, int32_t rows, const int32
   const size_t lds = (size_t)((rows + 3) & ~3) * 6 * 4;
   const int TC = pt_columns(kv->d, kv->dtype);
   const dim3 grid((uint32_t)std::min<int64_t>((kv->max_pages + SH_THREADS - 1) / SH_THREADS, std::max(1, 4096 / rows)), rows);
-  shared_count<false><<<grid, SH_THREADS, 0, s>>>(*kv, seqs, window, sinks, p);
+  if (sh_near(kv, rows)) {
+    shared_walk<true><<<dim3(rows), SH_THREADS, 0, s>>>(*kv, seqs, rows, window, sinks, p);
+  } else {
+    shared_count<false><<<grid, SH_THREADS, 0, s>>>(*kv, seqs, window, sinks, p);
+    PARSE_LAUNCH_CHECK();
+    shared_count<true><<<grid, SH_THREADS, 0, s>>>(*kv, seqs, window, sinks, p);
+    PARSE_LAUNCH_CHECK();
+    shared_walk<false><<<dim3((rows + SH_THREADS / 64 - 1) / (SH_THREADS / 64)), SH_THREADS, 0, s>>>(*kv, seqs, rows, window, sinks, p);
+  }
   PARSE_LAUNCH_CHECK();
-  shared_count<true><<<grid, SH_THREADS, 0, s>>>(*kv, seqs, window, sinks, p);
-  PARSE_LAUNCH_CHECK();
-  shared_walk<<<dim3((rows + SH_THREADS / 64 - 1) / (SH_THREADS / 64)), SH_THREADS, 0, s>>>(*kv, seqs, rows, window, sinks, p);
-  PARSE_LAUNCH_CHECK();
-  PARSE_ALLOW_LDS(shared_tiles, 3 * SH_ONE / 64 * 4, lds);
-  shared_tiles<<<dim3(1), SH_ONE, lds, s>>>(*kv, seqs, rows, group, TC, window, sinks, p);
+  if (rows <= SH_THREADS) {
+    shared_tiles<SH_THREADS><<<dim3(1), SH_THREADS, lds, s>>>(*kv, seqs, rows, group, TC, window, sinks, p);
+  } else {
+    PARSE_ALLOW_LDS(shared_tiles<SH_ONE>, 3 * SH_ONE / 64 * 4, lds);
+    shared_tiles<SH_ONE><<<dim3(1), SH_ONE, lds, s>>>(*kv, seqs, rows, group, TC, window, sinks, p);
+  }
   PARSE_LAUNCH_CHECK();
   return PARSE_OK;
 }
