@@ -20,23 +20,29 @@ struct KbArgs {
 // smaller of two, NaN if one of them is
 __device__ __forceinline__ float kb_min(float a, float b) { return __builtin_elementwise_minimum(a, b); }
 
-// Smaller of two over lanes that stand opposite each other: N values a lane become N / 2, the lower ones where `upper` is clear, the upper ones where it is set
-template <int CTRL, int N>
-__device__ __forceinline__ void kb_fold(float *v, bool upper) {
+// Least over lanes that differ in one bit: N values a lane become N / 2, the lower ones where the bit is clear, the upper ones where it is set.  Bits 5 and 4 by exchanges of
+// halves and rows of two registers, bits 3 and 2 value by value.
+template <int BIT, int N> __device__ __forceinline__ void kb_fold(float *v) {
+  const bool upper = threadIdx.x & BIT;
 #pragma unroll
   for (int k = 0; k < N / 2; ++k) {
-    const float keep = upper ? v[k + N / 2] : v[k], give = upper ? v[k] : v[k + N / 2];
-    v[k] = kb_min(keep, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(give), CTRL, 0xf, 0xf, false)));
+    const uint32_t x = __float_as_uint(v[k]), y = __float_as_uint(v[k + N / 2]), keep = upper ? y : x, give = upper ? x : y;
+    u32x2 r;
+    if constexpr (BIT == 32) r = __builtin_amdgcn_permlane32_swap(x, y, false, false);
+    else if constexpr (BIT == 16) r = __builtin_amdgcn_permlane16_swap(x, y, false, false);
+    else if constexpr (BIT == 8) r = u32x2{keep, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)give, 0x128, 0xf, 0xf, false)};       // a row turned by eight lanes
+    else r = u32x2{keep, (uint32_t)__shfl_xor((int)give, BIT, 64)};
+    v[k] = kb_min(__uint_as_float(r[0]), __uint_as_float(r[1]));
   }
 }
 
-// A wavefront has pages of single heads: a load brings 64 pieces of eight columns, lane % 16 the token, so that a block's sixteen tokens are a row of lanes; the rows fold
-// to one value a lane in 60 exchanges (values and negated values side by side: the largest is the least of the negated).  Bound: reads; pages of 16 tokens by the vector unit as much (bf16 to fp32, two comparisons a value, the
-// folding).  A cache of 100003 tokens, 8 heads of 128 columns of bf16, 205 MB: 38 us, 5.4 TB/s; 8 prompts of 512 15 us.  Heads one after another in a wavefront, the next one's loads
-// before this one's folding: 39 and 15.6.
-template <class T, int DT>
+// A wavefront has pages of single heads.  A load brings eight pieces of eight columns of eight tokens (heads of 32 columns: four of sixteen), so that lines are whole; a lane keeps the
+// least of the tokens that it sees of its pieces, and lanes with other tokens of them fold, half by half (values and negated values side by side: the largest is the least of
+// the negated).  Bound: reads; small calls by three dependent trips to memory.  A cache of 100003 tokens, 8 heads of 128 columns of bf16, pages of 64, 205 MB: 37.6 us, 5.4 TB/s; 8 prompts of
+// 512, 32 heads, pages of 16 12.0.  Lanes with a token each (all pieces their own, 60 exchanges of single values): 39 and 15; whole rows of pieces a load (64 bytes a line) 42 and 13.
+template <class T, int DT, bool NT>
 __global__ __launch_bounds__(SP_THREADS) void kv_bounds(KbArgs a) {
-  constexpr int D = DT * 32;
+  constexpr int D = DT * 32, LP = DT == 1 ? 4 : 8, OWN = LP / 4, G = (D / 8 + LP - 1) / LP, LEFT = LP / 4;      // lanes of a token, loads of a block, groups of pieces, columns left
   typedef typename Op<T>::frag frag;
   extern __shared__ int pre[];
   int *wave_sums = pre + a.P + 1;
@@ -53,47 +59,67 @@ __global__ __launch_bounds__(SP_THREADS) void kv_bounds(KbArgs a) {
     const int lh = (int)(w % per) * SP_WAVES + wave;
     if (id >= 0 && id < a.kv.n_pages && lh < heads) {
       const int layer = lh / a.kv.n_kv, head = lh - layer * a.kv.n_kv;
-      const T *k = reinterpret_cast<const T *>(a.K) + layer * a.k_layer + ((int64_t)id * a.kv.n_kv + head) * page * D + lane * 8;
-      frag x[DT];
+      const T *k = reinterpret_cast<const T *>(a.K) + layer * a.k_layer + ((int64_t)id * a.kv.n_kv + head) * page * D + lane / LP * 8;
+      auto piece = [&](int g) { return g * LP + lane % LP; };
+      auto has = [&](int g) { return D / 8 % LP == 0 || g < G - 1 || piece(g) < D / 8; };
+      auto get = [&](frag *x, int b) {
 #pragma unroll
-      for (int p = 0; p < DT; ++p) x[p] = Op<T>::load_nt(k + p * 512);
-      float v[16 * DT];                                            // [least, largest negated][column of the piece][piece]
+        for (int g = 0; g < G; ++g)
 #pragma unroll
-      for (int i = 0; i < 16 * DT; ++i) v[i] = INFINITY;
-      auto take = [&](const frag &y, int p) {
-        float z[8];
-        if constexpr (sizeof(T) == 2) {
+          for (int t = 0; t < OWN; ++t) {
+            const T *p = k + b * 16 * D + (has(g) ? piece(g) : 0) * 128 + t * (64 / LP) * 8;
+            x[g * OWN + t] = NT ? Op<T>::load_nt(p) : Op<T>::load(p);
+          }
+      };
+      float v[G][16];                                              // least of the columns, largest negated
 #pragma unroll
-          for (int e = 0; e < 4; ++e) { z[2 * e] = __uint_as_float(y[e] << 16); z[2 * e + 1] = __uint_as_float(y[e] & 0xffff0000u); }
-        } else {
+      for (int i = 0; i < 16 * G; ++i) v[i / 16][i % 16] = INFINITY;
+      auto take = [&](const frag *x) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) { z[e] = y.lo[e]; z[4 + e] = y.hi[e]; }
-        }
+        for (int i = 0; i < G * OWN; ++i) {
+          float z[8], *w = v[i / OWN];
+          if constexpr (sizeof(T) == 2) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          v[e * DT + p] = kb_min(v[e * DT + p], z[e]);
-          v[(8 + e) * DT + p] = kb_min(v[(8 + e) * DT + p], -z[e]);
+            for (int e = 0; e < 4; ++e) { z[2 * e] = __uint_as_float(x[i][e] << 16); z[2 * e + 1] = __uint_as_float(x[i][e] & 0xffff0000u); }
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { z[e] = x[i].lo[e]; z[4 + e] = x[i].hi[e]; }
+          }
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            w[e] = kb_min(w[e], z[e]);
+            w[8 + e] = kb_min(w[8 + e], -z[e]);
+          }
         }
       };
+      frag x[G * OWN];
+      get(x, 0);
       for (int b = 1; b < blocks; ++b) {
-        frag y[DT];
+        frag y[G * OWN];
+        get(y, b);
+        take(x);
 #pragma unroll
-        for (int p = 0; p < DT; ++p) y[p] = Op<T>::load_nt(k + b * 16 * D + p * 512);
-#pragma unroll
-        for (int p = 0; p < DT; ++p) { take(x[p], p); x[p] = y[p]; }
+        for (int i = 0; i < G * OWN; ++i) x[i] = y[i];
       }
+      take(x);
+      // bit 5 chose least or largest, bit 4 the upper four columns, bit 3 of those the upper two, bit 2 the upper one
+      const int at = (lane & 16 ? 4 : 0) + (lane & 8 ? 2 : 0) + (LP == 4 && (lane & 4) ? 1 : 0);
+      T *to = reinterpret_cast<T *>(a.bounds) + layer * a.b_layer + ((int64_t)id * a.kv.n_kv + head) * 2 * D + (lane & 32 ? D : 0) + at;
 #pragma unroll
-      for (int p = 0; p < DT; ++p) take(x[p], p);
-      kb_fold<0x140, 16 * DT>(v, lane & 8);                        // row_mirror: lane ^ 15
-      kb_fold<0x141, 8 * DT>(v, lane & 4);                         // row_half_mirror: lane ^ 7
-      kb_fold<0x1b, 4 * DT>(v, lane & 2);                          // quad_perm 3 2 1 0
-      kb_fold<0xb1, 2 * DT>(v, lane & 1);                          // quad_perm 1 0 3 2
-      T *to = reinterpret_cast<T *>(a.bounds) + layer * a.b_layer + ((int64_t)id * a.kv.n_kv + head) * 2 * D + (lane & 8 ? D : 0) + (lane >> 4) * 8 + (lane & 7);
+      for (int g = 0; g < G; ++g) {
+        kb_fold<32, 16>(v[g]);
+        kb_fold<16, 8>(v[g]);
+        kb_fold<8, 4>(v[g]);
+        if constexpr (LP == 4) kb_fold<4, 2>(v[g]);
+        typedef __attribute__((ext_vector_type(LEFT))) T out_t;
+        out_t out;
 #pragma unroll
-      for (int p = 0; p < DT; ++p) {
-        const float r = lane & 8 ? -v[p] : v[p];
-        if constexpr (sizeof(T) == 2) to[p * 32] = (T)(__float_as_uint(r) >> 16);          // it is one of the keys
-        else to[p * 32] = r;
+        for (int e = 0; e < LEFT; ++e) {
+          const float r = lane & 32 ? -v[g][e] : v[g][e];
+          if constexpr (sizeof(T) == 2) out[e] = (T)(__float_as_uint(r) >> 16);            // it is one of the keys
+          else out[e] = r;
+        }
+        if (has(g)) *reinterpret_cast<out_t *>(to + piece(g) * 8) = out;
       }
     }
     if (a.P > 64) __syncthreads();                                 // the prompts' sums are made anew
@@ -440,17 +466,23 @@ __global__ __launch_bounds__(SC_FUSED, 2) void page_select(SpArgs a) {
   choose_pages<SC_FUSED>(cols.n, a.top, a.sel + ((int64_t)row * a.kv.n_kv + head) * a.top, sh, [&](int c) { return sh.keys[c]; });
 }
 
+template <class T, int DT>
+static void kb_go(const KbArgs &a, dim3 grid, size_t lds, hipStream_t s) {
+  // Loads past the caches for pools that do not stay there.  Without / with, us: pools of 67 MB (three in turn) 12.0 / 13.3, one of 410 MB 44.1 / 37.6
+  if ((size_t)a.kv.n_layers * a.kv.n_pages * a.kv.n_kv * a.kv.page * a.kv.d * sizeof(T) * 2 > ((size_t)192 << 20)) kv_bounds<T, DT, true><<<grid, SP_THREADS, lds, s>>>(a);
+  else kv_bounds<T, DT, false><<<grid, SP_THREADS, lds, s>>>(a);
+}
 template <class T>
 static void kb_launch(const KbArgs &a, dim3 grid, size_t lds, hipStream_t s) {
   switch (a.kv.d / 32) {
-    case 1: kv_bounds<T, 1><<<grid, SP_THREADS, lds, s>>>(a); break;
-    case 2: kv_bounds<T, 2><<<grid, SP_THREADS, lds, s>>>(a); break;
-    case 3: kv_bounds<T, 3><<<grid, SP_THREADS, lds, s>>>(a); break;
-    case 4: kv_bounds<T, 4><<<grid, SP_THREADS, lds, s>>>(a); break;
-    case 5: kv_bounds<T, 5><<<grid, SP_THREADS, lds, s>>>(a); break;
-    case 6: kv_bounds<T, 6><<<grid, SP_THREADS, lds, s>>>(a); break;
-    case 7: kv_bounds<T, 7><<<grid, SP_THREADS, lds, s>>>(a); break;
-    default: kv_bounds<T, 8><<<grid, SP_THREADS, lds, s>>>(a); break;
+    case 1: kb_go<T, 1>(a, grid, lds, s); break;
+    case 2: kb_go<T, 2>(a, grid, lds, s); break;
+    case 3: kb_go<T, 3>(a, grid, lds, s); break;
+    case 4: kb_go<T, 4>(a, grid, lds, s); break;
+    case 5: kb_go<T, 5>(a, grid, lds, s); break;
+    case 6: kb_go<T, 6>(a, grid, lds, s); break;
+    case 7: kb_go<T, 7>(a, grid, lds, s); break;
+    default: kb_go<T, 8>(a, grid, lds, s); break;
   }
 }
 // One launch where a workgroup a head fills the card about once, or there is little to score.  Two launches / one, us, 128 columns of bf16, heads of all rows x columns of the

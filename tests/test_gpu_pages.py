@@ -66,6 +66,10 @@ def test_bounds_of_many_sequences_and_missing_pages():
     run_bounds(Case("bf16", 1, 32, 16, lens, lambda s, c: (s + c) % 4 == 0, seed=1), None)
 
 
+def test_bounds_in_a_pool_that_does_not_stay_in_the_caches():
+    run_bounds(Case("bf16", 8, 128, 64, [64 * 250 + 63, 64 * 140, 5], seed=7), [64 * 3, 64 * 139 + 1, 5])
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_bounds_of_many_heads(dtype):
     """Heads one after another in a wavefront, their number not a multiple of it."""

@@ -167,6 +167,15 @@ def test_more_rows_than_a_workgroup_has_threads(dtype, d, rows):
     assert tiles_of(plan) == len({sh[0][0] for sh, _ in family if sum(x[0][0][0] == sh[0][0] for x in family) > 1})
 
 
+@pytest.mark.parametrize("rows,cols", [(3, 375), (64, 30), (70, 30), (70, 300)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (300, 40), (4000, 4)])
+def test_windows_of_few_and_many_rows(rows, cols, window, sinks):
+    """Plans of a wavefront and of a workgroup a row, of more columns than that has threads."""
+    f = Family("bf16", 1, 32, 16, [([("s", 9), (f"p{r % 3}", cols + r % 3)], 1 + 7 * r % 50) for r in range(rows)], seed=rows)
+    # three rows have a prompt each; of the text before them, 144 tokens, the windows leave the sinks' pages: ceil(40 / 16) * 16 = 48 tokens, ceil(4 / 16) * 16 = 16, both below 128
+    run(f, 1, window, sinks, seqs=list(range(rows)), shares=rows > 3 or window == 0)
+
+
 def test_many_groups_in_any_order():
     rng = np.random.default_rng(5)
     family = [([("s", 9), (f"g{g}", 8 + g % 3), (f"g{g}.{c}", 12)], int(rng.integers(1, 60))) for g in range(11) for c in range(2) for _ in range(3)]
