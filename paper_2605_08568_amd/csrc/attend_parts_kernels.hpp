@@ -16,6 +16,13 @@ template <class T, int DT> constexpr int pt_lds_own() {
 // Steps of a share where there are tiles, at least.  8 / 12 / 16, us: 32 samples of 8192 tokens 39.5 / 42.4 / 46.9 with the join
 constexpr int PT_WIDE_STEPS = 8;
 
+// Steps of an equal share, in twos.  By fours / twos / ones, us: 36 rows behind a common text 30.5 / 28.4 / 29.6, 64 samples of 8192 tokens 39.2 / 36.9 / 35.6 (join 9.2 / 9.8 / 10.0), 128 samples
+// 55.4 / 53.4 / 53.5, 96 rows of a window 35.6 / 35.8 / 39.4; lists the same
+__host__ __device__ constexpr int pt_share(int64_t total, int shares, int least) {
+  const int even = (int)((total + shares - 1) / shares + 1) / 2 * 2;
+  return even > least ? even : least;
+}
+
 // Entry x is share x, whole, where no entry has more steps than an equal share would and these: it costs what the longest entry is longer, and saves parts and, where rows
 // share nothing, the join.  4 / 12 / 24, us with the join: 32 caches of 100 to 356 tokens 19.3 / 17.7 / 17.7, 32 lists of 32 pages of 32 30.9 / 31.1 / 36.0
 constexpr int PT_SLACK = 12;
@@ -87,7 +94,7 @@ __global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_part
   const int entries = tiles + a.rows * a.per_row;
   auto before_of = [&](int e) { return LISTED ? e * list_steps : pre[e]; };
   // Tiles are cut in shares of PT_WIDE_STEPS at least: a part of them is as many bytes as four steps, written and read again
-  const int per = max(((total + a.shares - 1) / a.shares + PT_WAVES - 1) / PT_WAVES * PT_WAVES, tiles > 0 ? PT_WIDE_STEPS : PT_WAVES);
+  const int per = pt_share(total, a.shares, tiles > 0 ? PT_WIDE_STEPS : PT_WAVES);
   bool by_rows = entries <= a.shares;
   if (by_rows) {
     bool longer = false;
@@ -691,7 +698,7 @@ static int pt_launch(const PtArgs &a, int64_t entries, hipStream_t s) {
   PARSE_LAUNCH_CHECK();
   if (LISTED && entries <= a.shares) {                             // the lists' steps are the host's to count: whether every entry is a share's, whole
     const int64_t steps = ((int64_t)a.top * a.kv.page + PT_STEP - 1) / PT_STEP, total = steps * entries;
-    if (steps <= std::max<int64_t>(((total + a.shares - 1) / a.shares + PT_WAVES - 1) / PT_WAVES, 1) * PT_WAVES + PT_SLACK) return PARSE_OK;
+    if (steps <= pt_share(total, a.shares, PT_WAVES) + PT_SLACK) return PARSE_OK;
   }
   attend_parts_join<T, DT, LISTED><<<dim3(a.n_q, a.rows), PT_THREADS, 0, s>>>(a);
   PARSE_LAUNCH_CHECK();
