@@ -573,7 +573,7 @@ __global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_part
 
 // The parts of one row's head; workgroup (head, row).  Four columns a lane, so many parts at once as the workgroup has lanes for, four of them on their way each; a group of lanes
 // joins its parts one after another, then the groups are joined, both in a fixed order.  Bound: three dependent trips to memory, then the parts' reads: 3.8 us (a part or two a
-// row) to 9.8 (96 rows of a window, up to 20 parts each); 8 where 32 rows have 64 parts each.
+// row) to 9.8 (96 rows of a window); 8 for 32 rows of a text that is cut in 32 parts.
 template <class T, int DT, bool LISTED>
 __global__ __launch_bounds__(PT_THREADS) void attend_parts_join(PtArgs a) {
   constexpr int D = DT * 32, RD = D + 4, TC = 64 * pt_blocks<T, DT>(), LANES = D / 4, GROUPS = PT_THREADS / LANES, N = 4;

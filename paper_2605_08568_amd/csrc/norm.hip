@@ -152,7 +152,7 @@ static int rn_piece(const RnArgs &a, hipStream_t s) {
   const int pieces = a.d / 8;
 #define RN_GO(LANES, PIECES) rmsnorm<T, W, LANES, PIECES, E4M3><<<dim3((a.rows + (LANES < 256 ? 256 / LANES : 1) - 1) / (LANES < 256 ? 256 / LANES : 1)), LANES < 256 ? 256 : LANES, 0, s>>>(a)
   // Threads of a row x pieces of a thread; us for 2^24 values of bf16 with the residual, taken / the others: 1024 columns 64 x 2 26.9 / 256 x 1 27.1; 2048 256 x 1 25.0 / 64 x 4
-  // 26.0; 4096 512 x 1 25.0 / 256 x 2 27.4, 64 x 8 24.1 (8 rows: a third longer); 8192 256 x 4 23.6 / 512 x 2 28.5, 1024 x 1 25.8; 16384 512 x 4 23.6 / 256 x 8 23.7 (8 rows 0.4
+  // 26.0; 4096 512 x 1 25.0 / 256 x 2 27.4, 64 x 8 24.1 (8 rows up to 0.6 longer); 8192 256 x 4 23.6 / 512 x 2 28.5, 1024 x 1 25.8; 16384 512 x 4 23.6 / 256 x 8 23.7 (8 rows 0.4
   // longer), 1024 x 2 27.8; 32768 1024 x 4 24.3 / 512 x 8 23.9 (8 rows 1 longer)
   if (pieces <= 64) RN_GO(64, 1);
   else if (pieces <= 128) RN_GO(64, 2);
