@@ -109,24 +109,38 @@ __device__ __forceinline__ PtSpan pt_span(int i0, int from, int to, int window, 
   return s;
 }
 
-// The shortest sequence of a tile's rows: its table's row (its window reaches back the furthest, and no other of them has given up pages that it still holds) and
-// position.  By a whole wavefront, a lane one or two rows: a tile has no more rows than its (at most 128) columns.
+// The first token that a row sees may stand in a page that the row has given up: pages are given up by what the NEXT token sees, so the page that ends with this one's first
+// token goes as well.  Its column, or -1 where the window does not begin with a page's last token.  (Of a page that holds a sink nothing is given up.)
+__device__ __forceinline__ int pt_edge(const parse_kv &kv, int lo) { return ((lo + 1) & (kv.page - 1)) == 0 ? lo / kv.page : -1; }
+__device__ __forceinline__ bool pt_holds(const parse_kv &kv, int row, int column) {
+  return (unsigned)kv.table[(int64_t)row * kv.max_pages + column] < (unsigned)kv.n_pages;
+}
+
+// The shortest sequence of a tile's rows: its table's row (its window reaches back the furthest, and no longer one has given up less; of equally short ones one that still
+// holds the page of the first token that they see) and position.  By a whole wavefront, a lane one or two rows: a tile has no more rows than its (at most 128) columns.
 struct PtShortest {
   int row, pos;
 };
 __device__ __forceinline__ PtShortest pt_shortest(const PtArgs &a, const PtTile &t) {
   const int m0 = t.first / a.group, m1 = (t.first + t.columns - 1) / a.group, m = m0 + (int)(threadIdx.x & 63);
-  KvSeq q = kv_seq(a.kv, a.seqs, a.plan.list[t.list + min(m, m1)]);
-  if (m1 - m0 >= 64) {
-    const KvSeq r = kv_seq(a.kv, a.seqs, a.plan.list[t.list + min(m + 64, m1)]);
-    if (q.len <= 0 || (r.len > 0 && r.len < q.len)) q = r;
-  }
-  const int len = q.len > 0 ? q.len : 0x7fffffff;
-  int least = len;
+  KvSeq q = kv_seq(a.kv, a.seqs, a.plan.list[t.list + min(m, m1)]), r = q;
+  if (m1 - m0 >= 64) r = kv_seq(a.kv, a.seqs, a.plan.list[t.list + min(m + 64, m1)]);
+  auto len = [](const KvSeq &s) { return s.len > 0 ? s.len : 0x7fffffff; };
+  int least = min(len(q), len(r));
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) least = min(least, __shfl_xor(least, o, 64));
-  const int at = __builtin_ctzll(__ballot(len == least));
-  return PtShortest{__builtin_amdgcn_readlane(q.row, at), least == 0x7fffffff ? -1 : __builtin_amdgcn_readfirstlane(least) - 1};
+  least = __builtin_amdgcn_readfirstlane(least);
+  if (least == 0x7fffffff) return PtShortest{0, -1};
+  const int edge = pt_edge(a.kv, kv_window_begin(least - 1, a.window));
+  bool of_q = len(q) == least, of_r = len(r) == least;
+  uint64_t q_lanes = __ballot(of_q), r_lanes = __ballot(of_r);
+  if (edge >= 0 && __popcll(q_lanes | r_lanes) > 1) {
+    of_q = of_q && pt_holds(a.kv, q.row, edge);
+    of_r = of_r && pt_holds(a.kv, r.row, edge);
+    if (__any(of_q || of_r)) { q_lanes = __ballot(of_q); r_lanes = __ballot(of_r); }
+  }
+  const int row = q_lanes ? __builtin_amdgcn_readlane(q.row, __builtin_ctzll(q_lanes)) : __builtin_amdgcn_readlane(r.row, __builtin_ctzll(r_lanes));
+  return PtShortest{row, least - 1};
 }
 
 // Whether the plan was made for such a call; one that was not shares nothing

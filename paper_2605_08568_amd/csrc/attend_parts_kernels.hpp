@@ -190,7 +190,7 @@ __global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_part
       constexpr int NB = decltype(of)::value, NA = NB > 0 ? NB : 1;
       auto column = [&](int b) { return WIDE ? 16 * (wave + PT_WAVES * b) + n : n; };
       frag qf[NA][KB];
-      int pos[NA], lo[NA], least = 0x7fffffff, most = 0;
+      int pos[NA], lo[NA], in_table[NA], least = 0x7fffffff, most = 0;
       // q and what the columns see.  Three trips to memory one behind another: the rows go with the pages' numbers, q and the lengths with the first steps.
       int r[NA], h[NA];
       auto ask_rows = [&]() {
@@ -210,7 +210,12 @@ __global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_part
         for (int b = 0; b < NA; ++b) {
           const T *q = reinterpret_cast<const T *>(a.q) + (int64_t)r[b] * a.q_stride + (int64_t)(kvh * a.group + h[b]) * D;
           pos[b] = pos_of;
-          if (tile) pos[b] = kv_seq(a.kv, a.seqs, r[b]).len - 1;
+          in_table[b] = seq;
+          if (tile) {
+            const KvSeq s = kv_seq(a.kv, a.seqs, r[b]);
+            pos[b] = s.len - 1;
+            in_table[b] = s.row;
+          }
 #pragma unroll
           for (int k = 0; k < KB; ++k) qf[b][k] = Op<T>::load(q + 32 * k + 8 * quad);
         }
@@ -219,6 +224,10 @@ __global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_part
 #pragma unroll
         for (int b = 0; b < NA; ++b) {
           lo[b] = LISTED ? 0 : kv_window_begin(pos[b], a.window);
+          if (!LISTED && tile && a.window > 0) {                   // the table that is read is another row's: what this one has given up of it
+            const int edge = pt_edge(a.kv, lo[b]);
+            if (edge >= 0 && !pt_holds(a.kv, in_table[b], edge)) ++lo[b];
+          }
           least = min(least, pos[b]);
           most = max(most, lo[b]);
         }

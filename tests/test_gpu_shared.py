@@ -385,3 +385,49 @@ def test_the_example_serves_samples_that_share_their_prompts(window, sinks):
     # weights rounded as two halves, the result once (2^-8); the plain form in 32 bits
     assert r["worst"] <= 2.0 ** -7 and r["steps"] == 30 and bool(torch.isfinite(r["x"].float()).all())
     assert r["lengths"] == [0, 0] + [330] * 5 + [293] * 5
+
+
+# ---- pages that a row has given up and others of its tile have not --------------------------------------------------------
+def give_up(f, window, sinks, which=None):
+    """What parse_kv_trim gives up at the present lengths."""
+    for s in range(len(f.lens)) if which is None else which:
+        for c in range(f.table.shape[1]):
+            if c * f.page >= sinks and (c + 1) * f.page <= f.lens[s] - window + 1:
+                f.table[s, c] = -1
+    f.kv.table.copy_(i32(f.table))
+
+
+def grow(f, n):
+    f.lens = [m + n for m in f.lens]
+    f.kv.len.copy_(i32(np.array(f.lens)))
+
+
+def marked(dtype, page, own, seed, n_kv=1, room=0):
+    """A prompt of 512 tokens and what the rows have behind it.  V of every page's last token is large: who counts one that the row has given up is far off."""
+    f = Family(dtype, n_kv, 64, page, [([("p", 512 // page)], n) for n in own], seed=seed, room=room)
+    for c in range(512 // page):
+        f.write_v(f.table[0, c], page - 1, 1000.0)
+    return f
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("page", [16, 32])
+@pytest.mark.parametrize("n_q", [2, 12, 40])
+def test_rows_of_a_tile_that_gave_up_the_first_token_that_they_see(dtype, page, n_q):
+    """parse_kv_trim gives up what the NEXT token does not see: a page that ends with the first token of the last one's window too.  The shortest row still has it."""
+    f = marked(dtype, page, (28, 43, 59, 44), seed=30, room=40)             # windows of 300 begin at 240, 255, 271, 256
+    _, _, plan, _ = run(f, n_q, 300, 4, shares=True)
+    for step in (0, 1, 15, 1, 0):
+        grow(f, step)
+        give_up(f, 300, 4)
+        run(f, n_q, 300, 4, plan=plan, seed=step)
+
+
+@pytest.mark.parametrize("rows,n_q", [(3, 4), (70, 1)])
+@pytest.mark.parametrize("keeps", ["first", "last", "none", "all"])
+def test_rows_of_one_length_of_which_some_gave_up_a_page(rows, n_q, keeps):
+    """Of rows of the least length one may hold a page that the others have given up: it is the one that is read."""
+    f = marked("bf16", 16, [43] * rows, seed=31)
+    _, _, plan, _ = run(f, n_q, 300, 4, shares=True)
+    give_up(f, 300, 4, {"first": range(1, rows), "last": range(rows - 1), "none": range(rows), "all": ()}[keeps])
+    run(f, n_q, 300, 4, plan=plan)
