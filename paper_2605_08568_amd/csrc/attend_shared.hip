@@ -23,6 +23,8 @@ struct ShRow {
   int columns, lo, page, sinks;
   bool windowed;
   __device__ __forceinline__ bool cares(int c) const { return !windowed || (int64_t)c * page < sinks || (c + 1) * page > lo; }
+  // ... where the table's word is known: the page that ends with the window's first token may have been given up already (pt_edge), and then the row does not see that token either
+  __device__ __forceinline__ bool cares(int c, bool there) const { return cares(c) && (there || !windowed || (int64_t)c * page < sinks || (c + 1) * page != lo + 1); }
 };
 __device__ __forceinline__ ShRow sh_row(const parse_kv &kv, const int32_t *seqs, int row, int window, int sinks) {
   ShRow r;
@@ -120,14 +122,16 @@ __global__ __launch_bounds__(SH_THREADS) void shared_walk(parse_kv kv, const int
     }
     if (NEAR && tid >= 64) continue;
     const int c = c0 + lane;
-    const bool care = c < r.columns && r.cares(c);
+    bool care = c < r.columns && r.cares(c);
     int o = -1, k = 0;
     if (NEAR) {
       o = near.owner[(c0 & (SH_THREADS - 1)) + lane];
       k = near.users[(c0 & (SH_THREADS - 1)) + lane];
+      care = care && r.cares(c, k > 0);
     } else if (care) {
       const int id = table[c];
       if (there(id)) { o = (int)(uint32_t)plan.owner[id]; k = plan.users[id]; }
+      care = r.cares(c, there(id));
     }
     const uint64_t cared = __ballot(care), below = cared & ((1ull << lane) - 1);
     const int prev = below ? 63 - __builtin_clzll(below) : 0;
@@ -161,8 +165,8 @@ __global__ __launch_bounds__(SH_THREADS) void shared_walk(parse_kv kv, const int
     const int32_t *other = kv.table + (int64_t)kv_seq(kv, seqs, min((unsigned)lead, (unsigned)rows - 1)).row * kv.max_pages;
     bool same = true;
     for (int c = found[l].x / page + lane; c < found[l].y / page; c += 64) {
-      if (!r.cares(c)) continue;
       const int x = table[c], y = other[c];
+      if (!r.cares(c, there(x))) continue;
       same &= x == y || (!there(x) && !there(y));
     }
     if (!__all(same)) level = l;

@@ -431,3 +431,21 @@ def test_rows_of_one_length_of_which_some_gave_up_a_page(rows, n_q, keeps):
     _, _, plan, _ = run(f, n_q, 300, 4, shares=True)
     give_up(f, 300, 4, {"first": range(1, rows), "last": range(rows - 1), "none": range(rows), "all": ()}[keeps])
     run(f, n_q, 300, 4, plan=plan)
+
+
+def levels_of(plan, rows):
+    return plan[64:64 + 32 * rows].view(torch.int32).view(rows, 8)[:, 1].tolist()
+
+
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("rows", [4, 70])
+def test_a_plan_made_after_pages_were_given_up_has_every_row(rows, page):
+    """Rows whose window begins with the last token of a page that they have given up share as the others do; the plan then holds as one made before."""
+    f = marked("bf16", page, [28, 43, 59, 44, *(28 + r % 60 for r in range(rows - 4))], seed=32, room=40)
+    give_up(f, 300, 4)
+    _, _, plan, _ = run(f, 2, 300, 4, shares=True)
+    assert levels_of(plan, rows) == [1] * rows
+    for step in (0, 1, 15):
+        grow(f, step)
+        give_up(f, 300, 4)
+        run(f, 2, 300, 4, plan=plan, seed=step)
