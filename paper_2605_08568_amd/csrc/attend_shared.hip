@@ -297,6 +297,8 @@ static bool as_size(const parse_kv *kv, int n_q, int rows, AsSize &z) {
   z.entries = z.tiles + (int64_t)rows * ((group + TC - 1) / TC);
   z.columns = (int64_t)pt_shares(kv) * TC + (int64_t)(PT_LEVELS + 1) * rows * group;
   z.bytes = pt_deal_bytes(z.entries) + round_up((size_t)z.columns * kv->n_kv * (kv->d + 4) * 4, 256);
+  // the steps of all entries are added up in an int
+  if (z.entries * (((int64_t)kv->max_pages * kv->page + PT_STEP - 1) / PT_STEP) > INT32_MAX - 65536) return false;
   return z.entries <= (kv->dtype == PARSE_F32 && kv->d > 160 ? PT_MAXENTRIES_WIDE : PT_MAXENTRIES);
 }
 
@@ -361,8 +363,6 @@ int parse_attend_shared(const parse_kv *kv, int32_t layer, const void *q, int64_
   if (!plan) return PARSE_EINVAL;
   AsSize z;
   if (!as_size(kv, n_q, rows, z) || (!seqs && rows > kv->n_seqs)) return PARSE_ESHAPE;
-  // the steps of all entries are added up in an int
-  if (z.entries * (((int64_t)kv->max_pages * kv->page + PT_STEP - 1) / PT_STEP) > INT32_MAX - 65536) return PARSE_ESHAPE;
   if (!workspace || workspace_bytes < z.bytes || plan_bytes < pt_plan(kv, rows, n_q / kv->n_kv, nullptr).bytes) return PARSE_EWORKSPACE;
   if (!aligned16(workspace) || !aligned16(plan)) return PARSE_EALIGN;
   const size_t at = (size_t)layer * kv->n_pages * kv->n_kv * kv->page * kv->d * elem_size(kv->dtype);

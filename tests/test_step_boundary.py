@@ -94,6 +94,17 @@ def test_shared_limits():
     assert calls()["shared"](long, rows=4096, n_q=8) == ESHAPE
 
 
+def test_shared_limit_of_steps_holds_for_plans_and_queries():
+    """16 tokens a page, 4096 rows of 8 heads over 4 with keys, 128 columns a tile: 3 * (4096 * 2 / 128 + 2048 + 1) + 4096 = 10435 entries of max_pages / 2 steps each."""
+    L = pa.lib()
+    most = 2 * ((2 ** 31 - 1 - 2 ** 16) // 10435)
+    for pages, good in ((most, True), (most + 2, False), (1 << 21, False)):
+        kv = cache(n_seqs=4096, max_pages=pages)
+        assert (L.parse_shared_plan_bytes(kv, 8, 4096) > 0) == good and (L.parse_attend_shared_workspace_bytes(kv, 8, 4096) > 0) == good, pages
+        if not good:
+            assert calls()["plan"](kv, rows=4096) == ESHAPE and calls()["shared"](kv, rows=4096) == ESHAPE
+
+
 def test_bounds_refuse_bad_arguments():
     c = calls()["bounds"]
     refused(c, EINVAL, [dict(bounds=None), dict(P=0), dict(layer=-2)])
