@@ -449,3 +449,29 @@ def test_a_plan_made_after_pages_were_given_up_has_every_row(rows, page):
         grow(f, step)
         give_up(f, 300, 4)
         run(f, 2, 300, 4, plan=plan, seed=step)
+
+
+# ---- tiles of many columns ---------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype,d", [("bf16", 32), ("bf16", 64), ("bf16", 96), ("bf16", 128), ("fp32", 32), ("fp32", 64)])
+@pytest.mark.parametrize("rows,n_q", [(5, 26), (9, 24), (33, 8), (20, 12)])
+def test_tiles_of_two_blocks_a_wavefront(dtype, d, rows, n_q):
+    """65 to 128 columns: 65, 108, 128 and a rest of 4, 120."""
+    run(Family(dtype, 2, d, 16, [([("p", 21)], 1 + 7 * s % 60) for s in range(rows)], seed=d + rows), n_q, shares=True)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("bf16", 160), ("fp32", 64), ("fp32", 128)])
+@pytest.mark.parametrize("bad", [np.inf, -np.inf, np.nan])
+@pytest.mark.parametrize("n_q", [12, 40])
+def test_values_that_some_rows_of_a_wide_tile_see(dtype, d, bad, n_q):
+    """24 and 80 columns, one block and two a wavefront where the heads are narrow: the sums are made once more, from the pages."""
+    rows = [([("p", 30)], n) for n in (1, 40, 100)]
+    f, clean = (Family(dtype, 1, d, 16, rows, seed=33) for _ in range(2))
+    at = 480 + 1 - 200 + 10                                        # the first row's window has it, the others' do not
+    f.write_v(f.table[0, at // 16], at % 16, bad)
+    out, _, plan, _ = run(f, n_q, 200, 0, shares=True, check=False)
+    assert levels_of(plan, 3) == [1, 1, 0]                         # the third row's window has 100 tokens of the prompt, from 380 on, fewer than 128
+    ref, _, _, _ = run(clean, n_q, 200, 0, shares=True)
+    assert bool(out[0].isnan().all() if np.isnan(bad) else (out[0] == bad).all())
+    # sums of 200 weighted values added in another order, 200 * 2^-24 of at most 4 in size; the result rounded once in either, half a step each
+    off = 200 * 2.0 ** -24 * 2 * 4 + (2.0 ** -7 * ref[1:].float().abs() if dtype == "bf16" else 0.0)
+    assert bool(((out[1:].float() - ref[1:].float()).abs() <= off).all())
