@@ -635,9 +635,9 @@ int parse_kv_bounds(const parse_kv *kv, void *bounds, int32_t layer, const int32
  * the last.  The first `first` and the last `last` pages that the sequence has are always among them (the last one, which may be begun, has no bounds yet); of the others
  * those with the largest
  *     score = sum over the kv head's query heads h and columns i of max(q_hi * least_i, q_hi * largest_i),
- * which no key of the page exceeds, taken over the head's queries together (a column where no q is positive, or none negative, does not look at the largest, or the least);
- * sums in 64 bits, the lower column first among equals, NaN before all.  A sequence of no more than `top`
- * pages takes all.  Columns without a page are not taken.
+ * which no key of the page exceeds, taken over the head's queries together (a column i where no q is positive, or none negative, does not look at the largest, or the least:
+ * one where all of them are zero looks at neither, whatever they hold, NaN too); sums in 64 bits, the lower column first among equals, a score that is NaN before all.  A sequence
+ * of no more than `top` pages takes all.  Columns without a page are not taken.
  *   bounds     as written by parse_kv_bounds;  layer 0 <= layer < n_layers
  *   q          device [rows][n_q][d], rows q_stride elements apart, 16-byte aligned, as it goes to parse_attend_pages
  *   top, first, last   first >= 0, last >= 1, first + last <= top

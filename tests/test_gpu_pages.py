@@ -159,6 +159,36 @@ def test_select_from_long_tables():
     run_select(*table_cache(np.random.default_rng(8), "fp32", 1, 32, 16, lens), lens, 4, 9, 2, 3, dtype="fp32")
 
 
+@pytest.mark.parametrize("dtype,d", WIDTHS)
+def test_select_widths_in_two_launches(dtype, d):
+    """Tables of more than 256 columns and few heads: scores by as many lanes a page as it is wide, several rounds of a wavefront's pages, the last one begun."""
+    lens = [16 * 2300 - 3, 16 * 261, 16 * 40]
+    run_select(*table_cache(np.random.default_rng(50 + d), dtype, 2, d, 16, lens), lens, 6, 33, 1, 2, dtype=dtype)
+
+
+def chosen(kv, b, q, top, dtype):
+    bounds = torch.zeros((2, kv.n_pages, kv.n_kv, 2, kv.d), dtype=kv.K.dtype, device=DEV)
+    bounds[1] = upload(b, dtype)
+    return pa.select_pages(kv, 1, bounds, upload(q, dtype), top)[0, 0].tolist()
+
+
+@pytest.mark.parametrize("cols", [30, 2600])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_select_looks_at_no_column_without_queries(dtype, cols):
+    """A column where all queries of the group are zero is not looked at, whatever its bounds hold, NaN too; where one is not zero NaN comes first."""
+    rng = np.random.default_rng(60 + cols)
+    lens = [16 * cols]
+    kv, table, b = table_cache(rng, dtype, 1, 64, 16, lens)
+    q = rounded(rng.standard_normal((1, 2, 64)), dtype)
+    q[:, :, 7] = 0.0
+    want = run_select(kv, table, b, lens, 2, 9, dtype=dtype, q=q)[0, 0].tolist()
+    b[table[0, 3:cols:5], 0, :, 7] = np.nan
+    b[table[0, 4:cols:5], 0, :, 7] = [-np.inf, np.inf]
+    assert chosen(kv, b, q, 9, dtype) == want
+    b[table[0, 20], 0, :, 8] = np.nan
+    assert 20 in chosen(kv, b, q, 3, dtype)
+
+
 def test_select_missing_pages_and_sequences():
     rng = np.random.default_rng(9)
     lens = [2000, 900, 300, 40]
