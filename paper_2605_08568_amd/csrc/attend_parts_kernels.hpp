@@ -99,7 +99,11 @@ __global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_part
   if (by_rows) {
     bool longer = false;
     for (int e = tid; e < entries; e += PT_THREADS) longer |= before_of(e + 1) - before_of(e) > per + PT_SLACK;
-    by_rows = !__syncthreads_or(longer);
+    const bool some = __any(longer);                               // with words of its own: __syncthreads_or has 256 bytes of LDS beside those that were asked for
+    if (lane == 0) wave_sums[wave] = some;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < PT_WAVES; ++w) by_rows &= wave_sums[w] == 0;
   }
   if (share == 0 && kvh == 0) {                                    // for the kernel that joins
     if (tid == 0) *reinterpret_cast<int4 *>(a.deal) = int4{per, by_rows, entries, tile_columns};

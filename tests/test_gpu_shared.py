@@ -475,3 +475,10 @@ def test_values_that_some_rows_of_a_wide_tile_see(dtype, d, bad, n_q):
     # sums of 200 weighted values added in another order, 200 * 2^-24 of at most 4 in size; the result rounded once in either, half a step each
     off = 200 * 2.0 ** -24 * 2 * 4 + (2.0 ** -7 * ref[1:].float().abs() if dtype == "bf16" else 0.0)
     assert bool(((out[1:].float() - ref[1:].float()).abs() <= off).all())
+
+
+def test_as_many_entries_as_are_allowed():
+    """3 * (3200 / 64 + 3200 / 2 + 1) + 3200 = 8153 entries of fp32 heads of 256 columns, 8176 at most: their sums stand beside a ring of 128 KiB in a unit's 160."""
+    rows = 3200
+    f = Family("fp32", 1, 256, 16, None, table=np.arange(rows)[:, None] % 8, lens=[1 + 7 * r % 16 for r in range(rows)], seed=41)
+    run(f, 1, shares=False)
