@@ -512,7 +512,7 @@ template <class T, int DT, bool NT, bool TICKETS>
 static int ad_launch(const AdArgs &a, hipStream_t s) {
   const int zs = (a.group + AD_HEADS - 1) / AD_HEADS, scan = a.rows > 64 ? a.rows + 1 : 0;
   const size_t lds = (size_t)AD_WAVES * AD_HEADS * (DT * 32 + 2) * 4 + (AD_WAVES + scan) * 4;
-  PARSE_ALLOW_LDS((attend_decode<T, DT, NT, TICKETS>), 0, lds);
+  PARSE_ALLOW_LDS((attend_decode<T, DT, NT, TICKETS>), LDS_OF_VOTES, lds);
   attend_decode<T, DT, NT, TICKETS><<<dim3(a.shares, a.kv.n_kv, zs), AD_THREADS, lds, s>>>(a);
   PARSE_LAUNCH_CHECK();
   if (!TICKETS && a.shares > 1 && !ad_sure(a)) {

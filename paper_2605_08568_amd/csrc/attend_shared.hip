@@ -343,7 +343,7 @@ int parse_shared_plan(const parse_kv *kv, int32_t n_q, int32_t rows, const int32
   if (rows <= SH_THREADS) {
     shared_tiles<SH_THREADS><<<dim3(1), SH_THREADS, lds, s>>>(*kv, seqs, rows, group, TC, window, sinks, p);
   } else {
-    PARSE_ALLOW_LDS(shared_tiles<SH_ONE>, 3 * SH_ONE / 64 * 4, lds);
+    PARSE_ALLOW_LDS(shared_tiles<SH_ONE>, 3 * SH_ONE / 64 * 4 + LDS_OF_VOTES, lds);
     shared_tiles<SH_ONE><<<dim3(1), SH_ONE, lds, s>>>(*kv, seqs, rows, group, TC, window, sinks, p);
   }
   PARSE_LAUNCH_CHECK();

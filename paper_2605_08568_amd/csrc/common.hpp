@@ -45,12 +45,16 @@ void set_hip_error(hipError_t e, const char *where);
     }                                               \
   } while (0)
 
-// A launch with more than 64 KiB of LDS, the dynamic part and the `own` bytes of the kernel's arrays together, needs the dynamic part's limit raised first
-// (gfx950 has 160 KiB per CU).  Only the rare large shapes take this path, so the attribute is simply set again on each such call.
+static inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
+
+// A launch with more than 64 KiB of LDS, the dynamic part and the `own` bytes of the kernel's arrays together, needs the dynamic part's limit raised first.  The limit is the
+// kernel's, for all threads: it is raised to all that a unit has beside those arrays, so that no call lowers it between another one's raise and launch.
+constexpr int LDS_OF_UNIT = 160 * 1024, LDS_OF_VOTES = 256;       // what __syncthreads_or has for itself
 #define PARSE_ALLOW_LDS(kernel, own, bytes)                                                                       \
   do {                                                                                                            \
     if ((size_t)(own) + (size_t)(bytes) > (size_t)65536)                                                          \
-      PARSE_HIP_TRY(hipFuncSetAttribute((const void *)(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)(bytes))); \
+      PARSE_HIP_TRY(hipFuncSetAttribute((const void *)(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,       \
+                                        ::parse::LDS_OF_UNIT - (int)::parse::round_up((own), 1024)));             \
   } while (0)
 
 // Kernels are told their grid and block sizes or work them out where a step launches them one after another: gridDim and blockDim are no arguments of the launch but
@@ -67,7 +71,6 @@ void set_hip_error(hipError_t e, const char *where);
   } while (0)
 
 static inline bool aligned16(const void *p) { return (((uintptr_t)p) & 15u) == 0; }
-static inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 static inline int elem_size(int dtype) { return dtype == PARSE_BF16 ? 2 : 4; }
 
 // Host-side check of a parse_layer: returns PARSE_OK or the status to hand back.

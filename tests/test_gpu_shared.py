@@ -1,5 +1,7 @@
 """Attention of batches that begin alike against the float64 oracle: every position that a row does not see holds NaN, pages stand in any order, rows
 share pages as forks leave them or in any other way, outputs, plans and workspaces between canaries."""
+import ctypes as C
+
 import numpy as np
 import pytest
 import torch
@@ -482,3 +484,61 @@ def test_as_many_entries_as_are_allowed():
     rows = 3200
     f = Family("fp32", 1, 256, 16, None, table=np.arange(rows)[:, None] % 8, lens=[1 + 7 * r % 16 for r in range(rows)], seed=41)
     run(f, 1, shares=False)
+
+
+class FuncAttributes(C.Structure):
+    """hipFuncAttributes, as far as it is read."""
+    _fields_ = [("binary_version", C.c_int), ("cache_mode", C.c_int), ("const_bytes", C.c_size_t), ("local_bytes", C.c_size_t), ("most_dynamic", C.c_int), ("most_threads", C.c_int),
+                ("registers", C.c_int), ("carveout", C.c_int), ("ptx_version", C.c_int), ("shared_bytes", C.c_size_t), ("room", C.c_char * 256)]
+
+
+def test_no_call_lowers_what_another_may_launch_with():
+    """The plan's and the attention's LDS go with their rows: 24 bytes a row; a ring of 64 KiB and 4 bytes an entry.  The limit that a call raises before its launch holds for all calls
+    of the kernel, of other threads too: behind a small call it still covers a large one."""
+    from paper_2605_08568_amd import build
+    most = 4000
+    kv = pa.KV(torch.zeros(1, 8, 1, 1, 16, 16, 8, device=DEV).bfloat16(), torch.zeros(1, 8, 1, 2, 128, 8, device=DEV).bfloat16(), i32(np.zeros((most, 1))), i32(np.ones(most)))
+    lib, hip = C.CDLL(build.LIB), C.CDLL("libamdhip64.so.7")
+    for rows in (most, 2800):
+        plan = pa.shared_plan(kv, 1, rows)
+        pa.attend_shared(kv, 0, torch.zeros(rows, 1, 128, device=DEV).bfloat16(), plan)
+    torch.cuda.synchronize()
+    for kernel, need in (("_ZN5parse12shared_tilesILi1024EEEv8parse_kvPKiiiiiiNS_6PtPlanE", 24 * most), ("_ZN5parse12attend_partsItLi4ELb0ELb0EEEvNS_6PtArgsE", 65536 + 4 * most)):
+        a = FuncAttributes()
+        assert hip.hipFuncGetAttributes(C.byref(a), C.c_void_p(C.addressof(C.c_char.in_dll(lib, kernel)))) == 0, kernel
+        assert a.most_dynamic >= need, (kernel, a.most_dynamic)
+
+
+def test_two_threads_with_batches_of_different_sizes():
+    """A plan and a call of either need LDS by their rows: what one asks for is not taken from the other between its asking and its launch."""
+    import threading
+    rng = np.random.default_rng(40)
+    most = 4000
+    kv = pa.KV(torch.randn(1, 8, 1, 1, 16, 16, 8, device=DEV).bfloat16(), torch.randn(1, 8, 1, 2, 128, 8, device=DEV).bfloat16(), i32(rng.integers(0, 8, (most, 1))),
+               i32(rng.integers(1, 17, most)))
+    jobs = []
+    for rows in (2800, most):
+        q, plan, ws = torch.randn(rows, 1, 128, device=DEV).bfloat16(), pa.shared_plan(kv, 1, rows), pa.attend_shared_workspace(kv, 1, rows)
+        jobs.append((rows, q, plan, ws, pa.attend_shared(kv, 0, q, plan, workspace=ws).clone(), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(rows, q, plan, ws, want, stream):
+        try:
+            with torch.cuda.stream(stream):
+                out = torch.empty_like(want)
+                for _ in range(300):
+                    pa.shared_plan(kv, 1, rows, plan=plan)
+                    pa.attend_shared(kv, 0, q, plan, out=out, workspace=ws)
+                stream.synchronize()
+                if not torch.equal(out, want):
+                    wrong.append(f"{rows} rows: another result")
+        except Exception as e:
+            wrong.append(f"{rows} rows: {e}")
+    threads = [threading.Thread(target=work, args=job) for job in jobs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not wrong, wrong
