@@ -609,6 +609,8 @@ int parse_attend_prefill(const parse_kv *kv, int32_t layer, const void *q, int64
  * Limits: rows 1..4096; 3 * (rows * n_q / n_kv / C + rows / 2 + 1) + rows * ceil(n_q / n_kv / C) <= 16384 (8176 for fp32 heads wider than 160
  * columns) with C = 128 (64 for heads wider than 128 columns of bf16, 64 of fp32), and that number times max_pages*page/32 below 2^31 - 2^16; the
  * queries give 0 otherwise, the calls PARSE_ESHAPE.
+ * A row sees what its own table holds: of the page that ends with the first token of its window, which the next token does not see, some rows may have given up what others still hold.
+ * Where nothing is shared parse_attend_decode is the call for short caches (two fifths less for 32 of 100 to 356 tokens; over long ones they are level).
  * Other arguments as in parse_attend_decode.  Same inputs and plan, same bits. */
 size_t parse_shared_plan_bytes(const parse_kv *kv, int32_t n_q, int32_t rows);
 int parse_shared_plan(const parse_kv *kv, int32_t n_q, int32_t rows, const int32_t *seqs, int32_t window, int32_t sinks, void *plan, size_t plan_bytes,
@@ -649,6 +651,7 @@ int parse_select_pages(const parse_kv *kv, const void *bounds, int32_t layer, co
 
 /* The attention of parse_attend_decode over the listed pages only: a row and kv head see the tokens of the columns in pages[row][kv head][0..top) that the sequence has
  * (j <= len - 1) and whose page is there.  Columns may stand in any order; -1 and others outside the table are passed over; one that stands twice counts twice.
+ * A call costs rows * top * page tokens for every kv head, whatever stands in the lists: rows with few pages are cheaper in a call of their own with a smaller top.
  *   pages      device int32 [rows][n_kv][top], 1 <= top, top * page < 2^31, rows * n_kv * top < 2^31, and
  *              rows * ceil(n_q / n_kv / 64) * top * page / 32 below 2^31 - 2^16
  *   workspace  any contents; one call at a time has it

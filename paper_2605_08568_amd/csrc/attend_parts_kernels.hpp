@@ -17,7 +17,7 @@ template <class T, int DT> constexpr int pt_lds_own() {
 constexpr int PT_WIDE_STEPS = 8;
 
 // Steps of an equal share, in twos.  By fours / twos / ones, us: 36 rows behind a common text 30.5 / 28.4 / 29.6, 64 samples of 8192 tokens 39.2 / 36.9 / 35.6 (join 9.2 / 9.8 / 10.0), 128 samples
-// 55.4 / 53.4 / 53.5, 96 rows of a window 35.6 / 35.8 / 39.4; lists the same
+// 55.4 / 53.4 / 53.5, 96 rows of a window 36.0 / 38.1 / 38.1 (16 steps or 14); lists the same
 __host__ __device__ constexpr int pt_share(int64_t total, int shares, int least) {
   const int even = (int)((total + shares - 1) / shares + 1) / 2 * 2;
   return even > least ? even : least;
@@ -51,6 +51,7 @@ __global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_part
   const int share = blockIdx.x, kvh = blockIdx.y;
   int tiles = 0, tile_columns = 0, total;
   bool fits = false;
+  // Steps of a list are what it has room for: which of its words are columns is not known here.  32 rows of 100 tokens, pages of 64: 7.7 us for lists of 2, 40.7 for lists of 64
   const int list_steps = LISTED ? (int)(((int64_t)a.top * a.kv.page + PT_STEP - 1) / PT_STEP) : 0;
   auto tile_span = [&](const PtTile &t) { return pt_span(t.pos, t.from, t.to, a.window, a.sinks); };
   auto own_span = [&](int from, const KvSeq &s) { return pt_span(s.len - 1, min(from, s.len), s.len, a.window, a.sinks); };
@@ -586,7 +587,7 @@ __global__ __launch_bounds__(PT_THREADS, (pt_at_once<T, DT>())) void attend_part
 
 // The parts of one row's head; workgroup (head, row).  Four columns a lane, so many parts at once as the workgroup has lanes for, four of them on their way each; a group of lanes
 // joins its parts one after another, then the groups are joined, both in a fixed order.  Bound: three dependent trips to memory, then the parts' reads: 3.8 us (a part or two a
-// row) to 9.8 (96 rows of a window); 8 for 32 rows of a text that is cut in 32 parts.
+// row) to 10 (96 rows of a window); 8 for 32 rows of a text that is cut in 32 parts.
 template <class T, int DT, bool LISTED>
 __global__ __launch_bounds__(PT_THREADS) void attend_parts_join(PtArgs a) {
   constexpr int D = DT * 32, RD = D + 4, TC = 64 * pt_blocks<T, DT>(), LANES = D / 4, GROUPS = PT_THREADS / LANES, N = 4;
